@@ -14,6 +14,10 @@
  *   cosine difference of two embedding tables (Section 4.4) -> tensair_cosine_difference
  *   a gradient message with bfloat16 rows (a variant beyond the paper) -> tensair_grad_pack,
  *       tensair_dasgd_apply_packed, tensair_step_packed
+ * Beyond the paper, for models that use such a table as their input and output layer (no model handle):
+ *   scaled lookup and its gradient by sorted tokens  -> tensair_embed, tensair_embed_grad, tensair_embed_grad_dense
+ *   softmax loss over the whole vocabulary, gradient -> tensair_softmax_loss, tensair_softmax_grad
+ *   AdamW over many tensors at once                  -> tensair_adamw_init, tensair_adamw_step
  *
  * Conventions for every call
  *   - Plain C ABI.  Pointers marked DEVICE point to GPU memory owned by the caller;
@@ -52,6 +56,7 @@ extern "C" {
 typedef struct tensair_model tensair_model; /* opaque host handle */
 
 enum { TENSAIR_F32 = 0, TENSAIR_BF16 = 1 }; /* table element type (gradients are always fp32) */
+enum { TENSAIR_FP8 = 2 };                   /* 8-bit floats (4 exponent, 3 mantissa bits): states of tensair_adamw_* only */
 
 enum {
     TENSAIR_OK = 0,
@@ -359,6 +364,96 @@ int tensair_dasgd_apply_static(void *w_in, void *w_out, int64_t vocab, int32_t d
                                int32_t dtype, const tensair_sparse_grad *own,
                                const tensair_sparse_grad *peers, int32_t n_peers, float lr,
                                int32_t *status, void *stream);
+
+/* ------------------------------------------------------------------------------------------------------
+ * A table as the input and output layer of a model.  None of these calls needs a model handle.
+ * Tables and matrices are DEVICE, row-major, of TENSAIR_F32 or TENSAIR_BF16, 16-byte aligned, with a row
+ * stride (in elements) >= dim that is a multiple of 4; what lies between dim and the stride does not
+ * matter and is not written.  dim: a multiple of 4, 4..TENSAIR_MAX_DIM.  ids and labels: DEVICE int32.  All sums are taken in
+ * fp32 and in an order that is a function of the arguments alone: the same call gives the same bits.
+ * workspace: DEVICE, 256-byte aligned; it holds nothing between calls and may be shared by calls on one stream.
+ * status: DEVICE int32 or NULL.  An id out of range never faults: bit 1 is OR-ed into *status, which the
+ * caller clears and reads. */
+
+/* out[i] = scale * table[ids[i]], i < n; the product in fp32, rounded once to out's type.  An id outside [0, vocab)
+ * yields a row of zeros and sets the status bit. */
+int tensair_embed(const void *table, int32_t dtype, int64_t vocab, int32_t dim, int64_t row_stride,
+                  const int32_t *ids, int64_t n, float scale, void *out, int32_t out_dtype,
+                  int64_t out_stride, int32_t *status, void *stream);
+
+/* Bytes of workspace of the two calls below (0: an argument is out of range). */
+size_t tensair_embed_workspace_bytes(int64_t vocab, int32_t dim, int64_t n);
+
+/* The gradient of tensair_embed with respect to the table: for every word r among the ids
+ * G[r] = scale * (sum of d_out[i] over the i with ids[i] = r).  Ids outside [0, vocab) are skipped and set the status bit.
+ * tensair_embed_grad writes one table's half of a gradient message: n_rows, the ascending unique row ids
+ * and the rows, of which the capacity has to allow min(vocab, n); what lies behind n_rows rows is not written.
+ * tensair_embed_grad_dense writes a gradient of the whole table, rows that no id names being zero, or, with
+ * accumulate != 0, adds the rows to what is there and leaves the others alone (one rounding; the gradient of a table that is
+ * the output layer too). */
+int tensair_embed_grad(const int32_t *ids, int64_t n, const void *d_out, int32_t d_dtype, int64_t d_stride,
+                       int64_t vocab, int32_t dim, float scale, const tensair_sparse_rows *grad,
+                       void *workspace, size_t workspace_bytes, int32_t *status, void *stream);
+int tensair_embed_grad_dense(const int32_t *ids, int64_t n, const void *d_out, int32_t d_dtype, int64_t d_stride,
+                             int64_t vocab, int32_t dim, float scale, void *grad, int32_t grad_dtype,
+                             int64_t grad_stride, int32_t accumulate, void *workspace,
+                             size_t workspace_bytes, int32_t *status, void *stream);
+
+/* Softmax cross entropy against every row of a table (what negative sampling stands in for), with
+ *   z[i][v] = scale * <hidden[i], table[v]>,  lse[i] = log sum_v exp z[i][v],  loss[i] = lse[i] - z[i][labels[i]].
+ * The logits are never kept.  A label equal to ignore_label gives loss 0; so does one outside [0, vocab), which also sets the
+ * status bit.  hidden and table have the same type; loss and lse: DEVICE fp32 [n].
+ * fp32 inputs are multiplied with the precision of fp32; n <= TENSAIR_MAX_TOKENS, vocab <= TENSAIR_MAX_VOCAB.
+ * tensair_softmax_grad: for the gradient d_loss (DEVICE fp32 [n]) of the losses, with p = exp(z - lse),
+ *   dz[i][v] = d_loss[i] * (p[i][v] - (v == labels[i])) for rows that have a loss, 0 for the others,
+ *   d_hidden[i] = scale * sum_v dz[i][v] table[v],   d_table[v] = scale * sum_i dz[i][v] hidden[i],
+ * both of the inputs' type (either may be NULL: not wanted).  lse: what tensair_softmax_loss gave for the same inputs. */
+#define TENSAIR_MAX_TOKENS 16777216 /* 2^24 */
+size_t tensair_softmax_workspace_bytes(int64_t n, int64_t vocab, int32_t dim, int32_t dtype, int32_t with_grad);
+int tensair_softmax_loss(const void *hidden, int64_t hidden_stride, const void *table, int64_t table_stride,
+                         int32_t dtype, int64_t n, int64_t vocab, int32_t dim, const int32_t *labels,
+                         int32_t ignore_label, float scale, float *loss, float *lse, void *workspace,
+                         size_t workspace_bytes, int32_t *status, void *stream);
+int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *table, int64_t table_stride,
+                         int32_t dtype, int64_t n, int64_t vocab, int32_t dim, const int32_t *labels,
+                         int32_t ignore_label, float scale, const float *lse, const float *d_loss,
+                         void *d_hidden, int64_t d_hidden_stride, void *d_table, int64_t d_table_stride,
+                         void *workspace, size_t workspace_bytes, int32_t *status, void *stream);
+
+/* AdamW over many tensors at once.  With t the step (counted from 1), g the gradient times *grad_scale (DEVICE float, NULL: 1),
+ * every operation in fp32, rounded by itself, in this order (the constants in 64 bits, each rounded once):
+ *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) (g g),
+ *   param <- param (1 - lr weight_decay) - (m (lr / (1 - beta1^t))) / (sqrt(v) (1 / sqrt(1 - beta2^t)) + eps).
+ * State types: TENSAIR_F32 -- m, v: fp32 [n].  TENSAIR_FP8 -- m, v: one 8-bit float (4 exponent, 3 mantissa bits, no
+ * infinities) per element, m_scale, v_scale: fp32 [ceil(n / 256)], one for every 256 elements of the tensor; the first moment
+ * is m * m_scale, the second (v * v_scale)^2.  The scale is the group's largest magnitude / 448 (0 where that is below 2^-100);
+ * m is rounded to nearest even, the root sqrt(v) in units of the scale, at least 2^-6 unless it is 0, is cut after
+ * ((i * 0x9E3779B1 + t * 0x85EBCA77) mod 2^32) / 2^32 of its last place was added, i being the element's number.
+ * A gradient that is not finite makes its element NaN, in 8-bit states the scales of its group, too.
+ * All-zero states (and scales) are a fresh start.  param_copy: DEVICE bfloat16 [n] or NULL, receives the new
+ * parameters rounded to nearest even.  Pointers need the alignment of their elements (16 bytes are faster);
+ * tensors must not overlap.  Gradients are read where they were at tensair_adamw_init: write new ones there. */
+#define TENSAIR_ADAMW_GROUP 256
+typedef struct {
+    void *param;          /* DEVICE [n] of param_dtype */
+    const void *grad;     /* DEVICE [n] of grad_dtype */
+    void *m, *v;          /* DEVICE [n] of the state type */
+    float *m_scale, *v_scale;
+    uint16_t *param_copy;
+    int64_t n;            /* 0 .. TENSAIR_MAX_DENSE */
+    int32_t param_dtype, grad_dtype;
+    float weight_decay;   /* >= 0 */
+} tensair_adamw_tensor;
+typedef struct tensair_adamw tensair_adamw; /* opaque host handle: the tensors of one optimizer */
+
+/* workspace: kept alive and untouched until tensair_adamw_destroy.  tensors: HOST array, read during the call, which waits for
+ * an upload on `stream`. */
+size_t tensair_adamw_workspace_bytes(const tensair_adamw_tensor *tensors, int32_t n_tensors, int32_t state_dtype);
+int tensair_adamw_init(tensair_adamw **out, const tensair_adamw_tensor *tensors, int32_t n_tensors,
+                       int32_t state_dtype, void *workspace, size_t workspace_bytes, void *stream);
+int tensair_adamw_step(tensair_adamw *h, double lr, int64_t step, double beta1, double beta2, double eps,
+                       const float *grad_scale, void *stream);
+int tensair_adamw_destroy(tensair_adamw *h);
 
 /* Waits for the library's own stream (a pending prefetch), then frees the host handle. */
 int tensair_model_destroy(tensair_model *m);

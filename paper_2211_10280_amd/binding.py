@@ -16,7 +16,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libtensair.so")
 
-F32, BF16 = 0, 1
+F32, BF16, FP8 = 0, 1, 2
 OK, EINVAL, ECAPACITY, EHIP, EDATA = 0, -1, -2, -3, -4
 MAX_PEERS = 31
 MAX_VOCAB = (1 << 28) - 64
@@ -34,6 +34,9 @@ SYMBOLS = [
     "tensair_prefetch", "tensair_grad_add", "tensair_dense_apply", "tensair_lookup",
     "tensair_cosine_difference", "tensair_grad_pack", "tensair_dasgd_apply_packed", "tensair_step_packed",
     "tensair_dasgd_apply_static", "tensair_stream_probe", "tensair_aligned_row_stride",
+    "tensair_embed", "tensair_embed_workspace_bytes", "tensair_embed_grad", "tensair_embed_grad_dense",
+    "tensair_softmax_workspace_bytes", "tensair_softmax_loss", "tensair_softmax_grad",
+    "tensair_adamw_workspace_bytes", "tensair_adamw_init", "tensair_adamw_step", "tensair_adamw_destroy",
 ]
 
 PROFILE_TAGS = {1: "keys", 2: "forward", 3: "sort", 4: "segments", 5: "reduce_in", 6: "reduce_out",
@@ -60,6 +63,12 @@ class SparseRows(C.Structure):
 
 class SparseGrad(C.Structure):
     _fields_ = [("in_", SparseRows), ("out", SparseRows)]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("param_copy", C.c_void_p),
+                ("n", C.c_int64), ("param_dtype", C.c_int32), ("grad_dtype", C.c_int32), ("weight_decay", C.c_float)]
 
 
 _lib = None
@@ -133,6 +142,30 @@ def lib():
         L.tensair_copy_probe.restype = C.c_int
         L.tensair_stream_probe.argtypes = [vp, vp, C.c_size_t, i32, vp]
         L.tensair_stream_probe.restype = C.c_int
+        f32, sz = C.c_float, C.c_size_t
+        L.tensair_embed.argtypes = [vp, i32, i64, i32, i64, vp, i64, f32, vp, i32, i64, vp, vp]
+        L.tensair_embed.restype = C.c_int
+        L.tensair_embed_workspace_bytes.argtypes = [i64, i32, i64]
+        L.tensair_embed_workspace_bytes.restype = sz
+        L.tensair_embed_grad.argtypes = [vp, i64, vp, i32, i64, i64, i32, f32, C.POINTER(SparseRows), vp, sz, vp, vp]
+        L.tensair_embed_grad.restype = C.c_int
+        L.tensair_embed_grad_dense.argtypes = [vp, i64, vp, i32, i64, i64, i32, f32, vp, i32, i64, i32, vp, sz, vp, vp]
+        L.tensair_embed_grad_dense.restype = C.c_int
+        L.tensair_softmax_workspace_bytes.argtypes = [i64, i64, i32, i32, i32]
+        L.tensair_softmax_workspace_bytes.restype = sz
+        L.tensair_softmax_loss.argtypes = [vp, i64, vp, i64, i32, i64, i64, i32, vp, i32, f32, vp, vp, vp, sz, vp, vp]
+        L.tensair_softmax_loss.restype = C.c_int
+        L.tensair_softmax_grad.argtypes = [vp, i64, vp, i64, i32, i64, i64, i32, vp, i32, f32, vp, vp, vp, i64, vp, i64,
+                                           vp, sz, vp, vp]
+        L.tensair_softmax_grad.restype = C.c_int
+        L.tensair_adamw_workspace_bytes.argtypes = [C.POINTER(AdamwTensor), i32, i32]
+        L.tensair_adamw_workspace_bytes.restype = sz
+        L.tensair_adamw_init.argtypes = [C.POINTER(vp), C.POINTER(AdamwTensor), i32, i32, vp, sz, vp]
+        L.tensair_adamw_init.restype = C.c_int
+        L.tensair_adamw_step.argtypes = [vp, C.c_double, i64, C.c_double, C.c_double, C.c_double, vp, vp]
+        L.tensair_adamw_step.restype = C.c_int
+        L.tensair_adamw_destroy.argtypes = [vp]
+        L.tensair_adamw_destroy.restype = C.c_int
         L.tensair_last_error.argtypes = []
         L.tensair_last_error.restype = C.c_char_p
         _lib = L
@@ -361,6 +394,206 @@ def tensair_cosine_difference(a, b, dim: int, diff, stream=None):
     dt = F32 if a.dtype == torch.float32 else BF16
     _check(lib().tensair_cosine_difference(_ptr(a), _ptr(b), dt, a.shape[0], dim, a.shape[1], _ptr(diff),
                                            _stream(stream)))
+
+
+# ---- a table as the input and output layer of a model
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float8_e4m3fn: FP8}
+
+
+def _dtype(t, what):
+    """The C dtype of a tensor or torch dtype; EINVAL for one that no entry point takes."""
+    code = _DTYPES.get(t if isinstance(t, torch.dtype) else t.dtype)
+    if code is None:
+        raise TensairError(EINVAL, f"{what}: unknown dtype")
+    return code
+
+
+def _matrix(t, rows, dim, what):
+    """(address, C dtype, row stride) of a [rows, >= dim] tensor whose rows are contiguous."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] < dim or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise TensairError(EINVAL, f"{what}: expected {rows} contiguous rows of at least {dim} elements")
+    return t.data_ptr(), _dtype(t, what), t.stride(0) if rows > 1 else max(t.stride(0), t.shape[1])
+
+
+def _vector(t, n, dtype, what):
+    """The address of a contiguous one-dimensional tensor of n elements."""
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise TensairError(EINVAL, f"{what}: expected {n} contiguous elements of {dtype}")
+    return t.data_ptr()
+
+
+def _ids(t, what="ids"):
+    return _vector(t, t.numel(), torch.int32, what)
+
+
+class RowBuffers:
+    """Device memory of one tensair_sparse_rows, one table's half of a gradient message."""
+
+    def __init__(self, capacity: int, dim: int, device="cuda"):
+        self.n_rows = torch.zeros(1, dtype=torch.int32, device=device)
+        self.row_ids = torch.empty(max(capacity, 1), dtype=torch.int32, device=device)
+        self.rows = torch.empty((max(capacity, 1), dim), dtype=torch.float32, device=device)
+
+    def __iter__(self):
+        return iter((self.n_rows, self.row_ids, self.rows))
+
+    def to_host(self):
+        """(ids, rows) as numpy arrays trimmed to n_rows."""
+        n = int(self.n_rows.item())
+        return self.row_ids[:n].cpu().numpy(), self.rows[:n].cpu().numpy()
+
+
+def tensair_embed(table, dim: int, ids, out, scale=1.0, status=None, stream=None):
+    """table: [vocab, >= dim] float32 or bfloat16; ids: int32 [n]; out: [n, >= dim] float32 or bfloat16."""
+    n = ids.numel()
+    tp, td, ts = _matrix(table, table.shape[0], dim, "table")
+    op, od, os_ = _matrix(out, n, dim, "out")
+    _check(lib().tensair_embed(tp, td, table.shape[0], dim, ts, _ids(ids), n, scale, op, od, os_, _ptr(status), _stream(stream)))
+
+
+def tensair_embed_workspace_bytes(vocab: int, dim: int, n: int) -> int:
+    nbytes = lib().tensair_embed_workspace_bytes(vocab, dim, n)
+    if nbytes == 0:
+        raise TensairError(EINVAL, lib().tensair_last_error().decode())
+    return nbytes
+
+
+def tensair_embed_grad(ids, d_out, dim: int, vocab: int, grad, workspace, scale=1.0, status=None, stream=None):
+    """grad: RowBuffers, or (n_rows int32 [1], row_ids int32 [capacity], rows float32 [capacity, dim])."""
+    n_rows, row_ids, rows = grad
+    n, cap = ids.numel(), row_ids.numel()
+    dp, dd, ds = _matrix(d_out, n, dim, "d_out")
+    if rows.dtype != torch.float32 or tuple(rows.shape) != (cap, dim) or not rows.is_contiguous():
+        raise TensairError(EINVAL, f"grad: expected contiguous float32 rows of shape ({cap}, {dim})")
+    c = SparseRows(cap, _vector(n_rows, 1, torch.int32, "n_rows"), _ids(row_ids, "row_ids"), rows.data_ptr())
+    _check(lib().tensair_embed_grad(_ids(ids), n, dp, dd, ds, vocab, dim, scale, C.byref(c), workspace.data_ptr(),
+                                    workspace.numel() * workspace.element_size(), _ptr(status), _stream(stream)))
+
+
+def tensair_embed_grad_dense(ids, d_out, dim: int, grad, workspace, scale=1.0, accumulate=False, status=None, stream=None):
+    """grad: [vocab, >= dim] float32 or bfloat16, overwritten or, with accumulate, added to."""
+    n, vocab = ids.numel(), grad.shape[0]
+    dp, dd, ds = _matrix(d_out, n, dim, "d_out")
+    gp, gd, gs = _matrix(grad, vocab, dim, "grad")
+    _check(lib().tensair_embed_grad_dense(_ids(ids), n, dp, dd, ds, vocab, dim, scale, gp, gd, gs, int(accumulate), workspace.data_ptr(),
+                                          workspace.numel() * workspace.element_size(), _ptr(status), _stream(stream)))
+
+
+def tensair_softmax_workspace_bytes(n: int, vocab: int, dim: int, dtype, with_grad: bool) -> int:
+    """dtype: torch.float32 or torch.bfloat16."""
+    nbytes = lib().tensair_softmax_workspace_bytes(n, vocab, dim, _dtype(dtype, "dtype"), int(with_grad))
+    if nbytes == 0:
+        raise TensairError(EINVAL, lib().tensair_last_error().decode())
+    return nbytes
+
+
+def tensair_softmax_loss(hidden, table, dim: int, labels, loss, lse, workspace, scale=1.0, ignore_label=-1, status=None, stream=None):
+    """hidden: [n, >= dim], table: [vocab, >= dim] of one type; labels: int32 [n]; loss, lse: float32 [n]."""
+    n, vocab = labels.numel(), table.shape[0]
+    hp, hd, hs = _matrix(hidden, n, dim, "hidden")
+    tp, td, ts = _matrix(table, vocab, dim, "table")
+    if hd != td:
+        raise TensairError(EINVAL, "hidden and table must have one type")
+    _check(lib().tensair_softmax_loss(hp, hs, tp, ts, td, n, vocab, dim, _ids(labels, "labels"), ignore_label, scale,
+                                      _vector(loss, n, torch.float32, "loss"), _vector(lse, n, torch.float32, "lse"), workspace.data_ptr(),
+                                      workspace.numel() * workspace.element_size(), _ptr(status), _stream(stream)))
+
+
+def tensair_softmax_grad(hidden, table, dim: int, labels, lse, d_loss, d_hidden, d_table, workspace, scale=1.0, ignore_label=-1,
+                         status=None, stream=None):
+    """lse: as tensair_softmax_loss gave it; d_loss: float32 [n]; d_hidden, d_table: like hidden and table, or None."""
+    n, vocab = labels.numel(), table.shape[0]
+    hp, hd, hs = _matrix(hidden, n, dim, "hidden")
+    tp, td, ts = _matrix(table, vocab, dim, "table")
+    dhp, dhd, dhs = _matrix(d_hidden, n, dim, "d_hidden") if d_hidden is not None else (None, td, dim)
+    dtp, dtd, dts = _matrix(d_table, vocab, dim, "d_table") if d_table is not None else (None, td, dim)
+    if not hd == td == dhd == dtd:
+        raise TensairError(EINVAL, "hidden, table and their gradients must have one type")
+    _check(lib().tensair_softmax_grad(hp, hs, tp, ts, td, n, vocab, dim, _ids(labels, "labels"), ignore_label, scale,
+                                      _vector(lse, n, torch.float32, "lse"), _vector(d_loss, n, torch.float32, "d_loss"), dhp, dhs, dtp, dts,
+                                      workspace.data_ptr(), workspace.numel() * workspace.element_size(), _ptr(status), _stream(stream)))
+
+
+def _adamw_tensors(tensors):
+    """(C array, state dtype) of a list of dicts: param, grad, m, v, for 8-bit states m_scale and v_scale, and on request
+    param_copy (bfloat16) and weight_decay."""
+    arr = (AdamwTensor * max(len(tensors), 1))()
+    state = None
+    for k, t in enumerate(tensors):
+        n, s = t["param"].numel(), _dtype(t["m"], f"tensor {k}: m")
+        if state is None:
+            state = s
+        scales = [t.get("m_scale"), t.get("v_scale")] if s == FP8 else []
+        if s == BF16 or s != state or t["v"].dtype != t["m"].dtype:
+            raise TensairError(EINVAL, f"tensor {k}: all states are float32 or all float8_e4m3fn")
+        if any(x is None for x in scales):
+            raise TensairError(EINVAL, f"tensor {k}: 8-bit states need scales")
+        groups = -(-n // 256)
+        for name, x, size in [(w, t[w], n) for w in ("grad", "m", "v")] + [("scales", x, groups) for x in scales] + \
+                ([("param_copy", t["param_copy"], n)] if t.get("param_copy") is not None else []):
+            if x.numel() != size or not x.is_contiguous():
+                raise TensairError(EINVAL, f"tensor {k}: {name}: expected {size} contiguous elements")
+        if not t["param"].is_contiguous() or any(x.dtype != torch.float32 for x in scales) or \
+                (t.get("param_copy") is not None and t["param_copy"].dtype != torch.bfloat16):
+            raise TensairError(EINVAL, f"tensor {k}: param must be contiguous, scales float32, param_copy bfloat16")
+        a = arr[k]
+        a.param, a.grad, a.m, a.v = (t[w].data_ptr() for w in ("param", "grad", "m", "v"))
+        a.m_scale, a.v_scale = (x.data_ptr() for x in scales) if scales else (None, None)
+        a.param_copy = t["param_copy"].data_ptr() if t.get("param_copy") is not None else None
+        a.n, a.param_dtype, a.grad_dtype = n, _dtype(t["param"], f"tensor {k}: param"), _dtype(t["grad"], f"tensor {k}: grad")
+        a.weight_decay = t.get("weight_decay", 0.0)
+    return arr, F32 if state is None else state
+
+
+def tensair_adamw_workspace_bytes(tensors) -> int:
+    arr, state = _adamw_tensors(tensors)
+    nbytes = lib().tensair_adamw_workspace_bytes(arr, len(tensors), state)
+    if nbytes == 0:
+        raise TensairError(EINVAL, lib().tensair_last_error().decode())
+    return nbytes
+
+
+def tensair_adamw_init(tensors, workspace, stream=None):
+    arr, state = _adamw_tensors(tensors)
+    h = C.c_void_p()
+    _check(lib().tensair_adamw_init(C.byref(h), arr, len(tensors), state, _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                    _stream(stream)))
+    return h
+
+
+def tensair_adamw_step(h, lr: float, step: int, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None, stream=None):
+    """grad_scale: float32 tensor of one element that the gradients are multiplied by, or None."""
+    _check(lib().tensair_adamw_step(h, lr, step, beta1, beta2, eps, _ptr(grad_scale), _stream(stream)))
+
+
+def tensair_adamw_destroy(h):
+    _check(lib().tensair_adamw_destroy(h))
+
+
+class AdamW:
+    """Owns the handle and the workspace of an optimizer over a list of tensors and keeps the tensors alive (their gradients are
+    read where they are when this is made)."""
+
+    def __init__(self, tensors, stream=None):
+        self.h = None
+        self.tensors = [dict(t) for t in tensors]
+        nbytes = tensair_adamw_workspace_bytes(self.tensors)
+        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.tensors[0]["param"].device)
+        self.h = tensair_adamw_init(self.tensors, self.workspace, stream)
+
+    def step(self, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None, stream=None):
+        tensair_adamw_step(self.h, lr, step, beta1, beta2, eps, grad_scale, stream)
+
+    def close(self):
+        if self.h is not None:
+            tensair_adamw_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 def tensair_status(h, stream=None):
