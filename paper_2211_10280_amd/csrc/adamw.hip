@@ -118,7 +118,7 @@ __device__ __forceinline__ float4 from_fp8(u32 c, float s)
     return make_float4(a.x * s, a.y * s, b.x * s, b.y * s);
 }
 // the factor that takes a group of this largest magnitude to the 8-bit float's range; below 2^-100 the group is zero
-__device__ __forceinline__ float to_range(float largest) { return largest >= 0x1p-100f || largest != largest ? 448.0f / largest : 0.0f; }
+__device__ __forceinline__ float to_range(float largest) { return largest >= 0x1p-100f || largest != largest ? (1.0f / largest) * 448.0f : 0.0f; }
 
 // the root's 8 bits: x in units of the scale, cut to 3 mantissa bits after `offset` (20 bits) was added below them
 __device__ __forceinline__ u32 root_code(float x, u32 offset)

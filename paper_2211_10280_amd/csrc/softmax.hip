@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_logits(LogitsArgs a)
     const int strip = work / a.token_tiles, tt = work % a.token_tiles;
     const int wave = uniform((int)(threadIdx.x >> 6)), wm = wave / WN, wn = wave % WN, lane = lane_id();
     const i64 tok0 = (i64)tt * P::BN;
-    const int t0 = strip * a.per, t1 = min(a.tiles, t0 + a.per);
+    const int t0 = strip * a.per, t1 = min(a.tiles, t0 + a.per), steps = a.ksteps * a.nseg;
     P p;
     float top[TN], sum[TN], l2[TN], d[TN];
     int label[TN];
@@ -214,24 +214,21 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_logits(LogitsArgs a)
     p.b.load(a.h, part_b(0, a.nseg), tok0, 0);
     for (int t = t0; t < t1; ++t, word += P::BM) {
         p.clear();
-        for (int seg = 0; seg < a.nseg; ++seg)
-            for (int k = 0; k < a.ksteps; ++k) {
-                p.stage(lds);
-                int nk = k + 1, ns = seg;
-                i64 nw = word;
-                if (nk == a.ksteps) {
-                    nk = 0;
-                    if (++ns == a.nseg) {
-                        ns = 0;
-                        nw += P::BM;
-                    }
+        int k = 0, seg = 0;
+        for (int s = 0; s < steps; ++s) {
+            p.stage(lds);
+            i64 next = word;
+            if (++k == a.ksteps) {
+                k = 0;
+                if (++seg == a.nseg) {
+                    seg = 0;
+                    next += P::BM;                            // behind the strip's last a tile is loaded that nobody uses
                 }
-                if (nw == word || t + 1 < t1) {
-                    p.a.load(a.w, part_a(ns, a.nseg), nw, (i64)nk * BK);
-                    p.b.load(a.h, part_b(ns, a.nseg), tok0, (i64)nk * BK);
-                }
-                p.multiply(lds, wm, wn);
             }
+            p.a.load(a.w, part_a(seg, a.nseg), next, (i64)k * BK);
+            p.b.load(a.h, part_b(seg, a.nseg), tok0, (i64)k * BK);
+            p.multiply(lds, wm, wn);
+        }
         const i64 w0 = word + wm * TM * 32;
         const bool whole = word + P::BM <= a.V;
         if constexpr (!GRAD) {
@@ -380,21 +377,20 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_product(ProductArgs a)
     p.clear();
     p.a.load(a.a, part_a(0, a.nseg), m0, k0);
     p.b.load(a.b, part_b(0, a.nseg), n0, k0);
-    for (int seg = 0; seg < a.nseg; ++seg)
-        for (i64 k = k0; k < k1; k += BK) {
-            p.stage(lds);
-            i64 nk = k + BK;
-            int ns = seg;
-            if (nk >= k1) {
-                nk = k0;
-                ++ns;
-            }
-            if (ns < a.nseg) {
-                p.a.load(a.a, part_a(ns, a.nseg), m0, nk);
-                p.b.load(a.b, part_b(ns, a.nseg), n0, nk);
-            }
-            p.multiply(lds, wm, wn);
+    const int steps = (int)((k1 - k0) / BK) * a.nseg;
+    int seg = 0;
+    i64 k = k0;
+    for (int s = 0; s < steps; ++s) {
+        p.stage(lds);
+        k += BK;
+        if (k >= k1) {
+            k = k0;
+            seg = min(seg + 1, a.nseg - 1);                   // behind the last step a tile is loaded that nobody uses
         }
+        p.a.load(a.a, part_a(seg, a.nseg), m0, k);
+        p.b.load(a.b, part_b(seg, a.nseg), n0, k);
+        p.multiply(lds, wm, wn);
+    }
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
         const i64 n = n0 + (wn * TN + j) * 32 + (lane & 31);
