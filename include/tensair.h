@@ -401,7 +401,7 @@ int tensair_embed_grad_dense(const int32_t *ids, int64_t n, const void *d_out, i
 
 /* Softmax cross entropy against every row of a table (what negative sampling stands in for), with
  *   z[i][v] = scale * <hidden[i], table[v]>,  lse[i] = log sum_v exp z[i][v],  loss[i] = lse[i] - z[i][labels[i]].
- * The logits are never kept.  A label equal to ignore_label gives loss 0; so does one outside [0, vocab), which also sets the
+ * scale: finite, not 0.  The logits are never kept.  A label equal to ignore_label gives loss 0; so does one outside [0, vocab), which also sets the
  * status bit.  hidden and table have the same type; loss and lse: DEVICE fp32 [n].
  * fp32 inputs are multiplied with the precision of fp32; n <= TENSAIR_MAX_TOKENS, vocab <= TENSAIR_MAX_VOCAB.
  * tensair_softmax_grad: for the gradient d_loss (DEVICE fp32 [n]) of the losses, with p = exp(z - lse),

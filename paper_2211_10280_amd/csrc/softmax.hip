@@ -8,7 +8,9 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstring>
+#include <type_traits>
 
 #include "../../include/tensair.h"
 #include "dev_common.h"
@@ -22,16 +24,27 @@ typedef short bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef u32 v4u __attribute__((ext_vector_type(4)));
 
+#ifndef PRIO
+#define PRIO(x)
+#endif
+#define SM_BM 256              // words of a tile of logits
 #define LOG2E 1.44269504088896340736f
 #define LN2 0.69314718055994530942f
-#define BK 64                  // elements of the summed index per step
-#define T_PAD 32               // elements behind a row of a tile kept by rows of the summed index: four rows, four groups of banks
 
-// A matrix of bfloat16 parts in memory.
+// A matrix of bfloat16 parts in memory, in blocks of 32 columns: a block is its rows one after the other, 64 bytes each.  So the
+// tile of a step is whole lines of memory whichever of its indices is summed, and so is what a wave writes of dz (rows of 64 bytes
+// a row's pitch apart were fetched at half the rate).
+#define BK 32                  // columns of a block, and of the summed index per step
 struct Operand {
     const bf16_t *p;
-    i64 pitch, plane;          // elements from row to row, from part to part
-    i64 rows, cols;
+    i64 rows, plane;           // rows of a block, elements from part to part
+    __device__ __forceinline__ const bf16_t *at(int part, i64 r, i64 c) const { return p + part * plane + (c / BK) * (rows * BK) + r * BK + (c & (BK - 1)); }
+    // the bytes from there to the part's end
+    __device__ __forceinline__ u32 left(i64 r, i64 c) const
+    {
+        const i64 n = (plane - ((c / BK) * (rows * BK) + r * BK + (c & (BK - 1)))) * 2;
+        return (u32)(n < 0 ? 0 : n > 0x7FFFFFF0 ? 0x7FFFFFF0 : n);
+    }
 };
 // which parts of either operand a product's segment takes, two bits each: (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
 #define PARTS_A 0x052u         // 2 0 1 1 0 0
@@ -39,60 +52,68 @@ struct Operand {
 __device__ __forceinline__ int part_a(int seg, int nseg) { return nseg == 1 ? 0 : (int)(PARTS_A >> (2 * seg)) & 3; }
 __device__ __forceinline__ int part_b(int seg, int nseg) { return nseg == 1 ? 0 : (int)(PARTS_B >> (2 * seg)) & 3; }
 
-// the bytes of a buffer that begins at row r, column c
-__device__ __forceinline__ u32 bytes_left(const Operand &o, i64 r, i64 c)
-{
-    const i64 n = r < o.rows ? ((o.rows - 1 - r) * o.pitch + o.cols - c) * 2 : 0;
-    return (u32)(n < 0 ? 0 : n > 0x7FFFFFF0 ? 0x7FFFFFF0 : n);
-}
-
-// The tile of one operand of one step, ROWS of the kept index by BK of the summed one, from memory into registers and from there
-// into LDS.  By rows of the kept index (T = false): rows of 128 bytes whose chunks of 16 change places by the row's number, so
-// that the 32 lanes of a fragment spread over the banks.  By rows of the summed index (T = true): as in memory, padded;
-// fragments are read with the transposing load.  What lies outside the matrix comes as zero.
+// The tile of one operand of one step, ROWS of the kept index by BK of the summed one, from memory straight into LDS, 16 bytes
+// a lane.  LDS holds it in the order of the lanes, so what keeps the 32 lanes of a fragment off each other's banks is which chunk
+// of 16 bytes a lane fetches.
+// By rows of the kept index (T = false): a row is BK elements, its chunks change places by the row's number.
+// By rows of the summed index (T = true): as in memory, a row's chunks turned round by its number, so that the four rows that
+// the transposing load takes lie in four groups of banks.  What lies outside the matrix comes as zero.
 template <int ROWS, int THREADS, bool T>
 struct Tile {
-    static constexpr int CHUNKS = ROWS * BK / 8, PER = CHUNKS / THREADS;
-    static constexpr int PITCH = T ? ROWS + T_PAD : BK;       // elements
-    static constexpr int LDS = (T ? BK : ROWS) * PITCH;       // elements
-    static_assert(CHUNKS % THREADS == 0, "");
-    v4u r[PER];
+    static constexpr int CHUNKS = ROWS * BK / 8, PER = (CHUNKS + THREADS - 1) / THREADS;
+    static constexpr int CPR = T ? ROWS / 8 : BK / 8;         // chunks of a row
+    static constexpr int LDS = ROWS * BK;                     // elements
+    static_assert(CHUNKS % WAVE == 0, "");                   // where the chunks do not go round, some are fetched twice
+    int offset[PER];           // of the lane's chunks from the tile's first element, in bytes
 
-    __device__ __forceinline__ void load(const Operand &o, int part, i64 row0, i64 k0)
+    static __device__ __forceinline__ int turn(int row)       // chunks that a row is turned by, or its mask of the places
+    {
+        if (!T) return (row >> 2) & 3;
+        return CPR % 16 == 0 ? 4 * (row & 3) : 4 * ((row >> 1) & 1);
+    }
+    __device__ __forceinline__ void place(const Operand &o)
+    {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int q = ((int)threadIdx.x + j * THREADS) % CHUNKS, row = q / CPR, at = q % CPR;
+            int c = T ? at - turn(row) : at ^ turn(row);
+            if (c < 0) c += CPR;
+            offset[j] = (int)(((u32)(8 * c / BK) * (u32)o.rows + (u32)row) * BK + (8 * c & (BK - 1))) * 2;
+        }
+    }
+    typedef __amdgpu_buffer_rsrc_t Source;
+    static __device__ __forceinline__ Source source(const Operand &o, int part, i64 row0, i64 k0)
     {
         const i64 r0 = T ? k0 : row0, c0 = T ? row0 : k0;
-        const bf16_t *base = o.p + part * o.plane + r0 * o.pitch + c0;
-        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)bytes_left(o, r0, c0), 0x00027000);
-#pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const int q = (int)threadIdx.x + j * THREADS;
-            const int row = T ? q / (ROWS / 8) : q / 8, c = T ? q % (ROWS / 8) : q % 8;
-            r[j] = __builtin_amdgcn_raw_buffer_load_b128(rs, (int)((u32)row * (u32)o.pitch + 8u * c) * 2, 0, 0);
-        }
+        return __builtin_amdgcn_make_buffer_rsrc((void *)o.at(part, r0, c0), 0, (int)o.left(r0, c0), 0x00027000);
     }
-    __device__ __forceinline__ void store(bf16_t *lds) const
+    __device__ __forceinline__ void fetch(Source from, int j, bf16_t *__restrict lds, int wave) const
+    {
+#ifdef __HIP_DEVICE_COMPILE__      // the host's pass does not know the 16-byte form and would leave the kernels' handles out
+        typedef __attribute__((address_space(3))) void lds_void;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void *)(lds + (j * THREADS + wave * WAVE) % CHUNKS * 8), 16, offset[j], 0, 0, 0);
+#endif
+    }
+    __device__ __forceinline__ void fetch_all(Source from, bf16_t *__restrict lds, int wave) const
     {
 #pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const int q = (int)threadIdx.x + j * THREADS;
-            const int row = T ? q / (ROWS / 8) : q / 8, c = T ? q % (ROWS / 8) : q % 8;
-            const int at = T ? row * PITCH + 8 * c : row * PITCH + 8 * (c ^ (row & 7));
-            *(v4u *)(lds + at) = r[j];
-        }
+        for (int j = 0; j < PER; ++j) fetch(from, j, lds, wave);
     }
     // the fragment of 32 rows from `row` on, 16 of the summed index from 16 * kk on: lane l holds row l % 32, 8 * (l / 32) and on
-    static __device__ __forceinline__ hw_bf16x8 fragment(const bf16_t *lds, int row, int kk)
+    static __device__ __forceinline__ hw_bf16x8 fragment(const bf16_t *__restrict lds, int row, int kk)
     {
         const int lane = lane_id();
         if constexpr (!T) {
             const int m = row + (lane & 31), c = 2 * kk + (lane >> 5);
-            return *(const hw_bf16x8 *)(lds + m * PITCH + 8 * (c ^ (m & 7)));
+            return *(const hw_bf16x8 *)(lds + m * BK + 8 * (c ^ turn(m)));
         } else {
             typedef __attribute__((address_space(3))) bf16x4 lds4;
-            const int g = lane >> 4, i = lane & 15;
-            const bf16_t *at = lds + (16 * kk + 8 * (g >> 1) + (i >> 2)) * PITCH + row + 16 * (g & 1) + 4 * (i & 3);
+            const int g = lane >> 4, i = lane & 15, k = 16 * kk + 8 * (g >> 1) + (i >> 2);
+            int c = row / 8 + 2 * (g & 1) + ((i & 3) >> 1) + turn(k);          // the same for k + 4
+            if (c >= CPR) c -= CPR;
+            const bf16_t *at = lds + k * ROWS + 8 * c + 4 * (i & 1);
             const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)at);
-            const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(at + 4 * PITCH));
+            const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(at + 4 * ROWS));
             const bf16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
             return __builtin_bit_cast(hw_bf16x8, v);
         }
@@ -101,47 +122,68 @@ struct Tile {
 
 // A workgroup's tile of a product: BM of A's rows by BN of B's, WM by WN waves of TM by TN fragments of 32 by 32.  Lane l of a
 // fragment holds the column (B's row) l % 32 and the rows (A's) 8 (r / 4) + 4 (l / 32) + r % 4 in its 16 registers r.
-template <int TM, int TN, int WM, int WN, bool AT, bool BT>
+template <int TM, int TN, int WM, int WN, int STAGES, bool AT, bool BT>
 struct Product {
     static constexpr int THREADS = 64 * WM * WN, BM = 32 * TM * WM, BN = 32 * TN * WN;
     typedef Tile<BM, THREADS, AT> A;
     typedef Tile<BN, THREADS, BT> B;
-    static constexpr int LDS = A::LDS + B::LDS;               // elements
+    static constexpr int LDS = A::LDS + B::LDS;               // elements of a stage
     f32x16 acc[TM][TN];
     A a;
     B b;
 
-    __device__ __forceinline__ void clear()
+    static __device__ __forceinline__ void fragments_a(const bf16_t *__restrict lds, int wm, int kk, hw_bf16x8 (&f)[TM])
     {
 #pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+        for (int i = 0; i < TM; ++i) f[i] = A::fragment(lds, (wm * TM + i) * 32, kk);
     }
-    // the registers' tiles into LDS, once every wave is done with what is there
-    __device__ __forceinline__ void stage(bf16_t *lds)
+    static __device__ __forceinline__ void fragments_b(const bf16_t *__restrict lds, int wn, int kk, hw_bf16x8 (&f)[TN])
     {
-        __syncthreads();
-        a.store(lds);
-        b.store(lds + A::LDS);
-        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < TN; ++j) f[j] = B::fragment(lds, (wn * TN + j) * 32, kk);
     }
-    __device__ __forceinline__ void multiply(const bf16_t *lds, int wm, int wn)
+    // Waits for all but the last N of this wave's fetches, which come back in order, and for its reads of LDS, then for the other waves.
+    template <int N>
+    static __device__ __forceinline__ void meet()
     {
+        static_assert(N < 64, "");
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | ((N >> 4) << 14));
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    }
+    // One step with STAGES tiles in LDS, that of the step itself in `cur`, of a sum that begins here (FIRST) or goes on: the tiles of the
+    // step STAGES - 1 later set out into `next`; fragments of 16 of the summed index are read while those before are multiplied; in
+    // the end the next step's tiles are there, and every wave is done with these.
+    template <bool FIRST>
+    __device__ __forceinline__ void step(typename A::Source from_a, typename B::Source from_b, bf16_t *__restrict next, const bf16_t *__restrict cur,
+                                         int wave, int wm, int wn)
+    {
+        constexpr int KK = BK / 16;
+        a.fetch_all(from_a, next, wave);
+        b.fetch_all(from_b, next + A::LDS, wave);
+        __builtin_amdgcn_sched_barrier(0);
+        hw_bf16x8 fa[2][TM], fb[2][TN];
+        f32x16 zero;
 #pragma unroll
-        for (int kk = 0; kk < BK / 16; ++kk) {
-            hw_bf16x8 fa[TM], fb[TN];
+        for (int r = 0; r < 16; ++r) zero[r] = 0.f;
+        fragments_a(cur, wm, 0, fa[0]);
+        fragments_b(cur + A::LDS, wn, 0, fb[0]);
 #pragma unroll
-            for (int i = 0; i < TM; ++i) fa[i] = A::fragment(lds, (wm * TM + i) * 32, kk);
-#pragma unroll
-            for (int j = 0; j < TN; ++j) fb[j] = B::fragment(lds + A::LDS, (wn * TN + j) * 32, kk);
+        for (int kk = 0; kk < KK; ++kk) {
+            if (kk + 1 < KK) {
+                fragments_a(cur, wm, kk + 1, fa[(kk + 1) & 1]);
+                fragments_b(cur + A::LDS, wn, kk + 1, fb[(kk + 1) & 1]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+                for (int j = 0; j < TN; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[kk & 1][i], fb[kk & 1][j], FIRST && kk == 0 ? zero : acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        meet<(STAGES - 2) * (A::PER + B::PER)>();
     }
 };
 
@@ -155,23 +197,26 @@ __device__ __forceinline__ int die_order(int b, int n)
 // ---------------------------------------------------------------- logits
 struct LogitsArgs {
     Operand w, h;              // words' and tokens' rows
-    int nseg, ksteps;
+    int nseg, K;
     i64 word0, V;              // first word of this launch's range; words in all
     int tiles, per, strips;    // tiles of words of the range, of a strip; strips
     int token_tiles;
     i64 Np;
-    float c;                   // scale * log2(e)
+    float c;                   // |scale| * log2(e): the scale's sign went into the tokens' rows
     const int *label;          // [Np], -1: none
     // loss
     float2 *part;              // [strips * WM][Np] maximum, sum (of powers of two)
     float *picked;             // [Np] the label's logit, in units of log 2
     // gradient
     const float *lse2, *d;     // [Np]
-    bf16_t *dz;                // [parts][Np][pitch]
-    i64 dz_pitch, dz_plane;
+    bf16_t *dz;                // an Operand: rows are tokens, columns words
+    i64 dz_plane;
 };
 
-__device__ __forceinline__ u32 pack2(float a, float b) { return (u32)f32_to_bf16(a) | ((u32)f32_to_bf16(b) << 16); }
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+// two floats rounded to nearest even, in one instruction
+__device__ __forceinline__ u32 pack2(float a, float b) { return __builtin_bit_cast(u32, __builtin_convertvector(f32x2{a, b}, bf16x2)); }
 
 // the four registers of a group of 4 rows from this lane and its partner 32 lanes on: 8 rows that follow one another (lanes below
 // 32: of group x, the others: of group y), as bfloat16
@@ -185,16 +230,16 @@ __device__ __forceinline__ v4u join_halves(u32 x0, u32 x1, u32 y0, u32 y1)
 
 // GRAD false: the running maximum and sum of every token over a strip of words; true: dz of the strip, in PARTS bfloat16 parts.
 // A strip's tiles follow one another without a pause: the next tile's first step is in flight while this one's logits are used.
-template <int TM, int TN, int WM, int WN, bool GRAD, int PARTS>
+template <int TM, int TN, int WM, int WN, int STAGES, bool GRAD, int PARTS>
 __global__ void __launch_bounds__(64 * WM * WN, 2) k_logits(LogitsArgs a)
 {
-    typedef Product<TM, TN, WM, WN, false, false> P;
-    __shared__ __attribute__((aligned(16))) bf16_t lds[P::LDS];
+    typedef Product<TM, TN, WM, WN, STAGES, false, false> P;
+    __shared__ __attribute__((aligned(16))) bf16_t lds[P::LDS * STAGES];
     const int work = die_order((int)blockIdx.x, (int)gridDim.x);
     const int strip = work / a.token_tiles, tt = work % a.token_tiles;
     const int wave = uniform((int)(threadIdx.x >> 6)), wm = wave / WN, wn = wave % WN, lane = lane_id();
     const i64 tok0 = (i64)tt * P::BN;
-    const int t0 = strip * a.per, t1 = min(a.tiles, t0 + a.per), steps = a.ksteps * a.nseg;
+    const int t0 = strip * a.per, t1 = min(a.tiles, t0 + a.per), steps = (a.K / BK) * a.nseg;
     P p;
     float top[TN], sum[TN], l2[TN], d[TN];
     int label[TN];
@@ -210,27 +255,46 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_logits(LogitsArgs a)
         }
     }
     i64 word = a.word0 + (i64)t0 * P::BM;
-    p.a.load(a.w, part_a(0, a.nseg), word, 0);
-    p.b.load(a.h, part_b(0, a.nseg), tok0, 0);
-    for (int t = t0; t < t1; ++t, word += P::BM) {
-        p.clear();
-        int k = 0, seg = 0;
-        for (int s = 0; s < steps; ++s) {
-            p.stage(lds);
-            i64 next = word;
-            if (++k == a.ksteps) {
-                k = 0;
-                if (++seg == a.nseg) {
-                    seg = 0;
-                    next += P::BM;                            // behind the strip's last a tile is loaded that nobody uses
-                }
+    p.a.place(a.w);
+    p.b.place(a.h);
+    // the step to be fetched next: tile of words, part, place in the rows; behind the strip's last nobody uses it
+    i64 fetch_word = (i64)t0 * P::BM;                         // of the range
+    int k = 0, seg = 0, cur = 0;
+    auto advance = [&] {
+        if ((k += BK) == a.K) {
+            k = 0;
+            if (++seg == a.nseg) {
+                seg = 0;
+                fetch_word += P::BM;
             }
-            p.a.load(a.w, part_a(seg, a.nseg), next, (i64)k * BK);
-            p.b.load(a.h, part_b(seg, a.nseg), tok0, (i64)k * BK);
-            p.multiply(lds, wm, wn);
         }
+    };
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) {
+        p.a.fetch_all(P::A::source(a.w, part_a(seg, a.nseg), fetch_word, k), lds + s * P::LDS, wave);
+        p.b.fetch_all(P::B::source(a.h, part_b(seg, a.nseg), tok0, k), lds + s * P::LDS + P::A::LDS, wave);
+        advance();
+    }
+    __syncthreads();
+    for (int t = t0; t < t1; ++t, word += P::BM) {
+        auto step = [&](auto first) {
+            p.template step<first()>(P::A::source(a.w, part_a(seg, a.nseg), fetch_word, k), P::B::source(a.h, part_b(seg, a.nseg), tok0, k),
+                                     lds + (cur == 0 ? STAGES - 1 : cur - 1) * P::LDS, lds + cur * P::LDS, wave, wm, wn);
+            advance();
+            cur = cur == STAGES - 1 ? 0 : cur + 1;
+        };
+        step(std::true_type{});
+        for (int s = 1; s < steps; ++s) step(std::false_type{});
         const i64 w0 = word + wm * TM * 32;
-        const bool whole = word + P::BM <= a.V;
+        if (word + P::BM > a.V) {                             // words that are none: no share in any sum
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (w0 + 32 * i + 8 * (r / 4) + 4 * (lane >> 5) + r % 4 >= a.V)
+#pragma unroll
+                        for (int j = 0; j < TN; ++j) p.acc[i][j][r] = -INFINITY;
+        }
         if constexpr (!GRAD) {
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
@@ -245,26 +309,21 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_logits(LogitsArgs a)
                                 a.picked[tok0 + (wn * TN + j) * 32 + (lane & 31)] = p.acc[i][j][r] * a.c;
                     }
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        float z = p.acc[i][j][r] * a.c;
-                        if (!whole && w0 + 32 * i + 8 * (r / 4) + 4 * (lane >> 5) + r % 4 >= a.V) z = -INFINITY;
-                        p.acc[i][j][r] = z;
-                        best = fmaxf(best, z);
-                    }
+                    for (int r = 0; r < 16; ++r) best = fmaxf(best, p.acc[i][j][r]);
                 }
-                const float now = fmaxf(best, top[j]), ref = now == -INFINITY ? 0.f : now;
+                const float now = fmaxf(best * a.c, top[j]), ref = now == -INFINITY ? 0.f : now;
                 float s = sum[j] * __builtin_amdgcn_exp2f(top[j] - ref);
 #pragma unroll
                 for (int i = 0; i < TM; ++i)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f(p.acc[i][j][r] - ref);
+                    for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f(fmaf(p.acc[i][j][r], a.c, -ref));
                 top[j] = now;
                 sum[j] = s;
             }
         } else {
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
-                bf16_t *row = a.dz + (tok0 + (wn * TN + j) * 32 + (lane & 31)) * a.dz_pitch + (w0 - a.word0) + 8 * (lane >> 5);
+                bf16_t *row = a.dz + (tok0 + (wn * TN + j) * 32 + (lane & 31)) * BK + 8 * (lane >> 5);
 #pragma unroll
                 for (int i = 0; i < TM; ++i) {
                     const i64 lw = (i64)label[j] - (w0 + 32 * i);
@@ -278,17 +337,12 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_logits(LogitsArgs a)
                             if (lw == 8 * (r / 4) + 4 * (lane >> 5) + r % 4)
                                 g[r] = d[j] * (__builtin_amdgcn_exp2f(fmaf(p.acc[i][j][r], a.c, -l2[j])) - 1.0f);
                     }
-                    if (!whole) {
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (w0 + 32 * i + 8 * (r / 4) + 4 * (lane >> 5) + r % 4 >= a.V) g[r] = 0.f;
-                    }
 #pragma unroll
                     for (int part = 0; part < PARTS; ++part) {
                         u32 q[8];
 #pragma unroll
                         for (int r = 0; r < 8; ++r) q[r] = pack2(g[2 * r], g[2 * r + 1]);
-                        bf16_t *to = row + part * a.dz_plane + 32 * i;
+                        bf16_t *to = row + part * a.dz_plane + ((i64)t * (P::BM / BK) + wm * TM + i) * (a.Np * BK);
                         *(v4u *)to = join_halves(q[0], q[1], q[2], q[3]);
                         *(v4u *)(to + 16) = join_halves(q[4], q[5], q[6], q[7]);
                         if (part + 1 < PARTS)
@@ -313,6 +367,13 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_logits(LogitsArgs a)
     }
 }
 
+// a maximum and a sum of powers of two relative to it, joined by another pair
+__device__ __forceinline__ void join_sums(float &top, float &sum, float t, float s)
+{
+    const float now = fmaxf(top, t), ref = now == -INFINITY ? 0.f : now;
+    sum = sum * __builtin_amdgcn_exp2f(top - ref) + s * __builtin_amdgcn_exp2f(t - ref);
+    top = now;
+}
 // maxima and sums of the strips put together: a workgroup takes 64 tokens, its waves the strips in turn
 struct LossArgs {
     const float2 *part;
@@ -328,24 +389,211 @@ __global__ void __launch_bounds__(1024) k_loss(LossArgs a)
     const int lane = lane_id(), wave = (int)(threadIdx.x >> 6);
     const i64 i = (i64)blockIdx.x * WAVE + lane;
     float top = -INFINITY, sum = 0.f;
-    for (int s = wave; s < a.slots; s += 16) {
-        const float2 v = a.part[(i64)s * a.Np + i];
-        const float now = fmaxf(top, v.x), ref = now == -INFINITY ? 0.f : now;
-        sum = sum * __builtin_amdgcn_exp2f(top - ref) + v.y * __builtin_amdgcn_exp2f(v.x - ref);
-        top = now;
+    for (int s = wave; s < a.slots; s += 16 * 8) {
+        float2 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = s + 16 * k < a.slots ? a.part[(i64)(s + 16 * k) * a.Np + i] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) join_sums(top, sum, v[k].x, v[k].y);
     }
     other[wave][lane] = make_float2(top, sum);
     __syncthreads();
     if (wave > 0 || i >= a.n) return;
     for (int w = 1; w < 16; ++w) {
-        const float2 v = other[w][lane];
-        const float now = fmaxf(top, v.x), ref = now == -INFINITY ? 0.f : now;
-        sum = sum * __builtin_amdgcn_exp2f(top - ref) + v.y * __builtin_amdgcn_exp2f(v.x - ref);
-        top = now;
+        join_sums(top, sum, other[w][lane].x, other[w][lane].y);
     }
     const float lse = top + log2f(sum);
     a.lse[i] = lse * LN2;
     a.loss[i] = a.label[i] >= 0 ? (lse - a.picked[i]) * LN2 : 0.f;
+}
+
+// ---------------------------------------------------------------- few tokens
+// At most FEW_TOKENS tokens: nothing is laid out and no matrix instruction used; the words' rows are read once, where they are, and
+// both gradients are made while a row is held (the least that memory has to move: n = 1, a million rows of 300 bfloat16, STATED_FEW).
+// G lanes hold a word's row, ITERS chunks of 4 elements each, ROWS rows at a time; the tokens' rows lie in LDS, fp32.
+#define FEW_TOKENS 8
+#define FEW_BLOCKS 1024
+struct FewArgs {
+    const void *hidden, *table;
+    i64 hidden_stride, table_stride, V;
+    int n, C4;
+    float c, sign;             // |scale| log2(e); the scale's sign goes into the tokens' rows
+    const int *label;
+    // loss: a slot per workgroup
+    float2 *part;
+    float *picked;
+    i64 Np;
+    // gradient
+    const float *lse2, *d;
+    float *slots;              // [workgroups][n][4 * C4]
+    void *d_table;             // NULL: not wanted
+    i64 d_stride;
+    float scale;               // of d_table
+};
+template <int G>
+__device__ __forceinline__ float group_sum(float x)
+{
+    x += dpp_get<0xB1, 0xF>(x);
+    x += dpp_get<0x4E, 0xF>(x);
+    x += dpp_get<0x141, 0xF>(x);
+    x += dpp_get<0x140, 0xF>(x);
+    if (G >= 32) x += __shfl_xor(x, 16, WAVE);
+    if (G >= 64) x += __shfl_xor(x, 32, WAVE);
+    return x;
+}
+template <typename T, int G, int ITERS, int NT, bool GRAD>
+__global__ void __launch_bounds__(BLOCK) k_few(FewArgs a)
+{
+    constexpr int ROWS = GRAD ? 2 : 4, SIDE = WAVE / G, C = G * ITERS;
+    __shared__ float4 h[NT][C];
+    __shared__ float2 stats[WAVES_PER_BLOCK][NT];
+    const int lane = lane_id(), l = lane % G, side = lane / G, wave = uniform((int)(threadIdx.x >> 6));
+    for (int x = threadIdx.x; x < NT * C; x += BLOCK) {
+        const int t = x / C, c = x % C;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (t < a.n && c < a.C4 && (!GRAD || a.label[t] >= 0)) v = ld4((const T *)a.hidden + t * a.hidden_stride + 4 * c);
+        h[t][c] = make_float4(v.x * a.sign, v.y * a.sign, v.z * a.sign, v.w * a.sign);
+    }
+    int label[NT];
+    float l2[NT], d[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        label[t] = t < a.n ? a.label[t] : -1;
+        l2[t] = GRAD && t < a.n ? a.lse2[t] : 0.f;
+        d[t] = GRAD && t < a.n ? a.d[t] : 0.f;
+    }
+    float top = -INFINITY, sum = 0.f;                         // of the token of this lane's number
+    float4 dh[GRAD ? NT : 1][ITERS];
+#pragma unroll
+    for (int t = 0; t < (GRAD ? NT : 1); ++t) zero_row<ITERS>(dh[t]);
+    __syncthreads();
+    const i64 step = (i64)gridDim.x * WAVES_PER_BLOCK * (SIDE * ROWS);
+    for (i64 base = ((i64)blockIdx.x * WAVES_PER_BLOCK + wave) * (SIDE * ROWS); base < a.V; base += step) {
+        typename Raw4<T>::type w[ROWS][ITERS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const i64 row = base + r * SIDE + side;
+            zero_row_raw<ITERS>(w[r]);
+#pragma unroll
+            for (int it = 0; it < ITERS; ++it)
+                if (row < a.V && l + G * it < a.C4) w[r][it] = ldraw_s((const T *)a.table + row * a.table_stride + 4 * (l + G * it));
+        }
+        float z[ROWS][NT];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) z[r][t] = 0.f;
+#pragma unroll
+        for (int it = 0; it < ITERS; ++it)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const float4 x = h[t][l + G * it];
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) {
+                    const float4 y = widen4(w[r][it]);
+                    z[r][t] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, z[r][t]))));
+                }
+            }
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) z[r][t] = group_sum<G>(z[r][t]);
+        if constexpr (!GRAD) {
+            float mine[ROWS];
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const i64 row = base + r * SIDE + side;
+                mine[r] = z[r][0];
+#pragma unroll
+                for (int t = 1; t < NT; ++t)
+                    if (l == t) mine[r] = z[r][t];
+                mine[r] = row < a.V ? mine[r] * a.c : -INFINITY;
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+                    if (l == t && row == label[t]) a.picked[t] = mine[r];
+            }
+            float best = mine[0];
+#pragma unroll
+            for (int r = 1; r < ROWS; ++r) best = fmaxf(best, mine[r]);
+            const float now = fmaxf(best, top), ref = now == -INFINITY ? 0.f : now;
+            sum *= __builtin_amdgcn_exp2f(top - ref);
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) sum += __builtin_amdgcn_exp2f(mine[r] - ref);
+            top = now;
+        } else {
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const i64 row = base + r * SIDE + side;
+                float g[NT];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    float p = __builtin_amdgcn_exp2f(fmaf(z[r][t], a.c, -l2[t]));
+                    if (row == label[t]) p -= 1.0f;
+                    g[t] = label[t] >= 0 && row < a.V ? d[t] * p : 0.f;
+                }
+#pragma unroll
+                for (int it = 0; it < ITERS; ++it) {
+                    const float4 y = widen4(w[r][it]);
+                    float4 dw = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const float4 x = h[t][l + G * it];
+                        dw = make_float4(fmaf(g[t], x.x, dw.x), fmaf(g[t], x.y, dw.y), fmaf(g[t], x.z, dw.z), fmaf(g[t], x.w, dw.w));
+                        float4 &e = dh[t][it];
+                        e = make_float4(fmaf(g[t], y.x, e.x), fmaf(g[t], y.y, e.y), fmaf(g[t], y.z, e.z), fmaf(g[t], y.w, e.w));
+                    }
+                    if (a.d_table && row < a.V && l + G * it < a.C4) {
+                        dw = make_float4(dw.x * a.scale, dw.y * a.scale, dw.z * a.scale, dw.w * a.scale);
+                        st4s((T *)a.d_table + row * a.d_stride + 4 * (l + G * it), dw);
+                    }
+                }
+            }
+        }
+    }
+    if constexpr (!GRAD) {
+        // the lanes of a token: one of every group
+#pragma unroll
+        for (int o = G; o < WAVE; o <<= 1) join_sums(top, sum, __shfl_xor(top, o, WAVE), __shfl_xor(sum, o, WAVE));
+        if (lane < NT) stats[wave][lane] = make_float2(top, sum);
+        __syncthreads();
+        if (threadIdx.x < NT && (int)threadIdx.x < a.n) {
+            for (int w = 1; w < WAVES_PER_BLOCK; ++w) join_sums(top, sum, stats[w][lane].x, stats[w][lane].y);
+            a.part[(i64)blockIdx.x * a.Np + threadIdx.x] = make_float2(top, sum);
+        }
+    } else {
+        // the groups of a wave, then the waves in turn (the tokens' rows have served: their place is taken)
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int it = 0; it < ITERS; ++it) {
+                float4 &e = dh[t][it];
+#pragma unroll
+                for (int o = G; o < WAVE; o <<= 1) {
+                    e.x += __shfl_xor(e.x, o, WAVE);
+                    e.y += __shfl_xor(e.y, o, WAVE);
+                    e.z += __shfl_xor(e.z, o, WAVE);
+                    e.w += __shfl_xor(e.w, o, WAVE);
+                }
+            }
+        __syncthreads();
+        for (int w = 0; w < WAVES_PER_BLOCK; ++w) {
+            if (wave == w && side == 0)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int it = 0; it < ITERS; ++it) {
+                        float4 e = dh[t][it];
+                        if (w > 0) {
+                            const float4 o = h[t][l + G * it];
+                            e = make_float4(o.x + e.x, o.y + e.y, o.z + e.z, o.w + e.w);
+                        }
+                        h[t][l + G * it] = e;
+                    }
+            __syncthreads();
+        }
+        for (int x = threadIdx.x; x < a.n * a.C4; x += BLOCK)
+            st4(a.slots + ((i64)blockIdx.x * a.n * a.C4 + x) * 4, h[x / a.C4][x % a.C4]);
+    }
 }
 
 // ---------------------------------------------------------------- products with dz
@@ -361,11 +609,11 @@ struct ProductArgs {
     int dtype;
     float scale;
 };
-template <int TM, int TN, int WM, int WN, bool BT>
+template <int TM, int TN, int WM, int WN, int STAGES, bool BT>
 __global__ void __launch_bounds__(64 * WM * WN, 2) k_product(ProductArgs a)
 {
-    typedef Product<TM, TN, WM, WN, true, BT> P;
-    __shared__ __attribute__((aligned(16))) bf16_t lds[P::LDS];
+    typedef Product<TM, TN, WM, WN, STAGES, true, BT> P;
+    __shared__ __attribute__((aligned(16))) bf16_t lds[P::LDS * STAGES];
     int work = die_order((int)blockIdx.x, (int)gridDim.x);
     const int mt = work % a.m_tiles;
     work /= a.m_tiles;
@@ -374,23 +622,32 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_product(ProductArgs a)
     const i64 m0 = (i64)mt * P::BM, n0 = (i64)nt * P::BN;
     const i64 k0 = split * a.k_per, k1 = min(a.K, k0 + a.k_per);
     P p;
-    p.clear();
-    p.a.load(a.a, part_a(0, a.nseg), m0, k0);
-    p.b.load(a.b, part_b(0, a.nseg), n0, k0);
+    p.a.place(a.a);
+    p.b.place(a.b);
     const int steps = (int)((k1 - k0) / BK) * a.nseg;
-    int seg = 0;
+    int seg = 0, cur = 0;
     i64 k = k0;
-    for (int s = 0; s < steps; ++s) {
-        p.stage(lds);
-        k += BK;
-        if (k >= k1) {
+    auto advance = [&] {
+        if ((k += BK) >= k1) {
             k = k0;
-            seg = min(seg + 1, a.nseg - 1);                   // behind the last step a tile is loaded that nobody uses
+            seg = min(seg + 1, a.nseg - 1);                   // behind the last step a tile is fetched that nobody uses
         }
-        p.a.load(a.a, part_a(seg, a.nseg), m0, k);
-        p.b.load(a.b, part_b(seg, a.nseg), n0, k);
-        p.multiply(lds, wm, wn);
+    };
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) {
+        p.a.fetch_all(P::A::source(a.a, part_a(seg, a.nseg), m0, k), lds + s * P::LDS, wave);
+        p.b.fetch_all(P::B::source(a.b, part_b(seg, a.nseg), n0, k), lds + s * P::LDS + P::A::LDS, wave);
+        advance();
     }
+    __syncthreads();
+    auto step = [&](auto first) {
+        p.template step<first()>(P::A::source(a.a, part_a(seg, a.nseg), m0, k), P::B::source(a.b, part_b(seg, a.nseg), n0, k),
+                                 lds + (cur == 0 ? STAGES - 1 : cur - 1) * P::LDS, lds + cur * P::LDS, wave, wm, wn);
+        advance();
+        cur = cur == STAGES - 1 ? 0 : cur + 1;
+    };
+    step(std::true_type{});
+    for (int s = 1; s < steps; ++s) step(std::false_type{});
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
         const i64 n = n0 + (wn * TN + j) * 32 + (lane & 31);
@@ -425,25 +682,36 @@ struct JoinArgs {
     int dtype;
     float scale;
 };
-__global__ void __launch_bounds__(BLOCK) k_join(JoinArgs a)
+// a workgroup takes 64 chunks of 4 elements, its 16 waves parts of the slots that follow one another
+__global__ void __launch_bounds__(1024) k_join(JoinArgs a)
 {
+    __shared__ float4 sums[15][WAVE];
     const i64 all = a.n * a.C4;
-    for (i64 c = (i64)blockIdx.x * BLOCK + threadIdx.x; c < all; c += (i64)gridDim.x * BLOCK) {
-        const i64 row = c / a.C4;
+    const int lane = lane_id(), wave = uniform((int)(threadIdx.x >> 6));
+    const int per = (a.n_slots + 15) / 16, lo = wave * per, hi = min(a.n_slots, lo + per);
+    for (i64 base = (i64)blockIdx.x * WAVE; base < all; base += (i64)gridDim.x * WAVE) {
+        const i64 c = base + lane;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (!a.label || a.label[row] >= 0) {
-            for (int s = 0; s < a.n_slots; ++s) {
+        if (c < all)
+#pragma unroll 4
+            for (int s = lo; s < hi; ++s) {
                 const float4 x = ld4(a.slots + ((i64)s * all + c) * 4);
-                v.x += x.x;
-                v.y += x.y;
-                v.z += x.z;
-                v.w += x.w;
+                v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
             }
+        if (wave > 0) sums[wave - 1][lane] = v;
+        __syncthreads();
+        if (wave == 0 && c < all) {
+            for (int w = 1; w < 16 && w * per < a.n_slots; ++w) {
+                const float4 x = sums[w - 1][lane];
+                v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+            }
+            const i64 row = c / a.C4, at = row * a.stride + 4 * (c - row * a.C4);
             v = make_float4(v.x * a.scale, v.y * a.scale, v.z * a.scale, v.w * a.scale);
+            if (a.label && a.label[row] < 0) v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (a.dtype == TENSAIR_F32) st4((float *)a.out + at, v);
+            else st4((bf16_t *)a.out + at, v);
         }
-        const i64 at = row * a.stride + 4 * (c - row * a.C4);
-        if (a.dtype == TENSAIR_F32) st4((float *)a.out + at, v);
-        else st4((bf16_t *)a.out + at, v);
+        __syncthreads();
     }
 }
 
@@ -451,37 +719,48 @@ __global__ void __launch_bounds__(BLOCK) k_join(JoinArgs a)
 struct PackArgs {
     const void *src;
     i64 stride, rows;          // of the source
-    int D, Dp;                 // columns, of the copy (zero from D on)
+    int D, blocks;             // columns; blocks of columns of the copy (zero from D on)
     i64 out_rows, plane;       // rows of the copy (zero from `rows` on), elements from part to part
     bf16_t *out;
     const int *label;          // rows without a label are zero (NULL: none are)
+    float sign;                // 1 or -1
 };
+// a thread takes 8 elements, a wave 16 rows of a block of columns
 template <typename T>
 __global__ void __launch_bounds__(BLOCK) k_parts(PackArgs a)
 {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
-    const int C4 = a.Dp / 4;
-    const i64 all = a.out_rows * C4;
-    for (i64 c = (i64)blockIdx.x * BLOCK + threadIdx.x; c < all; c += (i64)gridDim.x * BLOCK) {
-        const i64 row = c / C4;
-        const int col = 4 * (int)(c - row * C4);
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (row < a.rows && col < a.D && (!a.label || a.label[row] >= 0)) v = ld4((const T *)a.src + row * a.stride + col);
-        float x[4] = {v.x, v.y, v.z, v.w};
-        bf16_t *to = a.out + row * a.Dp + col;
+    const i64 groups = a.out_rows / 16 * a.blocks, step = (i64)gridDim.x * WAVES_PER_BLOCK;
+    const int lane = lane_id();
+    for (i64 g = (i64)blockIdx.x * WAVES_PER_BLOCK + uniform((int)(threadIdx.x >> 6)); g < groups; g += step) {
+        const i64 row = g / a.blocks * 16 + lane / 4;
+        const int block = (int)(g % a.blocks), col = block * BK + lane % 4 * 8;
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (row < a.rows && (!a.label || a.label[row] >= 0)) {
+#pragma unroll
+            for (int k = 0; k < 8; k += 4)
+                if (col + k < a.D) {
+                    const float4 v = ld4((const T *)a.src + row * a.stride + col + k);
+                    x[k] = v.x * a.sign;
+                    x[k + 1] = v.y * a.sign;
+                    x[k + 2] = v.z * a.sign;
+                    x[k + 3] = v.w * a.sign;
+                }
+        }
+        bf16_t *to = a.out + (i64)block * a.out_rows * BK + row * BK + lane % 4 * 8;
 #pragma unroll
         for (int part = 0; part < PARTS; ++part) {
-            bf16_t h[4];
+            u32 h[8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < 8; ++k) {
                 h[k] = f32_to_bf16(x[k]);
                 if (PARTS > 1) {
                     // beyond the largest bfloat16: cut, so that the rest is finite
-                    if ((h[k] & 0x7FFFu) == 0x7F80u && fabsf(x[k]) < INFINITY) h[k] = (bf16_t)((h[k] & 0x8000u) | 0x7F7Fu);
-                    x[k] = (h[k] & 0x7F80u) == 0x7F80u ? 0.f : x[k] - bf16_to_f32(h[k]);
+                    if ((h[k] & 0x7FFFu) == 0x7F80u && fabsf(x[k]) < INFINITY) h[k] = (h[k] & 0x8000u) | 0x7F7Fu;
+                    x[k] = (h[k] & 0x7F80u) == 0x7F80u ? 0.f : x[k] - __uint_as_float(h[k] << 16);
                 }
             }
-            *(uint2 *)(to + part * a.plane) = make_uint2((u32)h[0] | ((u32)h[1] << 16), (u32)h[2] | ((u32)h[3] << 16));
+            *(v4u *)(to + part * a.plane) = v4u{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
         }
     }
 }
@@ -531,51 +810,51 @@ int launched(const char *what)
 // workgroups for so many items, a thread each or, of very many, several
 unsigned blocks_for(i64 items) { return (unsigned)std::min<i64>(cdiv(items, BLOCK), 1 << 20); }
 
-#define SM_BM 256              // words of a tile of logits
-#define SM_BN 128              // tokens of one
+// Tiles of logits: 256 words by 128 tokens, a wave's 128 by 64, two workgroups to a compute unit, so that one's exponentials run
+// beside the other's products; three stages, as much as LDS holds twice.
+#define SM_BN 128              // tokens of a tile
 #define SM_BN_FEW 64           // ... where there are at most so many
 #define SM_WAVES_M 2           // rows of waves of a tile, each with a maximum and a sum of its own
+#define SM_PN 128              // rows of a tile of the products with dz
+#define SM_RANGE_TILES 4096    // tiles of a range, at most: how far a fetch is off its tile's first element fits 31 bits
 #define SM_BLOCKS 512          // workgroups that fill the chip, two to a compute unit
-#define SM_DZ_BYTES ((i64)512 << 20)
+#define SM_DZ_BYTES ((i64)1 << 30)   // dz of a range, about: with half as much the products took 3 to 8 % longer
 
 struct SoftmaxPlan {
-    int parts, nseg, Dp, ksteps, bn, token_tiles, wm;
-    bool pack;                 // the table is copied (padded, or in parts)
+    bool few;                  // at most FEW_TOKENS tokens
+    int few_blocks;
+    int parts, nseg, Dp, bn, token_tiles, wm;
     i64 Np, tiles;             // tokens, padded; tiles of words
-    int per, strips;           // loss: tiles to a strip
-    // gradient
-    i64 range_tiles, ranges;   // tiles of words whose dz is kept at a time
-    int dz_per, dz_strips;
+    i64 range_tiles, ranges;   // tiles of words that are laid out, and whose dz is kept, at a time
+    int per, strips;           // tiles to a strip, strips of a range
     int tm, m_tiles;           // of the products: fragments of a wave along the row length, tiles
     int h_splits, t_splits;    // of d_hidden's sum over a range's words, of d_table's over the tokens
     i64 h_k, t_k;
 };
 
-SoftmaxPlan plan_of(i64 n, i64 V, int D, int dtype, i64 table_stride, const void *table)
+SoftmaxPlan plan_of(i64 n, i64 V, int D, int dtype, bool grad)
 {
     SoftmaxPlan s;
     memset(&s, 0, sizeof(s));
+    s.few = n <= FEW_TOKENS;
+    s.few_blocks = (int)std::max<i64>(1, std::min<i64>(cdiv(V, 64), grad ? FEW_BLOCKS / 2 : FEW_BLOCKS));
     s.parts = dtype == TENSAIR_F32 ? 3 : 1;
     s.nseg = dtype == TENSAIR_F32 ? 6 : 1;
     s.Dp = (int)cdiv(D, BK) * BK;
-    s.ksteps = s.Dp / BK;
-    s.pack = dtype == TENSAIR_F32 || D % BK || table_stride % 8 || ((uintptr_t)table & 15);
     const bool few = n <= SM_BN_FEW;
     s.bn = few ? SM_BN_FEW : SM_BN;
     s.wm = few ? 4 : SM_WAVES_M;
     s.Np = cdiv(n, s.bn) * s.bn;
     s.token_tiles = (int)(s.Np / s.bn);
     s.tiles = cdiv(V, SM_BM);
-    const i64 want = std::max<i64>(1, std::min<i64>(s.tiles, cdiv(SM_BLOCKS * 2, s.token_tiles)));
-    s.per = (int)cdiv(s.tiles, want);
-    s.strips = (int)cdiv(s.tiles, s.per);
-    s.range_tiles = std::max<i64>(1, std::min(s.tiles, SM_DZ_BYTES / (s.Np * SM_BM * 2 * s.parts)));
+    s.range_tiles = std::min<i64>(s.tiles, SM_RANGE_TILES);
+    if (grad) s.range_tiles = std::max<i64>(1, std::min(s.range_tiles, SM_DZ_BYTES / (s.Np * SM_BM * 2 * s.parts)));
     s.ranges = cdiv(s.tiles, s.range_tiles);
     s.range_tiles = cdiv(s.tiles, s.ranges);
     s.ranges = cdiv(s.tiles, s.range_tiles);
-    const i64 dz_want = std::max<i64>(1, std::min<i64>(s.range_tiles, cdiv(SM_BLOCKS * 2, s.token_tiles)));
-    s.dz_per = (int)cdiv(s.range_tiles, dz_want);
-    s.dz_strips = (int)cdiv(s.range_tiles, s.dz_per);
+    const i64 want = std::max<i64>(1, std::min<i64>(s.range_tiles, cdiv(SM_BLOCKS * 2, s.token_tiles)));
+    s.per = (int)cdiv(s.range_tiles, want);
+    s.strips = (int)cdiv(s.range_tiles, s.per);
     // fragments of a wave (two to a tile along the row length): the fewest columns beyond the row, then the largest tile
     i64 least = -1;
     for (int tm = 1; tm <= 5; ++tm) {
@@ -587,7 +866,7 @@ SoftmaxPlan plan_of(i64 n, i64 V, int D, int dtype, i64 table_stride, const void
     }
     s.m_tiles = (int)cdiv(s.Dp, 64 * s.tm);
     const i64 range_words = s.range_tiles * SM_BM;
-    const i64 h_tiles = s.m_tiles * cdiv(s.Np, 128), t_tiles = s.m_tiles * cdiv(range_words, 128);
+    const i64 h_tiles = s.m_tiles * cdiv(s.Np, SM_PN), t_tiles = s.m_tiles * cdiv(range_words, SM_PN);
     i64 splits = std::max<i64>(1, std::min<i64>(cdiv(SM_BLOCKS, h_tiles), range_words / 512));
     s.h_k = cdiv(cdiv(range_words, splits), BK) * BK;
     s.h_splits = (int)cdiv(range_words, s.h_k);
@@ -614,11 +893,23 @@ size_t softmax_carve(const SoftmaxPlan &s, i64 n, i64 V, int D, bool grad, char 
     SoftmaxBuffers x;
     memset(&x, 0, sizeof(x));
     x.label = (int *)take(4 * (size_t)s.Np);
+    if (s.few) {
+        x.picked = (float *)take(4 * (size_t)s.Np);
+        x.part = (float2 *)take(8 * (size_t)s.few_blocks * s.Np);
+        if (grad) {
+            x.lse2 = (float *)take(4 * (size_t)s.Np);
+            x.d = (float *)take(4 * (size_t)s.Np);
+            x.h_slots = (float *)take(4 * (size_t)s.few_blocks * n * D);
+        }
+        if (b) *b = x;
+        // the loss of the same sizes has more workgroups than the gradient
+        return grad ? std::max(at, softmax_carve(plan_of(n, V, D, s.parts == 3 ? TENSAIR_F32 : TENSAIR_BF16, false), n, V, D, false, nullptr, nullptr)) : at;
+    }
     x.h = (bf16_t *)take(2 * (size_t)s.Np * s.Dp * s.parts);
-    if (s.pack) x.w = (bf16_t *)take(2 * (size_t)V * s.Dp * s.parts);
+    x.w = (bf16_t *)take(2 * (size_t)s.range_tiles * SM_BM * s.Dp * s.parts);
     const size_t head = at;
     x.picked = (float *)take(4 * (size_t)s.Np);
-    x.part = (float2 *)take(8 * (size_t)s.strips * s.wm * s.Np);
+    x.part = (float2 *)take(8 * (size_t)s.ranges * s.strips * s.wm * s.Np);
     const size_t loss_end = at;
     at = head;
     if (grad) {
@@ -640,6 +931,11 @@ int check_softmax(i64 n, i64 vocab, int32_t dim, int32_t dtype)
     if (dtype != TENSAIR_F32 && dtype != TENSAIR_BF16) return tn_fail(TENSAIR_EINVAL, "unknown dtype");
     return TENSAIR_OK;
 }
+int check_scale(float scale)
+{
+    if (!(fabsf(scale) > 0.f) || !(fabsf(scale) < INFINITY)) return tn_fail(TENSAIR_EINVAL, "scale must be finite and not zero");
+    return TENSAIR_OK;
+}
 int check_rows(const void *p, i64 rows, i64 stride, int32_t dim, const char *what)
 {
     if (rows > 0 && !p) return tn_fail(TENSAIR_EINVAL, "%s is NULL", what);
@@ -648,72 +944,120 @@ int check_rows(const void *p, i64 rows, i64 stride, int32_t dim, const char *wha
     return TENSAIR_OK;
 }
 
-// tokens, hidden and, where it is copied, the table
-void lay_out(const SoftmaxPlan &s, const SoftmaxBuffers &b, const void *hidden, i64 hidden_stride, const void *table, i64 table_stride,
-             int dtype, i64 n, i64 V, int D, bool grad, hipStream_t st)
+// rows [0, rows) of a matrix laid out for the products, out_rows (a multiple of 16) with what is zero
+void lay_out(const SoftmaxPlan &s, const void *src, i64 stride, i64 rows, i64 out_rows, int dtype, int D, const int *label, float sign, bf16_t *out,
+             hipStream_t st)
 {
-    PackArgs p;
-    memset(&p, 0, sizeof(p));
-    p.D = D;
-    p.Dp = s.Dp;
-    for (int side = 0; side < (s.pack ? 2 : 1); ++side) {
-        p.src = side ? table : hidden;
-        p.stride = side ? table_stride : hidden_stride;
-        p.rows = side ? V : n;
-        p.out_rows = side ? V : s.Np;
-        p.plane = p.out_rows * s.Dp;
-        p.out = side ? b.w : b.h;
-        p.label = !side && grad ? b.label : nullptr;      // what a token without a loss holds must reach no sum
-        const dim3 grid(blocks_for(p.out_rows * (s.Dp / 4))), blk(BLOCK);
-        if (dtype == TENSAIR_F32) hipLaunchKernelGGL(k_parts<float>, grid, blk, 0, st, p);
-        else hipLaunchKernelGGL(k_parts<bf16_t>, grid, blk, 0, st, p);
-    }
+    PackArgs p = {src, stride, rows, D, s.Dp / BK, out_rows, out_rows * s.Dp, out, label, sign};
+    const i64 groups = out_rows / 16 * p.blocks;
+    const dim3 grid(blocks_for(groups * WAVE)), blk(BLOCK);
+    if (dtype == TENSAIR_F32) hipLaunchKernelGGL(k_parts<float>, grid, blk, 0, st, p);
+    else hipLaunchKernelGGL(k_parts<bf16_t>, grid, blk, 0, st, p);
 }
-LogitsArgs logits_args(const SoftmaxPlan &s, const SoftmaxBuffers &b, const void *table, i64 table_stride, i64 V, float scale)
+// one range of words: its rows laid out, and what its logits' launch needs
+struct Range {
+    i64 word0, words, tiles, rows;
+};
+Range range_of(const SoftmaxPlan &s, i64 range, i64 V)
 {
+    Range r;
+    const i64 tile0 = range * s.range_tiles;
+    r.tiles = std::min(s.range_tiles, s.tiles - tile0);
+    r.word0 = tile0 * SM_BM;
+    r.words = std::min(r.tiles * SM_BM, V - r.word0);
+    r.rows = r.tiles * SM_BM;
+    return r;
+}
+LogitsArgs lay_out_range(const SoftmaxPlan &s, const SoftmaxBuffers &b, const Range &r, const void *table, i64 table_stride, int dtype, int D, i64 V,
+                         float scale, hipStream_t st)
+{
+    const char *src = (const char *)table + (size_t)r.word0 * table_stride * (dtype == TENSAIR_F32 ? 4 : 2);
+    lay_out(s, src, table_stride, r.words, r.rows, dtype, D, nullptr, 1.f, b.w, st);
     LogitsArgs a;
     memset(&a, 0, sizeof(a));
-    a.w = s.pack ? Operand{b.w, s.Dp, V * s.Dp, V, s.Dp} : Operand{(const bf16_t *)table, table_stride, 0, V, s.Dp};
-    a.h = Operand{b.h, s.Dp, s.Np * s.Dp, s.Np, s.Dp};
+    a.w = Operand{b.w, r.rows, r.rows * s.Dp};
+    a.h = Operand{b.h, s.Np, s.Np * s.Dp};
     a.nseg = s.nseg;
-    a.ksteps = s.ksteps;
+    a.K = s.Dp;
+    a.word0 = r.word0;
     a.V = V;
+    a.tiles = (int)r.tiles;
+    a.per = s.per;
+    a.strips = (int)cdiv(r.tiles, s.per);
     a.token_tiles = s.token_tiles;
     a.Np = s.Np;
-    a.c = scale * LOG2E;
+    a.c = fabsf(scale) * LOG2E;
     a.label = b.label;
     a.part = b.part;
     a.picked = b.picked;
     a.lse2 = b.lse2;
     a.d = b.d;
     a.dz = b.dz;
-    a.dz_pitch = s.range_tiles * SM_BM;
-    a.dz_plane = s.Np * a.dz_pitch;
+    a.dz_plane = s.Np * s.range_tiles * SM_BM;
+    return a;
+}
+template <typename T, int NT, bool GRAD>
+void launch_few_n(const FewArgs &a, int blocks, hipStream_t st)
+{
+    const dim3 grid((unsigned)blocks), blk(BLOCK);
+    if (a.C4 <= 32) hipLaunchKernelGGL((k_few<T, 16, 2, NT, GRAD>), grid, blk, 0, st, a);
+    else if (a.C4 <= 96) hipLaunchKernelGGL((k_few<T, 32, 3, NT, GRAD>), grid, blk, 0, st, a);
+    else hipLaunchKernelGGL((k_few<T, 64, 4, NT, GRAD>), grid, blk, 0, st, a);
+}
+template <typename T, bool GRAD>
+void launch_few_t(const FewArgs &a, int blocks, hipStream_t st)
+{
+    if (a.n == 1) launch_few_n<T, 1, GRAD>(a, blocks, st);
+    else if (a.n <= 4) launch_few_n<T, 4, GRAD>(a, blocks, st);
+    else launch_few_n<T, FEW_TOKENS, GRAD>(a, blocks, st);
+}
+FewArgs few_args(const SoftmaxPlan &s, const SoftmaxBuffers &b, const void *hidden, i64 hidden_stride, const void *table, i64 table_stride, i64 n, i64 V,
+                 int D, float scale)
+{
+    FewArgs a;
+    memset(&a, 0, sizeof(a));
+    a.hidden = hidden;
+    a.table = table;
+    a.hidden_stride = hidden_stride;
+    a.table_stride = table_stride;
+    a.V = V;
+    a.n = (int)n;
+    a.C4 = D / 4;
+    a.c = fabsf(scale) * LOG2E;
+    a.sign = scale < 0.f ? -1.f : 1.f;
+    a.label = b.label;
+    a.part = b.part;
+    a.picked = b.picked;
+    a.Np = s.Np;
+    a.lse2 = b.lse2;
+    a.d = b.d;
+    a.slots = b.h_slots;
+    a.scale = fabsf(scale);
     return a;
 }
 template <bool GRAD, int PARTS>
 void launch_logits(const SoftmaxPlan &s, const LogitsArgs &a, hipStream_t st)
 {
     const dim3 grid((unsigned)(a.strips * a.token_tiles)), blk(256);
-    if (s.bn == SM_BN_FEW) hipLaunchKernelGGL((k_logits<2, 2, 4, 1, GRAD, PARTS>), grid, blk, 0, st, a);
-    else hipLaunchKernelGGL((k_logits<4, 2, 2, 2, GRAD, PARTS>), grid, blk, 0, st, a);
+    if (s.bn == SM_BN_FEW) hipLaunchKernelGGL((k_logits<2, 2, 4, 1, 3, GRAD, PARTS>), grid, blk, 0, st, a);
+    else hipLaunchKernelGGL((k_logits<4, 2, 2, 2, 3, GRAD, PARTS>), grid, blk, 0, st, a);
 }
 template <bool BT>
 void launch_product(int tm, const ProductArgs &a, hipStream_t st)
 {
     const dim3 grid((unsigned)(a.m_tiles * a.n_tiles * a.splits)), blk(256);
     switch (tm) {
-    case 1: hipLaunchKernelGGL((k_product<1, 2, 2, 2, BT>), grid, blk, 0, st, a); break;
-    case 2: hipLaunchKernelGGL((k_product<2, 2, 2, 2, BT>), grid, blk, 0, st, a); break;
-    case 3: hipLaunchKernelGGL((k_product<3, 2, 2, 2, BT>), grid, blk, 0, st, a); break;
-    case 4: hipLaunchKernelGGL((k_product<4, 2, 2, 2, BT>), grid, blk, 0, st, a); break;
-    default: hipLaunchKernelGGL((k_product<5, 2, 2, 2, BT>), grid, blk, 0, st, a); break;
+    case 1: hipLaunchKernelGGL((k_product<1, 2, 2, 2, 2, BT>), grid, blk, 0, st, a); break;
+    case 2: hipLaunchKernelGGL((k_product<2, 2, 2, 2, 2, BT>), grid, blk, 0, st, a); break;
+    case 3: hipLaunchKernelGGL((k_product<3, 2, 2, 2, 2, BT>), grid, blk, 0, st, a); break;
+    case 4: hipLaunchKernelGGL((k_product<4, 2, 2, 2, 2, BT>), grid, blk, 0, st, a); break;
+    default: hipLaunchKernelGGL((k_product<5, 2, 2, 2, 2, BT>), grid, blk, 0, st, a); break;
     }
 }
 void launch_join(const float *slots, int n_slots, i64 rows, i64 stride, int D, const int *label, void *out, int dtype, float scale, hipStream_t st)
 {
     JoinArgs j = {slots, n_slots, rows, stride, D / 4, label, out, dtype, scale};
-    hipLaunchKernelGGL(k_join, dim3(blocks_for(rows * (D / 4))), dim3(BLOCK), 0, st, j);
+    hipLaunchKernelGGL(k_join, dim3((unsigned)std::min<i64>(cdiv(rows * (D / 4), WAVE), 1 << 18)), dim3(1024), 0, st, j);
 }
 
 }  // namespace
@@ -724,8 +1068,7 @@ size_t tensair_softmax_workspace_bytes(int64_t n, int64_t vocab, int32_t dim, in
 {
     if (check_softmax(n, vocab, dim, dtype)) return 0;
     if (n == 0) return 256;
-    // as if the table had to be copied: whether it has depends on its stride
-    return softmax_carve(plan_of(n, vocab, dim, dtype, 4, nullptr), n, vocab, dim, with_grad != 0, nullptr, nullptr);
+    return softmax_carve(plan_of(n, vocab, dim, dtype, with_grad != 0), n, vocab, dim, with_grad != 0, nullptr, nullptr);
 }
 
 int tensair_softmax_loss(const void *hidden, int64_t hidden_stride, const void *table, int64_t table_stride, int32_t dtype, int64_t n,
@@ -734,13 +1077,14 @@ int tensair_softmax_loss(const void *hidden, int64_t hidden_stride, const void *
 {
     int rc;
     if ((rc = check_softmax(n, vocab, dim, dtype))) return rc;
+    if ((rc = check_scale(scale))) return rc;
     if ((rc = check_rows(hidden, n, hidden_stride, dim, "hidden"))) return rc;
     if ((rc = check_rows(table, vocab, table_stride, dim, "table"))) return rc;
     if (n > 0 && (!labels || !loss || !lse)) return tn_fail(TENSAIR_EINVAL, "NULL pointer argument");
     if (((uintptr_t)labels | (uintptr_t)loss | (uintptr_t)lse | (uintptr_t)status) & 3)
         return tn_fail(TENSAIR_EINVAL, "labels, loss, lse and status must be 4-byte aligned");
     if (n == 0) return TENSAIR_OK;
-    const SoftmaxPlan s = plan_of(n, vocab, dim, dtype, table_stride, table);
+    const SoftmaxPlan s = plan_of(n, vocab, dim, dtype, false);
     if (workspace_bytes < softmax_carve(s, n, vocab, dim, false, nullptr, nullptr))
         return tn_fail(TENSAIR_ECAPACITY, "workspace too small: see tensair_softmax_workspace_bytes");
     if (!workspace || ((uintptr_t)workspace & 255)) return tn_fail(TENSAIR_EINVAL, "workspace must be 256-byte aligned");
@@ -749,13 +1093,22 @@ int tensair_softmax_loss(const void *hidden, int64_t hidden_stride, const void *
     hipStream_t st = (hipStream_t)stream;
     TokenArgs t = {labels, nullptr, nullptr, n, s.Np, vocab, ignore_label, b.label, status, nullptr, nullptr};
     hipLaunchKernelGGL(k_tokens, dim3((unsigned)cdiv(s.Np, BLOCK)), dim3(BLOCK), 0, st, t);
-    lay_out(s, b, hidden, hidden_stride, table, table_stride, dtype, n, vocab, dim, false, st);
-    LogitsArgs a = logits_args(s, b, table, table_stride, vocab, scale);
-    a.tiles = (int)s.tiles;
-    a.per = s.per;
-    a.strips = s.strips;
-    launch_logits<false, 1>(s, a, st);
-    LossArgs l = {b.part, s.strips * s.wm, s.Np, n, b.picked, b.label, loss, lse};
+    int slots = 0;
+    if (s.few) {
+        const FewArgs f = few_args(s, b, hidden, hidden_stride, table, table_stride, n, vocab, dim, scale);
+        if (dtype == TENSAIR_F32) launch_few_t<float, false>(f, s.few_blocks, st);
+        else launch_few_t<bf16_t, false>(f, s.few_blocks, st);
+        slots = s.few_blocks;
+    } else {
+        lay_out(s, hidden, hidden_stride, n, s.Np, dtype, dim, nullptr, scale < 0.f ? -1.f : 1.f, b.h, st);
+    }
+    for (i64 range = 0; range < (s.few ? 0 : s.ranges); ++range) {
+        LogitsArgs a = lay_out_range(s, b, range_of(s, range, vocab), table, table_stride, dtype, dim, vocab, scale, st);
+        a.part += (i64)slots * s.Np;
+        launch_logits<false, 1>(s, a, st);
+        slots += a.strips * s.wm;
+    }
+    LossArgs l = {b.part, slots, s.Np, n, b.picked, b.label, loss, lse};
     hipLaunchKernelGGL(k_loss, dim3((unsigned)(s.Np / WAVE)), dim3(1024), 0, st, l);
     return launched("softmax_loss");
 }
@@ -767,6 +1120,7 @@ int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *
 {
     int rc;
     if ((rc = check_softmax(n, vocab, dim, dtype))) return rc;
+    if ((rc = check_scale(scale))) return rc;
     if ((rc = check_rows(hidden, n, hidden_stride, dim, "hidden"))) return rc;
     if ((rc = check_rows(table, vocab, table_stride, dim, "table"))) return rc;
     if (d_hidden && (rc = check_rows(d_hidden, n, d_hidden_stride, dim, "d_hidden"))) return rc;
@@ -781,7 +1135,7 @@ int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *
             hipLaunchKernelGGL(k_zero_rows, dim3(blocks_for(vocab * (dim / 4))), dim3(BLOCK), 0, st, d_table, (int)dtype, vocab, d_table_stride, dim / 4);
         return launched("softmax_grad");
     }
-    const SoftmaxPlan s = plan_of(n, vocab, dim, dtype, table_stride, table);
+    const SoftmaxPlan s = plan_of(n, vocab, dim, dtype, true);
     if (workspace_bytes < softmax_carve(s, n, vocab, dim, true, nullptr, nullptr))
         return tn_fail(TENSAIR_ECAPACITY, "workspace too small: see tensair_softmax_workspace_bytes");
     if (!workspace || ((uintptr_t)workspace & 255)) return tn_fail(TENSAIR_EINVAL, "workspace must be 256-byte aligned");
@@ -789,18 +1143,22 @@ int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *
     softmax_carve(s, n, vocab, dim, true, (char *)workspace, &b);
     TokenArgs t = {labels, lse, d_loss, n, s.Np, vocab, ignore_label, b.label, status, b.lse2, b.d};
     hipLaunchKernelGGL(k_tokens, dim3((unsigned)cdiv(s.Np, BLOCK)), dim3(BLOCK), 0, st, t);
-    lay_out(s, b, hidden, hidden_stride, table, table_stride, dtype, n, vocab, dim, true, st);
+    if (s.few) {
+        FewArgs f = few_args(s, b, hidden, hidden_stride, table, table_stride, n, vocab, dim, scale);
+        f.d_table = d_table;
+        f.d_stride = d_table_stride;
+        if (dtype == TENSAIR_F32) launch_few_t<float, true>(f, s.few_blocks, st);
+        else launch_few_t<bf16_t, true>(f, s.few_blocks, st);
+        if (d_hidden) launch_join(b.h_slots, s.few_blocks, n, d_hidden_stride, dim, b.label, d_hidden, dtype, scale, st);
+        return launched("softmax_grad");
+    }
+    lay_out(s, hidden, hidden_stride, n, s.Np, dtype, dim, b.label, scale < 0.f ? -1.f : 1.f, b.h, st);   // what a token without a loss holds must reach no sum
     for (i64 range = 0; range < s.ranges; ++range) {
-        const i64 tile0 = range * s.range_tiles, tiles = std::min(s.range_tiles, s.tiles - tile0);
-        const i64 word0 = tile0 * SM_BM, words = std::min(tiles * SM_BM, vocab - word0);
-        LogitsArgs a = logits_args(s, b, table, table_stride, vocab, scale);
-        a.word0 = word0;
-        a.tiles = (int)tiles;
-        a.per = s.dz_per;
-        a.strips = (int)cdiv(tiles, s.dz_per);
+        const Range r = range_of(s, range, vocab);
+        const LogitsArgs a = lay_out_range(s, b, r, table, table_stride, dtype, dim, vocab, scale, st);
         if (s.parts == 1) launch_logits<true, 1>(s, a, st);
         else launch_logits<true, 3>(s, a, st);
-        const Operand dz = {b.dz, a.dz_pitch, a.dz_plane, s.Np, a.dz_pitch};
+        const Operand dz = {b.dz, s.Np, a.dz_plane};
         ProductArgs p;
         memset(&p, 0, sizeof(p));
         p.nseg = s.nseg;
@@ -810,38 +1168,35 @@ int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *
         p.scale = scale;
         if (d_hidden) {
             p.a = a.w;
-            p.a.p += word0 * a.w.pitch;
-            p.a.rows = vocab - word0;
             p.b = dz;
             p.N = n;
-            p.K = cdiv(words, BK) * BK;
-            p.n_tiles = (int)cdiv(s.Np, 128);
+            p.K = cdiv(r.words, BK) * BK;
+            p.n_tiles = (int)cdiv(s.Np, SM_PN);
             p.k_per = s.h_k;
             p.splits = (int)cdiv(p.K, p.k_per);
             p.slots = b.h_slots + range * s.h_splits * n * dim;
             launch_product<false>(s.tm, p, st);
         }
         if (d_table) {
+            p.scale = fabsf(scale);                           // the tokens' rows have its sign
             p.a = a.h;
             p.b = dz;
-            p.N = words;
+            p.N = r.words;
             p.K = s.Np;
-            p.n_tiles = (int)cdiv(words, 128);
+            p.n_tiles = (int)cdiv(r.words, SM_PN);
             p.k_per = s.t_k;
             p.splits = s.t_splits;
             p.slots = s.t_splits > 1 ? b.t_slots : nullptr;
-            char *out = (char *)d_table + (size_t)word0 * d_table_stride * (dtype == TENSAIR_F32 ? 4 : 2);
+            char *out = (char *)d_table + (size_t)r.word0 * d_table_stride * (dtype == TENSAIR_F32 ? 4 : 2);
             p.out = out;
             p.out_stride = d_table_stride;
             launch_product<true>(s.tm, p, st);
-            if (s.t_splits > 1) launch_join(b.t_slots, s.t_splits, words, d_table_stride, dim, nullptr, out, dtype, scale, st);
+            if (s.t_splits > 1) launch_join(b.t_slots, s.t_splits, r.words, d_table_stride, dim, nullptr, out, dtype, fabsf(scale), st);
         }
     }
     if (d_hidden) {
         // the last range may have fewer splits than the others
-        const i64 last = std::min(s.range_tiles, s.tiles - (s.ranges - 1) * s.range_tiles) * SM_BM;
-        const i64 words = std::min(last, vocab - (s.ranges - 1) * s.range_tiles * SM_BM);
-        const int slots = (int)((s.ranges - 1) * s.h_splits + cdiv(cdiv(words, BK) * BK, s.h_k));
+        const int slots = (int)((s.ranges - 1) * s.h_splits + cdiv(cdiv(range_of(s, s.ranges - 1, vocab).words, BK) * BK, s.h_k));
         launch_join(b.h_slots, slots, n, d_hidden_stride, dim, b.label, d_hidden, dtype, scale, st);
     }
     return launched("softmax_grad");
