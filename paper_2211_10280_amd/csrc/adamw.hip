@@ -23,6 +23,7 @@ namespace {
 
 #define ADAMW_CHUNK 4096       // elements of a workgroup
 #define ADAMW_GROUP 256        // elements that share a scale: a wave, four to a lane
+#define ADAMW_STREAM_BYTES ((i64)256 << 20)
 #define ADAMW_VECS (ADAMW_CHUNK / (BLOCK * 4))
 
 struct AdamwTensor {
@@ -47,9 +48,10 @@ struct AdamwStep {
 typedef float v2f __attribute__((ext_vector_type(2)));
 
 // 4 elements at p + i of n
+template <bool STREAM>
 __device__ __forceinline__ float4 get4(const float *p, i64 i, i64 n, bool vec)
 {
-    if (vec && i + 4 <= n) return ld4(p + i);
+    if (vec && i + 4 <= n) return STREAM ? ld4s(p + i) : ld4(p + i);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (i < n) v.x = p[i];
     if (i + 1 < n) v.y = p[i + 1];
@@ -57,9 +59,10 @@ __device__ __forceinline__ float4 get4(const float *p, i64 i, i64 n, bool vec)
     if (i + 3 < n) v.w = p[i + 3];
     return v;
 }
+template <bool STREAM>
 __device__ __forceinline__ float4 get4(const bf16_t *p, i64 i, i64 n, bool vec)
 {
-    if (vec && i + 4 <= n) return ld4(p + i);
+    if (vec && i + 4 <= n) return STREAM ? ld4s(p + i) : ld4(p + i);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (i < n) v.x = bf16_to_f32(p[i]);
     if (i + 1 < n) v.y = bf16_to_f32(p[i + 1]);
@@ -67,9 +70,10 @@ __device__ __forceinline__ float4 get4(const bf16_t *p, i64 i, i64 n, bool vec)
     if (i + 3 < n) v.w = bf16_to_f32(p[i + 3]);
     return v;
 }
+template <bool STREAM>
 __device__ __forceinline__ u32 get4(const unsigned char *p, i64 i, i64 n, bool vec)
 {
-    if (vec && i + 4 <= n) return *(const u32 *)(p + i);
+    if (vec && i + 4 <= n) return STREAM ? __builtin_nontemporal_load((const GLOBAL_AS u32 *)(p + i)) : *(const u32 *)(p + i);
     u32 v = 0;
     for (int k = 0; k < 4; ++k)
         if (i + k < n) v |= (u32)p[i + k] << (8 * k);
@@ -77,11 +81,12 @@ __device__ __forceinline__ u32 get4(const unsigned char *p, i64 i, i64 n, bool v
 }
 __device__ __forceinline__ void put1(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put1(bf16_t *p, float v) { *p = f32_to_bf16(v); }
-template <typename T>
+template <bool STREAM, typename T>
 __device__ __forceinline__ void put4(T *p, i64 i, i64 n, bool vec, float4 v)
 {
     if (vec && i + 4 <= n) {
-        st4(p + i, v);
+        if (STREAM) st4s(p + i, v);
+        else st4(p + i, v);
         return;
     }
     if (i < n) put1(p + i, v.x);
@@ -89,10 +94,12 @@ __device__ __forceinline__ void put4(T *p, i64 i, i64 n, bool vec, float4 v)
     if (i + 2 < n) put1(p + i + 2, v.z);
     if (i + 3 < n) put1(p + i + 3, v.w);
 }
+template <bool STREAM>
 __device__ __forceinline__ void put4(unsigned char *p, i64 i, i64 n, bool vec, u32 v)
 {
     if (vec && i + 4 <= n) {
-        *(u32 *)(p + i) = v;
+        if (STREAM) __builtin_nontemporal_store(v, (GLOBAL_AS u32 *)(p + i));
+        else *(u32 *)(p + i) = v;
         return;
     }
     for (int k = 0; k < 4; ++k)
@@ -136,7 +143,8 @@ __device__ __forceinline__ void adamw1(float &p, float g, float &m, float &v, fl
     p = p * keep - (m * a.size) / (r * a.fix + a.eps);
 }
 
-template <typename TP, typename TG, bool EIGHT>
+// STREAM: around the caches, where the tensors do not fit the memory-side cache
+template <typename TP, typename TG, bool EIGHT, bool STREAM>
 __global__ void __launch_bounds__(BLOCK) k_adamw(AdamwStep a, u32 first_chunk)
 {
     const u32 chunk = first_chunk + blockIdx.x;
@@ -150,8 +158,8 @@ __global__ void __launch_bounds__(BLOCK) k_adamw(AdamwStep a, u32 first_chunk)
     float4 p[ADAMW_VECS], g[ADAMW_VECS];
 #pragma unroll
     for (int j = 0; j < ADAMW_VECS; ++j) {
-        p[j] = get4(param, base + j * (BLOCK * 4), n, vec);
-        g[j] = get4(grad, base + j * (BLOCK * 4), n, vec);
+        p[j] = get4<STREAM>(param, base + j * (BLOCK * 4), n, vec);
+        g[j] = get4<STREAM>(grad, base + j * (BLOCK * 4), n, vec);
     }
     if (a.grad_scale) {
 #pragma unroll
@@ -162,8 +170,8 @@ __global__ void __launch_bounds__(BLOCK) k_adamw(AdamwStep a, u32 first_chunk)
         float4 mm[ADAMW_VECS], vv[ADAMW_VECS];
 #pragma unroll
         for (int j = 0; j < ADAMW_VECS; ++j) {
-            mm[j] = get4(m, base + j * (BLOCK * 4), n, vec);
-            vv[j] = get4(v, base + j * (BLOCK * 4), n, vec);
+            mm[j] = get4<STREAM>(m, base + j * (BLOCK * 4), n, vec);
+            vv[j] = get4<STREAM>(v, base + j * (BLOCK * 4), n, vec);
         }
 #pragma unroll
         for (int j = 0; j < ADAMW_VECS; ++j) {
@@ -173,10 +181,10 @@ __global__ void __launch_bounds__(BLOCK) k_adamw(AdamwStep a, u32 first_chunk)
             adamw1(p[j].y, g[j].y, mm[j].y, vv[j].y, r, a, keep);
             adamw1(p[j].z, g[j].z, mm[j].z, vv[j].z, r, a, keep);
             adamw1(p[j].w, g[j].w, mm[j].w, vv[j].w, r, a, keep);
-            put4(param, i, n, vec, p[j]);
-            put4(m, i, n, vec, mm[j]);
-            put4(v, i, n, vec, vv[j]);
-            if (t.copy) put4(t.copy, i, n, vec, p[j]);
+            put4<STREAM>(param, i, n, vec, p[j]);
+            put4<STREAM>(m, i, n, vec, mm[j]);
+            put4<STREAM>(v, i, n, vec, vv[j]);
+            if (t.copy) put4<STREAM>(t.copy, i, n, vec, p[j]);
         }
     } else {
         unsigned char *m = (unsigned char *)t.m, *v = (unsigned char *)t.v;
@@ -185,8 +193,8 @@ __global__ void __launch_bounds__(BLOCK) k_adamw(AdamwStep a, u32 first_chunk)
 #pragma unroll
         for (int j = 0; j < ADAMW_VECS; ++j) {
             const i64 i = base + j * (BLOCK * 4), group = i / ADAMW_GROUP;       // a wave's elements are one group
-            mc[j] = get4(m, i, n, vec);
-            vc[j] = get4(v, i, n, vec);
+            mc[j] = get4<STREAM>(m, i, n, vec);
+            vc[j] = get4<STREAM>(v, i, n, vec);
             const bool in = group * ADAMW_GROUP < n;
             ms[j] = in ? t.m_scale[group] : 0.0f;
             vs[j] = in ? t.v_scale[group] : 0.0f;
@@ -208,10 +216,10 @@ __global__ void __launch_bounds__(BLOCK) k_adamw(AdamwStep a, u32 first_chunk)
             const u32 off = (u32)i * 0x9E3779B1u + a.walk;
             const u32 root = root_code(r.x * ri, off >> 12) | root_code(r.y * ri, (off + 0x9E3779B1u) >> 12) << 8 |
                              root_code(r.z * ri, (off + 2u * 0x9E3779B1u) >> 12) << 16 | root_code(r.w * ri, (off + 3u * 0x9E3779B1u) >> 12) << 24;
-            put4(param, i, n, vec, p[j]);
-            put4(m, i, n, vec, (u32)code);
-            put4(v, i, n, vec, root);
-            if (t.copy) put4(t.copy, i, n, vec, p[j]);
+            put4<STREAM>(param, i, n, vec, p[j]);
+            put4<STREAM>(m, i, n, vec, (u32)code);
+            put4<STREAM>(v, i, n, vec, root);
+            if (t.copy) put4<STREAM>(t.copy, i, n, vec, p[j]);
             if (lane_id() == 0 && i < n) {
                 t.m_scale[group] = mi == 0.0f && mx < 1.0f ? 0.0f : mx * (1.0f / 448.0f);
                 t.v_scale[group] = ri == 0.0f && rx < 1.0f ? 0.0f : rx * (1.0f / 448.0f);
@@ -253,7 +261,7 @@ struct tensair_adamw {
     const AdamwTensor *tensors;
     const u32 *chunks;
     u32 first[4], count[4];    // chunks by types: parameters fp32 or bfloat16, gradients fp32 or bfloat16
-    bool eight;
+    bool eight, stream;
 };
 
 template <typename TP, typename TG>
@@ -261,8 +269,10 @@ static void launch_adamw(const tensair_adamw *h, const AdamwStep &a, int kind, h
 {
     if (!h->count[kind]) return;
     const dim3 grid(h->count[kind]), blk(BLOCK);
-    if (h->eight) hipLaunchKernelGGL((k_adamw<TP, TG, true>), grid, blk, 0, st, a, h->first[kind]);
-    else hipLaunchKernelGGL((k_adamw<TP, TG, false>), grid, blk, 0, st, a, h->first[kind]);
+    if (h->eight && h->stream) hipLaunchKernelGGL((k_adamw<TP, TG, true, true>), grid, blk, 0, st, a, h->first[kind]);
+    else if (h->eight) hipLaunchKernelGGL((k_adamw<TP, TG, true, false>), grid, blk, 0, st, a, h->first[kind]);
+    else if (h->stream) hipLaunchKernelGGL((k_adamw<TP, TG, false, true>), grid, blk, 0, st, a, h->first[kind]);
+    else hipLaunchKernelGGL((k_adamw<TP, TG, false, false>), grid, blk, 0, st, a, h->first[kind]);
 }
 
 extern "C" {
@@ -294,6 +304,7 @@ int tensair_adamw_init(tensair_adamw **out, const tensair_adamw_tensor *tensors,
         h = new tensair_adamw;
         memset(h, 0, sizeof(*h));
         h->eight = state_dtype == TENSAIR_FP8;
+        i64 bytes = 0;
         u32 at = 0;
         for (int kind = 0; kind < 4; ++kind) {
             h->first[kind] = at;
@@ -301,6 +312,7 @@ int tensair_adamw_init(tensair_adamw **out, const tensair_adamw_tensor *tensors,
                 const tensair_adamw_tensor &x = tensors[k];
                 if (x.n == 0 || kind_of(x) != kind) continue;
                 const uintptr_t pa = x.param_dtype == TENSAIR_F32 ? 15 : 7, ga = x.grad_dtype == TENSAIR_F32 ? 15 : 7, sa = h->eight ? 3 : 15;
+                bytes += x.n * ((x.param_dtype == TENSAIR_F32 ? 4 : 2) + (x.grad_dtype == TENSAIR_F32 ? 4 : 2) + (h->eight ? 2 : 8));
                 AdamwTensor &d = dt[k];
                 d.param = x.param;
                 d.grad = x.grad;
@@ -318,6 +330,7 @@ int tensair_adamw_init(tensair_adamw **out, const tensair_adamw_tensor *tensors,
             }
             h->count[kind] = at - h->first[kind];
         }
+        h->stream = bytes > ADAMW_STREAM_BYTES;
         h->tensors = (const AdamwTensor *)workspace;
         h->chunks = (const u32 *)((char *)workspace + head);
         hipStream_t st = (hipStream_t)stream;

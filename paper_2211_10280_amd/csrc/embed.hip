@@ -90,6 +90,8 @@ struct EmbedGradArgs {
     int *valid;                  // [1] tokens whose ids are in range: they come first in the sorted order
     float *part;                 // [tiles][2][4 * C4]
     int *long_n, *long_list;     // rows that cross a border of tiles, by the tile that they begin in
+    int tile, tiles;             // tokens to a tile, a power of two; tiles
+    float *blocks;               // [tiles / EMBED_BLOCK][4 * C4] shares of a row that has all of a block's tiles (NULL: few tiles)
 };
 
 template <typename T>
@@ -352,8 +354,7 @@ __global__ void __launch_bounds__(BLOCK) k_embed_segments(EmbedGradArgs a, u64 *
     }
 }
 
-#define EMBED_TILE 32
-// G lanes sum a tile of EMBED_TILE sorted tokens, row by row; a row that neither begins before the tile nor goes on behind it
+// G lanes sum a tile of sorted tokens, row by row; a row that neither begins before the tile nor goes on behind it
 // is written, of another the tile's share is kept: slot 0 where the row began before, else slot 1.
 template <typename T, int G, int ITERS>
 __global__ void __launch_bounds__(BLOCK) k_embed_reduce(EmbedGradArgs a)
@@ -361,9 +362,9 @@ __global__ void __launch_bounds__(BLOCK) k_embed_reduce(EmbedGradArgs a)
     constexpr int FLIGHT = ITERS > 2 ? 4 : 8;
     const int l = (int)threadIdx.x % G;
     const i64 tile = ((i64)blockIdx.x * BLOCK + threadIdx.x) / G;
-    const int base = (int)(tile * EMBED_TILE), valid = *a.valid;
-    if (tile * EMBED_TILE >= valid) return;
-    const int end = min(valid, base + EMBED_TILE);
+    const int base = (int)(tile * a.tile), valid = *a.valid;
+    if (tile * a.tile >= valid) return;
+    const int end = min(valid, base + a.tile);
     int cur = a.seg_of[base];
     bool before = base > 0 && a.seg_of[base - 1] == cur;
     const int next = end < valid ? a.seg_of[end] : -1;
@@ -421,51 +422,103 @@ __global__ void __launch_bounds__(BLOCK) k_embed_reduce(EmbedGradArgs a)
     if (on && !before && l == 0) a.long_list[atomicAdd(a.long_n, 1)] = (int)tile;
 }
 
-#define EMBED_JOIN 1024
-// A workgroup per row that crosses tiles: its tiles' shares in order, in EMBED_JOIN / G parts.
-template <int G, int ITERS>
-__global__ void __launch_bounds__(EMBED_JOIN) k_embed_join(EmbedGradArgs a)
+#define EMBED_BLOCK 64
+#define EMBED_BLOCK_MIN 1024      // tiles from which on adding up whole blocks of them is worth a launch
+// adds up what at() gives for every share, in THREADS / G parts of shares that follow one another (the same for every thread of the
+// workgroup); true for the threads that have the sum
+template <int G, int ITERS, int THREADS, typename F>
+__device__ __forceinline__ bool sum_shares(float4 (&acc)[ITERS], int shares, int C4, float4 *sums, F at)
 {
-    constexpr int PARTS = EMBED_JOIN / G;
-    __shared__ float4 sums[(PARTS - 1) * G * ITERS];
+    constexpr int PARTS = THREADS / G, FLIGHT = ITERS > 2 ? 4 : 8;
     const int l = (int)threadIdx.x % G, part = (int)threadIdx.x / G;
+    const int per = (shares + PARTS - 1) / PARTS, lo = part * per, hi = min(shares, lo + per);
+    zero_row<ITERS>(acc);
+    for (int e = lo; e < hi; e += FLIGHT) {
+        float4 r[FLIGHT][ITERS];
+#pragma unroll
+        for (int k = 0; k < FLIGHT; ++k)
+#pragma unroll
+            for (int it = 0; it < ITERS; ++it) {
+                const int c = l + G * it;
+                r[k][it] = e + k < hi && c < C4 ? ld4(at(e + k) + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+        for (int k = 0; k < FLIGHT; ++k)
+            if (e + k < hi) add_row<ITERS>(acc, r[k]);
+    }
+    if (part > 0)
+#pragma unroll
+        for (int it = 0; it < ITERS; ++it) sums[((part - 1) * ITERS + it) * G + l] = acc[it];
+    __syncthreads();
+    if (part == 0) {
+        const int used = (shares + per - 1) / per;
+        for (int s = 1; s < used; ++s)
+#pragma unroll
+            for (int it = 0; it < ITERS; ++it) add4(acc[it], sums[((s - 1) * ITERS + it) * G + l]);
+    }
+    __syncthreads();
+    return part == 0;
+}
+// A block of EMBED_BLOCK tiles that one row has all of, having begun before: their shares summed.  (A word that is a third of
+// 262 143 tokens: 2 700 shares, by one workgroup of k_embed_join alone 35 us.)
+template <int G, int ITERS>
+__global__ void __launch_bounds__(BLOCK) k_embed_blocks(EmbedGradArgs a)
+{
+    __shared__ float4 sums[(BLOCK / G > 1 ? BLOCK / G - 1 : 1) * G * ITERS];
+    const i64 tile = (i64)blockIdx.x * EMBED_BLOCK;
+    const int valid = *a.valid;
+    if ((tile + EMBED_BLOCK) * a.tile > valid) return;
+    const int seg = a.seg_of[tile * a.tile];
+    if (a.seg_start[seg] >= tile * a.tile || a.seg_start[seg + 1] < (tile + EMBED_BLOCK) * a.tile) return;
+    float4 acc[ITERS];
+    if (!sum_shares<G, ITERS, BLOCK>(acc, EMBED_BLOCK, a.C4, sums, [&](int e) -> const float * { return a.part + 2 * (tile + e) * a.C4 * 4; })) return;
+    const int l = (int)threadIdx.x % G;
+#pragma unroll
+    for (int it = 0; it < ITERS; ++it)
+        if (l + G * it < a.C4) st4(a.blocks + ((i64)blockIdx.x * a.C4 + l + G * it) * 4, acc[it]);
+}
+// A row that crosses tiles: its shares are those of the tiles up to a border of blocks, whole blocks, the tiles behind them.
+struct LongRow {
+    i64 tile, first_block, end_block;
+    int seg, head, blocks, tail;
+    __device__ __forceinline__ LongRow(const EmbedGradArgs &a, int x)
+    {
+        tile = a.long_list[x];
+        seg = a.seg_of[tile * a.tile + a.tile - 1];                             // its first tile's last token's: it goes on behind it
+        const i64 end = (i64)a.seg_start[seg + 1], last = (end - 1) / a.tile;
+        first_block = tile / EMBED_BLOCK + 1;
+        end_block = end / ((i64)a.tile * EMBED_BLOCK);
+        blocks = a.blocks && end_block > first_block ? (int)(end_block - first_block) : 0;
+        head = blocks ? (int)(first_block * EMBED_BLOCK - tile) : (int)(last - tile) + 1;
+        tail = blocks ? (int)(last + 1 - end_block * EMBED_BLOCK) : 0;
+    }
+    __device__ __forceinline__ int shares() const { return head + blocks + tail; }
+    __device__ __forceinline__ const float *at(const EmbedGradArgs &a, int e) const
+    {
+        if (e < head) return a.part + (2 * (tile + e) + (e == 0 ? 1 : 0)) * a.C4 * 4;
+        if (e < head + blocks) return a.blocks + (first_block + e - head) * a.C4 * 4;
+        return a.part + 2 * (end_block * EMBED_BLOCK + e - head - blocks) * a.C4 * 4;
+    }
+    template <int G, int ITERS>
+    __device__ __forceinline__ void put(const EmbedGradArgs &a, const float4 (&acc)[ITERS], int l) const
+    {
+        const i64 to = a.out.by_id ? (i64)a.row_ids[seg] : (i64)seg;
+#pragma unroll
+        for (int it = 0; it < ITERS; ++it)
+            if (l + G * it < a.C4) put_row_chunk(a.out, to, l + G * it, acc[it]);
+    }
+};
+// A workgroup per row that crosses tiles.
+template <int G, int ITERS>
+__global__ void __launch_bounds__(BLOCK) k_embed_join(EmbedGradArgs a)
+{
+    __shared__ float4 sums[(BLOCK / G > 1 ? BLOCK / G - 1 : 1) * G * ITERS];
     const int rows = *a.long_n;
     for (int x = (int)blockIdx.x; x < rows; x += (int)gridDim.x) {
-        const i64 tile = a.long_list[x];
-        const int seg = a.seg_of[tile * EMBED_TILE + EMBED_TILE - 1];           // its last token's: the row goes on behind it
-        const int shares = (int)((a.seg_start[seg + 1] - 1) / EMBED_TILE - tile) + 1;
-        const int per = (shares + PARTS - 1) / PARTS, lo = part * per, hi = min(shares, lo + per);
+        const LongRow row(a, x);
         float4 acc[ITERS];
-        zero_row<ITERS>(acc);
-        for (int e = lo; e < hi; e += 4) {
-            float4 r[4][ITERS];
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int it = 0; it < ITERS; ++it) {
-                    const int c = l + G * it;
-                    r[k][it] = e + k < hi && c < a.C4 ? ld4(a.part + ((2 * (tile + e + k) + (e + k == 0 ? 1 : 0)) * a.C4 + c) * 4)
-                                                      : make_float4(0.f, 0.f, 0.f, 0.f);
-                }
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (e + k < hi) add_row<ITERS>(acc, r[k]);
-        }
-        if (part > 0)
-#pragma unroll
-            for (int it = 0; it < ITERS; ++it) sums[((part - 1) * ITERS + it) * G + l] = acc[it];
-        __syncthreads();
-        if (part == 0) {
-            const int used = (shares + per - 1) / per;
-            for (int s = 1; s < used; ++s)
-#pragma unroll
-                for (int it = 0; it < ITERS; ++it) add4(acc[it], sums[((s - 1) * ITERS + it) * G + l]);
-            const i64 at = a.out.by_id ? (i64)a.row_ids[seg] : (i64)seg;
-#pragma unroll
-            for (int it = 0; it < ITERS; ++it)
-                if (l + G * it < a.C4) put_row_chunk(a.out, at, l + G * it, acc[it]);
-        }
-        __syncthreads();
+        if (sum_shares<G, ITERS, BLOCK>(acc, row.shares(), a.C4, sums, [&](int e) { return row.at(a, e); }))
+            row.template put<G, ITERS>(a, acc, (int)threadIdx.x % G);
     }
 }
 
@@ -485,7 +538,7 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 struct EmbedSizes {
     bool few, chained;
-    int passes, bits, tiles, seg_tiles, sum_tiles;
+    int passes, bits, tiles, seg_tiles, sum_tiles, tile;
     size_t nd, pub, clear, tile0, per_pass, seg_state, hist, none;     // words of the published area
 };
 EmbedSizes embed_sizes(i64 V, i64 n)
@@ -499,7 +552,9 @@ EmbedSizes embed_sizes(i64 V, i64 n)
     s.nd = (size_t)1 << s.bits;
     s.tiles = tn_prep_tiles(n);
     s.seg_tiles = tn_prep_seg_tiles(n);
-    s.sum_tiles = (int)((n + EMBED_TILE - 1) / EMBED_TILE);
+    s.tile = 4;
+    while (s.tile < 64 && n / s.tile > 8192) s.tile *= 2;
+    s.sum_tiles = (int)((n + s.tile - 1) / s.tile);
     s.chained = s.tiles <= TN_PREP_CHAIN_OWN;
     // tickets (a word per pass and one of the segments), the segments' words, digit counts, the tiles' words of each pass
     s.seg_state = 8;
@@ -536,6 +591,8 @@ size_t embed_carve(const EmbedSizes &s, i64 V, i64 n, int dim, char *base, Embed
     }
     char *seg_of = take(4 * N), *seg_start = take(4 * rows), *flags = take(256), *list = take(4 * (size_t)s.sum_tiles);
     char *part = take((size_t)s.sum_tiles * 2 * dim * 4), *words = take(4 * s.pub);
+    const bool many = s.sum_tiles > EMBED_BLOCK_MIN;
+    char *blocks = take(many ? ((size_t)s.sum_tiles / EMBED_BLOCK + 1) * dim * 4 : 0);
     if (a) {
         a->seg_of = (int *)seg_of;
         a->seg_start = (int *)seg_start;
@@ -543,6 +600,9 @@ size_t embed_carve(const EmbedSizes &s, i64 V, i64 n, int dim, char *base, Embed
         a->long_n = (int *)flags + 1;
         a->long_list = (int *)list;
         a->part = (float *)part;
+        a->tile = s.tile;
+        a->tiles = s.sum_tiles;
+        a->blocks = many ? (float *)blocks : nullptr;
     }
     if (pub) *pub = (u32 *)words;
     return at;
@@ -557,8 +617,10 @@ void launch_sums(const EmbedGradArgs &a, const EmbedSizes &s, hipStream_t st)
     }
     const i64 blocks = ((i64)s.sum_tiles * G + BLOCK - 1) / BLOCK;
     hipLaunchKernelGGL((k_embed_reduce<T, G, ITERS>), dim3((unsigned)blocks), dim3(BLOCK), 0, st, a);
+    if (a.blocks && s.sum_tiles / EMBED_BLOCK > 0)
+        hipLaunchKernelGGL((k_embed_blocks<G, ITERS>), dim3((unsigned)(s.sum_tiles / EMBED_BLOCK)), dim3(BLOCK), 0, st, a);
     if (s.sum_tiles > 1)
-        hipLaunchKernelGGL((k_embed_join<G, ITERS>), dim3((unsigned)std::min(s.sum_tiles, 512)), dim3(EMBED_JOIN), 0, st, a);
+        hipLaunchKernelGGL((k_embed_join<G, ITERS>), dim3((unsigned)std::min(s.sum_tiles, 4096)), dim3(BLOCK), 0, st, a);
 }
 // G lanes to a row: the fewest of 8, 16, 32, 64 that hold it in one chunk a lane; then several chunks a lane
 template <typename T>

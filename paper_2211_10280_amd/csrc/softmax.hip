@@ -46,11 +46,14 @@ struct Operand {
         return (u32)(n < 0 ? 0 : n > 0x7FFFFFF0 ? 0x7FFFFFF0 : n);
     }
 };
-// which parts of either operand a product's segment takes, two bits each: (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
-#define PARTS_A 0x052u         // 2 0 1 1 0 0
-#define PARTS_B 0x118u         // 0 2 1 0 1 0
-__device__ __forceinline__ int part_a(int seg, int nseg) { return nseg == 1 ? 0 : (int)(PARTS_A >> (2 * seg)) & 3; }
-__device__ __forceinline__ int part_b(int seg, int nseg) { return nseg == 1 ? 0 : (int)(PARTS_B >> (2 * seg)) & 3; }
+// which parts of either operand are multiplied, in this order: of three parts (0 the largest) six pairs, the smallest products first
+template <int PARTS> struct Pairs;
+template <> struct Pairs<1> {
+    static constexpr int N = 1, A[1] = {0}, B[1] = {0};
+};
+template <> struct Pairs<3> {
+    static constexpr int N = 6, A[6] = {2, 0, 1, 1, 0, 0}, B[6] = {0, 2, 1, 0, 1, 0};
+};
 
 // The tile of one operand of one step, ROWS of the kept index by BK of the summed one, from memory straight into LDS, 16 bytes
 // a lane.  LDS holds it in the order of the lanes, so what keeps the 32 lanes of a fragment off each other's banks is which chunk
@@ -122,25 +125,32 @@ struct Tile {
 
 // A workgroup's tile of a product: BM of A's rows by BN of B's, WM by WN waves of TM by TN fragments of 32 by 32.  Lane l of a
 // fragment holds the column (B's row) l % 32 and the rows (A's) 8 (r / 4) + 4 (l / 32) + r % 4 in its 16 registers r.
-template <int TM, int TN, int WM, int WN, int STAGES, bool AT, bool BT>
+template <int TM, int TN, int WM, int WN, int STAGES, int PARTS, bool AT, bool BT>
 struct Product {
     static constexpr int THREADS = 64 * WM * WN, BM = 32 * TM * WM, BN = 32 * TN * WN;
     typedef Tile<BM, THREADS, AT> A;
     typedef Tile<BN, THREADS, BT> B;
-    static constexpr int LDS = A::LDS + B::LDS;               // elements of a stage
+    static constexpr int LDS = PARTS * (A::LDS + B::LDS);     // elements of a stage: A's parts, B's parts
     f32x16 acc[TM][TN];
     A a;
     B b;
 
-    static __device__ __forceinline__ void fragments_a(const bf16_t *__restrict lds, int wm, int kk, hw_bf16x8 (&f)[TM])
+    static __device__ __forceinline__ void fragments(const bf16_t *__restrict lds, int wm, int wn, int kk, hw_bf16x8 (&fa)[PARTS][TM], hw_bf16x8 (&fb)[PARTS][TN])
     {
 #pragma unroll
-        for (int i = 0; i < TM; ++i) f[i] = A::fragment(lds, (wm * TM + i) * 32, kk);
+        for (int part = 0; part < PARTS; ++part) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i) fa[part][i] = A::fragment(lds + part * A::LDS, (wm * TM + i) * 32, kk);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) fb[part][j] = B::fragment(lds + PARTS * A::LDS + part * B::LDS, (wn * TN + j) * 32, kk);
+        }
     }
-    static __device__ __forceinline__ void fragments_b(const bf16_t *__restrict lds, int wn, int kk, hw_bf16x8 (&f)[TN])
+    __device__ __forceinline__ void fetch(const Operand &x, i64 row_x, const Operand &y, i64 row_y, i64 k, bf16_t *__restrict lds, int wave) const
     {
 #pragma unroll
-        for (int j = 0; j < TN; ++j) f[j] = B::fragment(lds, (wn * TN + j) * 32, kk);
+        for (int part = 0; part < PARTS; ++part) a.fetch_all(A::source(x, part, row_x, k), lds + part * A::LDS, wave);
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) b.fetch_all(B::source(y, part, row_y, k), lds + PARTS * A::LDS + part * B::LDS, wave);
     }
     // Waits for all but the last N of this wave's fetches, which come back in order, and for its reads of LDS, then for the other waves.
     template <int N>
@@ -156,34 +166,32 @@ struct Product {
     // step STAGES - 1 later set out into `next`; fragments of 16 of the summed index are read while those before are multiplied; in
     // the end the next step's tiles are there, and every wave is done with these.
     template <bool FIRST>
-    __device__ __forceinline__ void step(typename A::Source from_a, typename B::Source from_b, bf16_t *__restrict next, const bf16_t *__restrict cur,
-                                         int wave, int wm, int wn)
+    __device__ __forceinline__ void step(const Operand &x, i64 row_x, const Operand &y, i64 row_y, i64 k, bf16_t *__restrict next,
+                                         const bf16_t *__restrict cur, int wave, int wm, int wn)
     {
         constexpr int KK = BK / 16;
-        a.fetch_all(from_a, next, wave);
-        b.fetch_all(from_b, next + A::LDS, wave);
+        fetch(x, row_x, y, row_y, k, next, wave);
         __builtin_amdgcn_sched_barrier(0);
-        hw_bf16x8 fa[2][TM], fb[2][TN];
+        hw_bf16x8 fa[2][PARTS][TM], fb[2][PARTS][TN];
         f32x16 zero;
 #pragma unroll
         for (int r = 0; r < 16; ++r) zero[r] = 0.f;
-        fragments_a(cur, wm, 0, fa[0]);
-        fragments_b(cur + A::LDS, wn, 0, fb[0]);
+        fragments(cur, wm, wn, 0, fa[0], fb[0]);
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) {
-            if (kk + 1 < KK) {
-                fragments_a(cur, wm, kk + 1, fa[(kk + 1) & 1]);
-                fragments_b(cur + A::LDS, wn, kk + 1, fb[(kk + 1) & 1]);
-            }
+            if (kk + 1 < KK) fragments(cur, wm, wn, kk + 1, fa[(kk + 1) & 1], fb[(kk + 1) & 1]);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+            for (int q = 0; q < Pairs<PARTS>::N; ++q)
 #pragma unroll
-                for (int j = 0; j < TN; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[kk & 1][i], fb[kk & 1][j], FIRST && kk == 0 ? zero : acc[i][j], 0, 0, 0);
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[kk & 1][Pairs<PARTS>::A[q]][i], fb[kk & 1][Pairs<PARTS>::B[q]][j],
+                                                                            FIRST && kk == 0 && q == 0 ? zero : acc[i][j], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
         }
-        meet<(STAGES - 2) * (A::PER + B::PER)>();
+        meet<(STAGES - 2) * PARTS * (A::PER + B::PER)>();
     }
 };
 
@@ -197,7 +205,7 @@ __device__ __forceinline__ int die_order(int b, int n)
 // ---------------------------------------------------------------- logits
 struct LogitsArgs {
     Operand w, h;              // words' and tokens' rows
-    int nseg, K;
+    int K;
     i64 word0, V;              // first word of this launch's range; words in all
     int tiles, per, strips;    // tiles of words of the range, of a strip; strips
     int token_tiles;
@@ -231,15 +239,16 @@ __device__ __forceinline__ v4u join_halves(u32 x0, u32 x1, u32 y0, u32 y1)
 // GRAD false: the running maximum and sum of every token over a strip of words; true: dz of the strip, in PARTS bfloat16 parts.
 // A strip's tiles follow one another without a pause: the next tile's first step is in flight while this one's logits are used.
 template <int TM, int TN, int WM, int WN, int STAGES, bool GRAD, int PARTS>
-__global__ void __launch_bounds__(64 * WM * WN, 2) k_logits(LogitsArgs a)
+__global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_logits(LogitsArgs a)
 {
-    typedef Product<TM, TN, WM, WN, STAGES, false, false> P;
+    typedef Product<TM, TN, WM, WN, STAGES, PARTS, false, false> P;
     __shared__ __attribute__((aligned(16))) bf16_t lds[P::LDS * STAGES];
     const int work = die_order((int)blockIdx.x, (int)gridDim.x);
     const int strip = work / a.token_tiles, tt = work % a.token_tiles;
     const int wave = uniform((int)(threadIdx.x >> 6)), wm = wave / WN, wn = wave % WN, lane = lane_id();
     const i64 tok0 = (i64)tt * P::BN;
-    const int t0 = strip * a.per, t1 = min(a.tiles, t0 + a.per), steps = (a.K / BK) * a.nseg;
+    constexpr int F = SM_BM / P::BM;
+    const int t0 = strip * a.per * F, t1 = min(a.tiles * F, t0 + a.per * F), steps = a.K / BK;
     P p;
     float top[TN], sum[TN], l2[TN], d[TN];
     int label[TN];
@@ -257,29 +266,24 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_logits(LogitsArgs a)
     i64 word = a.word0 + (i64)t0 * P::BM;
     p.a.place(a.w);
     p.b.place(a.h);
-    // the step to be fetched next: tile of words, part, place in the rows; behind the strip's last nobody uses it
+    // the step to be fetched next: tile of words, place in the rows; behind the strip's last nobody uses it
     i64 fetch_word = (i64)t0 * P::BM;                         // of the range
-    int k = 0, seg = 0, cur = 0;
+    int k = 0, cur = 0;
     auto advance = [&] {
         if ((k += BK) == a.K) {
             k = 0;
-            if (++seg == a.nseg) {
-                seg = 0;
-                fetch_word += P::BM;
-            }
+            fetch_word += P::BM;
         }
     };
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) {
-        p.a.fetch_all(P::A::source(a.w, part_a(seg, a.nseg), fetch_word, k), lds + s * P::LDS, wave);
-        p.b.fetch_all(P::B::source(a.h, part_b(seg, a.nseg), tok0, k), lds + s * P::LDS + P::A::LDS, wave);
+        p.fetch(a.w, fetch_word, a.h, tok0, k, lds + s * P::LDS, wave);
         advance();
     }
     __syncthreads();
     for (int t = t0; t < t1; ++t, word += P::BM) {
         auto step = [&](auto first) {
-            p.template step<first()>(P::A::source(a.w, part_a(seg, a.nseg), fetch_word, k), P::B::source(a.h, part_b(seg, a.nseg), tok0, k),
-                                     lds + (cur == 0 ? STAGES - 1 : cur - 1) * P::LDS, lds + cur * P::LDS, wave, wm, wn);
+            p.template step<first()>(a.w, fetch_word, a.h, tok0, k, lds + (cur == 0 ? STAGES - 1 : cur - 1) * P::LDS, lds + cur * P::LDS, wave, wm, wn);
             advance();
             cur = cur == STAGES - 1 ? 0 : cur + 1;
         };
@@ -599,7 +603,6 @@ __global__ void __launch_bounds__(BLOCK) k_few(FewArgs a)
 // ---------------------------------------------------------------- products with dz
 struct ProductArgs {
     Operand a, b;              // C[n][m] = sum_k a(m, k) b(n, k)
-    int nseg;
     i64 M, N, K;
     int m_tiles, n_tiles, splits;
     i64 k_per;                 // of a split, a multiple of BK
@@ -609,10 +612,10 @@ struct ProductArgs {
     int dtype;
     float scale;
 };
-template <int TM, int TN, int WM, int WN, int STAGES, bool BT>
-__global__ void __launch_bounds__(64 * WM * WN, 2) k_product(ProductArgs a)
+template <int TM, int TN, int WM, int WN, int STAGES, int PARTS, bool BT>
+__global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_product(ProductArgs a)
 {
-    typedef Product<TM, TN, WM, WN, STAGES, true, BT> P;
+    typedef Product<TM, TN, WM, WN, STAGES, PARTS, true, BT> P;
     __shared__ __attribute__((aligned(16))) bf16_t lds[P::LDS * STAGES];
     int work = die_order((int)blockIdx.x, (int)gridDim.x);
     const int mt = work % a.m_tiles;
@@ -624,26 +627,15 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_product(ProductArgs a)
     P p;
     p.a.place(a.a);
     p.b.place(a.b);
-    const int steps = (int)((k1 - k0) / BK) * a.nseg;
-    int seg = 0, cur = 0;
-    i64 k = k0;
-    auto advance = [&] {
-        if ((k += BK) >= k1) {
-            k = k0;
-            seg = min(seg + 1, a.nseg - 1);                   // behind the last step a tile is fetched that nobody uses
-        }
-    };
+    const int steps = (int)((k1 - k0) / BK);
+    int cur = 0;
+    i64 k = k0;                                               // behind the last step tiles are fetched that nobody uses
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s) {
-        p.a.fetch_all(P::A::source(a.a, part_a(seg, a.nseg), m0, k), lds + s * P::LDS, wave);
-        p.b.fetch_all(P::B::source(a.b, part_b(seg, a.nseg), n0, k), lds + s * P::LDS + P::A::LDS, wave);
-        advance();
-    }
+    for (int s = 0; s < STAGES - 1; ++s, k += BK) p.fetch(a.a, m0, a.b, n0, k, lds + s * P::LDS, wave);
     __syncthreads();
     auto step = [&](auto first) {
-        p.template step<first()>(P::A::source(a.a, part_a(seg, a.nseg), m0, k), P::B::source(a.b, part_b(seg, a.nseg), n0, k),
-                                 lds + (cur == 0 ? STAGES - 1 : cur - 1) * P::LDS, lds + cur * P::LDS, wave, wm, wn);
-        advance();
+        p.template step<first()>(a.a, m0, a.b, n0, k, lds + (cur == 0 ? STAGES - 1 : cur - 1) * P::LDS, lds + cur * P::LDS, wave, wm, wn);
+        k += BK;
         cur = cur == STAGES - 1 ? 0 : cur + 1;
     };
     step(std::true_type{});
@@ -682,6 +674,28 @@ struct JoinArgs {
     int dtype;
     float scale;
 };
+__device__ __forceinline__ void put_joined(const JoinArgs &a, i64 c, float4 v)
+{
+    const i64 row = c / a.C4, at = row * a.stride + 4 * (c - row * a.C4);
+    v = make_float4(v.x * a.scale, v.y * a.scale, v.z * a.scale, v.w * a.scale);
+    if (a.label && a.label[row] < 0) v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (a.dtype == TENSAIR_F32) st4((float *)a.out + at, v);
+    else st4((bf16_t *)a.out + at, v);
+}
+// a thread takes a chunk of 4 elements of all slots
+__global__ void __launch_bounds__(BLOCK) k_join_flat(JoinArgs a)
+{
+    const i64 all = a.n * a.C4;
+    for (i64 c = (i64)blockIdx.x * BLOCK + threadIdx.x; c < all; c += (i64)gridDim.x * BLOCK) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int s = 0; s < a.n_slots; ++s) {
+            const float4 x = ld4(a.slots + ((i64)s * all + c) * 4);
+            v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
+        }
+        put_joined(a, c, v);
+    }
+}
 // a workgroup takes 64 chunks of 4 elements, its 16 waves parts of the slots that follow one another
 __global__ void __launch_bounds__(1024) k_join(JoinArgs a)
 {
@@ -705,11 +719,7 @@ __global__ void __launch_bounds__(1024) k_join(JoinArgs a)
                 const float4 x = sums[w - 1][lane];
                 v = make_float4(v.x + x.x, v.y + x.y, v.z + x.z, v.w + x.w);
             }
-            const i64 row = c / a.C4, at = row * a.stride + 4 * (c - row * a.C4);
-            v = make_float4(v.x * a.scale, v.y * a.scale, v.z * a.scale, v.w * a.scale);
-            if (a.label && a.label[row] < 0) v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (a.dtype == TENSAIR_F32) st4((float *)a.out + at, v);
-            else st4((bf16_t *)a.out + at, v);
+            put_joined(a, c, v);
         }
         __syncthreads();
     }
@@ -811,11 +821,11 @@ int launched(const char *what)
 unsigned blocks_for(i64 items) { return (unsigned)std::min<i64>(cdiv(items, BLOCK), 1 << 20); }
 
 // Tiles of logits: 256 words by 128 tokens, a wave's 128 by 64, two workgroups to a compute unit, so that one's exponentials run
-// beside the other's products; three stages, as much as LDS holds twice.
+// beside the other's products; three stages, as much as LDS holds twice.  Of three parts 64 words by 128 tokens, for the same reason
+// (50 000 words, 1 024 tokens, rows of 300: 228 us and with dz 272; with 256 words, one workgroup, 244 and 299).
 #define SM_BN 128              // tokens of a tile
 #define SM_BN_FEW 64           // ... where there are at most so many
 #define SM_WAVES_M 2           // rows of waves of a tile, each with a maximum and a sum of its own
-#define SM_PN 128              // rows of a tile of the products with dz
 #define SM_RANGE_TILES 4096    // tiles of a range, at most: how far a fetch is off its tile's first element fits 31 bits
 #define SM_BLOCKS 512          // workgroups that fill the chip, two to a compute unit
 #define SM_DZ_BYTES ((i64)1 << 30)   // dz of a range, about: with half as much the products took 3 to 8 % longer
@@ -823,11 +833,11 @@ unsigned blocks_for(i64 items) { return (unsigned)std::min<i64>(cdiv(items, BLOC
 struct SoftmaxPlan {
     bool few;                  // at most FEW_TOKENS tokens
     int few_blocks;
-    int parts, nseg, Dp, bn, token_tiles, wm;
+    int parts, Dp, bn, token_tiles, wm;
     i64 Np, tiles;             // tokens, padded; tiles of words
     i64 range_tiles, ranges;   // tiles of words that are laid out, and whose dz is kept, at a time
     int per, strips;           // tiles to a strip, strips of a range
-    int tm, m_tiles;           // of the products: fragments of a wave along the row length, tiles
+    int tm, m_tiles, pn;       // of the products: fragments of a wave along the row length, tiles; rows of a tile
     int h_splits, t_splits;    // of d_hidden's sum over a range's words, of d_table's over the tokens
     i64 h_k, t_k;
 };
@@ -839,7 +849,6 @@ SoftmaxPlan plan_of(i64 n, i64 V, int D, int dtype, bool grad)
     s.few = n <= FEW_TOKENS;
     s.few_blocks = (int)std::max<i64>(1, std::min<i64>(cdiv(V, 64), grad ? FEW_BLOCKS / 2 : FEW_BLOCKS));
     s.parts = dtype == TENSAIR_F32 ? 3 : 1;
-    s.nseg = dtype == TENSAIR_F32 ? 6 : 1;
     s.Dp = (int)cdiv(D, BK) * BK;
     const bool few = n <= SM_BN_FEW;
     s.bn = few ? SM_BN_FEW : SM_BN;
@@ -855,19 +864,22 @@ SoftmaxPlan plan_of(i64 n, i64 V, int D, int dtype, bool grad)
     const i64 want = std::max<i64>(1, std::min<i64>(s.range_tiles, cdiv(SM_BLOCKS * 2, s.token_tiles)));
     s.per = (int)cdiv(s.range_tiles, want);
     s.strips = (int)cdiv(s.range_tiles, s.per);
-    // fragments of a wave (two to a tile along the row length): the fewest columns beyond the row, then the largest tile
+    // fragments of a wave along the row length, two waves to a tile: few columns beyond the row, but a wider tile fetches less.  Of three
+    // parts one: six products a fetch are enough, and two workgroups find room on a compute unit (50 000 words, 1 024 tokens, rows of
+    // 300: the two products 188 and 182 us, with three fragments 241 and 281).
     i64 least = -1;
-    for (int tm = 1; tm <= 5; ++tm) {
-        const i64 cols = cdiv(s.Dp, 64 * tm) * 64 * tm;
-        if (least < 0 || cols <= least) {
-            least = cols;
+    for (int tm = 1; tm <= (s.parts == 1 ? 5 : 1); ++tm) {
+        const i64 cost = cdiv(s.Dp, 64 * tm) * 64 * (2 * tm + 1); // columns times 1 + 1 / (2 tm)
+        if (least < 0 || cost <= least) {
+            least = cost;
             s.tm = tm;
         }
     }
     s.m_tiles = (int)cdiv(s.Dp, 64 * s.tm);
+    s.pn = s.parts == 1 && s.tm <= 2 ? 256 : 128;                             // short rows: what is fetched for a product would be more than the memory pipe gives
     const i64 range_words = s.range_tiles * SM_BM;
-    const i64 h_tiles = s.m_tiles * cdiv(s.Np, SM_PN), t_tiles = s.m_tiles * cdiv(range_words, SM_PN);
-    i64 splits = std::max<i64>(1, std::min<i64>(cdiv(SM_BLOCKS, h_tiles), range_words / 512));
+    const i64 h_tiles = s.m_tiles * cdiv(s.Np, s.pn), t_tiles = s.m_tiles * cdiv(range_words, s.pn);
+    i64 splits = std::max<i64>(1, std::min<i64>(SM_BLOCKS / h_tiles, range_words / 512));
     s.h_k = cdiv(cdiv(range_words, splits), BK) * BK;
     s.h_splits = (int)cdiv(range_words, s.h_k);
     splits = std::max<i64>(1, std::min<i64>(SM_BLOCKS / t_tiles, s.Np / 512));
@@ -977,7 +989,6 @@ LogitsArgs lay_out_range(const SoftmaxPlan &s, const SoftmaxBuffers &b, const Ra
     memset(&a, 0, sizeof(a));
     a.w = Operand{b.w, r.rows, r.rows * s.Dp};
     a.h = Operand{b.h, s.Np, s.Np * s.Dp};
-    a.nseg = s.nseg;
     a.K = s.Dp;
     a.word0 = r.word0;
     a.V = V;
@@ -1038,25 +1049,40 @@ FewArgs few_args(const SoftmaxPlan &s, const SoftmaxBuffers &b, const void *hidd
 template <bool GRAD, int PARTS>
 void launch_logits(const SoftmaxPlan &s, const LogitsArgs &a, hipStream_t st)
 {
+    constexpr int STAGES = PARTS == 1 ? 3 : 2;
     const dim3 grid((unsigned)(a.strips * a.token_tiles)), blk(256);
-    if (s.bn == SM_BN_FEW) hipLaunchKernelGGL((k_logits<2, 2, 4, 1, 3, GRAD, PARTS>), grid, blk, 0, st, a);
-    else hipLaunchKernelGGL((k_logits<4, 2, 2, 2, 3, GRAD, PARTS>), grid, blk, 0, st, a);
+    if (s.bn == SM_BN_FEW) hipLaunchKernelGGL((k_logits<2, 2, 4, 1, STAGES, GRAD, PARTS>), grid, blk, 0, st, a);
+    else hipLaunchKernelGGL((k_logits<PARTS == 1 ? 4 : 1, 2, 2, 2, STAGES, GRAD, PARTS>), grid, blk, 0, st, a);
 }
-template <bool BT>
-void launch_product(int tm, const ProductArgs &a, hipStream_t st)
+template <int PARTS, bool BT>
+void launch_product_p(int tm, const ProductArgs &a, hipStream_t st)
 {
     const dim3 grid((unsigned)(a.m_tiles * a.n_tiles * a.splits)), blk(256);
     switch (tm) {
-    case 1: hipLaunchKernelGGL((k_product<1, 2, 2, 2, 2, BT>), grid, blk, 0, st, a); break;
-    case 2: hipLaunchKernelGGL((k_product<2, 2, 2, 2, 2, BT>), grid, blk, 0, st, a); break;
-    case 3: hipLaunchKernelGGL((k_product<3, 2, 2, 2, 2, BT>), grid, blk, 0, st, a); break;
-    case 4: hipLaunchKernelGGL((k_product<4, 2, 2, 2, 2, BT>), grid, blk, 0, st, a); break;
-    default: hipLaunchKernelGGL((k_product<5, 2, 2, 2, 2, BT>), grid, blk, 0, st, a); break;
+    case 1: hipLaunchKernelGGL((k_product<1, PARTS == 1 ? 4 : 2, 2, 2, 2, PARTS, BT>), grid, blk, 0, st, a); break;
+    case 2: hipLaunchKernelGGL((k_product<2, PARTS == 1 ? 4 : 2, 2, 2, 2, PARTS, BT>), grid, blk, 0, st, a); break;
+    case 3: hipLaunchKernelGGL((k_product<3, 2, 2, 2, 2, PARTS, BT>), grid, blk, 0, st, a); break;
+    case 4: hipLaunchKernelGGL((k_product<4, 2, 2, 2, 2, PARTS, BT>), grid, blk, 0, st, a); break;
+    default:
+        if constexpr (PARTS == 1) hipLaunchKernelGGL((k_product<5, 2, 2, 2, 2, PARTS, BT>), grid, blk, 0, st, a);
+        break;
     }
+}
+template <bool BT>
+void launch_product(const SoftmaxPlan &s, const ProductArgs &a, hipStream_t st)
+{
+    if (s.parts == 1) launch_product_p<1, BT>(s.tm, a, st);
+    else launch_product_p<3, BT>(s.tm, a, st);
 }
 void launch_join(const float *slots, int n_slots, i64 rows, i64 stride, int D, const int *label, void *out, int dtype, float scale, hipStream_t st)
 {
     JoinArgs j = {slots, n_slots, rows, stride, D / 4, label, out, dtype, scale};
+    // many slots of a small matrix (one token against a million words: 512) want the parallel form, others fill the chip without
+    const i64 chunks = rows * (D / 4);
+    if (n_slots <= 16 || chunks >= 65536) {
+        hipLaunchKernelGGL(k_join_flat, dim3(blocks_for(chunks)), dim3(BLOCK), 0, st, j);
+        return;
+    }
     hipLaunchKernelGGL(k_join, dim3((unsigned)std::min<i64>(cdiv(rows * (D / 4), WAVE), 1 << 18)), dim3(1024), 0, st, j);
 }
 
@@ -1105,7 +1131,8 @@ int tensair_softmax_loss(const void *hidden, int64_t hidden_stride, const void *
     for (i64 range = 0; range < (s.few ? 0 : s.ranges); ++range) {
         LogitsArgs a = lay_out_range(s, b, range_of(s, range, vocab), table, table_stride, dtype, dim, vocab, scale, st);
         a.part += (i64)slots * s.Np;
-        launch_logits<false, 1>(s, a, st);
+        if (s.parts == 1) launch_logits<false, 1>(s, a, st);
+        else launch_logits<false, 3>(s, a, st);
         slots += a.strips * s.wm;
     }
     LossArgs l = {b.part, slots, s.Np, n, b.picked, b.label, loss, lse};
@@ -1161,7 +1188,6 @@ int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *
         const Operand dz = {b.dz, s.Np, a.dz_plane};
         ProductArgs p;
         memset(&p, 0, sizeof(p));
-        p.nseg = s.nseg;
         p.m_tiles = s.m_tiles;
         p.M = dim;
         p.dtype = dtype;
@@ -1171,11 +1197,11 @@ int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *
             p.b = dz;
             p.N = n;
             p.K = cdiv(r.words, BK) * BK;
-            p.n_tiles = (int)cdiv(s.Np, SM_PN);
+            p.n_tiles = (int)cdiv(s.Np, s.pn);
             p.k_per = s.h_k;
             p.splits = (int)cdiv(p.K, p.k_per);
             p.slots = b.h_slots + range * s.h_splits * n * dim;
-            launch_product<false>(s.tm, p, st);
+            launch_product<false>(s, p, st);
         }
         if (d_table) {
             p.scale = fabsf(scale);                           // the tokens' rows have its sign
@@ -1183,14 +1209,14 @@ int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *
             p.b = dz;
             p.N = r.words;
             p.K = s.Np;
-            p.n_tiles = (int)cdiv(r.words, SM_PN);
+            p.n_tiles = (int)cdiv(r.words, s.pn);
             p.k_per = s.t_k;
             p.splits = s.t_splits;
             p.slots = s.t_splits > 1 ? b.t_slots : nullptr;
             char *out = (char *)d_table + (size_t)r.word0 * d_table_stride * (dtype == TENSAIR_F32 ? 4 : 2);
             p.out = out;
             p.out_stride = d_table_stride;
-            launch_product<true>(s.tm, p, st);
+            launch_product<true>(s, p, st);
             if (s.t_splits > 1) launch_join(b.t_slots, s.t_splits, r.words, d_table_stride, dim, nullptr, out, dtype, fabsf(scale), st);
         }
     }
