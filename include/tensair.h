@@ -421,7 +421,8 @@ int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *
                          void *workspace, size_t workspace_bytes, int32_t *status, void *stream);
 
 /* AdamW over many tensors at once.  With t the step (counted from 1), g the gradient times *grad_scale (DEVICE float, NULL: 1),
- * every operation in fp32, rounded by itself, in this order (the constants in 64 bits, each rounded once):
+ * every operation in fp32, rounded by itself (the root within a unit in its last place), in this order (the constants in 64 bits,
+ * each rounded once):
  *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) (g g),
  *   param <- param (1 - lr weight_decay) - (m (lr / (1 - beta1^t))) / (sqrt(v) (1 / sqrt(1 - beta2^t)) + eps).
  * State types: TENSAIR_F32 -- m, v: fp32 [n].  TENSAIR_FP8 -- m, v: one 8-bit float (4 exponent, 3 mantissa bits, no

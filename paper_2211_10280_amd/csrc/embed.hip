@@ -808,6 +808,7 @@ int tensair_embed_grad_dense(const int32_t *ids, int64_t n, const void *d_out, i
     if (workspace_bytes < tensair_embed_workspace_bytes(vocab, dim, n))
         return tn_fail(TENSAIR_ECAPACITY, "workspace too small: see tensair_embed_workspace_bytes");
     hipStream_t st = (hipStream_t)stream;
+    if (n == 0 && accumulate) return TENSAIR_OK;
     if (!accumulate) {
         const i64 want = (vocab * (dim / 4) + BLOCK - 1) / BLOCK;
         const dim3 grid((unsigned)std::min<i64>(want, 16384)), blk(BLOCK);
