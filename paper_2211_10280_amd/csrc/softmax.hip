@@ -39,11 +39,18 @@ struct Operand {
     const bf16_t *p;
     i64 rows, plane;           // rows of a block, elements from part to part
     __device__ __forceinline__ const bf16_t *at(int part, i64 r, i64 c) const { return p + part * plane + (c / BK) * (rows * BK) + r * BK + (c & (BK - 1)); }
-    // the bytes from there to the part's end
-    __device__ __forceinline__ u32 left(i64 r, i64 c) const
+    // the bytes from there to the part's end (none beyond it)
+    __device__ __forceinline__ i64 left(i64 r, i64 c) const { return (plane - ((c / BK) * (rows * BK) + r * BK + (c & (BK - 1)))) * 2; }
+};
+// Where the next step's tile of an operand begins: kept from step to step, since working it out anew takes the scalar unit longer than
+// the step has to spare (loss of 4 096 tokens, a million words, rows of 300: STATED_CURSOR).
+struct Cursor {
+    const char *p;
+    i64 left;
+    __device__ __forceinline__ void move(i64 bytes)
     {
-        const i64 n = (plane - ((c / BK) * (rows * BK) + r * BK + (c & (BK - 1)))) * 2;
-        return (u32)(n < 0 ? 0 : n > 0x7FFFFFF0 ? 0x7FFFFFF0 : n);
+        p += bytes;
+        left -= bytes;
     }
 };
 // which parts of either operand are multiplied, in this order: of three parts (0 the largest) six pairs, the smallest products first
@@ -85,10 +92,17 @@ struct Tile {
         }
     }
     typedef __amdgpu_buffer_rsrc_t Source;
-    static __device__ __forceinline__ Source source(const Operand &o, int part, i64 row0, i64 k0)
+    static __device__ __forceinline__ Cursor begin(const Operand &o, i64 row0, i64 k0)
     {
         const i64 r0 = T ? k0 : row0, c0 = T ? row0 : k0;
-        return __builtin_amdgcn_make_buffer_rsrc((void *)o.at(part, r0, c0), 0, (int)o.left(r0, c0), 0x00027000);
+        return Cursor{(const char *)o.at(0, r0, c0), o.left(r0, c0)};
+    }
+    // bytes from a step's tile to the next one's
+    static __device__ __forceinline__ i64 stride(const Operand &o) { return T ? BK * BK * 2 : o.rows * (BK * 2); }
+    static __device__ __forceinline__ Source source(const Cursor &c, i64 part_bytes)
+    {
+        const i64 n = c.left < 0 ? 0 : c.left > 0x7FFFFFF0 ? 0x7FFFFFF0 : c.left;
+        return __builtin_amdgcn_make_buffer_rsrc((void *)(c.p + part_bytes), 0, (int)n, 0x00027000);
     }
     __device__ __forceinline__ void fetch(Source from, int j, bf16_t *__restrict lds, int wave) const
     {
@@ -145,12 +159,12 @@ struct Product {
             for (int j = 0; j < TN; ++j) fb[part][j] = B::fragment(lds + PARTS * A::LDS + part * B::LDS, (wn * TN + j) * 32, kk);
         }
     }
-    __device__ __forceinline__ void fetch(const Operand &x, i64 row_x, const Operand &y, i64 row_y, i64 k, bf16_t *__restrict lds, int wave) const
+    __device__ __forceinline__ void fetch(const Cursor &x, i64 plane_x, const Cursor &y, i64 plane_y, bf16_t *__restrict lds, int wave) const
     {
 #pragma unroll
-        for (int part = 0; part < PARTS; ++part) a.fetch_all(A::source(x, part, row_x, k), lds + part * A::LDS, wave);
+        for (int part = 0; part < PARTS; ++part) a.fetch_all(A::source(x, part * plane_x), lds + part * A::LDS, wave);
 #pragma unroll
-        for (int part = 0; part < PARTS; ++part) b.fetch_all(B::source(y, part, row_y, k), lds + PARTS * A::LDS + part * B::LDS, wave);
+        for (int part = 0; part < PARTS; ++part) b.fetch_all(B::source(y, part * plane_y), lds + PARTS * A::LDS + part * B::LDS, wave);
     }
     // Waits for all but the last N of this wave's fetches, which come back in order, and for its reads of LDS, then for the other waves.
     template <int N>
@@ -166,11 +180,11 @@ struct Product {
     // step STAGES - 1 later set out into `next`; fragments of 16 of the summed index are read while those before are multiplied; in
     // the end the next step's tiles are there, and every wave is done with these.
     template <bool FIRST>
-    __device__ __forceinline__ void step(const Operand &x, i64 row_x, const Operand &y, i64 row_y, i64 k, bf16_t *__restrict next,
+    __device__ __forceinline__ void step(const Cursor &x, i64 plane_x, const Cursor &y, i64 plane_y, bf16_t *__restrict next,
                                          const bf16_t *__restrict cur, int wave, int wm, int wn)
     {
         constexpr int KK = BK / 16;
-        fetch(x, row_x, y, row_y, k, next, wave);
+        fetch(x, plane_x, y, plane_y, next, wave);
         __builtin_amdgcn_sched_barrier(0);
         hw_bf16x8 fa[2][PARTS][TM], fb[2][PARTS][TN];
         f32x16 zero;
@@ -279,24 +293,28 @@ __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_logits(Log
     i64 word = a.word0 + (i64)t0 * P::BM;
     p.a.place(a.w);
     p.b.place(a.h);
-    // the step to be fetched next: tile of words, place in the rows; behind the strip's last nobody uses it
-    i64 fetch_word = (i64)t0 * P::BM;                         // of the range
+    // the step to be fetched next: its number within its tile of words; behind the strip's last nobody uses it
+    Cursor from_w = P::A::begin(a.w, (i64)t0 * P::BM, 0), from_h = P::B::begin(a.h, tok0, 0);
+    const i64 stride_w = P::A::stride(a.w), stride_h = P::B::stride(a.h), plane_w = a.w.plane * 2, plane_h = a.h.plane * 2;
     int k = 0, cur = 0;
     auto advance = [&] {
-        if ((k += BK) == a.K) {
+        from_w.move(stride_w);
+        from_h.move(stride_h);
+        if (++k == steps) {
             k = 0;
-            fetch_word += P::BM;
+            from_w.move(P::BM * BK * 2 - steps * stride_w);
+            from_h.move(-steps * stride_h);
         }
     };
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) {
-        p.fetch(a.w, fetch_word, a.h, tok0, k, lds + s * P::LDS, wave);
+        p.fetch(from_w, plane_w, from_h, plane_h, lds + s * P::LDS, wave);
         advance();
     }
     __syncthreads();
     for (int t = t0; t < t1; ++t, word += P::BM) {
         auto step = [&](auto first) {
-            p.template step<first()>(a.w, fetch_word, a.h, tok0, k, lds + (cur == 0 ? STAGES - 1 : cur - 1) * P::LDS, lds + cur * P::LDS, wave, wm, wn);
+            p.template step<first()>(from_w, plane_w, from_h, plane_h, lds + (cur == 0 ? STAGES - 1 : cur - 1) * P::LDS, lds + cur * P::LDS, wave, wm, wn);
             advance();
             cur = cur == STAGES - 1 ? 0 : cur + 1;
         };
@@ -643,14 +661,22 @@ __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_product(Pr
     p.a.place(a.a);
     p.b.place(a.b);
     const int steps = (int)((k1 - k0) / BK);
+    Cursor from_a = P::A::begin(a.a, m0, k0), from_b = P::B::begin(a.b, n0, k0);      // behind the last step tiles are fetched that nobody uses
+    const i64 stride_a = P::A::stride(a.a), stride_b = P::B::stride(a.b), plane_a = a.a.plane * 2, plane_b = a.b.plane * 2;
     int cur = 0;
-    i64 k = k0;                                               // behind the last step tiles are fetched that nobody uses
+    auto advance = [&] {
+        from_a.move(stride_a);
+        from_b.move(stride_b);
+    };
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s, k += BK) p.fetch(a.a, m0, a.b, n0, k, lds + s * P::LDS, wave);
+    for (int s = 0; s < STAGES - 1; ++s) {
+        p.fetch(from_a, plane_a, from_b, plane_b, lds + s * P::LDS, wave);
+        advance();
+    }
     __syncthreads();
     auto step = [&](auto first) {
-        p.template step<first()>(a.a, m0, a.b, n0, k, lds + (cur == 0 ? STAGES - 1 : cur - 1) * P::LDS, lds + cur * P::LDS, wave, wm, wn);
-        k += BK;
+        p.template step<first()>(from_a, plane_a, from_b, plane_b, lds + (cur == 0 ? STAGES - 1 : cur - 1) * P::LDS, lds + cur * P::LDS, wave, wm, wn);
+        advance();
         cur = cur == STAGES - 1 ? 0 : cur + 1;
     };
     step(std::true_type{});
