@@ -90,7 +90,7 @@ struct EmbedGradArgs {
     int *valid;                  // [1] tokens whose ids are in range: they come first in the sorted order
     float *part;                 // [tiles][2][4 * C4]
     int *long_n, *long_list;     // rows that cross a border of tiles, by the tile that they begin in
-    int tile, tiles;             // tokens to a tile, a power of two; tiles
+    int tile;                    // tokens to a tile, a power of two
     float *blocks;               // [tiles / EMBED_BLOCK][4 * C4] shares of a row that has all of a block's tiles (NULL: few tiles)
 };
 
@@ -610,7 +610,6 @@ size_t embed_carve(const EmbedSizes &s, i64 V, i64 n, int dim, char *base, Embed
         a->long_list = (int *)list;
         a->part = (float *)part;
         a->tile = s.tile;
-        a->tiles = s.sum_tiles;
         a->blocks = many ? (float *)blocks : nullptr;
     }
     if (pub) *pub = (u32 *)words;

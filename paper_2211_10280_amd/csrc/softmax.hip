@@ -24,9 +24,6 @@ typedef short bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef u32 v4u __attribute__((ext_vector_type(4)));
 
-#ifndef PRIO
-#define PRIO(x)
-#endif
 #define SM_BM 256              // words of a tile of logits
 #define LOG2E 1.44269504088896340736f
 #define LN2 0.69314718055994530942f
@@ -43,7 +40,7 @@ struct Operand {
     __device__ __forceinline__ i64 left(i64 r, i64 c) const { return (plane - ((c / BK) * (rows * BK) + r * BK + (c & (BK - 1)))) * 2; }
 };
 // Where the next step's tile of an operand begins: kept from step to step, since working it out anew takes the scalar unit longer than
-// the step has to spare (loss of 4 096 tokens, a million words, rows of 300: STATED_CURSOR).
+// the step has to spare (loss of 4 096 tokens, a million words, rows of 300: 2.6 ms, so 2.4).
 struct Cursor {
     const char *p;
     i64 left;
@@ -73,7 +70,7 @@ struct Tile {
     static constexpr int CHUNKS = ROWS * BK / 8, PER = (CHUNKS + THREADS - 1) / THREADS;
     static constexpr int CPR = T ? ROWS / 8 : BK / 8;         // chunks of a row
     static constexpr int LDS = ROWS * BK;                     // elements
-    static_assert(CHUNKS % WAVE == 0, "");                   // where the chunks do not go round, some are fetched twice
+    static_assert(CHUNKS % WAVE == 0, "whole waves");                   // where the chunks do not go round, some are fetched twice
     int offset[PER];           // of the lane's chunks from the tile's first element, in bytes
 
     static __device__ __forceinline__ int turn(int row)       // chunks that a row is turned by, or its mask of the places
@@ -444,7 +441,7 @@ __global__ void __launch_bounds__(1024) k_loss(LossArgs a)
 
 // ---------------------------------------------------------------- few tokens
 // At most FEW_TOKENS tokens: nothing is laid out and no matrix instruction used; the words' rows are read once, where they are, and
-// both gradients are made while a row is held (the least that memory has to move: n = 1, a million rows of 300 bfloat16, STATED_FEW).
+// both gradients are made while a row is held.  Memory bounds it: one token, a million rows of 300 bfloat16, 97 us, 6.2 TB/s.
 // G lanes hold a word's row, ITERS chunks of 4 elements each, ROWS rows at a time; the tokens' rows lie in LDS, fp32.
 #define FEW_TOKENS 8
 #define FEW_BLOCKS 1024
@@ -640,6 +637,7 @@ struct ProductArgs {
     int m_tiles, n_tiles, splits;
     i64 k_per;                 // of a split, a multiple of BK
     float *slots;              // [splits][N][M] sums (NULL: written as the output)
+    int add;                   // to what the slots hold
     void *out;
     i64 out_stride;
     int dtype;
@@ -693,7 +691,12 @@ __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_product(Pr
                 if (m >= a.M) continue;
                 float4 v = make_float4(p.acc[i][j][r], p.acc[i][j][r + 1], p.acc[i][j][r + 2], p.acc[i][j][r + 3]);
                 if (a.slots) {
-                    st4(a.slots + ((i64)split * a.N + n) * a.M + m, v);
+                    float *slot = a.slots + ((i64)split * a.N + n) * a.M + m;
+                    if (a.add) {
+                        const float4 o = ld4(slot);
+                        v = make_float4(v.x + o.x, v.y + o.y, v.z + o.z, v.w + o.w);
+                    }
+                    st4(slot, v);
                 } else {
                     v = make_float4(v.x * a.scale, v.y * a.scale, v.z * a.scale, v.w * a.scale);
                     if (a.dtype == TENSAIR_F32) st4((float *)a.out + n * a.out_stride + m, v);
@@ -874,9 +877,11 @@ unsigned blocks_for(i64 items) { return (unsigned)std::min<i64>(cdiv(items, BLOC
 #define SM_BN 128              // tokens of a tile
 #define SM_BN_FEW 64           // ... where there are at most so many
 #define SM_WAVES_M 2           // rows of waves of a tile, each with a maximum and a sum of its own
-#define SM_RANGE_TILES 4096    // tiles of a range, at most: how far a fetch is off its tile's first element fits 31 bits
+#define SM_RANGE_TILES 4096    // tiles of a range, at most: a fetch is off its tile's first element by up to 10 blocks of columns, which fits 31 bits
+                               // (of words here, of tokens by TENSAIR_MAX_TOKENS)
 #define SM_BLOCKS 512          // workgroups that fill the chip, two to a compute unit
 #define SM_DZ_BYTES ((i64)1 << 30)   // dz of a range, about: with half as much the products took 3 to 8 % longer
+#define SM_DZ_TILES 8          // ... but never fewer tiles, since each range reads and writes d_hidden's sums
 
 struct SoftmaxPlan {
     bool few;                  // at most FEW_TOKENS tokens
@@ -905,7 +910,7 @@ SoftmaxPlan plan_of(i64 n, i64 V, int D, int dtype, bool grad)
     s.token_tiles = (int)(s.Np / s.bn);
     s.tiles = cdiv(V, SM_BM);
     s.range_tiles = std::min<i64>(s.tiles, SM_RANGE_TILES);
-    if (grad) s.range_tiles = std::max<i64>(1, std::min(s.range_tiles, SM_DZ_BYTES / (s.Np * SM_BM * 2 * s.parts)));
+    if (grad) s.range_tiles = std::min(s.range_tiles, std::max<i64>(SM_DZ_TILES, SM_DZ_BYTES / (s.Np * SM_BM * 2 * s.parts)));
     s.ranges = cdiv(s.tiles, s.range_tiles);
     s.range_tiles = cdiv(s.tiles, s.ranges);
     s.ranges = cdiv(s.tiles, s.range_tiles);
@@ -924,7 +929,7 @@ SoftmaxPlan plan_of(i64 n, i64 V, int D, int dtype, bool grad)
         }
     }
     s.m_tiles = (int)cdiv(s.Dp, 64 * s.tm);
-    s.pn = s.parts == 1 && s.tm <= 2 ? 256 : 128;                             // short rows: what is fetched for a product would be more than the memory pipe gives
+    s.pn = s.parts == 1 && s.tm <= 2 ? 256 : 128;             // short rows: what is fetched for a product would be more than the memory pipe gives
     const i64 range_words = s.range_tiles * SM_BM;
     const i64 h_tiles = s.m_tiles * cdiv(s.Np, s.pn), t_tiles = s.m_tiles * cdiv(range_words, s.pn);
     i64 splits = std::max<i64>(1, std::min<i64>(SM_BLOCKS / h_tiles, range_words / 512));
@@ -972,7 +977,7 @@ size_t softmax_carve(const SoftmaxPlan &s, i64 n, i64 V, int D, bool grad, char 
         x.lse2 = (float *)take(4 * (size_t)s.Np);
         x.d = (float *)take(4 * (size_t)s.Np);
         x.dz = (bf16_t *)take(2 * (size_t)s.Np * s.range_tiles * SM_BM * s.parts);
-        x.h_slots = (float *)take(4 * (size_t)s.ranges * s.h_splits * n * D);
+        x.h_slots = (float *)take(4 * (size_t)s.h_splits * n * D);
         if (s.t_splits > 1) x.t_slots = (float *)take(4 * (size_t)s.t_splits * s.range_tiles * SM_BM * D);
     }
     if (b) *b = x;
@@ -1098,25 +1103,16 @@ void launch_logits(const SoftmaxPlan &s, const LogitsArgs &a, hipStream_t st)
     if (s.bn == SM_BN_FEW) hipLaunchKernelGGL((k_logits<2, 2, 4, 1, STAGES, GRAD, PARTS>), grid, blk, 0, st, a);
     else hipLaunchKernelGGL((k_logits<PARTS == 1 ? 4 : 1, 2, 2, 2, STAGES, GRAD, PARTS>), grid, blk, 0, st, a);
 }
-template <int PARTS, bool BT>
-void launch_product_p(int tm, const ProductArgs &a, hipStream_t st)
-{
-    const dim3 grid((unsigned)(a.m_tiles * a.n_tiles * a.splits)), blk(256);
-    switch (tm) {
-    case 1: hipLaunchKernelGGL((k_product<1, PARTS == 1 ? 4 : 2, 2, 2, 2, PARTS, BT>), grid, blk, 0, st, a); break;
-    case 2: hipLaunchKernelGGL((k_product<2, PARTS == 1 ? 4 : 2, 2, 2, 2, PARTS, BT>), grid, blk, 0, st, a); break;
-    case 3: hipLaunchKernelGGL((k_product<3, 2, 2, 2, 2, PARTS, BT>), grid, blk, 0, st, a); break;
-    case 4: hipLaunchKernelGGL((k_product<4, 2, 2, 2, 2, PARTS, BT>), grid, blk, 0, st, a); break;
-    default:
-        if constexpr (PARTS == 1) hipLaunchKernelGGL((k_product<5, 2, 2, 2, 2, PARTS, BT>), grid, blk, 0, st, a);
-        break;
-    }
-}
 template <bool BT>
 void launch_product(const SoftmaxPlan &s, const ProductArgs &a, hipStream_t st)
 {
-    if (s.parts == 1) launch_product_p<1, BT>(s.tm, a, st);
-    else launch_product_p<3, BT>(s.tm, a, st);
+    const dim3 grid((unsigned)(a.m_tiles * a.n_tiles * a.splits)), blk(256);
+    if (s.parts == 3) hipLaunchKernelGGL((k_product<1, 2, 2, 2, 2, 3, BT>), grid, blk, 0, st, a);
+    else if (s.tm == 1) hipLaunchKernelGGL((k_product<1, 4, 2, 2, 2, 1, BT>), grid, blk, 0, st, a);
+    else if (s.tm == 2) hipLaunchKernelGGL((k_product<2, 4, 2, 2, 2, 1, BT>), grid, blk, 0, st, a);
+    else if (s.tm == 3) hipLaunchKernelGGL((k_product<3, 2, 2, 2, 2, 1, BT>), grid, blk, 0, st, a);
+    else if (s.tm == 4) hipLaunchKernelGGL((k_product<4, 2, 2, 2, 2, 1, BT>), grid, blk, 0, st, a);
+    else hipLaunchKernelGGL((k_product<5, 2, 2, 2, 2, 1, BT>), grid, blk, 0, st, a);
 }
 void launch_join(const float *slots, int n_slots, i64 rows, i64 stride, int D, Labels labels, void *out, int dtype, float scale, hipStream_t st)
 {
@@ -1252,8 +1248,10 @@ int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *
             p.n_tiles = (int)cdiv(s.Np, s.pn);
             p.k_per = s.h_k;
             p.splits = (int)cdiv(p.K, p.k_per);
-            p.slots = b.h_slots + range * s.h_splits * n * dim;
+            p.slots = b.h_slots;                              // the first range has all splits, the last may have fewer
+            p.add = range > 0;
             launch_product<false>(s, p, st);
+            p.add = 0;
         }
         if (d_table) {
             p.scale = fabsf(scale);                           // the tokens' rows have its sign
@@ -1273,8 +1271,7 @@ int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *
         }
     }
     if (d_hidden) {
-        // the last range may have fewer splits than the others
-        const int slots = (int)((s.ranges - 1) * s.h_splits + cdiv(cdiv(range_of(s, s.ranges - 1, vocab).words, BK) * BK, s.h_k));
+        const int slots = (int)cdiv(cdiv(range_of(s, 0, vocab).words, BK) * BK, s.h_k);
         launch_join(b.h_slots, slots, n, d_hidden_stride, dim, lab, d_hidden, dtype, scale, st);
     }
     return launched("softmax_grad");

@@ -254,6 +254,12 @@ def test_softmax(n, V, D, dtype, pad):
     assert torch.equal(_softmax(h, w, D, labels, d, scale, want=(True, False))[2][:, :D], dh[:, :D])
 
 
+@pytest.mark.parametrize("n,V,D,dtype", [(4_100, 140_000, 36, "f32"), (9_000, 70_000, 64, "bf16")])
+def test_softmax_in_several_ranges_of_words(n, V, D, dtype):
+    """dz of all words is more than is kept at a time: d_hidden's sums go on from range to range, the last of which is shorter."""
+    test_softmax(n, V, D, dtype, 0)
+
+
 @pytest.mark.parametrize("n", [3, 40, 200])
 def test_softmax_gradient_against_differences(n):
     """Central differences of the loss itself (fp32 inputs), along the gradient of either input.  Along a line a token's logits grow

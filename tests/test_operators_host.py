@@ -61,6 +61,10 @@ def test_softmax(mem):
     assert need >= B.tensair_softmax_workspace_bytes(4, 10, 8, torch.float32, False) > 0
     # the logits are never kept: what a large vocabulary needs does not grow with tokens times words
     assert B.tensair_softmax_workspace_bytes(16_384, 2_000_000, 512, torch.bfloat16, True) < 6 << 30
+    # nor do d_hidden's sums with the ranges of words
+    assert B.tensair_softmax_workspace_bytes(262_144, 1_000_000, 300, torch.bfloat16, True) < 4 << 30
+    with pytest.raises(B.TensairError):
+        B.tensair_softmax_workspace_bytes((1 << 21) + 1, 10, 8, torch.float32, False)
     for bad in ((-1, 10, 8, torch.float32), (4, 0, 8, torch.float32), (4, 10, 6, torch.float32), (4, 10, 8, torch.float8_e4m3fn), (4, 10, 8, torch.float16),
                 ((1 << 24) + 1, 10, 8, torch.float32)):
         with pytest.raises(B.TensairError):
