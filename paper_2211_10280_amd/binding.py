@@ -409,7 +409,7 @@ def _dtype(t, what):
 
 
 # The smallest calls below take the GPU less time than Python takes to check and pass their arguments: plain numbers instead of
-# C objects, every attribute of a tensor asked for once (tensair_embed 7.0 -> 3.8 us a call).
+# C objects, every attribute of a tensor asked for once (tensair_embed of 64 words, GPU and all: 7.4 -> 6.1 us a call).
 def _matrix(t, rows, dim, what):
     """(address, C dtype, row stride) of a [rows, >= dim] tensor whose rows are contiguous."""
     shape, stride, code = t.shape, t.stride(), _DTYPES.get(t.dtype)

@@ -134,6 +134,17 @@ struct Tile {
     }
 };
 
+// Waits for all but the last N of this wave's fetches, which come back in order, and for its reads of LDS, then for the other waves.
+template <int N>
+__device__ __forceinline__ void meet()
+{
+    static_assert(N < 64, "the counter's bits");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | ((N >> 4) << 14));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // A workgroup's tile of a product: BM of A's rows by BN of B's, WM by WN waves of TM by TN fragments of 32 by 32.  Lane l of a
 // fragment holds the column (B's row) l % 32 and the rows (A's) 8 (r / 4) + 4 (l / 32) + r % 4 in its 16 registers r.
 template <int TM, int TN, int WM, int WN, int STAGES, int PARTS, bool AT, bool BT>
@@ -162,16 +173,6 @@ struct Product {
         for (int part = 0; part < PARTS; ++part) a.fetch_all(A::source(x, part * plane_x), lds + part * A::LDS, wave);
 #pragma unroll
         for (int part = 0; part < PARTS; ++part) b.fetch_all(B::source(y, part * plane_y), lds + PARTS * A::LDS + part * B::LDS, wave);
-    }
-    // Waits for all but the last N of this wave's fetches, which come back in order, and for its reads of LDS, then for the other waves.
-    template <int N>
-    static __device__ __forceinline__ void meet()
-    {
-        static_assert(N < 64, "");
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | ((N >> 4) << 14));
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
     }
     // One step with STAGES tiles in LDS, that of the step itself in `cur`, of a sum that begins here (FIRST) or goes on: the tiles of the
     // step STAGES - 1 later set out into `next`; fragments of 16 of the summed index are read while those before are multiplied; in
@@ -231,7 +232,7 @@ struct LogitsArgs {
     Operand w, h;              // words' and tokens' rows
     int K;
     i64 word0, V;              // first word of this launch's range; words in all
-    int tiles, per, strips;    // tiles of words of the range, of a strip; strips
+    int tiles, per, strips;    // tiles of words (of the kernel's size) of the range, of a strip; strips
     int token_tiles;
     i64 Np;
     float c;                   // |scale| * log2(e): the scale's sign went into the tokens' rows
@@ -260,6 +261,108 @@ __device__ __forceinline__ v4u join_halves(u32 x0, u32 x1, u32 y0, u32 y1)
     return v4u{(u32)p[0], (u32)q[0], (u32)p[1], (u32)q[1]};
 }
 
+// a maximum and a sum of powers of two relative to it, joined by another pair
+__device__ __forceinline__ void join_sums(float &top, float &sum, float t, float s)
+{
+    const float now = fmaxf(top, t), ref = now == -INFINITY ? 0.f : now;
+    sum = sum * __builtin_amdgcn_exp2f(top - ref) + s * __builtin_amdgcn_exp2f(t - ref);
+    top = now;
+}
+// What is done with a wave's tile of logits, acc: TM by TN fragments of words from w0 on by tokens from tok on.
+// words that are none: no share in any sum
+template <int TM, int TN>
+__device__ __forceinline__ void no_words(f32x16 (&acc)[TM][TN], i64 w0, i64 V)
+{
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            if (w0 + 32 * i + 8 * (r / 4) + 4 * (lane_id() >> 5) + r % 4 >= V)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) acc[i][j][r] = -INFINITY;
+}
+// into the running maxima and sums; the label's logit kept
+template <int TM, int TN>
+__device__ __forceinline__ void add_words(f32x16 (&acc)[TM][TN], const LogitsArgs &a, i64 w0, i64 tok, const int (&label)[TN], float (&top)[TN], float (&sum)[TN])
+{
+    const int lane = lane_id();
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        float best = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const i64 lw = (i64)label[j] - (w0 + 32 * i);      // the label's row in this fragment
+            if (__ballot(lw >= 0 && lw < 32)) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (lw == 8 * (r / 4) + 4 * (lane >> 5) + r % 4) a.picked[tok + 32 * j + (lane & 31)] = acc[i][j][r] * a.c;
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) best = fmaxf(best, acc[i][j][r]);
+        }
+        const float now = fmaxf(best * a.c, top[j]), ref = now == -INFINITY ? 0.f : now;
+        float s = sum[j] * __builtin_amdgcn_exp2f(top[j] - ref);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], a.c, -ref));
+        top[j] = now;
+        sum[j] = s;
+    }
+}
+// dz, to the blocks of columns from `block` on
+template <int TM, int TN, int PARTS>
+__device__ __forceinline__ void put_dz(f32x16 (&acc)[TM][TN], const LogitsArgs &a, i64 w0, i64 block, i64 tok, const int (&label)[TN], const float (&l2)[TN],
+                                       const float (&d)[TN])
+{
+    const int lane = lane_id();
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        bf16_t *row = a.dz + (tok + 32 * j + (lane & 31)) * BK + 8 * (lane >> 5);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const int lw = label[j] - (int)(w0 + 32 * i);
+            float g[16];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) g[r] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], a.c, -l2[j]));
+            if (__ballot((u32)lw < 32u)) {
+                const int at = lw - 4 * (lane >> 5);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) g[r] -= at == 8 * (r / 4) + r % 4 ? 1.0f : 0.0f;
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) g[r] *= d[j];
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) {
+                u32 q[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) q[r] = pack2(g[2 * r], g[2 * r + 1]);
+                bf16_t *to = row + part * a.dz_plane + (block + i) * (a.Np * BK);
+                *(v4u *)to = join_halves(q[0], q[1], q[2], q[3]);
+                *(v4u *)(to + 16) = join_halves(q[4], q[5], q[6], q[7]);
+                if (part + 1 < PARTS)
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        g[2 * r] -= __uint_as_float(q[r] << 16);
+                        g[2 * r + 1] -= __uint_as_float(q[r] & 0xFFFF0000u);
+                    }
+            }
+        }
+    }
+}
+// a wave's maxima and sums, of the two halves of its rows together
+template <int TN>
+__device__ __forceinline__ void put_sums(const LogitsArgs &a, int slot, i64 tok, const float (&top)[TN], const float (&sum)[TN])
+{
+    const int lane = lane_id();
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        float t = top[j], s = sum[j];
+        join_sums(t, s, __shfl_xor(top[j], 32, WAVE), __shfl_xor(sum[j], 32, WAVE));
+        if (lane < 32) a.part[(i64)slot * a.Np + tok + 32 * j + lane] = make_float2(t, s);
+    }
+}
+
 // GRAD false: the running maximum and sum of every token over a strip of words; true: dz of the strip, in PARTS bfloat16 parts.
 // A strip's tiles follow one another without a pause: the next tile's first step is in flight while this one's logits are used.
 template <int TM, int TN, int WM, int WN, int STAGES, bool GRAD, int PARTS>
@@ -271,8 +374,7 @@ __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_logits(Log
     const int strip = work / a.token_tiles, tt = work % a.token_tiles;
     const int wave = uniform((int)(threadIdx.x >> 6)), wm = wave / WN, wn = wave % WN, lane = lane_id();
     const i64 tok0 = (i64)tt * P::BN;
-    constexpr int F = SM_BM / P::BM;
-    const int t0 = strip * a.per * F, t1 = min(a.tiles * F, t0 + a.per * F), steps = a.K / BK;
+    const int t0 = strip * a.per, t1 = min(a.tiles, t0 + a.per), steps = a.K / BK;
     P p;
     float top[TN], sum[TN], l2[TN], d[TN];
     int label[TN];
@@ -318,94 +420,109 @@ __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_logits(Log
         step(std::true_type{});
         for (int s = 1; s < steps; ++s) step(std::false_type{});
         const i64 w0 = word + wm * TM * 32;
-        if (word + P::BM > a.V) {                             // words that are none: no share in any sum
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (w0 + 32 * i + 8 * (r / 4) + 4 * (lane >> 5) + r % 4 >= a.V)
-#pragma unroll
-                        for (int j = 0; j < TN; ++j) p.acc[i][j][r] = -INFINITY;
-        }
-        if constexpr (!GRAD) {
-#pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                float best = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < TM; ++i) {
-                    const i64 lw = (i64)label[j] - (w0 + 32 * i);              // the label's row in this fragment
-                    if (__ballot(lw >= 0 && lw < 32)) {
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (lw == 8 * (r / 4) + 4 * (lane >> 5) + r % 4)
-                                a.picked[tok0 + (wn * TN + j) * 32 + (lane & 31)] = p.acc[i][j][r] * a.c;
-                    }
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) best = fmaxf(best, p.acc[i][j][r]);
-                }
-                const float now = fmaxf(best * a.c, top[j]), ref = now == -INFINITY ? 0.f : now;
-                float s = sum[j] * __builtin_amdgcn_exp2f(top[j] - ref);
-#pragma unroll
-                for (int i = 0; i < TM; ++i)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f(fmaf(p.acc[i][j][r], a.c, -ref));
-                top[j] = now;
-                sum[j] = s;
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < TN; ++j) {
-                bf16_t *row = a.dz + (tok0 + (wn * TN + j) * 32 + (lane & 31)) * BK + 8 * (lane >> 5);
-#pragma unroll
-                for (int i = 0; i < TM; ++i) {
-                    const i64 lw = (i64)label[j] - (w0 + 32 * i);
-                    const bool any = __ballot(lw >= 0 && lw < 32) != 0;
-                    float g[16];
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) g[r] = d[j] * __builtin_amdgcn_exp2f(fmaf(p.acc[i][j][r], a.c, -l2[j]));
-                    if (any) {
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (lw == 8 * (r / 4) + 4 * (lane >> 5) + r % 4)
-                                g[r] = d[j] * (__builtin_amdgcn_exp2f(fmaf(p.acc[i][j][r], a.c, -l2[j])) - 1.0f);
-                    }
-#pragma unroll
-                    for (int part = 0; part < PARTS; ++part) {
-                        u32 q[8];
-#pragma unroll
-                        for (int r = 0; r < 8; ++r) q[r] = pack2(g[2 * r], g[2 * r + 1]);
-                        bf16_t *to = row + part * a.dz_plane + ((i64)t * (P::BM / BK) + wm * TM + i) * (a.Np * BK);
-                        *(v4u *)to = join_halves(q[0], q[1], q[2], q[3]);
-                        *(v4u *)(to + 16) = join_halves(q[4], q[5], q[6], q[7]);
-                        if (part + 1 < PARTS)
-#pragma unroll
-                            for (int r = 0; r < 8; ++r) {
-                                g[2 * r] -= __uint_as_float(q[r] << 16);
-                                g[2 * r + 1] -= __uint_as_float(q[r] & 0xFFFF0000u);
-                            }
-                    }
-                }
-            }
-        }
+        if (word + P::BM > a.V) no_words<TM, TN>(p.acc, w0, a.V);
+        if constexpr (GRAD) put_dz<TM, TN, PARTS>(p.acc, a, w0, t * (P::BM / BK) + wm * TM, tok0 + wn * TN * 32, label, l2, d);
+        else add_words<TM, TN>(p.acc, a, w0, tok0 + wn * TN * 32, label, top, sum);
     }
-    if constexpr (!GRAD) {
-#pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const float ot = __shfl_xor(top[j], 32, WAVE), os = __shfl_xor(sum[j], 32, WAVE);
-            const float now = fmaxf(top[j], ot), ref = now == -INFINITY ? 0.f : now;
-            const float s = sum[j] * __builtin_amdgcn_exp2f(top[j] - ref) + os * __builtin_amdgcn_exp2f(ot - ref);
-            if (lane < 32) a.part[(i64)(strip * WM + wm) * a.Np + tok0 + (wn * TN + j) * 32 + lane] = make_float2(now, s);
-        }
-    }
+    if constexpr (!GRAD) put_sums<TN>(a, strip * WM + wm, tok0 + wn * TN * 32, top, sum);
 }
 
-// a maximum and a sum of powers of two relative to it, joined by another pair
-__device__ __forceinline__ void join_sums(float &top, float &sum, float t, float s)
+// The same for rows of up to 32 KB elements: a wave holds 64 tokens' whole rows in registers, as fragments, and the words' rows alone come
+// through LDS, 32 words to a tile, for the 256 tokens of a workgroup: a third of what the other form fetches, which is what bounds
+// that one.  Two workgroups to a compute unit: one's exponentials run beside the other's products.
+// 4 096 tokens, rows of 300 in bfloat16: the loss against a million words 1.86 ms (the other form 2.5), 1.3 PFLOP/s, the matrix units busy
+// 81 % of it; dz of 125 000 words 385 us (514).  129 to 256 tokens: 172 us (195 to 203), dz 241 (282 to 288); 300 tokens, of which
+// two tiles are half empty: 254 (271), dz 426 (406).  Short rows are bound by the exponentials: rows of 128, 50 000 words, 63 us.
+#define HELD_WORDS 32
+#define HELD_STAGES 4
+template <int KB, bool GRAD>
+__global__ void __launch_bounds__(256, 2) k_logits_held(LogitsArgs a)
 {
-    const float now = fmaxf(top, t), ref = now == -INFINITY ? 0.f : now;
-    sum = sum * __builtin_amdgcn_exp2f(top - ref) + s * __builtin_amdgcn_exp2f(t - ref);
-    top = now;
+    typedef Tile<HELD_WORDS, 256, false> Words;               // of a block of columns
+    constexpr int TN = 2, KK = 2 * KB, GROUP = 4, PER = KB / 2, LDS = Words::LDS * KB;
+    constexpr int STORES = GRAD ? 2 * TN : 0;                 // of a tile, by a lane
+    static_assert(KB % 2 == 0, "a fetch of all threads is two blocks of columns");
+    __shared__ __attribute__((aligned(16))) bf16_t lds[LDS * HELD_STAGES];
+    const int work = die_order((int)blockIdx.x, (int)gridDim.x);
+    const int strip = work / a.token_tiles, tt = work % a.token_tiles;
+    const int wave = uniform((int)(threadIdx.x >> 6)), lane = lane_id();
+    const i64 tok0 = (i64)tt * 256 + wave * (32 * TN);
+    const int t0 = strip * a.per, t1 = min(a.tiles, t0 + a.per);
+    hw_bf16x8 h[TN][KK];
+    float top[TN], sum[TN], l2[TN], d[TN];
+    int label[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        const i64 tok = tok0 + 32 * j + (lane & 31);
+        label[j] = a.label[tok];
+        top[j] = -INFINITY;
+        sum[j] = 0.f;
+        if (GRAD) {
+            l2[j] = a.lse2[tok];
+            d[j] = a.d[tok];
+        }
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) h[j][kk] = *(const hw_bf16x8 *)a.h.at(0, tok, 16 * kk + 8 * (lane >> 5));
+    }
+    // a thread's chunk of a tile's first two blocks; of the next ones and of other tiles it is as far off for all threads
+    const int row = ((int)threadIdx.x & 127) / 4, chunk = ((int)threadIdx.x & 3) ^ Words::turn(row);
+    [[maybe_unused]] const u32 own = ((u32)(threadIdx.x / 128) * (u32)a.w.rows + (u32)row) * (BK * 2) + 16u * chunk;
+    [[maybe_unused]] const auto from = __builtin_amdgcn_make_buffer_rsrc((void *)a.w.p, 0, (int)(a.w.plane * 2), 0x00027000);
+    auto fetch = [&](int t, int stage) {
+        [[maybe_unused]] const u32 at = (u32)min(t, t1 - 1) * (HELD_WORDS * BK * 2);   // behind the last tile: once more that
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+#ifdef __HIP_DEVICE_COMPILE__
+            typedef __attribute__((address_space(3))) void lds_void;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_void *)(lds + stage * LDS + (j * 256 + wave * WAVE) * 8), 16, (int)own,
+                                                     (int)(at + (u32)j * 2 * (u32)a.w.rows * (BK * 2)), 0, 0);
+#endif
+        }
+    };
+#pragma unroll
+    for (int x = 0; x < HELD_STAGES - 1; ++x) fetch(t0 + x, x);
+    __syncthreads();
+    int cur = 0;
+    for (int t = t0; t < t1; ++t) {
+        fetch(t + HELD_STAGES - 1, (cur + HELD_STAGES - 1) % HELD_STAGES);
+        __builtin_amdgcn_sched_barrier(0);
+        const bf16_t *__restrict tile = lds + cur * LDS;
+        hw_bf16x8 w[2][GROUP];
+        f32x16 acc[1][TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[0][j][r] = 0.f;
+        auto read = [&](int group) {
+#pragma unroll
+            for (int k = 0; k < GROUP; ++k) {
+                const int kk = group * GROUP + k;
+                w[group & 1][k] = Words::fragment(tile + kk / 2 * Words::LDS, 0, kk & 1);
+            }
+        };
+        read(0);
+#pragma unroll
+        for (int group = 0; group < KK / GROUP; ++group) {
+            if (group + 1 < KK / GROUP) read(group + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int k = 0; k < GROUP; ++k)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+                    acc[0][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[group & 1][k], h[j][group * GROUP + k], acc[0][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        const i64 w0 = a.word0 + (i64)t * HELD_WORDS;
+        if (w0 + HELD_WORDS > a.V) no_words<1, TN>(acc, w0, a.V);
+        if constexpr (GRAD) put_dz<1, TN, 1>(acc, a, w0, t, tok0, label, l2, d);
+        else add_words<1, TN>(acc, a, w0, tok0, label, top, sum);
+        // of the fetches and writes, which come back in order, those behind the next tile's may be under way
+        meet<(HELD_STAGES - 2) * PER + (HELD_STAGES - 1) * STORES>();
+        cur = (cur + 1) % HELD_STAGES;
+    }
+    if constexpr (!GRAD) put_sums<TN>(a, strip, tok0, top, sum);
 }
+
 // maxima and sums of the strips put together: a workgroup takes 64 tokens, its waves the strips in turn
 struct LossArgs {
     const float2 *part;
@@ -637,7 +754,7 @@ struct ProductArgs {
     int m_tiles, n_tiles, splits;
     i64 k_per;                 // of a split, a multiple of BK
     float *slots;              // [splits][N][M] sums (NULL: written as the output)
-    int add;                   // to what the slots hold
+    int add;                   // the sums begin with what the slots hold
     void *out;
     i64 out_stride;
     int dtype;
@@ -662,6 +779,23 @@ __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_product(Pr
     Cursor from_a = P::A::begin(a.a, m0, k0), from_b = P::B::begin(a.b, n0, k0);      // behind the last step tiles are fetched that nobody uses
     const i64 stride_a = P::A::stride(a.a), stride_b = P::B::stride(a.b), plane_a = a.a.plane * 2, plane_b = a.b.plane * 2;
     int cur = 0;
+    // (read behind the products instead, a chunk at a time, what the slots hold cost 12 % of the launch)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        const i64 n = n0 + (wn * TN + j) * 32 + (lane & 31);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const i64 m = m0 + (wm * TM + i) * 32 + 8 * (r / 4) + 4 * (lane >> 5);
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (a.add && n < a.N && m < a.M) v = ld4(a.slots + ((i64)split * a.N + n) * a.M + m);
+                p.acc[i][j][r] = v.x;
+                p.acc[i][j][r + 1] = v.y;
+                p.acc[i][j][r + 2] = v.z;
+                p.acc[i][j][r + 3] = v.w;
+            }
+    }
     auto advance = [&] {
         from_a.move(stride_a);
         from_b.move(stride_b);
@@ -672,13 +806,11 @@ __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_product(Pr
         advance();
     }
     __syncthreads();
-    auto step = [&](auto first) {
-        p.template step<first()>(from_a, plane_a, from_b, plane_b, lds + (cur == 0 ? STAGES - 1 : cur - 1) * P::LDS, lds + cur * P::LDS, wave, wm, wn);
+    for (int s = 0; s < steps; ++s) {
+        p.template step<false>(from_a, plane_a, from_b, plane_b, lds + (cur == 0 ? STAGES - 1 : cur - 1) * P::LDS, lds + cur * P::LDS, wave, wm, wn);
         advance();
         cur = cur == STAGES - 1 ? 0 : cur + 1;
-    };
-    step(std::true_type{});
-    for (int s = 1; s < steps; ++s) step(std::false_type{});
+    }
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
         const i64 n = n0 + (wn * TN + j) * 32 + (lane & 31);
@@ -691,12 +823,7 @@ __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_product(Pr
                 if (m >= a.M) continue;
                 float4 v = make_float4(p.acc[i][j][r], p.acc[i][j][r + 1], p.acc[i][j][r + 2], p.acc[i][j][r + 3]);
                 if (a.slots) {
-                    float *slot = a.slots + ((i64)split * a.N + n) * a.M + m;
-                    if (a.add) {
-                        const float4 o = ld4(slot);
-                        v = make_float4(v.x + o.x, v.y + o.y, v.z + o.z, v.w + o.w);
-                    }
-                    st4(slot, v);
+                    st4(a.slots + ((i64)split * a.N + n) * a.M + m, v);
                 } else {
                     v = make_float4(v.x * a.scale, v.y * a.scale, v.z * a.scale, v.w * a.scale);
                     if (a.dtype == TENSAIR_F32) st4((float *)a.out + n * a.out_stride + m, v);
@@ -871,10 +998,13 @@ int launched(const char *what)
 // workgroups for so many items, a thread each or, of very many, several
 unsigned blocks_for(i64 items) { return (unsigned)std::min<i64>(cdiv(items, BLOCK), 1 << 20); }
 
-// Tiles of logits: 256 words by 128 tokens, a wave's 128 by 64, two workgroups to a compute unit, so that one's exponentials run
-// beside the other's products; three stages, as much as LDS holds twice.  Of three parts 64 words by 128 tokens, for the same reason
-// (50 000 words, 1 024 tokens, rows of 300: 228 us and with dz 272; with 256 words, one workgroup, 244 and 299).
+// Tiles of logits where tokens are not held in registers: 256 words by 128 tokens, a wave's 128 by 64, two workgroups to a compute
+// unit, so that one's exponentials run beside the other's products; three stages, as much as LDS holds twice.  Of three parts 64 words
+// by 128 tokens, for the same reason (50 000 words, 1 024 tokens, rows of 300: 228 us and with dz 272; with 256 words, one workgroup,
+// 244 and 299).
 #define SM_BN 128              // tokens of a tile
+#define SM_BN_HELD 256         // ... of tokens held in registers
+#define SM_HELD_DIM 320        // rows that are: longer ones want more registers than a wave of two to a SIMD has
 #define SM_BN_FEW 64           // ... where there are at most so many
 #define SM_WAVES_M 2           // rows of waves of a tile, each with a maximum and a sum of its own
 #define SM_RANGE_TILES 4096    // tiles of a range, at most: a fetch is off its tile's first element by up to 10 blocks of columns, which fits 31 bits
@@ -887,9 +1017,10 @@ struct SoftmaxPlan {
     bool few;                  // at most FEW_TOKENS tokens
     int few_blocks;
     int parts, Dp, bn, token_tiles, wm;
+    bool held;                 // tokens held in registers
     i64 Np, tiles;             // tokens, padded; tiles of words
     i64 range_tiles, ranges;   // tiles of words that are laid out, and whose dz is kept, at a time
-    int per, strips;           // tiles to a strip, strips of a range
+    int unit, per, strips;     // tiles of the logits' kernel to SM_BM words; of those to a strip; strips of a range
     int tm, m_tiles, pn;       // of the products: fragments of a wave along the row length, tiles; rows of a tile
     int h_splits, t_splits;    // of d_hidden's sum over a range's words, of d_table's over the tokens
     i64 h_k, t_k;
@@ -902,10 +1033,11 @@ SoftmaxPlan plan_of(i64 n, i64 V, int D, int dtype, bool grad)
     s.few = n <= FEW_TOKENS;
     s.few_blocks = (int)std::max<i64>(1, std::min<i64>(cdiv(V, 64), grad ? FEW_BLOCKS / 2 : FEW_BLOCKS));
     s.parts = dtype == TENSAIR_F32 ? 3 : 1;
-    s.Dp = (int)cdiv(D, BK) * BK;
     const bool few = n <= SM_BN_FEW;
-    s.bn = few ? SM_BN_FEW : SM_BN;
-    s.wm = few ? 4 : SM_WAVES_M;
+    s.held = s.parts == 1 && D <= SM_HELD_DIM && n > SM_BN;
+    s.Dp = (int)cdiv(D, s.held ? 2 * BK : BK) * (s.held ? 2 * BK : BK);
+    s.bn = s.held ? SM_BN_HELD : few ? SM_BN_FEW : SM_BN;
+    s.wm = s.held ? 1 : few ? 4 : SM_WAVES_M;
     s.Np = cdiv(n, s.bn) * s.bn;
     s.token_tiles = (int)(s.Np / s.bn);
     s.tiles = cdiv(V, SM_BM);
@@ -914,30 +1046,40 @@ SoftmaxPlan plan_of(i64 n, i64 V, int D, int dtype, bool grad)
     s.ranges = cdiv(s.tiles, s.range_tiles);
     s.range_tiles = cdiv(s.tiles, s.ranges);
     s.ranges = cdiv(s.tiles, s.range_tiles);
-    const i64 want = std::max<i64>(1, std::min<i64>(s.range_tiles, cdiv(SM_BLOCKS * 2, s.token_tiles)));
-    s.per = (int)cdiv(s.range_tiles, want);
-    s.strips = (int)cdiv(s.range_tiles, s.per);
+    // strips of such a length that the workgroups fill the chip a whole number of times, each with two tiles' time to begin (fp32, 50 000
+    // words, 1 024 tokens, rows of 128: 85 us, as 784 workgroups for 512 places 103)
+    s.unit = s.held ? SM_BM / HELD_WORDS : s.parts == 3 && !few ? 4 : 1;
+    const i64 units = s.range_tiles * s.unit, room = s.held && s.Dp <= 64 ? 2 * SM_BLOCKS : s.held && s.Dp <= 128 ? SM_BLOCKS / 2 * 3 : SM_BLOCKS;
+    i64 shortest = -1;
+    for (int k = 1; k <= 4; ++k) {
+        const i64 per = cdiv(units, std::max<i64>(1, k * room / s.token_tiles)), time = cdiv(cdiv(units, per) * s.token_tiles, room) * (per + 2);
+        if (shortest < 0 || time < shortest) {
+            shortest = time;
+            s.per = (int)per;
+        }
+    }
+    s.strips = (int)cdiv(units, s.per);
     // fragments of a wave along the row length, two waves to a tile: few columns beyond the row, but a wider tile fetches less.  Of three
     // parts one: six products a fetch are enough, and two workgroups find room on a compute unit (50 000 words, 1 024 tokens, rows of
     // 300: the two products 188 and 182 us, with three fragments 241 and 281).
     i64 least = -1;
     for (int tm = 1; tm <= (s.parts == 1 ? 5 : 1); ++tm) {
-        const i64 cost = cdiv(s.Dp, 64 * tm) * 64 * (2 * tm + 1); // columns times 1 + 1 / (2 tm)
+        const i64 cost = cdiv(D, 64 * tm) * 64 * (2 * tm + 1); // columns times 1 + 1 / (2 tm)
         if (least < 0 || cost <= least) {
             least = cost;
             s.tm = tm;
         }
     }
-    s.m_tiles = (int)cdiv(s.Dp, 64 * s.tm);
+    s.m_tiles = (int)cdiv(D, 64 * s.tm);
     s.pn = s.parts == 1 && s.tm <= 2 ? 256 : 128;             // short rows: what is fetched for a product would be more than the memory pipe gives
     const i64 range_words = s.range_tiles * SM_BM;
-    const i64 h_tiles = s.m_tiles * cdiv(s.Np, s.pn), t_tiles = s.m_tiles * cdiv(range_words, s.pn);
+    const i64 h_tiles = s.m_tiles * cdiv(n, s.pn), t_tiles = s.m_tiles * cdiv(range_words, s.pn);
     i64 splits = std::max<i64>(1, std::min<i64>(SM_BLOCKS / h_tiles, range_words / 512));
     s.h_k = cdiv(cdiv(range_words, splits), BK) * BK;
     s.h_splits = (int)cdiv(range_words, s.h_k);
-    splits = std::max<i64>(1, std::min<i64>(SM_BLOCKS / t_tiles, s.Np / 512));
-    s.t_k = cdiv(cdiv(s.Np, splits), BK) * BK;
-    s.t_splits = (int)cdiv(s.Np, s.t_k);
+    splits = std::max<i64>(1, std::min<i64>(SM_BLOCKS / t_tiles, n / 512));
+    s.t_k = cdiv(cdiv(n, splits), BK) * BK;
+    s.t_splits = (int)cdiv(n, s.t_k);
     return s;
 }
 
@@ -1042,9 +1184,9 @@ LogitsArgs lay_out_range(const SoftmaxPlan &s, const SoftmaxBuffers &b, const Ra
     a.K = s.Dp;
     a.word0 = r.word0;
     a.V = V;
-    a.tiles = (int)r.tiles;
+    a.tiles = (int)r.tiles * s.unit;
     a.per = s.per;
-    a.strips = (int)cdiv(r.tiles, s.per);
+    a.strips = (int)cdiv(a.tiles, s.per);
     a.token_tiles = s.token_tiles;
     a.Np = s.Np;
     a.c = fabsf(scale) * LOG2E;
@@ -1100,6 +1242,15 @@ void launch_logits(const SoftmaxPlan &s, const LogitsArgs &a, hipStream_t st)
 {
     constexpr int STAGES = PARTS == 1 ? 3 : 2;
     const dim3 grid((unsigned)(a.strips * a.token_tiles)), blk(256);
+    if constexpr (PARTS == 1)
+        if (s.held) {
+            if (s.Dp <= 64) hipLaunchKernelGGL((k_logits_held<2, GRAD>), grid, blk, 0, st, a);
+            else if (s.Dp <= 128) hipLaunchKernelGGL((k_logits_held<4, GRAD>), grid, blk, 0, st, a);
+            else if (s.Dp <= 192) hipLaunchKernelGGL((k_logits_held<6, GRAD>), grid, blk, 0, st, a);
+            else if (s.Dp <= 256) hipLaunchKernelGGL((k_logits_held<8, GRAD>), grid, blk, 0, st, a);
+            else hipLaunchKernelGGL((k_logits_held<10, GRAD>), grid, blk, 0, st, a);
+            return;
+        }
     if (s.bn == SM_BN_FEW) hipLaunchKernelGGL((k_logits<2, 2, 4, 1, STAGES, GRAD, PARTS>), grid, blk, 0, st, a);
     else hipLaunchKernelGGL((k_logits<PARTS == 1 ? 4 : 1, 2, 2, 2, STAGES, GRAD, PARTS>), grid, blk, 0, st, a);
 }
@@ -1245,7 +1396,7 @@ int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *
             p.b = dz;
             p.N = n;
             p.K = cdiv(r.words, BK) * BK;
-            p.n_tiles = (int)cdiv(s.Np, s.pn);
+            p.n_tiles = (int)cdiv(n, s.pn);
             p.k_per = s.h_k;
             p.splits = (int)cdiv(p.K, p.k_per);
             p.slots = b.h_slots;                              // the first range has all splits, the last may have fewer
@@ -1258,7 +1409,7 @@ int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *
             p.a = a.h;
             p.b = dz;
             p.N = r.words;
-            p.K = s.Np;
+            p.K = cdiv(n, BK) * BK;
             p.n_tiles = (int)cdiv(r.words, s.pn);
             p.k_per = s.t_k;
             p.splits = s.t_splits;

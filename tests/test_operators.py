@@ -254,6 +254,13 @@ def test_softmax(n, V, D, dtype, pad):
     assert torch.equal(_softmax(h, w, D, labels, d, scale, want=(True, False))[2][:, :D], dh[:, :D])
 
 
+@pytest.mark.parametrize("n,V,D,pad", [(129, 3_000, 40, 24), (256, 33, 64, 0), (257, 1_000, 100, 0), (300, 2_001, 132, 0), (700, 511, 256, 4), (513, 31, 320, 0),
+                                       (1_025, 257, 324, 0)])
+def test_softmax_with_tokens_in_registers(n, V, D, pad):
+    """The form for many tokens with short rows in bfloat16, every number of blocks of columns; one row length beyond it."""
+    test_softmax(n, V, D, "bf16", pad)
+
+
 @pytest.mark.parametrize("n,V,D,dtype", [(4_100, 140_000, 36, "f32"), (9_000, 70_000, 64, "bf16")])
 def test_softmax_in_several_ranges_of_words(n, V, D, dtype):
     """dz of all words is more than is kept at a time: d_hidden's sums go on from range to range, the last of which is shorter."""
