@@ -94,33 +94,29 @@ struct EmbedGradArgs {
     float *blocks;               // [tiles / EMBED_BLOCK][4 * C4] shares of a row that has all of a block's tiles (NULL: few tiles)
 };
 
-template <typename T>
-__device__ __forceinline__ void put_chunk(T *p, float4 v, int add)
-{
-    if (add) {
-        const float4 o = ld4(p);
-        v.x += o.x;
-        v.y += o.y;
-        v.z += o.z;
-        v.w += o.w;
-    }
-    st4(p, v);
-}
-__device__ __forceinline__ void put_row_chunk(const RowsOut &o, i64 at, int chunk, float4 v)
-{
-    v.x *= o.scale;
-    v.y *= o.scale;
-    v.z *= o.scale;
-    v.w *= o.scale;
-    if (o.dtype == TENSAIR_F32) put_chunk((float *)o.rows + at * o.stride + 4 * chunk, v, o.add);
-    else put_chunk((bf16_t *)o.rows + at * o.stride + 4 * chunk, v, o.add);
-}
 __device__ __forceinline__ void add4(float4 &a, float4 b)
 {
     a.x += b.x;
     a.y += b.y;
     a.z += b.z;
     a.w += b.w;
+}
+// `old`: what is there, where the row is added to it and that was read before
+__device__ __forceinline__ void put_row_chunk(const RowsOut &o, i64 at, int chunk, float4 v, const float4 *old = nullptr)
+{
+    v.x *= o.scale;
+    v.y *= o.scale;
+    v.z *= o.scale;
+    v.w *= o.scale;
+    at = at * o.stride + 4 * chunk;
+    if (old) add4(v, *old);
+    if (o.dtype == TENSAIR_F32) {
+        if (o.add && !old) add4(v, ld4((const float *)o.rows + at));
+        st4((float *)o.rows + at, v);
+    } else {
+        if (o.add && !old) add4(v, ld4((const bf16_t *)o.rows + at));
+        st4((bf16_t *)o.rows + at, v);
+    }
 }
 
 // ---- few tokens: no sort.  Every token looks through all ids; the first of its word sums the word's tokens.
@@ -356,80 +352,87 @@ __global__ void __launch_bounds__(BLOCK) k_embed_segments(EmbedGradArgs a, u64 *
 
 #define EMBED_MAX_TILE 64
 // G lanes sum a tile of sorted tokens, row by row; a row that neither begins before the tile nor goes on behind it
-// is written, of another the tile's share is kept: slot 0 where the row began before, else slot 1.
-template <typename T, int G, int ITERS>
+// is written, of another the tile's share is kept: slot 0 where the row began before, else slot 1.  ADD: what a row of the table holds is
+// read beside the tokens' rows, not when its sum is done.
+// What bounds it is the way to rows in random order: 262 143 rows of 256 in bfloat16 27.5 us (4.9 TB/s), 32 767 rows of 300 in fp32 added
+// to a table 18 us (39 MB read, 9 840 rows read and written).
+template <typename T, int G, int ITERS, bool ADD>
 __global__ void __launch_bounds__(BLOCK) k_embed_reduce(EmbedGradArgs a)
 {
-    constexpr int FLIGHT = ITERS > 2 ? 4 : 8, SIDE = WAVE / G;
-    // the places and rows of a wave's tokens, which follow one another
+    constexpr int FLIGHT = ITERS > (ADD ? 1 : 2) ? 4 : 8, SIDE = WAVE / G;
+    // the places and rows of a wave's tokens, which follow one another, and where the rows go
     __shared__ int2 entries[WAVES_PER_BLOCK][SIDE * EMBED_MAX_TILE];
+    __shared__ int targets[WAVES_PER_BLOCK][SIDE * EMBED_MAX_TILE];
     const int l = (int)threadIdx.x % G, valid = *a.valid, wave = (int)threadIdx.x / WAVE;
     const i64 tile = ((i64)blockIdx.x * BLOCK + threadIdx.x) / G, wave0 = (tile - lane_id() / G) * a.tile;
     const int here = (int)min((i64)SIDE * a.tile, valid - wave0);
-    for (int x = lane_id(); x < here; x += WAVE) entries[wave][x] = make_int2((int)a.vals[wave0 + x], a.seg_of[wave0 + x]);
+    for (int x = lane_id(); x < here; x += WAVE) {
+        const int seg = a.seg_of[wave0 + x];
+        entries[wave][x] = make_int2((int)a.vals[wave0 + x], seg);
+        targets[wave][x] = a.out.by_id ? (int)a.keys[wave0 + x] : seg;
+    }
     __syncthreads();
     if (tile * a.tile >= valid) return;
     const int base = (int)(tile * a.tile), end = min(valid, base + a.tile);
     const int2 *mine = entries[wave] + (base - wave0);
-    int cur = mine[0].y;
-    bool before = base > 0 && a.seg_of[base - 1] == cur;
-    const int next = end < valid ? a.seg_of[end] : -1;
+    const int *to = targets[wave] + (base - wave0);
+    const int first = mine[0].y, next = end < valid ? a.seg_of[end] : -1;
+    bool before = base > 0 && a.seg_of[base - 1] == first, open = false;
+    const bool began = before;
     float4 acc[ITERS];
     zero_row<ITERS>(acc);
     for (int e = base; e < end; e += FLIGHT) {
-        int seg[FLIGHT];
-        u32 pos[FLIGHT];
+        bool ends[FLIGHT];                                        // tokens that are their rows' last
         typename Raw4<T>::type r[FLIGHT][ITERS];
-#pragma unroll
-        for (int k = 0; k < FLIGHT; ++k) {
-            const int2 x = e + k < end ? mine[e + k - base] : make_int2(0, -1);
-            pos[k] = (u32)x.x;
-            seg[k] = x.y;
-        }
+        float4 old[ADD ? FLIGHT : 1][ITERS];
 #pragma unroll
         for (int k = 0; k < FLIGHT; ++k) {
             zero_row_raw<ITERS>(r[k]);
+            ends[k] = false;
             if (e + k < end) {
-                const T *row = (const T *)a.d + (i64)pos[k] * a.d_stride;
+                const int2 x = mine[e + k - base];
+                ends[k] = (e + k + 1 < end ? mine[e + k + 1 - base].y : next) != x.y;
+                const T *row = (const T *)a.d + (i64)(u32)x.x * a.d_stride;
 #pragma unroll
                 for (int it = 0; it < ITERS; ++it)
                     if (l + G * it < a.C4) r[k][it] = ldraw(row + 4 * (l + G * it));
+                if (ADD && ends[k] && !(began && x.y == first)) {
+                    const i64 at = to[e + k - base] * a.out.stride + 4 * l;
+#pragma unroll
+                    for (int it = 0; it < ITERS; ++it)
+                        if (l + G * it < a.C4)
+                            old[k][it] = a.out.dtype == TENSAIR_F32 ? ld4((const float *)a.out.rows + at + 4 * G * it) : ld4((const bf16_t *)a.out.rows + at + 4 * G * it);
+                }
             }
         }
 #pragma unroll
         for (int k = 0; k < FLIGHT; ++k) {
-            if (e + k < end && seg[k] != cur) {
-                const i64 at = a.out.by_id ? (i64)a.row_ids[cur] : (i64)cur;
+            add_row_raw<ITERS>(acc, r[k]);                        // zero behind the tile's end
+            open |= e + k < end;
+            if (ends[k]) {
 #pragma unroll
                 for (int it = 0; it < ITERS; ++it) {
                     const int c = l + G * it;
                     if (c < a.C4) {
                         if (before) st4(a.part + ((2 * tile) * a.C4 + c) * 4, acc[it]);
-                        else put_row_chunk(a.out, at, c, acc[it]);
+                        else put_row_chunk(a.out, to[e + k - base], c, acc[it], ADD ? &old[k][it] : nullptr);
                     }
                 }
                 zero_row<ITERS>(acc);
-                cur = seg[k];
-                before = false;
+                before = open = false;
             }
-            add_row_raw<ITERS>(acc, r[k]);                        // zero behind the tile's end
         }
     }
-    const bool on = next == cur;
-    const i64 at = a.out.by_id ? (i64)a.row_ids[cur] : (i64)cur;
+    if (!open) return;                                            // the last row goes on behind the tile
 #pragma unroll
     for (int it = 0; it < ITERS; ++it) {
         const int c = l + G * it;
-        if (c < a.C4) {
-            if (before || on) st4(a.part + ((2 * tile + (before ? 0 : 1)) * a.C4 + c) * 4, acc[it]);
-            else put_row_chunk(a.out, at, c, acc[it]);
-        }
+        if (c < a.C4) st4(a.part + ((2 * tile + (before ? 0 : 1)) * a.C4 + c) * 4, acc[it]);
     }
-    if (on && !before && l == 0) a.long_list[atomicAdd(a.long_n, 1)] = (int)tile;
+    if (!before && l == 0) a.long_list[atomicAdd(a.long_n, 1)] = (int)tile;
 }
 
-#define EMBED_BLOCK 64
-
+#define EMBED_BLOCK 32            // of tiles (32 767 tokens added to a table of 300: k_embed_join 9.3 us, 14 with 64)
 #define EMBED_BLOCK_MIN 1024      // tiles from which on adding up whole blocks of them is worth a launch
 // adds up what at() gives for every share, in THREADS / G parts of shares that follow one another (the same for every thread of the
 // workgroup); true for the threads that have the sum
@@ -559,10 +562,11 @@ EmbedSizes embed_sizes(i64 V, i64 n)
     s.nd = (size_t)1 << s.bits;
     s.tiles = tn_prep_tiles(n);
     s.seg_tiles = tn_prep_seg_tiles(n);
-    // few tokens to a tile where there are few, so that enough waves are there to hide the way to memory (32 767 tokens, rows of 300
-    // added to a table: tiles of 32 50 us, of 8 23.7, of 4 23.9; 262 143 tokens, rows of 256 in bfloat16: of 64 37.6 us, of 32 30.8)
+    // few tokens to a tile where there are few, so that enough waves are there to hide the way to memory, but more tiles have more
+    // shares to write and to read again (32 767 tokens, rows of 300 added to a table: tiles of 4 26 us, of 8 22, of 16 18, of 32 26;
+    // 262 143 tokens, rows of 256 in bfloat16: of 64 37.6 us, of 32 30.8)
     s.tile = 4;
-    while (s.tile < EMBED_MAX_TILE && n / s.tile > 8192) s.tile *= 2;
+    while (s.tile < EMBED_MAX_TILE && n / s.tile > (s.tile < 32 ? 2048 : 16384)) s.tile *= 2;
     s.sum_tiles = (int)((n + s.tile - 1) / s.tile);
     s.chained = s.tiles <= TN_PREP_CHAIN_OWN;
     // tickets (a word per pass and one of the segments), the segments' words, digit counts, the tiles' words of each pass
@@ -624,7 +628,8 @@ void launch_sums(const EmbedGradArgs &a, const EmbedSizes &s, hipStream_t st)
         return;
     }
     const i64 blocks = ((i64)s.sum_tiles * G + BLOCK - 1) / BLOCK;
-    hipLaunchKernelGGL((k_embed_reduce<T, G, ITERS>), dim3((unsigned)blocks), dim3(BLOCK), 0, st, a);
+    if (a.out.add) hipLaunchKernelGGL((k_embed_reduce<T, G, ITERS, true>), dim3((unsigned)blocks), dim3(BLOCK), 0, st, a);
+    else hipLaunchKernelGGL((k_embed_reduce<T, G, ITERS, false>), dim3((unsigned)blocks), dim3(BLOCK), 0, st, a);
     if (a.blocks && s.sum_tiles / EMBED_BLOCK > 0)
         hipLaunchKernelGGL((k_embed_blocks<G, ITERS>), dim3((unsigned)(s.sum_tiles / EMBED_BLOCK)), dim3(BLOCK), 0, st, a);
     if (s.sum_tiles > 1)
