@@ -365,6 +365,8 @@ __device__ __forceinline__ void put_sums(const LogitsArgs &a, int slot, i64 tok,
 
 // GRAD false: the running maximum and sum of every token over a strip of words; true: dz of the strip, in PARTS bfloat16 parts.
 // A strip's tiles follow one another without a pause: the next tile's first step is in flight while this one's logits are used.
+// What bounds it is what comes to LDS (87 operations a byte): 10 000 words, 16 384 tokens, rows of 512 in bfloat16 185 us, 0.9 PFLOP/s; fp32,
+// 50 000 words, 1 024 tokens, rows of 128 85 us, 0.93 PFLOP/s of its bfloat16 products.
 template <int TM, int TN, int WM, int WN, int STAGES, bool GRAD, int PARTS>
 __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_logits(LogitsArgs a)
 {
@@ -523,7 +525,8 @@ __global__ void __launch_bounds__(256, 2) k_logits_held(LogitsArgs a)
     if constexpr (!GRAD) put_sums<TN>(a, strip, tok0, top, sum);
 }
 
-// maxima and sums of the strips put together: a workgroup takes 64 tokens, its waves the strips in turn
+// maxima and sums of the strips put together: a workgroup takes 64 tokens, its waves the strips in turn (4.8 us, which is the way to
+// memory and back a few times)
 struct LossArgs {
     const float2 *part;
     int slots;
@@ -532,6 +535,12 @@ struct LossArgs {
     Labels labels;
     float *loss, *lse;
 };
+__device__ __forceinline__ void put_loss(const LossArgs &a, i64 i, float top, float sum)
+{
+    const float lse = top + log2f(sum);
+    a.lse[i] = lse * LN2;
+    a.loss[i] = a.labels.at(i) >= 0 ? (lse - a.picked[i]) * LN2 : 0.f;
+}
 __global__ void __launch_bounds__(1024) k_loss(LossArgs a)
 {
     __shared__ float2 other[16][WAVE];
@@ -551,14 +560,13 @@ __global__ void __launch_bounds__(1024) k_loss(LossArgs a)
     for (int w = 1; w < 16; ++w) {
         join_sums(top, sum, other[w][lane].x, other[w][lane].y);
     }
-    const float lse = top + log2f(sum);
-    a.lse[i] = lse * LN2;
-    a.loss[i] = a.labels.at(i) >= 0 ? (lse - a.picked[i]) * LN2 : 0.f;
+    put_loss(a, i, top, sum);
 }
 
 // ---------------------------------------------------------------- few tokens
 // At most FEW_TOKENS tokens: nothing is laid out and no matrix instruction used; the words' rows are read once, where they are, and
 // both gradients are made while a row is held.  Memory bounds it: one token, a million rows of 300 bfloat16, 97 us, 6.2 TB/s.
+// (8 tokens: the loss 245 us, by tiles 424; the gradient, which the vector units bound, 833 and 845.)
 // G lanes hold a word's row, ITERS chunks of 4 elements each, ROWS rows at a time; the tokens' rows lie in LDS, fp32.
 #define FEW_TOKENS 8
 #define FEW_BLOCKS 1024
@@ -569,10 +577,9 @@ struct FewArgs {
     float c, sign;             // |scale| log2(e); the scale's sign goes into the tokens' rows
     Labels labels;
     int *status;
-    // loss: a slot per workgroup
-    float2 *part;
+    // loss
+    float2 *part;              // [n][workgroups]
     float *picked;
-    i64 Np;
     // gradient
     const float *lse, *d_loss;
     float *slots;              // [workgroups][n][4 * C4]
@@ -709,7 +716,7 @@ __global__ void __launch_bounds__(BLOCK) k_few(FewArgs a)
         __syncthreads();
         if (threadIdx.x < NT && (int)threadIdx.x < a.n) {
             for (int w = 1; w < WAVES_PER_BLOCK; ++w) join_sums(top, sum, stats[w][lane].x, stats[w][lane].y);
-            a.part[(i64)blockIdx.x * a.Np + threadIdx.x] = make_float2(top, sum);
+            a.part[(i64)threadIdx.x * gridDim.x + blockIdx.x] = make_float2(top, sum);
         }
     } else {
         // the groups of a wave, then the waves in turn (the tokens' rows have served: their place is taken)
@@ -746,8 +753,35 @@ __global__ void __launch_bounds__(BLOCK) k_few(FewArgs a)
             st4(a.slots + ((i64)blockIdx.x * a.n * a.C4 + x) * 4, h[x / a.C4][x % a.C4]);
     }
 }
+// the workgroups' maxima and sums of a token put together, by a workgroup
+__global__ void __launch_bounds__(BLOCK) k_loss_few(LossArgs a)
+{
+    __shared__ float2 other[WAVES_PER_BLOCK];
+    const int i = (int)blockIdx.x;
+    const float2 *part = a.part + (i64)i * a.slots;
+    float top = -INFINITY, sum = 0.f;
+    float2 v[FEW_BLOCKS / BLOCK];
+#pragma unroll
+    for (int k = 0; k < FEW_BLOCKS / BLOCK; ++k) {
+        const int s = k * BLOCK + (int)threadIdx.x;
+        v[k] = s < a.slots ? part[s] : make_float2(-INFINITY, 0.f);
+    }
+#pragma unroll
+    for (int k = 0; k < FEW_BLOCKS / BLOCK; ++k) join_sums(top, sum, v[k].x, v[k].y);
+#pragma unroll
+    for (int o = 1; o < WAVE; o <<= 1) join_sums(top, sum, __shfl_xor(top, o, WAVE), __shfl_xor(sum, o, WAVE));
+    if (lane_id() == 0) other[threadIdx.x / WAVE] = make_float2(top, sum);
+    __syncthreads();
+    if (threadIdx.x > 0) return;
+    for (int w = 1; w < WAVES_PER_BLOCK; ++w) join_sums(top, sum, other[w].x, other[w].y);
+    put_loss(a, i, top, sum);
+}
 
 // ---------------------------------------------------------------- products with dz
+// d_hidden = dz table (the summed index: words, split so that every compute unit has work, the splits' sums kept apart) and
+// d_table = dz^T hidden (tokens).  A tile is as wide as short rows are, so that dz is read once.  4 096 tokens, 125 000 words, rows of
+// 300 in bfloat16 (dz: 1 GB): 357 and 330 us, 0.9 PFLOP/s, the matrix units busy 44 % of it, the waves waiting for tiles as long (256
+// tokens to a tile, 8 waves, 3 stages: 336 and 335); fp32, 1 024 tokens, 50 000 words of 128: 92 and 96 us.
 struct ProductArgs {
     Operand a, b;              // C[n][m] = sum_k a(m, k) b(n, k)
     i64 M, N, K;
@@ -897,6 +931,7 @@ __global__ void __launch_bounds__(1024) k_join(JoinArgs a)
 }
 
 // ---------------------------------------------------------------- inputs laid out for the products
+// One pass over the inputs, which memory bounds: 125 000 words of 300 in bfloat16 57 us where they come from memory.
 struct PackArgs {
     const void *src;
     i64 stride, rows;          // of the source
@@ -1102,7 +1137,7 @@ size_t softmax_carve(const SoftmaxPlan &s, i64 n, i64 V, int D, bool grad, char 
     x.label = (int *)take(4 * (size_t)s.Np);
     if (s.few) {
         x.picked = (float *)take(4 * (size_t)s.Np);
-        x.part = (float2 *)take(8 * (size_t)s.few_blocks * s.Np);
+        x.part = (float2 *)take(8 * (size_t)s.few_blocks * n);
         if (grad) x.h_slots = (float *)take(4 * (size_t)s.few_blocks * n * D);
         if (b) *b = x;
         // the loss of the same sizes has more workgroups than the gradient
@@ -1232,7 +1267,6 @@ FewArgs few_args(const SoftmaxPlan &s, const SoftmaxBuffers &b, const void *hidd
     a.status = status;
     a.part = b.part;
     a.picked = b.picked;
-    a.Np = s.Np;
     a.slots = b.h_slots;
     a.scale = fabsf(scale);
     return a;
@@ -1330,7 +1364,8 @@ int tensair_softmax_loss(const void *hidden, int64_t hidden_stride, const void *
         }
     }
     LossArgs l = {b.part, slots, s.Np, n, b.picked, lab, loss, lse};
-    hipLaunchKernelGGL(k_loss, dim3((unsigned)(s.Np / WAVE)), dim3(1024), 0, st, l);
+    if (s.few) hipLaunchKernelGGL(k_loss_few, dim3((unsigned)n), dim3(BLOCK), 0, st, l);
+    else hipLaunchKernelGGL(k_loss, dim3((unsigned)(s.Np / WAVE)), dim3(1024), 0, st, l);
     return launched("softmax_loss");
 }
 

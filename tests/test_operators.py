@@ -128,6 +128,12 @@ def test_embed_grad(V, D, n, dtype, pad, hot):
     assert torch.equal(half, torch.where(touched[:, None], (base.bfloat16().float() + want).bfloat16(), base.bfloat16()))
 
 
+@pytest.mark.parametrize("V,D,n,dtype,pad,hot", [(5_000, 8, 600_001, "f32", 0, 0.2), (40_000, 300, 33_000, "f32", 4, 0.1), (20_000, 64, 140_000, "bf16", 0, 0.0),
+                                                 (300, 520, 12_000, "bf16", 0, 0.6)])
+def test_embed_grad_tiles_of_every_length(V, D, n, dtype, pad, hot):
+    test_embed_grad(V, D, n, dtype, pad, hot)
+
+
 @pytest.mark.parametrize("n", [0, 5, 5_000])
 def test_embed_grad_of_nothing(n):
     V, D = 100, 8
