@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_logits(Log
     i64 word = a.word0 + (i64)t0 * P::BM;
     p.a.place(a.w);
     p.b.place(a.h);
-    // the step to be fetched next: its number within its tile of words; behind the strip's last nobody uses it
+    // the step to be fetched next: its number within its tile of words; behind the strip's last nobody uses it (a wave's end waits for it)
     Cursor from_w = P::A::begin(a.w, (i64)t0 * P::BM, 0), from_h = P::B::begin(a.h, tok0, 0);
     const i64 stride_w = P::A::stride(a.w), stride_h = P::B::stride(a.h), plane_w = a.w.plane * 2, plane_h = a.h.plane * 2;
     int k = 0, cur = 0;
