@@ -281,9 +281,15 @@ __device__ __forceinline__ void no_words(f32x16 (&acc)[TM][TN], i64 w0, i64 V)
 #pragma unroll
                 for (int j = 0; j < TN; ++j) acc[i][j][r] = -INFINITY;
 }
-// into the running maxima and sums; the label's logit kept
+// A token's running sum over a strip of words, of powers of two relative to `top`, with what its roundings have cut off so far: a
+// strip is up to the whole vocabulary, and added to the plain sum its many small words would be lost one by one beside a large one.
+// `top` is the largest logit so far or the whole number above it, so that a sum is brought to another one without a rounding.
+struct Running {
+    float top, sum, low;
+};
+// into the running sums; the label's logit kept
 template <int TM, int TN>
-__device__ __forceinline__ void add_words(f32x16 (&acc)[TM][TN], const LogitsArgs &a, i64 w0, i64 tok, const int (&label)[TN], float (&top)[TN], float (&sum)[TN])
+__device__ __forceinline__ void add_words(f32x16 (&acc)[TM][TN], const LogitsArgs &a, i64 w0, i64 tok, const int (&label)[TN], Running (&run)[TN])
 {
     const int lane = lane_id();
 #pragma unroll
@@ -300,14 +306,17 @@ __device__ __forceinline__ void add_words(f32x16 (&acc)[TM][TN], const LogitsArg
 #pragma unroll
             for (int r = 0; r < 16; ++r) best = fmaxf(best, acc[i][j][r]);
         }
-        const float now = fmaxf(best * a.c, top[j]), ref = now == -INFINITY ? 0.f : now;
-        float s = sum[j] * __builtin_amdgcn_exp2f(top[j] - ref);
+        Running &x = run[j];
+        const float now = fmaxf(ceilf(best * a.c), x.top), ref = now == -INFINITY ? 0.f : now, f = __builtin_amdgcn_exp2f(x.top - ref);
+        float s = 0.f;
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], a.c, -ref));
-        top[j] = now;
-        sum[j] = s;
+        const float before = x.sum * f, more = s - x.low * f;
+        x.top = now;
+        x.sum = before + more;
+        x.low = (x.sum - before) - more;
     }
 }
 // dz, to the blocks of columns from `block` on
@@ -352,13 +361,13 @@ __device__ __forceinline__ void put_dz(f32x16 (&acc)[TM][TN], const LogitsArgs &
 }
 // a wave's maxima and sums, of the two halves of its rows together
 template <int TN>
-__device__ __forceinline__ void put_sums(const LogitsArgs &a, int slot, i64 tok, const float (&top)[TN], const float (&sum)[TN])
+__device__ __forceinline__ void put_sums(const LogitsArgs &a, int slot, i64 tok, const Running (&run)[TN])
 {
     const int lane = lane_id();
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-        float t = top[j], s = sum[j];
-        join_sums(t, s, __shfl_xor(top[j], 32, WAVE), __shfl_xor(sum[j], 32, WAVE));
+        float t = run[j].top, s = run[j].sum;
+        join_sums(t, s, __shfl_xor(t, 32, WAVE), __shfl_xor(s, 32, WAVE));
         if (lane < 32) a.part[(i64)slot * a.Np + tok + 32 * j + lane] = make_float2(t, s);
     }
 }
@@ -378,14 +387,14 @@ __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_logits(Log
     const i64 tok0 = (i64)tt * P::BN;
     const int t0 = strip * a.per, t1 = min(a.tiles, t0 + a.per), steps = a.K / BK;
     P p;
-    float top[TN], sum[TN], l2[TN], d[TN];
+    Running run[TN];
+    float l2[TN], d[TN];
     int label[TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
         const i64 tok = tok0 + (wn * TN + j) * 32 + (lane & 31);
         label[j] = a.label[tok];
-        top[j] = -INFINITY;
-        sum[j] = 0.f;
+        run[j] = Running{-INFINITY, 0.f, 0.f};
         if (GRAD) {
             l2[j] = a.lse2[tok];
             d[j] = a.d[tok];
@@ -424,9 +433,9 @@ __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_logits(Log
         const i64 w0 = word + wm * TM * 32;
         if (word + P::BM > a.V) no_words<TM, TN>(p.acc, w0, a.V);
         if constexpr (GRAD) put_dz<TM, TN, PARTS>(p.acc, a, w0, t * (P::BM / BK) + wm * TM, tok0 + wn * TN * 32, label, l2, d);
-        else add_words<TM, TN>(p.acc, a, w0, tok0 + wn * TN * 32, label, top, sum);
+        else add_words<TM, TN>(p.acc, a, w0, tok0 + wn * TN * 32, label, run);
     }
-    if constexpr (!GRAD) put_sums<TN>(a, strip * WM + wm, tok0 + wn * TN * 32, top, sum);
+    if constexpr (!GRAD) put_sums<TN>(a, strip * WM + wm, tok0 + wn * TN * 32, run);
 }
 
 // The same for rows of up to 32 KB elements: a wave holds 64 tokens' whole rows in registers, as fragments, and the words' rows alone come
@@ -451,14 +460,14 @@ __global__ void __launch_bounds__(256, 2) k_logits_held(LogitsArgs a)
     const i64 tok0 = (i64)tt * 256 + wave * (32 * TN);
     const int t0 = strip * a.per, t1 = min(a.tiles, t0 + a.per);
     hw_bf16x8 h[TN][KK];
-    float top[TN], sum[TN], l2[TN], d[TN];
+    Running run[TN];
+    float l2[TN], d[TN];
     int label[TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
         const i64 tok = tok0 + 32 * j + (lane & 31);
         label[j] = a.label[tok];
-        top[j] = -INFINITY;
-        sum[j] = 0.f;
+        run[j] = Running{-INFINITY, 0.f, 0.f};
         if (GRAD) {
             l2[j] = a.lse2[tok];
             d[j] = a.d[tok];
@@ -517,12 +526,12 @@ __global__ void __launch_bounds__(256, 2) k_logits_held(LogitsArgs a)
         const i64 w0 = a.word0 + (i64)t * HELD_WORDS;
         if (w0 + HELD_WORDS > a.V) no_words<1, TN>(acc, w0, a.V);
         if constexpr (GRAD) put_dz<1, TN, 1>(acc, a, w0, t, tok0, label, l2, d);
-        else add_words<1, TN>(acc, a, w0, tok0, label, top, sum);
+        else add_words<1, TN>(acc, a, w0, tok0, label, run);
         // of the fetches and writes, which come back in order, those behind the next tile's may be under way
         meet<(HELD_STAGES - 2) * PER + (HELD_STAGES - 1) * STORES>();
         cur = (cur + 1) % HELD_STAGES;
     }
-    if constexpr (!GRAD) put_sums<TN>(a, strip, tok0, top, sum);
+    if constexpr (!GRAD) put_sums<TN>(a, strip, tok0, run);
 }
 
 // maxima and sums of the strips put together: a workgroup takes 64 tokens, its waves the strips in turn (4.8 us, which is the way to
