@@ -328,6 +328,7 @@ __device__ __forceinline__ void put_dz(f32x16 (&acc)[TM][TN], const LogitsArgs &
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
         bf16_t *row = a.dz + (tok + 32 * j + (lane & 31)) * BK + 8 * (lane >> 5);
+        const u32 keep = label[j] >= 0 ? ~0u : 0u;             // a token without a loss: zero even where a word's row makes its logit NaN
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             const int lw = label[j] - (int)(w0 + 32 * i);
@@ -345,7 +346,7 @@ __device__ __forceinline__ void put_dz(f32x16 (&acc)[TM][TN], const LogitsArgs &
             for (int part = 0; part < PARTS; ++part) {
                 u32 q[8];
 #pragma unroll
-                for (int r = 0; r < 8; ++r) q[r] = pack2(g[2 * r], g[2 * r + 1]);
+                for (int r = 0; r < 8; ++r) q[r] = pack2(g[2 * r], g[2 * r + 1]) & keep;
                 bf16_t *to = row + part * a.dz_plane + (block + i) * (a.Np * BK);
                 *(v4u *)to = join_halves(q[0], q[1], q[2], q[3]);
                 *(v4u *)(to + 16) = join_halves(q[4], q[5], q[6], q[7]);

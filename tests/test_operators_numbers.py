@@ -45,3 +45,53 @@ def test_small_words_beside_a_large_one(n, D, dtype, at):
     assert float((lse.double() - want).abs().max()) <= bound
     value = torch.where(labels == at, math.log1p(tail), want).double()
     assert float((loss.double() - value).abs().max()) <= bound
+
+
+# ---------------------------------------------------------------- words masked by infinities and the largest numbers
+def _grad(h, w, labels, lse, d, scale=1.0, ignore=-1):
+    n, (V, D) = labels.numel(), w.shape
+    ws = torch.empty(B.tensair_softmax_workspace_bytes(n, V, D, w.dtype, True), dtype=torch.uint8, device="cuda")
+    ws.fill_(0xFF)
+    dh, dw = torch.full_like(h, 3.0), torch.full_like(w, 3.0)
+    B.tensair_softmax_grad(h, w, D, labels, lse, d, dh, dw, ws, scale, ignore)
+    return dh, dw
+
+
+@pytest.mark.parametrize("how", ["infinite", "lowest", "large hidden"])
+@pytest.mark.parametrize("n,D,dtype", [(2, 32, "f32"), (8, 32, "bf16"), (30, 32, "bf16"), (130, 32, "bf16"), (300, 332, "bf16")])
+def test_softmax_words_masked_in_one_column(n, D, dtype, how):
+    """The first column holds a mask: minus infinity, the lowest number or a plain one that the hidden rows make as large.  The masked words have
+    no share in anything, and their gradient is zero whatever tokens lie beside them: those without a loss, those that fill up a tile."""
+    from test_operators import _softmax_reference, _gen
+    V, scale = 700, -0.7
+    g = _gen(n + D)
+    h = (torch.randn((n, D), generator=g, device="cuda") * 0.3).to(DT[dtype])
+    w = (torch.randn((V, D), generator=g, device="cuda") * 0.3).to(DT[dtype])
+    one = 1.0 + torch.rand(n, generator=g, device="cuda")
+    masked = torch.arange(0, V, 3, device="cuda")
+    rest = torch.ones(V, dtype=torch.bool, device="cuda")
+    rest[masked] = False
+    w[:, 0] = 0
+    if how == "infinite":
+        h[:, 0], w[masked, 0] = 1.0, float("inf")              # the scale is negative
+    elif how == "lowest":
+        h[:, 0], w[masked, 0] = 300.7 * one, torch.finfo(DT[dtype]).max
+    else:
+        h[:, 0], w[masked, 0] = 1.1e38 * one, 300.7
+    place = torch.cumsum(rest, 0) - 1
+    labels = rest.nonzero()[:, 0][torch.randint(0, int(rest.sum()), (n,), generator=g, device="cuda")].int()
+    labels[::3] = -1
+    d = torch.rand(n, generator=g, device="cuda") / n
+    loss, lse = _loss(h, w, labels, scale)
+    among = torch.where(labels >= 0, place[labels.clamp(min=0).long()], -1).int()
+    ref = _softmax_reference(h, w[rest], among, d, scale, dtype)
+    assert bool(((lse.double() - ref[0][0]).abs() <= ref[0][1]).all()) and bool(((loss.double() - ref[1][0]).abs() <= ref[1][1]).all())
+    dh, dw = _grad(h, w, labels, lse, d, scale)
+    assert bool((dw[masked] == 0).all())
+    assert bool(((dw[rest].double() - ref[3][0]).abs() <= ref[3][1]).all())
+    # (zero times infinity is in the first column's sum where the mask is infinite: what the definition gives)
+    at = slice(1 if how == "infinite" else 0, None)
+    assert bool(((dh.double() - ref[2][0]).abs() <= ref[2][1])[:, at].all()) and bool((dh[labels < 0] == 0).all())
+    # the loss of a masked word is infinite
+    labels[n - 1] = 3
+    assert float(_loss(h, w, labels, scale)[0][n - 1]) == math.inf
