@@ -240,6 +240,11 @@ struct LogitsArgs {
     // loss
     float2 *part;              // [strips * WM][Np] maximum, sum (of powers of two)
     float *picked;             // [Np] the label's logit, in units of log 2
+    // inputs of three parts: the numbers themselves
+    const float *table, *hidden;
+    i64 table_stride, hidden_stride, n;
+    int D;
+    float sign;
     // gradient
     const float *lse2, *d;     // [Np]
     bf16_t *dz;                // an Operand: rows are tokens, columns words
@@ -280,6 +285,43 @@ __device__ __forceinline__ void no_words(f32x16 (&acc)[TM][TN], i64 w0, i64 V)
             if (w0 + 32 * i + 8 * (r / 4) + 4 * (lane_id() >> 5) + r % 4 >= V)
 #pragma unroll
                 for (int j = 0; j < TN; ++j) acc[i][j][r] = -INFINITY;
+}
+// Products of parts that are NaN or infinite where the product of the numbers need not be: those that overflow beside one of the other
+// sign (a word masked by the lowest number, times several hundred), an infinity times a number below the smallest bfloat16.  Such logits
+// are made once more, from the numbers in 64 bits, a lane each; minus infinity is right as it is.
+template <int TM, int TN>
+__device__ __forceinline__ void mend_logits(f32x16 (&acc)[TM][TN], const LogitsArgs &a, i64 w0, i64 tok)
+{
+    const int lane = lane_id();
+    float all = 0.f;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) all += acc[i][j][r];
+    if (!__ballot(!(all < INFINITY))) return;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const i64 token = tok + 32 * j + (lane & 31), word0 = w0 + 32 * i + 4 * (lane >> 5);
+            u32 bad = 0;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) bad |= !(acc[i][j][r] < INFINITY) && token < a.n && word0 + 8 * (r / 4) + r % 4 < a.V ? 1u << r : 0u;
+            for (; bad; bad &= bad - 1) {
+                const int at = __ffs((int)bad) - 1;
+                const float *w = a.table + (word0 + 8 * (at / 4) + at % 4) * a.table_stride, *h = a.hidden + token * a.hidden_stride;
+                double z = 0.0;
+                for (int k = 0; k < a.D; k += 4) {
+                    const float4 x = ld4(w + k), y = ld4(h + k);
+                    z = fma((double)x.x, (double)y.x, fma((double)x.y, (double)y.y, fma((double)x.z, (double)y.z, fma((double)x.w, (double)y.w, z))));
+                }
+                const float v = (float)z * a.sign;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = r == at ? v : acc[i][j][r];
+            }
+        }
 }
 // A token's running sum over a strip of words, of powers of two relative to `top`, with what its roundings have cut off so far: a
 // strip is up to the whole vocabulary, and added to the plain sum its many small words would be lost one by one beside a large one.
@@ -432,6 +474,7 @@ __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_logits(Log
         step(std::true_type{});
         for (int s = 1; s < steps; ++s) step(std::false_type{});
         const i64 w0 = word + wm * TM * 32;
+        if constexpr (PARTS > 1) mend_logits<TM, TN>(p.acc, a, w0, tok0 + wn * TN * 32);
         if (word + P::BM > a.V) no_words<TM, TN>(p.acc, w0, a.V);
         if constexpr (GRAD) put_dz<TM, TN, PARTS>(p.acc, a, w0, t * (P::BM / BK) + wm * TM, tok0 + wn * TN * 32, label, l2, d);
         else add_words<TM, TN>(p.acc, a, w0, tok0 + wn * TN * 32, label, run);
@@ -1000,9 +1043,12 @@ __device__ __forceinline__ void parts(const PackArgs &a, int first, int blocks)
             for (int k = 0; k < 8; ++k) {
                 h[k] = f32_to_bf16(x[k]);
                 if (PARTS > 1) {
+                    // Infinity is the last part, which is multiplied by the other number's first one alone: that is zero where the number is.
+                    const bool infinite = fabsf(x[k]) == INFINITY;
+                    if (infinite && part + 1 < PARTS) h[k] = 0;
                     // beyond the largest bfloat16: cut, so that the rest is finite
-                    if ((h[k] & 0x7FFFu) == 0x7F80u && fabsf(x[k]) < INFINITY) h[k] = (h[k] & 0x8000u) | 0x7F7Fu;
-                    x[k] = (h[k] & 0x7F80u) == 0x7F80u ? 0.f : x[k] - __uint_as_float(h[k] << 16);
+                    if ((h[k] & 0x7FFFu) == 0x7F80u && !infinite) h[k] = (h[k] & 0x8000u) | 0x7F7Fu;
+                    if (!infinite) x[k] = (h[k] & 0x7F80u) == 0x7F80u ? 0.f : x[k] - __uint_as_float(h[k] << 16);
                 }
             }
             *(v4u *)(to + part * a.plane) = v4u{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
@@ -1235,6 +1281,13 @@ LogitsArgs lay_out_range(const SoftmaxPlan &s, const SoftmaxBuffers &b, const Ra
     a.token_tiles = s.token_tiles;
     a.Np = s.Np;
     a.c = fabsf(scale) * LOG2E;
+    a.table = (const float *)table;
+    a.table_stride = table_stride;
+    a.hidden = (const float *)x.h.src;
+    a.hidden_stride = x.h.stride;
+    a.n = x.h.rows;
+    a.D = D;
+    a.sign = x.h.sign;
     a.label = b.label;
     a.part = b.part;
     a.picked = b.picked;

@@ -58,9 +58,11 @@ def _grad(h, w, labels, lse, d, scale=1.0, ignore=-1):
 
 
 @pytest.mark.parametrize("how", ["infinite", "lowest", "large hidden"])
-@pytest.mark.parametrize("n,D,dtype", [(2, 32, "f32"), (8, 32, "bf16"), (30, 32, "bf16"), (130, 32, "bf16"), (300, 332, "bf16")])
+@pytest.mark.parametrize("n,D,dtype", [(2, 32, "f32"), (8, 32, "bf16"), (9, 32, "f32"), (30, 64, "f32"), (30, 32, "bf16"), (64, 36, "f32"), (130, 32, "f32"), (130, 32, "bf16"),
+                                       (128, 300, "f32"), (300, 332, "bf16"), (600, 128, "f32")])
 def test_softmax_words_masked_in_one_column(n, D, dtype, how):
-    """The first column holds a mask: minus infinity, the lowest number or a plain one that the hidden rows make as large.  The masked words have
+    """The first column holds a mask: minus infinity, the lowest number or a plain one that the hidden rows make as large.  In bits that are not
+    those of a bfloat16, so that a product of parts overflows where the number itself is of the other sign or not at all.  The masked words have
     no share in anything, and their gradient is zero whatever tokens lie beside them: those without a loss, those that fill up a tile."""
     from test_operators import _softmax_reference, _gen
     V, scale = 700, -0.7
