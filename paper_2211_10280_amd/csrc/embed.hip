@@ -674,14 +674,19 @@ int launched(const char *what)
     return e == hipSuccess ? TENSAIR_OK : tn_fail(TENSAIR_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-// the gradient's sums, where a.out and the sparse gradient's buffers are set
-int embed_grad(EmbedGradArgs &a, int32_t d_dtype, int dim, void *workspace, size_t workspace_bytes, hipStream_t st)
+// of the gradient of n > 0 tokens; before anything is launched
+int check_workspace(i64 vocab, i64 n, int dim, const void *workspace, size_t workspace_bytes)
 {
-    const EmbedSizes s = embed_sizes(a.V, a.n);
-    if (workspace_bytes < embed_carve(s, a.V, a.n, dim, nullptr, nullptr, nullptr, nullptr, nullptr))
+    if (workspace_bytes < embed_carve(embed_sizes(vocab, n), vocab, n, dim, nullptr, nullptr, nullptr, nullptr, nullptr))
         return tn_fail(TENSAIR_ECAPACITY, "workspace too small: see tensair_embed_workspace_bytes");
     if (!workspace) return tn_fail(TENSAIR_EINVAL, "workspace is NULL");
     if ((uintptr_t)workspace & 255) return tn_fail(TENSAIR_EINVAL, "workspace must be 256-byte aligned");
+    return TENSAIR_OK;
+}
+// the gradient's sums, where a.out and the sparse gradient's buffers are set
+int embed_grad(EmbedGradArgs &a, int32_t d_dtype, int dim, void *workspace, hipStream_t st)
+{
+    const EmbedSizes s = embed_sizes(a.V, a.n);
     int *row_ids = a.row_ids;
     u32 *keys[2] = {}, *vals[2] = {}, *pub = nullptr;
     embed_carve(s, a.V, a.n, dim, (char *)workspace, &a, keys, vals, &pub);
@@ -795,6 +800,7 @@ int tensair_embed_grad(const int32_t *ids, int64_t n, const void *d_out, int32_t
         tn_launch_prep_clear((u32 *)grad->n_rows, 1, st);
         return launched("embed_grad");
     }
+    if ((rc = check_workspace(vocab, n, dim, workspace, workspace_bytes))) return rc;
     EmbedGradArgs a;
     memset(&a, 0, sizeof(a));
     a.ids = ids;
@@ -810,7 +816,7 @@ int tensair_embed_grad(const int32_t *ids, int64_t n, const void *d_out, int32_t
     a.row_ids = grad->row_ids;
     a.n_rows = grad->n_rows;
     a.status = status;
-    return embed_grad(a, d_dtype, dim, workspace, workspace_bytes, st);
+    return embed_grad(a, d_dtype, dim, workspace, st);
 }
 
 int tensair_embed_grad_dense(const int32_t *ids, int64_t n, const void *d_out, int32_t d_dtype, int64_t d_stride, int64_t vocab,
@@ -822,8 +828,7 @@ int tensair_embed_grad_dense(const int32_t *ids, int64_t n, const void *d_out, i
     if ((rc = check_matrix(d_out, n, d_stride, dim, d_dtype, "d_out"))) return rc;
     if ((rc = check_matrix(grad, vocab, grad_stride, dim, grad_dtype, "grad"))) return rc;
     if ((uintptr_t)status & 3) return tn_fail(TENSAIR_EINVAL, "status must be 4-byte aligned");
-    if (workspace_bytes < tensair_embed_workspace_bytes(vocab, dim, n))
-        return tn_fail(TENSAIR_ECAPACITY, "workspace too small: see tensair_embed_workspace_bytes");
+    if (n > 0 && (rc = check_workspace(vocab, n, dim, workspace, workspace_bytes))) return rc;
     hipStream_t st = (hipStream_t)stream;
     if (n == 0 && accumulate) return TENSAIR_OK;
     if (!accumulate) {
@@ -848,7 +853,7 @@ int tensair_embed_grad_dense(const int32_t *ids, int64_t n, const void *d_out, i
     a.out.add = accumulate != 0;
     a.out.scale = scale;
     a.status = status;
-    return embed_grad(a, d_dtype, dim, workspace, workspace_bytes, st);
+    return embed_grad(a, d_dtype, dim, workspace, st);
 }
 
 }  // extern "C"
