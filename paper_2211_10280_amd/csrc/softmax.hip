@@ -1180,7 +1180,7 @@ struct SoftmaxBuffers {
     bf16_t *h, *w, *dz;
     float2 *part;
 };
-size_t softmax_carve(const SoftmaxPlan &s, i64 n, i64 V, int D, bool grad, char *base, SoftmaxBuffers *b)
+size_t softmax_carve(const SoftmaxPlan &s, i64 n, int D, bool grad, char *base, SoftmaxBuffers *b)
 {
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -1196,17 +1196,14 @@ size_t softmax_carve(const SoftmaxPlan &s, i64 n, i64 V, int D, bool grad, char 
         x.part = (float2 *)take(8 * (size_t)s.few_blocks * n);
         if (grad) x.h_slots = (float *)take(4 * (size_t)s.few_blocks * n * D);
         if (b) *b = x;
-        // the loss of the same sizes has more workgroups than the gradient
-        return grad ? std::max(at, softmax_carve(plan_of(n, V, D, s.parts == 3 ? TENSAIR_F32 : TENSAIR_BF16, false), n, V, D, false, nullptr, nullptr)) : at;
+        return at;
     }
     x.h = (bf16_t *)take(2 * (size_t)s.Np * s.Dp * s.parts);
     x.w = (bf16_t *)take(2 * (size_t)s.range_tiles * SM_BM * s.Dp * s.parts);
-    const size_t head = at;
-    x.picked = (float *)take(4 * (size_t)s.Np);
-    x.part = (float2 *)take(8 * (size_t)s.ranges * s.strips * s.wm * s.Np);
-    const size_t loss_end = at;
-    at = head;
-    if (grad) {
+    if (!grad) {
+        x.picked = (float *)take(4 * (size_t)s.Np);
+        x.part = (float2 *)take(8 * (size_t)s.ranges * s.strips * s.wm * s.Np);
+    } else {
         x.lse2 = (float *)take(4 * (size_t)s.Np);
         x.d = (float *)take(4 * (size_t)s.Np);
         x.dz = (bf16_t *)take(2 * (size_t)s.Np * s.range_tiles * SM_BM * s.parts);
@@ -1214,7 +1211,7 @@ size_t softmax_carve(const SoftmaxPlan &s, i64 n, i64 V, int D, bool grad, char 
         if (s.t_splits > 1) x.t_slots = (float *)take(4 * (size_t)s.t_splits * s.range_tiles * SM_BM * D);
     }
     if (b) *b = x;
-    return std::max(at, loss_end);
+    return at;
 }
 
 int check_softmax(i64 n, i64 vocab, int32_t dim, int32_t dtype)
@@ -1382,7 +1379,9 @@ size_t tensair_softmax_workspace_bytes(int64_t n, int64_t vocab, int32_t dim, in
 {
     if (check_softmax(n, vocab, dim, dtype)) return 0;
     if (n == 0) return 256;
-    return softmax_carve(plan_of(n, vocab, dim, dtype, with_grad != 0), n, vocab, dim, with_grad != 0, nullptr, nullptr);
+    // the loss has a plan of its own, with more words to a range where dz need not be kept
+    const size_t loss = softmax_carve(plan_of(n, vocab, dim, dtype, false), n, dim, false, nullptr, nullptr);
+    return with_grad ? std::max(loss, softmax_carve(plan_of(n, vocab, dim, dtype, true), n, dim, true, nullptr, nullptr)) : loss;
 }
 
 int tensair_softmax_loss(const void *hidden, int64_t hidden_stride, const void *table, int64_t table_stride, int32_t dtype, int64_t n,
@@ -1399,11 +1398,11 @@ int tensair_softmax_loss(const void *hidden, int64_t hidden_stride, const void *
         return tn_fail(TENSAIR_EINVAL, "labels, loss, lse and status must be 4-byte aligned");
     if (n == 0) return TENSAIR_OK;
     const SoftmaxPlan s = plan_of(n, vocab, dim, dtype, false);
-    if (workspace_bytes < softmax_carve(s, n, vocab, dim, false, nullptr, nullptr))
+    if (workspace_bytes < softmax_carve(s, n, dim, false, nullptr, nullptr))
         return tn_fail(TENSAIR_ECAPACITY, "workspace too small: see tensair_softmax_workspace_bytes");
     if (!workspace || ((uintptr_t)workspace & 255)) return tn_fail(TENSAIR_EINVAL, "workspace must be 256-byte aligned");
     SoftmaxBuffers b;
-    softmax_carve(s, n, vocab, dim, false, (char *)workspace, &b);
+    softmax_carve(s, n, dim, false, (char *)workspace, &b);
     hipStream_t st = (hipStream_t)stream;
     const Labels lab = {labels, ignore_label, vocab};
     int slots = 0;
@@ -1455,11 +1454,11 @@ int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *
         return launched("softmax_grad");
     }
     const SoftmaxPlan s = plan_of(n, vocab, dim, dtype, true);
-    if (workspace_bytes < softmax_carve(s, n, vocab, dim, true, nullptr, nullptr))
+    if (workspace_bytes < softmax_carve(s, n, dim, true, nullptr, nullptr))
         return tn_fail(TENSAIR_ECAPACITY, "workspace too small: see tensair_softmax_workspace_bytes");
     if (!workspace || ((uintptr_t)workspace & 255)) return tn_fail(TENSAIR_EINVAL, "workspace must be 256-byte aligned");
     SoftmaxBuffers b;
-    softmax_carve(s, n, vocab, dim, true, (char *)workspace, &b);
+    softmax_carve(s, n, dim, true, (char *)workspace, &b);
     const Labels lab = {labels, ignore_label, vocab};
     if (s.few) {
         FewArgs f = few_args(s, b, hidden, hidden_stride, table, table_stride, n, dim, scale, lab, status);
