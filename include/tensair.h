@@ -409,7 +409,7 @@ int tensair_embed_grad_dense(const int32_t *ids, int64_t n, const void *d_out, i
  *   d_hidden[i] = scale * sum_v dz[i][v] table[v],   d_table[v] = scale * sum_i dz[i][v] hidden[i],
  * both of the inputs' type (either may be NULL: not wanted).  lse: what tensair_softmax_loss gave for the same inputs. */
 #define TENSAIR_MAX_TOKENS 2097152 /* 2^21 */
-/* Bytes of workspace of the loss or, with_grad != 0, of both calls (0: an argument is out of range). */
+/* Bytes of workspace of the loss or, with_grad != 0, of both calls, of n tokens or fewer (0: an argument is out of range). */
 size_t tensair_softmax_workspace_bytes(int64_t n, int64_t vocab, int32_t dim, int32_t dtype, int32_t with_grad);
 int tensair_softmax_loss(const void *hidden, int64_t hidden_stride, const void *table, int64_t table_stride,
                          int32_t dtype, int64_t n, int64_t vocab, int32_t dim, const int32_t *labels,

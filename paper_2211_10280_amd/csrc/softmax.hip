@@ -1114,6 +1114,7 @@ struct SoftmaxPlan {
     int unit, per, strips;     // tiles of the logits' kernel to SM_BM words; of those to a strip; strips of a range
     int tm, m_tiles, pn;       // of the products: fragments of a wave along the row length, tiles; rows of a tile
     int h_splits, t_splits;    // of d_hidden's sum over a range's words, of d_table's over the tokens
+    int t_most;                // ... of as many tokens as fill the last SM_CLASS of them, at most
     i64 h_k, t_k;
 };
 
@@ -1169,6 +1170,7 @@ SoftmaxPlan plan_of(i64 n, i64 V, int D, int dtype, bool grad)
     s.h_k = cdiv(cdiv(range_words, splits), BK) * BK;
     s.h_splits = (int)cdiv(range_words, s.h_k);
     splits = std::max<i64>(1, std::min<i64>(SM_BLOCKS / t_tiles, n / 512));
+    s.t_most = (int)splits;
     s.t_k = cdiv(cdiv(n, splits), BK) * BK;
     s.t_splits = (int)cdiv(n, s.t_k);
     return s;
@@ -1180,6 +1182,9 @@ struct SoftmaxBuffers {
     bf16_t *h, *w, *dz;
     float2 *part;
 };
+// Of more than FEW_TOKENS tokens the size is the same for all n that are the same number of SM_CLASS, which every border in plan_of is a
+// multiple of, the last one rounded up.
+#define SM_CLASS 64
 size_t softmax_carve(const SoftmaxPlan &s, i64 n, int D, bool grad, char *base, SoftmaxBuffers *b)
 {
     size_t at = 0;
@@ -1207,8 +1212,8 @@ size_t softmax_carve(const SoftmaxPlan &s, i64 n, int D, bool grad, char *base, 
         x.lse2 = (float *)take(4 * (size_t)s.Np);
         x.d = (float *)take(4 * (size_t)s.Np);
         x.dz = (bf16_t *)take(2 * (size_t)s.Np * s.range_tiles * SM_BM * s.parts);
-        x.h_slots = (float *)take(4 * (size_t)s.h_splits * n * D);
-        if (s.t_splits > 1) x.t_slots = (float *)take(4 * (size_t)s.t_splits * s.range_tiles * SM_BM * D);
+        x.h_slots = (float *)take(4 * (size_t)s.h_splits * (cdiv(n, SM_CLASS) * SM_CLASS) * D);
+        if (s.t_most > 1) x.t_slots = (float *)take(4 * (size_t)s.t_most * s.range_tiles * SM_BM * D);
     }
     if (b) *b = x;
     return at;
@@ -1379,9 +1384,17 @@ size_t tensair_softmax_workspace_bytes(int64_t n, int64_t vocab, int32_t dim, in
 {
     if (check_softmax(n, vocab, dim, dtype)) return 0;
     if (n == 0) return 256;
-    // the loss has a plan of its own, with more words to a range where dz need not be kept
-    const size_t loss = softmax_carve(plan_of(n, vocab, dim, dtype, false), n, dim, false, nullptr, nullptr);
-    return with_grad ? std::max(loss, softmax_carve(plan_of(n, vocab, dim, dtype, true), n, dim, true, nullptr, nullptr)) : loss;
+    // The loss has a plan of its own, with more words to a range where dz need not be kept; and fewer tokens may want more than more of
+    // them do, since a range then holds more words: the most of all numbers of tokens up to n.
+    size_t most = 0;
+    auto take = [&](i64 k) {
+        most = std::max(most, softmax_carve(plan_of(k, vocab, dim, dtype, false), k, dim, false, nullptr, nullptr));
+        if (with_grad) most = std::max(most, softmax_carve(plan_of(k, vocab, dim, dtype, true), k, dim, true, nullptr, nullptr));
+    };
+    take(std::min<i64>(n, FEW_TOKENS));
+    if (n > FEW_TOKENS)
+        for (i64 k = SM_CLASS; k < n + SM_CLASS; k += SM_CLASS) take(k);
+    return most;
 }
 
 int tensair_softmax_loss(const void *hidden, int64_t hidden_stride, const void *table, int64_t table_stride, int32_t dtype, int64_t n,
