@@ -381,7 +381,7 @@ int tensair_embed(const void *table, int32_t dtype, int64_t vocab, int32_t dim, 
                   const int32_t *ids, int64_t n, float scale, void *out, int32_t out_dtype,
                   int64_t out_stride, int32_t *status, void *stream);
 
-/* Bytes of workspace of the two calls below (0: an argument is out of range). */
+/* Bytes of workspace of the two calls below, of n ids or fewer (0: an argument is out of range). */
 size_t tensair_embed_workspace_bytes(int64_t vocab, int32_t dim, int64_t n);
 
 /* The gradient of tensair_embed with respect to the table: for every word r among the ids

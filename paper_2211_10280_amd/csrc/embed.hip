@@ -555,6 +555,8 @@ struct EmbedSizes {
     int passes, bits, tiles, seg_tiles, sum_tiles, tile;
     size_t nd, pub, clear, tile0, per_pass, seg_state, hist, none;     // words of the published area
 };
+// most tokens that are summed in tiles of so many
+i64 most_in_tiles(int tile) { return (i64)(tile < 32 ? 2048 : 16384) * tile + tile - 1; }
 EmbedSizes embed_sizes(i64 V, i64 n)
 {
     EmbedSizes s;
@@ -570,7 +572,7 @@ EmbedSizes embed_sizes(i64 V, i64 n)
     // shares to write and to read again (32 767 tokens, rows of 300 added to a table: tiles of 4 26 us, of 8 22, of 16 18, of 32 26;
     // 262 143 tokens, rows of 256 in bfloat16: of 64 37.6 us, of 32 30.8)
     s.tile = 4;
-    while (s.tile < EMBED_MAX_TILE && n / s.tile > (s.tile < 32 ? 2048 : 16384)) s.tile *= 2;
+    while (s.tile < EMBED_MAX_TILE && n > most_in_tiles(s.tile)) s.tile *= 2;
     s.sum_tiles = (int)((n + s.tile - 1) / s.tile);
     s.chained = s.tiles <= TN_PREP_CHAIN_OWN;
     // tickets (a word per pass and one of the segments), the segments' words, digit counts, the tiles' words of each pass
@@ -779,7 +781,16 @@ int tensair_embed(const void *table, int32_t dtype, int64_t vocab, int32_t dim, 
 size_t tensair_embed_workspace_bytes(int64_t vocab, int32_t dim, int64_t n)
 {
     if (check_ids((const int32_t *)4, n, vocab, dim)) return 0;
-    return embed_carve(embed_sizes(vocab, n), vocab, n, dim, nullptr, nullptr, nullptr, nullptr, nullptr);
+    // the most of all numbers of tokens up to n: it grows with them but for where tiles become longer and the sort is another
+    size_t most = 0;
+    auto take = [&](i64 k) {
+        if (k <= n) most = std::max(most, embed_carve(embed_sizes(vocab, k), vocab, k, dim, nullptr, nullptr, nullptr, nullptr, nullptr));
+    };
+    take(n);
+    for (int tile = 4; tile < EMBED_MAX_TILE; tile *= 2) take(most_in_tiles(tile));
+    take(EMBED_FEW);
+    take((i64)TN_PREP_CHAIN_OWN * TN_RADIX_TILE);
+    return most;
 }
 
 int tensair_embed_grad(const int32_t *ids, int64_t n, const void *d_out, int32_t d_dtype, int64_t d_stride, int64_t vocab, int32_t dim,

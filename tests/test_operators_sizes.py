@@ -55,6 +55,19 @@ def test_a_softmax_workspace_serves_fewer_tokens(mem):
                 assert _softmax_fits(mem, k, V, D, dtype, nbytes, False) and (not grad or _softmax_fits(mem, k, V, D, dtype, nbytes, True)), (n, k, V, D, dtype, grad)
 
 
+def test_a_gradient_s_workspace_serves_fewer_ids(mem):
+    L, rng = B.lib(), random.Random(6)
+    borders = [2_048 * t + t + e for t in (2, 4, 8, 16, 32, 64, 128) for e in (-2, -1, 0, 1)] + [k + e for k in (4_096, 262_144, 524_288) for e in (-1, 0, 1, 31, 32)]
+    for case in range(60):
+        n, V, D = int(2 ** rng.uniform(0, 22)), int(2 ** rng.uniform(0, 27)), 4 * int(2 ** rng.uniform(0, 8))
+        if case < len(borders):
+            n = borders[case]
+        nbytes = B.tensair_embed_workspace_bytes(V, D, n)
+        for k in {n, max(1, n - 1), 1} | {rng.randint(1, n) for _ in range(30)} | {b for b in borders if b <= n}:
+            rc = L.tensair_embed_grad_dense(mem, k, mem, B.F32, D, V, D, 1.0, mem, B.F32, D, 1, mem + 64, nbytes, None, None)
+            assert rc == B.EINVAL, (n, k, V, D)          # refused for the workspace's alignment, not for its size
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("n,V,D,dtype", [(2_000, 262_144, 512, "f32"), (4_096, 1_000_000, 1_024, "bf16")])
 def test_both_calls_in_one_workspace(n, V, D, dtype):
