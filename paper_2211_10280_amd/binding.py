@@ -431,16 +431,36 @@ def _ids(t, what="ids"):
     return _vector(t, t.numel(), torch.int32, what)
 
 
-def _word(t):
+def _device(t, *others):
+    """The number of the GPU that a tensor is on, and all others (None: not given): the kernels take addresses as they are."""
+    dev = t.get_device()
+    if dev < 0:
+        raise TensairError(EINVAL, "a tensor is not on a GPU")
+    for x in others:
+        if x is not None and x.get_device() != dev:
+            raise TensairError(EINVAL, "the tensors are not on one GPU")
+    return dev
+
+
+def _word(t, dtype=torch.int32, what="status"):
     """The address of a status word or a scale, or None."""
-    return None if t is None else t.data_ptr()
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() < 1:
+        raise TensairError(EINVAL, f"{what}: expected an element of {dtype}")
+    return t.data_ptr()
 
 
-def _on(t, stream):
-    """The handle of `stream`, by default the current one of the tensor's device."""
-    if stream is None and _raw_stream is not None and t.is_cuda:
-        return _raw_stream(t.get_device())
-    return _stream(stream)
+def _bytes(workspace):
+    """The bytes of a workspace, a tensor of any type."""
+    if not workspace.is_contiguous():
+        raise TensairError(EINVAL, "workspace: expected a contiguous tensor")
+    return workspace.numel() * workspace.element_size()
+
+
+def _on(dev, stream):
+    """The handle of `stream`, by default the current one of the GPU of that number."""
+    return _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream)
 
 
 class RowBuffers:
@@ -462,10 +482,10 @@ class RowBuffers:
 
 def tensair_embed(table, dim: int, ids, out, scale=1.0, status=None, stream=None):
     """table: [vocab, >= dim] float32 or bfloat16; ids: int32 [n]; out: [n, >= dim] float32 or bfloat16."""
-    n = ids.numel()
+    n, dev = ids.numel(), _device(table, ids, out, status)
     tp, td, ts = _matrix(table, table.shape[0], dim, "table")
     op, od, os_ = _matrix(out, n, dim, "out")
-    rc = (_lib or lib()).tensair_embed(tp, td, table.shape[0], dim, ts, _ids(ids), n, scale, op, od, os_, _word(status), _on(table, stream))
+    rc = (_lib or lib()).tensair_embed(tp, td, table.shape[0], dim, ts, _ids(ids), n, scale, op, od, os_, _word(status), _on(dev, stream))
     if rc:
         _check(rc)
 
@@ -480,24 +500,24 @@ def tensair_embed_workspace_bytes(vocab: int, dim: int, n: int) -> int:
 def tensair_embed_grad(ids, d_out, dim: int, vocab: int, grad, workspace, scale=1.0, status=None, stream=None):
     """grad: RowBuffers, or (n_rows int32 [1], row_ids int32 [capacity], rows float32 [capacity, dim])."""
     n_rows, row_ids, rows = grad
-    n, cap = ids.numel(), row_ids.numel()
+    n, cap, dev = ids.numel(), row_ids.numel(), _device(d_out, ids, n_rows, row_ids, rows, workspace, status)
     dp, dd, ds = _matrix(d_out, n, dim, "d_out")
     if rows.dtype != torch.float32 or tuple(rows.shape) != (cap, dim) or not rows.is_contiguous():
         raise TensairError(EINVAL, f"grad: expected contiguous float32 rows of shape ({cap}, {dim})")
     c = SparseRows(cap, _vector(n_rows, 1, torch.int32, "n_rows"), _ids(row_ids, "row_ids"), rows.data_ptr())
     rc = (_lib or lib()).tensair_embed_grad(_ids(ids), n, dp, dd, ds, vocab, dim, scale, C.byref(c), workspace.data_ptr(),
-                                    workspace.numel() * workspace.element_size(), _word(status), _on(d_out, stream))
+                                    _bytes(workspace), _word(status), _on(dev, stream))
     if rc:
         _check(rc)
 
 
 def tensair_embed_grad_dense(ids, d_out, dim: int, grad, workspace, scale=1.0, accumulate=False, status=None, stream=None):
     """grad: [vocab, >= dim] float32 or bfloat16, overwritten or, with accumulate, added to."""
-    n, vocab = ids.numel(), grad.shape[0]
+    n, vocab, dev = ids.numel(), grad.shape[0], _device(d_out, ids, grad, workspace, status)
     dp, dd, ds = _matrix(d_out, n, dim, "d_out")
     gp, gd, gs = _matrix(grad, vocab, dim, "grad")
     rc = (_lib or lib()).tensair_embed_grad_dense(_ids(ids), n, dp, dd, ds, vocab, dim, scale, gp, gd, gs, int(accumulate), workspace.data_ptr(),
-                                          workspace.numel() * workspace.element_size(), _word(status), _on(d_out, stream))
+                                          _bytes(workspace), _word(status), _on(dev, stream))
     if rc:
         _check(rc)
 
@@ -513,13 +533,14 @@ def tensair_softmax_workspace_bytes(n: int, vocab: int, dim: int, dtype, with_gr
 def tensair_softmax_loss(hidden, table, dim: int, labels, loss, lse, workspace, scale=1.0, ignore_label=-1, status=None, stream=None):
     """hidden: [n, >= dim], table: [vocab, >= dim] of one type; labels: int32 [n]; loss, lse: float32 [n]."""
     n, vocab = labels.numel(), table.shape[0]
+    dev = _device(table, hidden, labels, loss, lse, workspace, status)
     hp, hd, hs = _matrix(hidden, n, dim, "hidden")
     tp, td, ts = _matrix(table, vocab, dim, "table")
     if hd != td:
         raise TensairError(EINVAL, "hidden and table must have one type")
     rc = (_lib or lib()).tensair_softmax_loss(hp, hs, tp, ts, td, n, vocab, dim, _ids(labels, "labels"), ignore_label, scale,
                                       _vector(loss, n, torch.float32, "loss"), _vector(lse, n, torch.float32, "lse"), workspace.data_ptr(),
-                                      workspace.numel() * workspace.element_size(), _word(status), _on(table, stream))
+                                      _bytes(workspace), _word(status), _on(dev, stream))
     if rc:
         _check(rc)
 
@@ -528,6 +549,7 @@ def tensair_softmax_grad(hidden, table, dim: int, labels, lse, d_loss, d_hidden,
                          status=None, stream=None):
     """lse: as tensair_softmax_loss gave it; d_loss: float32 [n]; d_hidden, d_table: like hidden and table, or None."""
     n, vocab = labels.numel(), table.shape[0]
+    dev = _device(table, hidden, labels, lse, d_loss, d_hidden, d_table, workspace, status)
     hp, hd, hs = _matrix(hidden, n, dim, "hidden")
     tp, td, ts = _matrix(table, vocab, dim, "table")
     dhp, dhd, dhs = _matrix(d_hidden, n, dim, "d_hidden") if d_hidden is not None else (None, td, dim)
@@ -536,7 +558,7 @@ def tensair_softmax_grad(hidden, table, dim: int, labels, lse, d_loss, d_hidden,
         raise TensairError(EINVAL, "hidden, table and their gradients must have one type")
     rc = (_lib or lib()).tensair_softmax_grad(hp, hs, tp, ts, td, n, vocab, dim, _ids(labels, "labels"), ignore_label, scale,
                                       _vector(lse, n, torch.float32, "lse"), _vector(d_loss, n, torch.float32, "d_loss"), dhp, dhs, dtp, dts,
-                                      workspace.data_ptr(), workspace.numel() * workspace.element_size(), _word(status), _on(table, stream))
+                                      workspace.data_ptr(), _bytes(workspace), _word(status), _on(dev, stream))
     if rc:
         _check(rc)
 
@@ -583,14 +605,16 @@ def tensair_adamw_workspace_bytes(tensors) -> int:
 def tensair_adamw_init(tensors, workspace, stream=None):
     arr, state = _adamw_tensors(tensors)
     h = C.c_void_p()
-    _check(lib().tensair_adamw_init(C.byref(h), arr, len(tensors), state, _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                    _stream(stream)))
+    dev = _device(workspace, *(t[w] for t in tensors for w in ("param", "grad", "m", "v", "m_scale", "v_scale", "param_copy") if t.get(w) is not None))
+    _check(lib().tensair_adamw_init(C.byref(h), arr, len(tensors), state, _ptr(workspace), _bytes(workspace), _on(dev, stream)))
     return h
 
 
 def tensair_adamw_step(h, lr: float, step: int, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None, stream=None):
     """grad_scale: float32 tensor of one element that the gradients are multiplied by, or None."""
-    _check(lib().tensair_adamw_step(h, lr, step, beta1, beta2, eps, _word(grad_scale), _stream(stream)))
+    if grad_scale is not None:
+        _device(grad_scale)
+    _check(lib().tensair_adamw_step(h, lr, step, beta1, beta2, eps, _word(grad_scale, torch.float32, "grad_scale"), _stream(stream)))
 
 
 def tensair_adamw_destroy(h):
@@ -609,7 +633,8 @@ class AdamW:
         self.h = tensair_adamw_init(self.tensors, self.workspace, stream)
 
     def step(self, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None, stream=None):
-        rc = _lib.tensair_adamw_step(self.h, lr, step, beta1, beta2, eps, _word(grad_scale), _on(self.workspace, stream))
+        rc = _lib.tensair_adamw_step(self.h, lr, step, beta1, beta2, eps, _word(grad_scale, torch.float32, "grad_scale"),
+                                     _on(_device(self.workspace, grad_scale), stream))
         if rc:
             _check(rc)
 
