@@ -455,6 +455,11 @@ int tensair_adamw_init(tensair_adamw **out, const tensair_adamw_tensor *tensors,
                        int32_t state_dtype, void *workspace, size_t workspace_bytes, void *stream);
 int tensair_adamw_step(tensair_adamw *h, double lr, int64_t step, double beta1, double beta2, double eps,
                        const float *grad_scale, void *stream);
+/* The same with lr (DEVICE double) and step (DEVICE int64, below 1 taken as 1) read when the work runs, for steps that are recorded
+ * into a graph: a recorded tensair_adamw_step repeats the step that it was called with, corrections and 8-bit offsets included, at every replay.
+ * The caller counts the step up, for example by a kernel in the same graph. */
+int tensair_adamw_step_at(tensair_adamw *h, const double *lr, const int64_t *step, double beta1, double beta2,
+                          double eps, const float *grad_scale, void *stream);
 int tensair_adamw_destroy(tensair_adamw *h);
 
 /* Waits for the library's own stream (a pending prefetch), then frees the host handle. */

@@ -36,7 +36,7 @@ SYMBOLS = [
     "tensair_dasgd_apply_static", "tensair_stream_probe", "tensair_aligned_row_stride",
     "tensair_embed", "tensair_embed_workspace_bytes", "tensair_embed_grad", "tensair_embed_grad_dense",
     "tensair_softmax_workspace_bytes", "tensair_softmax_loss", "tensair_softmax_grad",
-    "tensair_adamw_workspace_bytes", "tensair_adamw_init", "tensair_adamw_step", "tensair_adamw_destroy",
+    "tensair_adamw_workspace_bytes", "tensair_adamw_init", "tensair_adamw_step", "tensair_adamw_step_at", "tensair_adamw_destroy",
 ]
 
 PROFILE_TAGS = {1: "keys", 2: "forward", 3: "sort", 4: "segments", 5: "reduce_in", 6: "reduce_out",
@@ -164,6 +164,8 @@ def lib():
         L.tensair_adamw_init.restype = C.c_int
         L.tensair_adamw_step.argtypes = [vp, C.c_double, i64, C.c_double, C.c_double, C.c_double, vp, vp]
         L.tensair_adamw_step.restype = C.c_int
+        L.tensair_adamw_step_at.argtypes = [vp, vp, vp, C.c_double, C.c_double, C.c_double, vp, vp]
+        L.tensair_adamw_step_at.restype = C.c_int
         L.tensair_adamw_destroy.argtypes = [vp]
         L.tensair_adamw_destroy.restype = C.c_int
         L.tensair_last_error.argtypes = []
@@ -617,6 +619,13 @@ def tensair_adamw_step(h, lr: float, step: int, beta1=0.9, beta2=0.999, eps=1e-8
     _check(lib().tensair_adamw_step(h, lr, step, beta1, beta2, eps, _word(grad_scale, torch.float32, "grad_scale"), _stream(stream)))
 
 
+def tensair_adamw_step_at(h, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None, stream=None):
+    """lr: float64 tensor, step: int64 tensor of one element each, read when the work runs (in a graph: at every replay)."""
+    dev = _device(lr, step, grad_scale)
+    _check(lib().tensair_adamw_step_at(h, _word(lr, torch.float64, "lr"), _word(step, torch.int64, "step"), beta1, beta2, eps,
+                                       _word(grad_scale, torch.float32, "grad_scale"), _on(dev, stream)))
+
+
 def tensair_adamw_destroy(h):
     _check(lib().tensair_adamw_destroy(h))
 
@@ -633,6 +642,10 @@ class AdamW:
         self.h = tensair_adamw_init(self.tensors, self.workspace, stream)
 
     def step(self, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None, stream=None):
+        """lr and step: numbers or, for a step that is recorded into a graph, float64 and int64 tensors of one element on the GPU."""
+        if isinstance(step, torch.Tensor):
+            _device(self.workspace, step)
+            return tensair_adamw_step_at(self.h, lr, step, beta1, beta2, eps, grad_scale, stream)
         rc = _lib.tensair_adamw_step(self.h, lr, step, beta1, beta2, eps, _word(grad_scale, torch.float32, "grad_scale"),
                                      _on(_device(self.workspace, grad_scale), stream))
         if rc:

@@ -37,13 +37,28 @@ struct AdamwTensor {
     u32 vec;                   // 4 elements can be loaded at a time
     u32 pad;
 };
+// what a step's number and size come to: in the arguments, or, where they are read on the device, in the workspace
+struct AdamwLive {
+    float lr, size, fix;
+    u32 walk;                  // the step's part of the offsets
+};
 struct AdamwStep {
     const AdamwTensor *tensors;
     const u32 *chunks;         // [chunks] the tensor of every chunk
     const float *grad_scale;
-    float lr, b1, c1, b2, c2, size, fix, eps;
-    u32 walk;                  // the step's part of the offsets
+    float b1, c1, b2, c2, eps;
+    AdamwLive now;
+    const AdamwLive *live;     // NULL: as in `now`
 };
+// in 64 bits, each rounded once
+__host__ __device__ __forceinline__ AdamwLive adamw_live(double lr, i64 step, double beta1, double beta2)
+{
+    return AdamwLive{(float)lr, (float)(lr / (1.0 - pow(beta1, (double)step))), (float)(1.0 / sqrt(1.0 - pow(beta2, (double)step))), (u32)step * 0x85EBCA77u};
+}
+__global__ void k_adamw_live(AdamwLive *out, const double *lr, const i64 *step, double beta1, double beta2)
+{
+    *out = adamw_live(*lr, max((i64)1, *step), beta1, beta2);
+}
 
 typedef float v2f __attribute__((ext_vector_type(2)));
 
@@ -135,12 +150,12 @@ __device__ __forceinline__ u32 root_code(float x, u32 offset)
     return x > 0.0f ? code : 0u;
 }
 
-__device__ __forceinline__ void adamw1(float &p, float g, float &m, float &v, float &r, const AdamwStep &a, float keep)
+__device__ __forceinline__ void adamw1(float &p, float g, float &m, float &v, float &r, const AdamwStep &a, const AdamwLive &now, float keep)
 {
     m = a.b1 * m + a.c1 * g;
     v = a.b2 * v + a.c2 * (g * g);
     r = sqrtf(v);
-    p = p * keep - (m * a.size) / (r * a.fix + a.eps);
+    p = p * keep - (m * now.size) / (r * now.fix + a.eps);
 }
 
 // One pass over parameters, gradients and states, which memory bounds: 600 M fp32 parameters with bfloat16 gradients and 8-bit
@@ -153,7 +168,8 @@ __global__ void __launch_bounds__(BLOCK) k_adamw(AdamwStep a, u32 first_chunk)
     const AdamwTensor &t = a.tensors[a.chunks[chunk]];
     const i64 n = t.n, base = (i64)(chunk - t.first) * ADAMW_CHUNK + (i64)threadIdx.x * 4;
     const bool vec = t.vec != 0;
-    const float keep = 1.0f - t.decay * a.lr;
+    const AdamwLive now = a.live ? *a.live : a.now;
+    const float keep = 1.0f - t.decay * now.lr;
     const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
     TP *param = (TP *)t.param;
     const TG *grad = (const TG *)t.grad;
@@ -179,10 +195,10 @@ __global__ void __launch_bounds__(BLOCK) k_adamw(AdamwStep a, u32 first_chunk)
         for (int j = 0; j < ADAMW_VECS; ++j) {
             const i64 i = base + j * (BLOCK * 4);
             float r;
-            adamw1(p[j].x, g[j].x, mm[j].x, vv[j].x, r, a, keep);
-            adamw1(p[j].y, g[j].y, mm[j].y, vv[j].y, r, a, keep);
-            adamw1(p[j].z, g[j].z, mm[j].z, vv[j].z, r, a, keep);
-            adamw1(p[j].w, g[j].w, mm[j].w, vv[j].w, r, a, keep);
+            adamw1(p[j].x, g[j].x, mm[j].x, vv[j].x, r, a, now, keep);
+            adamw1(p[j].y, g[j].y, mm[j].y, vv[j].y, r, a, now, keep);
+            adamw1(p[j].z, g[j].z, mm[j].z, vv[j].z, r, a, now, keep);
+            adamw1(p[j].w, g[j].w, mm[j].w, vv[j].w, r, a, now, keep);
             put4<STREAM>(param, i, n, vec, p[j]);
             put4<STREAM>(m, i, n, vec, mm[j]);
             put4<STREAM>(v, i, n, vec, vv[j]);
@@ -206,16 +222,16 @@ __global__ void __launch_bounds__(BLOCK) k_adamw(AdamwStep a, u32 first_chunk)
             const i64 i = base + j * (BLOCK * 4), group = i / ADAMW_GROUP;
             float4 mm = from_fp8(mc[j], ms[j]), vv = from_fp8(vc[j], vs[j]), r;
             vv = make_float4(vv.x * vv.x, vv.y * vv.y, vv.z * vv.z, vv.w * vv.w);
-            adamw1(p[j].x, g[j].x, mm.x, vv.x, r.x, a, keep);
-            adamw1(p[j].y, g[j].y, mm.y, vv.y, r.y, a, keep);
-            adamw1(p[j].z, g[j].z, mm.z, vv.z, r.z, a, keep);
-            adamw1(p[j].w, g[j].w, mm.w, vv.w, r.w, a, keep);
+            adamw1(p[j].x, g[j].x, mm.x, vv.x, r.x, a, now, keep);
+            adamw1(p[j].y, g[j].y, mm.y, vv.y, r.y, a, now, keep);
+            adamw1(p[j].z, g[j].z, mm.z, vv.z, r.z, a, now, keep);
+            adamw1(p[j].w, g[j].w, mm.w, vv.w, r.w, a, now, keep);
             const float mx = __uint_as_float(wave_max_bits(max(max(magnitude(mm.x), magnitude(mm.y)), max(magnitude(mm.z), magnitude(mm.w)))));
             const float rx = __uint_as_float(wave_max_bits(max(max(magnitude(r.x), magnitude(r.y)), max(magnitude(r.z), magnitude(r.w)))));
             const float mi = to_range(mx), ri = to_range(rx);
             int code = __builtin_amdgcn_cvt_pk_fp8_f32(mm.x * mi, mm.y * mi, 0, false);
             code = __builtin_amdgcn_cvt_pk_fp8_f32(mm.z * mi, mm.w * mi, code, true);
-            const u32 off = (u32)i * 0x9E3779B1u + a.walk;
+            const u32 off = (u32)i * 0x9E3779B1u + now.walk;
             const u32 root = root_code(r.x * ri, off >> 12) | root_code(r.y * ri, (off + 0x9E3779B1u) >> 12) << 8 |
                              root_code(r.z * ri, (off + 2u * 0x9E3779B1u) >> 12) << 16 | root_code(r.w * ri, (off + 3u * 0x9E3779B1u) >> 12) << 24;
             put4<STREAM>(param, i, n, vec, p[j]);
@@ -263,6 +279,7 @@ struct tensair_adamw {
     const AdamwTensor *tensors;
     const u32 *chunks;
     u32 first[4], count[4];    // chunks by types: parameters fp32 or bfloat16, gradients fp32 or bfloat16
+    AdamwLive *live;
     bool eight, stream;
 };
 
@@ -277,13 +294,33 @@ static void launch_adamw(const tensair_adamw *h, const AdamwStep &a, int kind, h
     else hipLaunchKernelGGL((k_adamw<TP, TG, false, false>), grid, blk, 0, st, a, h->first[kind]);
 }
 
+static int check_step(const tensair_adamw *h, double beta1, double beta2, double eps, const float *grad_scale)
+{
+    if (!h) return tn_fail(TENSAIR_EINVAL, "handle is NULL");
+    if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return tn_fail(TENSAIR_EINVAL, "betas must be in [0, 1)");
+    if (!((float)eps > 0.0f)) return tn_fail(TENSAIR_EINVAL, "eps must be positive");
+    if ((uintptr_t)grad_scale & 3) return tn_fail(TENSAIR_EINVAL, "grad_scale must be 4-byte aligned");
+    return TENSAIR_OK;
+}
+static int adamw_step(const tensair_adamw *h, const AdamwLive &now, const AdamwLive *live, double beta1, double beta2, double eps, const float *grad_scale,
+                      hipStream_t st)
+{
+    const AdamwStep a = {h->tensors, h->chunks, grad_scale, (float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps, now, live};
+    launch_adamw<float, float>(h, a, 0, st);
+    launch_adamw<float, bf16_t>(h, a, 1, st);
+    launch_adamw<bf16_t, float>(h, a, 2, st);
+    launch_adamw<bf16_t, bf16_t>(h, a, 3, st);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? TENSAIR_OK : tn_fail(TENSAIR_EHIP, "adamw_step: %s", hipGetErrorString(e));
+}
+
 extern "C" {
 
 size_t tensair_adamw_workspace_bytes(const tensair_adamw_tensor *tensors, int32_t n_tensors, int32_t state_dtype)
 {
     i64 chunks;
     if (check_tensors(tensors, n_tensors, state_dtype, &chunks)) return 0;
-    return up256(sizeof(AdamwTensor) * (size_t)n_tensors) + up256(4 * (size_t)(chunks > 0 ? chunks : 1));
+    return up256(sizeof(AdamwTensor) * (size_t)n_tensors) + up256(4 * (size_t)(chunks > 0 ? chunks : 1)) + up256(sizeof(AdamwLive));
 }
 
 int tensair_adamw_init(tensair_adamw **out, const tensair_adamw_tensor *tensors, int32_t n_tensors, int32_t state_dtype, void *workspace,
@@ -335,6 +372,7 @@ int tensair_adamw_init(tensair_adamw **out, const tensair_adamw_tensor *tensors,
         h->stream = bytes > ADAMW_STREAM_BYTES;
         h->tensors = (const AdamwTensor *)workspace;
         h->chunks = (const u32 *)((char *)workspace + head);
+        h->live = (AdamwLive *)((char *)workspace + head + up256(4 * (size_t)(chunks > 0 ? chunks : 1)));
         hipStream_t st = (hipStream_t)stream;
         hipError_t e = hipMemcpyAsync(workspace, image.data(), image.size(), hipMemcpyHostToDevice, st);
         if (e == hipSuccess) e = hipStreamSynchronize(st);
@@ -352,33 +390,20 @@ int tensair_adamw_init(tensair_adamw **out, const tensair_adamw_tensor *tensors,
 
 int tensair_adamw_step(tensair_adamw *h, double lr, int64_t step, double beta1, double beta2, double eps, const float *grad_scale, void *stream)
 {
-    if (!h) return tn_fail(TENSAIR_EINVAL, "handle is NULL");
+    if (int rc = check_step(h, beta1, beta2, eps, grad_scale)) return rc;
     if (step < 1) return tn_fail(TENSAIR_EINVAL, "steps count from 1");
     if (!(lr == lr)) return tn_fail(TENSAIR_EINVAL, "lr is NaN");
-    if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return tn_fail(TENSAIR_EINVAL, "betas must be in [0, 1)");
-    if (!((float)eps > 0.0f)) return tn_fail(TENSAIR_EINVAL, "eps must be positive");
-    if ((uintptr_t)grad_scale & 3) return tn_fail(TENSAIR_EINVAL, "grad_scale must be 4-byte aligned");
-    AdamwStep a;
-    a.tensors = h->tensors;
-    a.chunks = h->chunks;
-    a.grad_scale = grad_scale;
-    // the constants in 64 bits, each rounded once
-    a.lr = (float)lr;
-    a.b1 = (float)beta1;
-    a.c1 = (float)(1.0 - beta1);
-    a.b2 = (float)beta2;
-    a.c2 = (float)(1.0 - beta2);
-    a.size = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
-    a.fix = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
-    a.eps = (float)eps;
-    a.walk = (u32)step * 0x85EBCA77u;
+    return adamw_step(h, adamw_live(lr, step, beta1, beta2), nullptr, beta1, beta2, eps, grad_scale, (hipStream_t)stream);
+}
+
+int tensair_adamw_step_at(tensair_adamw *h, const double *lr, const int64_t *step, double beta1, double beta2, double eps, const float *grad_scale, void *stream)
+{
+    if (int rc = check_step(h, beta1, beta2, eps, grad_scale)) return rc;
+    if (!lr || !step) return tn_fail(TENSAIR_EINVAL, "NULL pointer argument");
+    if (((uintptr_t)lr | (uintptr_t)step) & 7) return tn_fail(TENSAIR_EINVAL, "lr and step must be 8-byte aligned");
     hipStream_t st = (hipStream_t)stream;
-    launch_adamw<float, float>(h, a, 0, st);
-    launch_adamw<float, bf16_t>(h, a, 1, st);
-    launch_adamw<bf16_t, float>(h, a, 2, st);
-    launch_adamw<bf16_t, bf16_t>(h, a, 3, st);
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? TENSAIR_OK : tn_fail(TENSAIR_EHIP, "adamw_step: %s", hipGetErrorString(e));
+    hipLaunchKernelGGL(k_adamw_live, dim3(1), dim3(1), 0, st, h->live, lr, (const i64 *)step, beta1, beta2);
+    return adamw_step(h, AdamwLive{}, h->live, beta1, beta2, eps, grad_scale, st);
 }
 
 int tensair_adamw_destroy(tensair_adamw *h)
