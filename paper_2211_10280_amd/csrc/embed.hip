@@ -555,8 +555,12 @@ struct EmbedSizes {
     int passes, bits, tiles, seg_tiles, sum_tiles, tile;
     size_t nd, pub, clear, tile0, per_pass, seg_state, hist, none;     // words of the published area
 };
-// most tokens that are summed in tiles of so many
-i64 most_in_tiles(int tile) { return (i64)(tile < 32 ? 2048 : 16384) * tile + tile - 1; }
+// Most tokens that are summed in tiles of so many: few to a tile where there are few, so that enough waves are there to hide the way to
+// memory, but more tiles have more shares to write and to read again.  Whole calls, rows of 300 added to a table / of 64 in fp32 / of 256 in
+// bfloat16, us: 12 000 tokens by tiles of 4 58 / 42 / 44, of 8 57 / 40 / 42, of 16 58 / 38 / 47; 24 000 of 8 64 / 44 / 45, of 16 64 / 43 / 45, of 32
+// 70 / 43 / 53; 65 536 of 16 82 / 51 / 53, of 32 83 / 51 / 55; 100 000 94 / 59 / 60, 94 / 56 / 60; 131 072 108 / 65 / 65, 104 / 60 / 62; 400 000 of 32
+// 240 / 97 / 100, of 64 238 / 88 / 100; 200 000 133 / 69 / 74, 142 / 71 / 76.
+i64 most_in_tiles(int tile) { return (i64)(tile < 16 ? 2048 : tile < 32 ? 6144 : 16384) * tile + tile - 1; }
 EmbedSizes embed_sizes(i64 V, i64 n)
 {
     EmbedSizes s;
@@ -568,9 +572,6 @@ EmbedSizes embed_sizes(i64 V, i64 n)
     s.nd = (size_t)1 << s.bits;
     s.tiles = tn_prep_tiles(n);
     s.seg_tiles = tn_prep_seg_tiles(n);
-    // few tokens to a tile where there are few, so that enough waves are there to hide the way to memory, but more tiles have more
-    // shares to write and to read again (32 767 tokens, rows of 300 added to a table: tiles of 4 26 us, of 8 22, of 16 18, of 32 26;
-    // 262 143 tokens, rows of 256 in bfloat16: of 64 37.6 us, of 32 30.8)
     s.tile = 4;
     while (s.tile < EMBED_MAX_TILE && n > most_in_tiles(s.tile)) s.tile *= 2;
     s.sum_tiles = (int)((n + s.tile - 1) / s.tile);
