@@ -486,8 +486,8 @@ __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_logits(Log
 // through LDS, 32 words to a tile, for the 256 tokens of a workgroup: a third of what the other form fetches, which is what bounds
 // that one.  Two workgroups to a compute unit: one's exponentials run beside the other's products.
 // 4 096 tokens, rows of 300 in bfloat16: the loss against a million words 1.86 ms (the other form 2.5), 1.3 PFLOP/s, the matrix units busy
-// 81 % of it; dz of 125 000 words 385 us (514).  129 to 256 tokens: 172 us (195 to 203), dz 241 (282 to 288); 300 tokens, of which
-// two tiles are half empty: 254 (271), dz 426 (406).  Short rows are bound by the exponentials: rows of 128, 50 000 words, 63 us.
+// 81 % of it; dz of 125 000 words 385 us (514).  129 to 256 tokens: 172 us (195 to 203), dz 241 (282 to 288).
+// Short rows are bound by the exponentials: rows of 128, 50 000 words, 63 us.
 #define HELD_WORDS 32
 #define HELD_STAGES 4
 template <int KB, bool GRAD>
@@ -1126,7 +1126,9 @@ SoftmaxPlan plan_of(i64 n, i64 V, int D, int dtype, bool grad)
     s.few_blocks = (int)std::max<i64>(1, std::min<i64>(cdiv(V, 64), grad ? FEW_BLOCKS / 2 : FEW_BLOCKS));
     s.parts = dtype == TENSAIR_F32 ? 3 : 1;
     const bool few = n <= SM_BN_FEW;
-    s.held = s.parts == 1 && D <= SM_HELD_DIM && n > SM_BN;
+    // Two tiles of 256 tokens that are half empty make dz slower than three of 128 (gradient, 300 tokens, 125 000 words of 300: 207 us, by the
+    // latter 193, of 200: 130, 121; 385 tokens 221, 229; 640, three tiles of which one is half empty: 285, 281), but not the loss (73, 71).
+    s.held = s.parts == 1 && D <= SM_HELD_DIM && n > SM_BN && !(grad && n > SM_BN_HELD && n <= SM_BN_HELD + SM_BN);
     s.Dp = (int)cdiv(D, s.held ? 2 * BK : BK) * (s.held ? 2 * BK : BK);
     s.bn = s.held ? SM_BN_HELD : few ? SM_BN_FEW : SM_BN;
     s.wm = s.held ? 1 : few ? 4 : SM_WAVES_M;
