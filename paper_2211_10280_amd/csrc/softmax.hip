@@ -266,6 +266,27 @@ __device__ __forceinline__ v4u join_halves(u32 x0, u32 x1, u32 y0, u32 y1)
     return v4u{(u32)p[0], (u32)q[0], (u32)p[1], (u32)q[1]};
 }
 
+// A token's running sum over many words, of powers of two relative to `top`, with what its roundings have cut off so far: the words may
+// be the whole vocabulary, and added to the plain sum its many small ones would be lost one by one beside a large one.  `top` is the
+// largest logit so far or the whole number above it, so that a sum is brought to another one without a rounding.
+struct Running {
+    float top, sum, low;
+    __device__ __forceinline__ float ref() const { return top == -INFINITY ? 0.f : top; }
+    __device__ __forceinline__ void raise(float logit)
+    {
+        const float was = top;
+        top = fmaxf(ceilf(logit), was);
+        const float f = __builtin_amdgcn_exp2f(was - ref());
+        sum *= f;
+        low *= f;
+    }
+    __device__ __forceinline__ void add(float x)
+    {
+        const float more = x - low, was = sum;
+        sum = was + more;
+        low = (sum - was) - more;
+    }
+};
 // a maximum and a sum of powers of two relative to it, joined by another pair
 __device__ __forceinline__ void join_sums(float &top, float &sum, float t, float s)
 {
@@ -323,12 +344,6 @@ __device__ __forceinline__ void mend_logits(f32x16 (&acc)[TM][TN], const LogitsA
             }
         }
 }
-// A token's running sum over a strip of words, of powers of two relative to `top`, with what its roundings have cut off so far: a
-// strip is up to the whole vocabulary, and added to the plain sum its many small words would be lost one by one beside a large one.
-// `top` is the largest logit so far or the whole number above it, so that a sum is brought to another one without a rounding.
-struct Running {
-    float top, sum, low;
-};
 // into the running sums; the label's logit kept
 template <int TM, int TN>
 __device__ __forceinline__ void add_words(f32x16 (&acc)[TM][TN], const LogitsArgs &a, i64 w0, i64 tok, const int (&label)[TN], Running (&run)[TN])
@@ -349,16 +364,14 @@ __device__ __forceinline__ void add_words(f32x16 (&acc)[TM][TN], const LogitsArg
             for (int r = 0; r < 16; ++r) best = fmaxf(best, acc[i][j][r]);
         }
         Running &x = run[j];
-        const float now = fmaxf(ceilf(best * a.c), x.top), ref = now == -INFINITY ? 0.f : now, f = __builtin_amdgcn_exp2f(x.top - ref);
+        x.raise(best * a.c);
+        const float ref = x.ref();
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], a.c, -ref));
-        const float before = x.sum * f, more = s - x.low * f;
-        x.top = now;
-        x.sum = before + more;
-        x.low = (x.sum - before) - more;
+        x.add(s);
     }
 }
 // dz, to the blocks of columns from `block` on
@@ -599,14 +612,18 @@ __global__ void __launch_bounds__(1024) k_loss(LossArgs a)
     __shared__ float2 other[16][WAVE];
     const int lane = lane_id(), wave = (int)(threadIdx.x >> 6);
     const i64 i = (i64)blockIdx.x * WAVE + lane;
-    float top = -INFINITY, sum = 0.f;
+    Running run = {-INFINITY, 0.f, 0.f};
     for (int s = wave; s < a.slots; s += 16 * 8) {
         float2 v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = s + 16 * k < a.slots ? a.part[(i64)(s + 16 * k) * a.Np + i] : make_float2(-INFINITY, 0.f);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) join_sums(top, sum, v[k].x, v[k].y);
+        for (int k = 0; k < 8; ++k) {
+            run.raise(v[k].x);
+            run.add(v[k].y * __builtin_amdgcn_exp2f(v[k].x - run.ref()));
+        }
     }
+    float top = run.top, sum = run.sum;
     other[wave][lane] = make_float2(top, sum);
     __syncthreads();
     if (wave > 0 || i >= a.n) return;
@@ -673,7 +690,7 @@ __global__ void __launch_bounds__(BLOCK) k_few(FewArgs a)
         d[t] = GRAD && label[t] >= 0 ? a.d_loss[t] : 0.f;
     }
     if (blockIdx.x == 0 && (int)threadIdx.x < a.n && a.status && a.labels.bad(threadIdx.x)) atomicOr(a.status, ST_BAD_ID);
-    float top = -INFINITY, sum = 0.f;                         // of the token of this lane's number
+    Running run = {-INFINITY, 0.f, 0.f};                      // of the token of this lane's number
     float4 dh[GRAD ? NT : 1][ITERS];
 #pragma unroll
     for (int t = 0; t < (GRAD ? NT : 1); ++t) zero_row<ITERS>(dh[t]);
@@ -726,11 +743,11 @@ __global__ void __launch_bounds__(BLOCK) k_few(FewArgs a)
             float best = mine[0];
 #pragma unroll
             for (int r = 1; r < ROWS; ++r) best = fmaxf(best, mine[r]);
-            const float now = fmaxf(best, top), ref = now == -INFINITY ? 0.f : now;
-            sum *= __builtin_amdgcn_exp2f(top - ref);
+            run.raise(best);
+            float s = 0.f;
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) sum += __builtin_amdgcn_exp2f(mine[r] - ref);
-            top = now;
+            for (int r = 0; r < ROWS; ++r) s += __builtin_amdgcn_exp2f(mine[r] - run.ref());
+            run.add(s);
         } else {
 #pragma unroll
             for (int r = 0; r < ROWS; ++r) {
@@ -762,6 +779,7 @@ __global__ void __launch_bounds__(BLOCK) k_few(FewArgs a)
         }
     }
     if constexpr (!GRAD) {
+        float top = run.top, sum = run.sum;
         // the lanes of a token: one of every group
 #pragma unroll
         for (int o = G; o < WAVE; o <<= 1) join_sums(top, sum, __shfl_xor(top, o, WAVE), __shfl_xor(sum, o, WAVE));

@@ -47,6 +47,21 @@ def test_small_words_beside_a_large_one(n, D, dtype, at):
     assert float((loss.double() - value).abs().max()) <= bound
 
 
+@pytest.mark.parametrize("n,V,a", [(1, 4_000_000, 18.0), (1, 64_000_000, 18.0), (8, 64_000_000, 18.0), (9, 4_000_000, 24.0), (60, 64_000_000, 24.0), (100, 4_000_000, 24.0),
+                                   (300, 4_000_000, 24.0), (300, 4_000_000, 22.0)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sums_of_many_strips_beside_a_large_word(n, V, a, dtype):
+    """Few tokens: the vocabulary is cut into thousands of strips, or walked through by single lanes, and what each has is small beside the strip
+    that has the large word."""
+    h, w = torch.zeros((n, 8), dtype=DT[dtype], device="cuda"), torch.zeros((V, 8), dtype=DT[dtype], device="cuda")
+    h[:, 3] = 1.0
+    w[V // 3, 3] = a
+    _, lse = _loss(h, w, torch.zeros(n, dtype=torch.int32, device="cuda"))
+    want = a + math.log1p((V - 1) * math.exp(-a))
+    # 18 to 26 joins that lose at most half a unit each, the result to a few of its own
+    assert float((lse.double() - want).abs().max()) <= 32 * U32 + 3 * U32 * want
+
+
 # ---------------------------------------------------------------- words masked by infinities and the largest numbers
 def _grad(h, w, labels, lse, d, scale=1.0, ignore=-1):
     n, (V, D) = labels.numel(), w.shape
