@@ -334,7 +334,7 @@ __device__ __forceinline__ void mend_logits(f32x16 (&acc)[TM][TN], const LogitsA
                 const int at = __ffs((int)bad) - 1;
                 const float *w = a.table + (word0 + 8 * (at / 4) + at % 4) * a.table_stride, *h = a.hidden + token * a.hidden_stride;
                 double z = 0.0;
-                for (int k = 0; k < a.D; k += 4) {
+                for (int k = 0; k < a.D && z == z; k += 4) {
                     const float4 x = ld4(w + k), y = ld4(h + k);
                     z = fma((double)x.x, (double)y.x, fma((double)x.y, (double)y.y, fma((double)x.z, (double)y.z, fma((double)x.w, (double)y.w, z))));
                 }

@@ -112,3 +112,27 @@ def test_softmax_words_masked_in_one_column(n, D, dtype, how):
     # the loss of a masked word is infinite
     labels[n - 1] = 3
     assert float(_loss(h, w, labels, scale)[0][n - 1]) == math.inf
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [5, 60, 200])
+def test_numbers_that_are_none_stay_where_they_belong(n, dtype):
+    """NaN in a token's row, in its first or its last column: its own loss and its row of the gradient, no other token's.  In a word's row: everything."""
+    V, D = 600, 40
+    g = torch.Generator(device="cuda").manual_seed(n)
+    h, w = ((torch.randn((k, D), generator=g, device="cuda") * 0.3).to(DT[dtype]) for k in (n, V))
+    labels, d = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32), torch.rand(n, generator=g, device="cuda")
+    loss, lse = _loss(h, w, labels)
+    dh, _ = _grad(h, w, labels, lse, d)
+    for col in (0, D - 1):
+        bad = h.clone()
+        bad[n // 2, col] = float("nan")
+        others = torch.arange(n, device="cuda") != n // 2
+        got, got_lse = _loss(bad, w, labels)
+        assert torch.equal(got[others], loss[others]) and bool(got[n // 2].isnan()) and bool(got_lse[n // 2].isnan())
+        gh, gw = _grad(bad, w, labels, got_lse, d)
+        assert torch.equal(gh[others], dh[others]) and bool(gh[n // 2].isnan().all()) and bool(gw.isnan().all())
+        worse = w.clone()
+        worse[V // 2, col] = float("nan")
+        got, got_lse = _loss(h, worse, labels)
+        assert bool(got.isnan().all()) and bool(got_lse.isnan().all())
