@@ -17,7 +17,7 @@
  * Beyond the paper, for models that use such a table as their input and output layer (no model handle):
  *   scaled lookup and its gradient by sorted tokens  -> tensair_embed, tensair_embed_grad, tensair_embed_grad_dense
  *   softmax loss over the whole vocabulary, gradient -> tensair_softmax_loss, tensair_softmax_grad
- *   AdamW over many tensors at once                  -> tensair_adamw_init, tensair_adamw_step
+ *   AdamW over many tensors at once                  -> tensair_adamw_init, tensair_adamw_step, tensair_adamw_step_at
  *
  * Conventions for every call
  *   - Plain C ABI.  Pointers marked DEVICE point to GPU memory owned by the caller;
@@ -401,13 +401,18 @@ int tensair_embed_grad_dense(const int32_t *ids, int64_t n, const void *d_out, i
 
 /* Softmax cross entropy against every row of a table (what negative sampling stands in for), with
  *   z[i][v] = scale * <hidden[i], table[v]>,  lse[i] = log sum_v exp z[i][v],  loss[i] = lse[i] - z[i][labels[i]].
- * scale: finite, not 0.  The logits are never kept.  A label equal to ignore_label gives loss 0; so does one outside [0, vocab), which also sets the
- * status bit.  hidden and table have the same type; loss and lse: DEVICE fp32 [n].
- * fp32 inputs are multiplied with the precision of fp32; n <= TENSAIR_MAX_TOKENS, vocab <= TENSAIR_MAX_VOCAB.
+ * scale: finite, not 0.  The logits are never kept; the largest of a row has to be below 2^30 in magnitude (an
+ * fp32 lse tells nothing beyond).  A label equal to ignore_label gives loss 0; so does one outside [0, vocab), which
+ * also sets the status bit.  hidden and table have the same type; loss and lse: DEVICE fp32 [n].
+ * fp32 inputs are multiplied with the precision of fp32 (a logit whose parts overflow is made in 64 bits);
+ * n <= TENSAIR_MAX_TOKENS, vocab <= TENSAIR_MAX_VOCAB.
  * tensair_softmax_grad: for the gradient d_loss (DEVICE fp32 [n]) of the losses, with p = exp(z - lse),
  *   dz[i][v] = d_loss[i] * (p[i][v] - (v == labels[i])) for rows that have a loss, 0 for the others,
  *   d_hidden[i] = scale * sum_v dz[i][v] table[v],   d_table[v] = scale * sum_i dz[i][v] hidden[i],
- * both of the inputs' type (either may be NULL: not wanted).  lse: what tensair_softmax_loss gave for the same inputs. */
+ * both of the inputs' type (either may be NULL: not wanted).  lse: what tensair_softmax_loss gave for the same inputs.  dz is rounded
+ * before it is multiplied: to bfloat16 (8 bits) for bfloat16 inputs, to 24 bits for fp32.
+ * A row without a loss has no share in a gradient whatever it holds and whatever the words' rows hold.  A word whose logit is minus
+ * infinity (a mask in one column of the table) has no share in a sum and a gradient of zero; d_hidden of that column is then 0 * infinity. */
 #define TENSAIR_MAX_TOKENS 2097152 /* 2^21 */
 /* Bytes of workspace of the loss or, with_grad != 0, of both calls, of n tokens or fewer (0: an argument is out of range). */
 size_t tensair_softmax_workspace_bytes(int64_t n, int64_t vocab, int32_t dim, int32_t dtype, int32_t with_grad);

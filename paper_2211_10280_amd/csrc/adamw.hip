@@ -159,7 +159,7 @@ __device__ __forceinline__ void adamw1(float &p, float g, float &m, float &v, fl
 }
 
 // One pass over parameters, gradients and states, which memory bounds: 600 M fp32 parameters with bfloat16 gradients and 8-bit
-// states 1.66 ms (8.4 GB, 5.1 TB/s, the rate of a large copy), 200 M with fp32 states 0.96 ms (5.8 TB/s), 96 tensors of 7 M in all 42 us.
+// states 1.67 ms (8.4 GB, 5.0 TB/s, the rate of a large copy), 200 M with fp32 states 0.96 ms (5.8 TB/s), 96 tensors of 7 M in all 43 us.
 // STREAM: around the caches, where the tensors do not fit the memory-side cache
 template <typename TP, typename TG, bool EIGHT, bool STREAM>
 __global__ void __launch_bounds__(BLOCK) k_adamw(AdamwStep a, u32 first_chunk)

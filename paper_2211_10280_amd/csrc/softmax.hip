@@ -2,7 +2,9 @@
 //   lse_i = log sum_v exp z_iv,   loss_i = lse_i - z_i,label,   dz_iv = d_i (exp(z_iv - lse_i) - [v = label_i]),
 //   d_hidden = scale * dz table,   d_table = scale * dz^T hidden.
 // The logits are never kept: the loss makes a pass over the words with a running maximum and sum per token; the gradient makes
-// the logits once more, a range of words at a time, and keeps dz of that range in bfloat16 for the two products.
+// the logits once more, a range of words at a time, and keeps dz of that range for the two products, in the inputs' type: a bfloat16
+// (16 384 tokens, 10 000 words of 512: the gradients are off by 0.00167 of their size, by the rounding of the outputs alone 0.00165; a second
+// part of dz would double what is written and read of it and the products) or three of them.
 // All products are tiles of matrix instructions in bfloat16 with fp32 sums.  fp32 inputs are three bfloat16 parts each (24 bits
 // together), and of the nine products of parts the six that matter at 2^-24 are summed, the smallest first.
 #include <hip/hip_runtime.h>
@@ -309,7 +311,8 @@ __device__ __forceinline__ void no_words(f32x16 (&acc)[TM][TN], i64 w0, i64 V)
 }
 // Products of parts that are NaN or infinite where the product of the numbers need not be: those that overflow beside one of the other
 // sign (a word masked by the lowest number, times several hundred), an infinity times a number below the smallest bfloat16.  Such logits
-// are made once more, from the numbers in 64 bits, a lane each; minus infinity is right as it is.
+// are made once more, from the numbers in 64 bits, a lane each; minus infinity is right as it is.  (4 096 tokens, 100 000 words of 300, a
+// hundredth of the words masked by the lowest number times several hundred: the loss 3.4 ms instead of 1.5, half of them 36.)
 template <int TM, int TN>
 __device__ __forceinline__ void mend_logits(f32x16 (&acc)[TM][TN], const LogitsArgs &a, i64 w0, i64 tok)
 {
@@ -430,8 +433,9 @@ __device__ __forceinline__ void put_sums(const LogitsArgs &a, int slot, i64 tok,
 
 // GRAD false: the running maximum and sum of every token over a strip of words; true: dz of the strip, in PARTS bfloat16 parts.
 // A strip's tiles follow one another without a pause: the next tile's first step is in flight while this one's logits are used.
-// What bounds it is what comes to LDS (87 operations a byte): 10 000 words, 16 384 tokens, rows of 512 in bfloat16 185 us, 0.9 PFLOP/s; fp32,
-// 50 000 words, 1 024 tokens, rows of 128 85 us, 0.93 PFLOP/s of its bfloat16 products.
+// What bounds it is what comes to LDS (a tile's products are 85 operations a byte of its operands, of either form): 10 000 words, 16 384
+// tokens, rows of 512 in bfloat16 155 to 190 us, 0.9 to 1.1 PFLOP/s; fp32, 50 000 words, 1 024 tokens, rows of 128 77 to 91 us, 0.86 to 1.0
+// PFLOP/s of its bfloat16 products.
 template <int TM, int TN, int WM, int WN, int STAGES, bool GRAD, int PARTS>
 __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_logits(LogitsArgs a)
 {
@@ -498,9 +502,9 @@ __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_logits(Log
 // The same for rows of up to 32 KB elements: a wave holds 64 tokens' whole rows in registers, as fragments, and the words' rows alone come
 // through LDS, 32 words to a tile, for the 256 tokens of a workgroup: a third of what the other form fetches, which is what bounds
 // that one.  Two workgroups to a compute unit: one's exponentials run beside the other's products.
-// 4 096 tokens, rows of 300 in bfloat16: the loss against a million words 1.86 ms (the other form 2.5), 1.3 PFLOP/s, the matrix units busy
-// 81 % of it; dz of 125 000 words 385 us (514).  129 to 256 tokens: 172 us (195 to 203), dz 241 (282 to 288).
-// Short rows are bound by the exponentials: rows of 128, 50 000 words, 63 us.
+// 4 096 tokens, rows of 300 in bfloat16: the loss against a million words 1.9 to 2.1 ms (the other form 2.5), 1.2 to 1.3 PFLOP/s, the matrix units
+// busy 79 % of it; dz of 125 000 words 385 to 400 us (514).  129 to 256 tokens: 172 us (195 to 203), dz 241 (282 to 288).
+// Short rows are bound by the exponentials: rows of 128, 50 000 words, 65 us.
 #define HELD_WORDS 32
 #define HELD_STAGES 4
 template <int KB, bool GRAD>
