@@ -410,7 +410,8 @@ int tensair_embed_grad_dense(const int32_t *ids, int64_t n, const void *d_out, i
  *   dz[i][v] = d_loss[i] * (p[i][v] - (v == labels[i])) for rows that have a loss, 0 for the others,
  *   d_hidden[i] = scale * sum_v dz[i][v] table[v],   d_table[v] = scale * sum_i dz[i][v] hidden[i],
  * both of the inputs' type (either may be NULL: not wanted).  lse: what tensair_softmax_loss gave for the same inputs.  dz is rounded
- * before it is multiplied: to bfloat16 (8 bits) for bfloat16 inputs, to 24 bits for fp32.
+ * before it is multiplied: for fp32 inputs to 24 bits, for bfloat16 ones to bfloat16 (8 bits), the significant digits of the
+ * first d_loss of a row that has a loss apart; d_hidden gets what that cuts off the labels' elements.
  * A row without a loss has no share in a gradient whatever it holds and whatever the words' rows hold.  A word whose logit is minus
  * infinity (a mask in one column of the table) has no share in a sum and a gradient of zero; d_hidden of that column is then 0 * infinity. */
 #define TENSAIR_MAX_TOKENS 2097152 /* 2^21 */

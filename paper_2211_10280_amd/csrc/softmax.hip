@@ -3,8 +3,13 @@
 //   d_hidden = scale * dz table,   d_table = scale * dz^T hidden.
 // The logits are never kept: the loss makes a pass over the words with a running maximum and sum per token; the gradient makes
 // the logits once more, a range of words at a time, and keeps dz of that range for the two products, in the inputs' type: a bfloat16
-// (16 384 tokens, 10 000 words of 512: the gradients are off by 0.00167 of their size, by the rounding of the outputs alone 0.00165; a second
-// part of dz would double what is written and read of it and the products) or three of them.
+// or three of them.
+// dz in one bfloat16: a second part would double what is written and read of it and the products.  Most of its elements are near nothing,
+// and their roundings are lost in the sums; a label's is near d_i, and its rounding would be as large in a gradient as that of the output (0.00165 of
+// its size).  So what the tokens have in common of d_i is taken out of dz, but for a power of two (the sums are no larger for it): a label's
+// element is then that of p - 1, which is nearly exact for the many tokens with a small p.  And d_hidden, which has a token's elements in one row, gets what the rounding cut off in its last step.
+// (26 tokens, 2 439 words of 148: d_hidden and d_table off from 64 bits by 0.00168 and 0.00171 of their size, without either 0.0034; 16 384
+// tokens, 10 000 words of 512 0.00167 both; a call of 4 096 tokens and a million words of 300 0.5 % longer.)
 // All products are tiles of matrix instructions in bfloat16 with fp32 sums.  fp32 inputs are three bfloat16 parts each (24 bits
 // together), and of the nine products of parts the six that matter at 2^-24 are summed, the smallest first.
 #include <hip/hip_runtime.h>
@@ -249,6 +254,8 @@ struct LogitsArgs {
     float sign;
     // gradient
     const float *lse2, *d;     // [Np]
+    const float *unit;         // of dz (NULL: 1)
+    float *rest;               // [Np] what the rounding of the label's element cut off
     bf16_t *dz;                // an Operand: rows are tokens, columns words
     i64 dz_plane;
 };
@@ -395,8 +402,17 @@ __device__ __forceinline__ void put_dz(f32x16 (&acc)[TM][TN], const LogitsArgs &
             for (int r = 0; r < 16; ++r) g[r] = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], a.c, -l2[j]));
             if (__ballot((u32)lw < 32u)) {
                 const int at = lw - 4 * (lane >> 5);
+                float own = 0.f;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) g[r] -= at == 8 * (r / 4) + r % 4 ? 1.0f : 0.0f;
+                for (int r = 0; r < 16; ++r) {
+                    const bool is = at == 8 * (r / 4) + r % 4;
+                    g[r] -= is ? 1.0f : 0.0f;
+                    own = is ? g[r] : own;
+                }
+                if (PARTS == 1 && (u32)lw < 32u && (lw >> 2 & 1) == lane >> 5) {       // the lane that has it
+                    own *= d[j];
+                    a.rest[tok + 32 * j + (lane & 31)] = own - __uint_as_float(pack2(own, 0.f) << 16);
+                }
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) g[r] *= d[j];
@@ -457,7 +473,7 @@ __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_logits(Log
         run[j] = Running{-INFINITY, 0.f, 0.f};
         if (GRAD) {
             l2[j] = a.lse2[tok];
-            d[j] = a.d[tok];
+            d[j] = a.unit ? a.d[tok] / *a.unit : a.d[tok];
         }
     }
     i64 word = a.word0 + (i64)t0 * P::BM;
@@ -531,7 +547,7 @@ __global__ void __launch_bounds__(256, 2) k_logits_held(LogitsArgs a)
         run[j] = Running{-INFINITY, 0.f, 0.f};
         if (GRAD) {
             l2[j] = a.lse2[tok];
-            d[j] = a.d[tok];
+            d[j] = a.unit ? a.d[tok] / *a.unit : a.d[tok];
         }
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) h[j][kk] = *(const hw_bf16x8 *)a.h.at(0, tok, 16 * kk + 8 * (lane >> 5));
@@ -868,6 +884,7 @@ struct ProductArgs {
     i64 out_stride;
     int dtype;
     float scale;
+    const float *unit;         // of dz (NULL: 1), for what is written as the output
 };
 template <int TM, int TN, int WM, int WN, int STAGES, int PARTS, bool BT>
 __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_product(ProductArgs a)
@@ -920,6 +937,7 @@ __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_product(Pr
         advance();
         cur = cur == STAGES - 1 ? 0 : cur + 1;
     }
+    const float scale = a.unit ? a.scale * *a.unit : a.scale;
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
         const i64 n = n0 + (wn * TN + j) * 32 + (lane & 31);
@@ -934,7 +952,7 @@ __global__ void __launch_bounds__(64 * WM * WN, PARTS == 1 ? 2 : 1) k_product(Pr
                 if (a.slots) {
                     st4(a.slots + ((i64)split * a.N + n) * a.M + m, v);
                 } else {
-                    v = make_float4(v.x * a.scale, v.y * a.scale, v.z * a.scale, v.w * a.scale);
+                    v = make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale);
                     if (a.dtype == TENSAIR_F32) st4((float *)a.out + n * a.out_stride + m, v);
                     else st4((bf16_t *)a.out + n * a.out_stride + m, v);
                 }
@@ -953,12 +971,23 @@ struct JoinArgs {
     void *out;
     int dtype;
     float scale;
+    const float *unit;         // of dz (NULL: 1)
+    const float *rest;         // what was cut off the labels' elements (NULL: nothing), to be multiplied by the words' rows
+    const bf16_t *table;
+    i64 table_stride;
 };
 __device__ __forceinline__ void put_joined(const JoinArgs &a, i64 c, float4 v)
 {
-    const i64 row = c / a.C4, at = row * a.stride + 4 * (c - row * a.C4);
-    v = make_float4(v.x * a.scale, v.y * a.scale, v.z * a.scale, v.w * a.scale);
-    if (a.labels.p && a.labels.at(row) < 0) v = make_float4(0.f, 0.f, 0.f, 0.f);
+    const i64 row = c / a.C4, col = 4 * (c - row * a.C4), at = row * a.stride + col;
+    const int label = a.labels.p ? a.labels.at(row) : 0;
+    if (a.rest && label >= 0) {
+        const float x = a.rest[row];
+        const float4 w = ld4(a.table + label * a.table_stride + col);
+        v = make_float4(fmaf(x, w.x, v.x), fmaf(x, w.y, v.y), fmaf(x, w.z, v.z), fmaf(x, w.w, v.w));
+    }
+    const float scale = a.unit ? a.scale * *a.unit : a.scale;
+    v = make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale);
+    if (label < 0) v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (a.dtype == TENSAIR_F32) st4((float *)a.out + at, v);
     else st4((bf16_t *)a.out + at, v);
 }
@@ -1022,7 +1051,7 @@ struct TokenArgs {
     const float *lse, *d_loss; // NULL: for the loss
     i64 n, Np;
     int *label, *status;
-    float *lse2, *d;
+    float *lse2, *d, *unit;    // unit: NULL where dz is in units of 1
 };
 __device__ __forceinline__ void tokens(const TokenArgs &a, i64 i)
 {
@@ -1034,6 +1063,26 @@ __device__ __forceinline__ void tokens(const TokenArgs &a, i64 i)
         a.lse2[i] = y >= 0 ? a.lse[i] * LOG2E : 0.f;
         a.d[i] = y >= 0 ? a.d_loss[i] : 0.f;
     }
+}
+// The unit of dz, by a workgroup: the significant digits, as a number from 1 to 2, of the first token's d_i that has one, as a rule the same for all
+// of them; 1 where it is none or not among the first of a great many tokens.
+#define SM_UNIT_TOKENS 16384
+__device__ __forceinline__ void find_unit(const TokenArgs &a)
+{
+    __shared__ int first;
+    if (threadIdx.x == 0) first = SM_UNIT_TOKENS;
+    __syncthreads();
+    for (int base = 0; base < SM_UNIT_TOKENS && base < a.n; base += BLOCK) {
+        const int i = base + (int)threadIdx.x;
+        if (i < a.n && a.labels.at(i) >= 0 && a.d_loss[i] != 0.f) atomicMin(&first, i);
+        __syncthreads();
+        const bool found = first < SM_UNIT_TOKENS;
+        __syncthreads();
+        if (found) break;
+    }
+    if (threadIdx.x > 0) return;
+    const float d = first < SM_UNIT_TOKENS ? fabsf(a.d_loss[first]) : 1.f;
+    *a.unit = d >= 0x1p-126f && d < INFINITY ? __uint_as_float((__float_as_uint(d) & 0x007FFFFFu) | 0x3F800000u) : 1.f;
 }
 // workgroup `first` of `blocks`: a thread takes 8 elements, a wave 16 rows of a block of columns
 template <typename T>
@@ -1082,14 +1131,16 @@ struct LayOutArgs {
     TokenArgs tokens;
     PackArgs h, w;
     int token_blocks, h_blocks, w_blocks;
+    int unit_block;            // 1: a workgroup for the unit of dz
 };
 template <typename T>
 __global__ void __launch_bounds__(BLOCK) k_lay_out(LayOutArgs a)
 {
     const int b = (int)blockIdx.x;
     if (b < a.token_blocks) tokens(a.tokens, (i64)b * BLOCK + threadIdx.x);
-    else if (b < a.token_blocks + a.h_blocks) parts<T>(a.h, b - a.token_blocks, a.h_blocks);
-    else parts<T>(a.w, b - a.token_blocks - a.h_blocks, a.w_blocks);
+    else if (b < a.token_blocks + a.unit_block) find_unit(a.tokens);
+    else if (b < a.token_blocks + a.unit_block + a.h_blocks) parts<T>(a.h, b - a.token_blocks - a.unit_block, a.h_blocks);
+    else parts<T>(a.w, b - a.token_blocks - a.unit_block - a.h_blocks, a.w_blocks);
 }
 __global__ void __launch_bounds__(BLOCK) k_zero_rows(void *out, int dtype, i64 rows, i64 stride, int C4)
 {
@@ -1202,7 +1253,7 @@ SoftmaxPlan plan_of(i64 n, i64 V, int D, int dtype, bool grad)
 
 struct SoftmaxBuffers {
     int *label;
-    float *lse2, *d, *picked, *h_slots, *t_slots;
+    float *lse2, *d, *unit, *rest, *picked, *h_slots, *t_slots;
     bf16_t *h, *w, *dz;
     float2 *part;
 };
@@ -1235,6 +1286,10 @@ size_t softmax_carve(const SoftmaxPlan &s, i64 n, int D, bool grad, char *base, 
     } else {
         x.lse2 = (float *)take(4 * (size_t)s.Np);
         x.d = (float *)take(4 * (size_t)s.Np);
+        if (s.parts == 1) {
+            x.unit = (float *)take(4);
+            x.rest = (float *)take(4 * (size_t)s.Np);
+        }
         x.dz = (bf16_t *)take(2 * (size_t)s.Np * s.range_tiles * SM_BM * s.parts);
         x.h_slots = (float *)take(4 * (size_t)s.h_splits * (cdiv(n, SM_CLASS) * SM_CLASS) * D);
         if (s.t_most > 1) x.t_slots = (float *)take(4 * (size_t)s.t_most * s.range_tiles * SM_BM * D);
@@ -1290,10 +1345,10 @@ LogitsArgs lay_out_range(const SoftmaxPlan &s, const SoftmaxBuffers &b, const Ra
 {
     const char *src = (const char *)table + (size_t)r.word0 * table_stride * (dtype == TENSAIR_F32 ? 4 : 2);
     x.w = lay_out(s, src, table_stride, r.words, r.rows, D, Labels{}, 1.f, b.w, &x.w_blocks);
-    const dim3 grid((unsigned)(x.token_blocks + x.h_blocks + x.w_blocks)), blk(BLOCK);
+    const dim3 grid((unsigned)(x.token_blocks + x.unit_block + x.h_blocks + x.w_blocks)), blk(BLOCK);
     if (dtype == TENSAIR_F32) hipLaunchKernelGGL(k_lay_out<float>, grid, blk, 0, st, x);
     else hipLaunchKernelGGL(k_lay_out<bf16_t>, grid, blk, 0, st, x);
-    x.token_blocks = x.h_blocks = 0;
+    x.token_blocks = x.h_blocks = x.unit_block = 0;
     LogitsArgs a;
     memset(&a, 0, sizeof(a));
     a.w = Operand{b.w, r.rows, r.rows * s.Dp};
@@ -1319,6 +1374,8 @@ LogitsArgs lay_out_range(const SoftmaxPlan &s, const SoftmaxBuffers &b, const Ra
     a.picked = b.picked;
     a.lse2 = b.lse2;
     a.d = b.d;
+    a.unit = b.unit;
+    a.rest = b.rest;
     a.dz = b.dz;
     a.dz_plane = s.Np * s.range_tiles * SM_BM;
     return a;
@@ -1388,9 +1445,10 @@ void launch_product(const SoftmaxPlan &s, const ProductArgs &a, hipStream_t st)
     else if (s.tm == 4) hipLaunchKernelGGL((k_product<4, 2, 2, 2, 2, 1, BT>), grid, blk, 0, st, a);
     else hipLaunchKernelGGL((k_product<5, 2, 2, 2, 2, 1, BT>), grid, blk, 0, st, a);
 }
-void launch_join(const float *slots, int n_slots, i64 rows, i64 stride, int D, Labels labels, void *out, int dtype, float scale, hipStream_t st)
+void launch_join(const float *slots, int n_slots, i64 rows, i64 stride, int D, Labels labels, void *out, int dtype, float scale, const float *unit,
+                 const float *rest, const void *table, i64 table_stride, hipStream_t st)
 {
-    JoinArgs j = {slots, n_slots, rows, stride, D / 4, labels, out, dtype, scale};
+    JoinArgs j = {slots, n_slots, rows, stride, D / 4, labels, out, dtype, scale, unit, rest, (const bf16_t *)table, table_stride};
     // many slots of a small matrix (one token against a million words: 512) want the parallel form, others fill the chip without
     const i64 chunks = rows * (D / 4);
     if (n_slots <= 16 || chunks >= 65536) {
@@ -1451,7 +1509,7 @@ int tensair_softmax_loss(const void *hidden, int64_t hidden_stride, const void *
     } else {
         LayOutArgs x;
         memset(&x, 0, sizeof(x));
-        x.tokens = TokenArgs{lab, nullptr, nullptr, n, s.Np, b.label, status, nullptr, nullptr};
+        x.tokens = TokenArgs{lab, nullptr, nullptr, n, s.Np, b.label, status, nullptr, nullptr, nullptr};
         x.token_blocks = (int)cdiv(s.Np, BLOCK);
         x.h = lay_out(s, hidden, hidden_stride, n, s.Np, dim, Labels{}, scale < 0.f ? -1.f : 1.f, b.h, &x.h_blocks);
         for (i64 range = 0; range < s.ranges; ++range) {
@@ -1505,12 +1563,13 @@ int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *
         f.d_stride = d_table_stride;
         if (dtype == TENSAIR_F32) launch_few_t<float, true>(f, s.few_blocks, st);
         else launch_few_t<bf16_t, true>(f, s.few_blocks, st);
-        if (d_hidden) launch_join(b.h_slots, s.few_blocks, n, d_hidden_stride, dim, lab, d_hidden, dtype, scale, st);
+        if (d_hidden) launch_join(b.h_slots, s.few_blocks, n, d_hidden_stride, dim, lab, d_hidden, dtype, scale, nullptr, nullptr, nullptr, 0, st);
         return launched("softmax_grad");
     }
     LayOutArgs x;
     memset(&x, 0, sizeof(x));
-    x.tokens = TokenArgs{lab, lse, d_loss, n, s.Np, b.label, status, b.lse2, b.d};
+    x.tokens = TokenArgs{lab, lse, d_loss, n, s.Np, b.label, status, b.lse2, b.d, b.unit};
+    x.unit_block = b.unit ? 1 : 0;
     x.token_blocks = (int)cdiv(s.Np, BLOCK);
     x.h = lay_out(s, hidden, hidden_stride, n, s.Np, dim, lab, scale < 0.f ? -1.f : 1.f, b.h, &x.h_blocks);   // what a token without a loss holds must reach no sum
     for (i64 range = 0; range < s.ranges; ++range) {
@@ -1525,6 +1584,7 @@ int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *
         p.M = dim;
         p.dtype = dtype;
         p.scale = scale;
+        p.unit = b.unit;
         if (d_hidden) {
             p.a = a.w;
             p.b = dz;
@@ -1552,12 +1612,12 @@ int tensair_softmax_grad(const void *hidden, int64_t hidden_stride, const void *
             p.out = out;
             p.out_stride = d_table_stride;
             launch_product<true>(s, p, st);
-            if (s.t_splits > 1) launch_join(b.t_slots, s.t_splits, r.words, d_table_stride, dim, Labels{}, out, dtype, fabsf(scale), st);
+            if (s.t_splits > 1) launch_join(b.t_slots, s.t_splits, r.words, d_table_stride, dim, Labels{}, out, dtype, fabsf(scale), b.unit, nullptr, nullptr, 0, st);
         }
     }
     if (d_hidden) {
         const int slots = (int)cdiv(cdiv(range_of(s, 0, vocab).words, BK) * BK, s.h_k);
-        launch_join(b.h_slots, slots, n, d_hidden_stride, dim, lab, d_hidden, dtype, scale, st);
+        launch_join(b.h_slots, slots, n, d_hidden_stride, dim, lab, d_hidden, dtype, scale, b.unit, b.rest, table, table_stride, st);
     }
     return launched("softmax_grad");
 }

@@ -136,3 +136,45 @@ def test_numbers_that_are_none_stay_where_they_belong(n, dtype):
         worse[V // 2, col] = float("nan")
         got, got_lse = _loss(h, worse, labels)
         assert bool(got.isnan().all()) and bool(got_lse.isnan().all())
+
+
+# ---------------------------------------------------------------- the label's share of a gradient
+@pytest.mark.parametrize("weights", ["mean", "each its own"])
+@pytest.mark.parametrize("n,V,D,pad", [(9, 300, 36, 0), (26, 2_439, 148, 0), (64, 5_000, 64, 4), (100, 1_000, 64, 0), (128, 257, 324, 0), (300, 5_000, 300, 0), (1_000, 777, 512, 4),
+                                       (5_615, 1_530, 120, 0), (2_100, 40_000, 192, 0), (4_096, 20_000, 1_024, 0), (16_383, 3_001, 256, 0), (9_000, 70_000, 64, 0)])
+def test_bfloat16_gradients_are_off_by_little_more_than_their_own_rounding(n, V, D, pad, weights):
+    """A number that is rounded to bfloat16 is off by up to 2^-9 of it, one below 1 and not below 1/2 by up to 2^-9; errors of their own add up as the root of the sum of
+    their squares does.  Beside the outputs' own rounding there is that of dz: of the words that are no labels, and, in the gradient of the table alone, of
+    the labels' p - 1, which is off by no more than p.  (What the tokens have in common of d_loss is not rounded at all: were it, the labels' elements
+    would be off by as much as the outputs, all of them to the same side.)"""
+    g = torch.Generator(device="cuda").manual_seed(n + V)
+    h, w = ((torch.randn((k, D + pad), generator=g, device="cuda") * s).bfloat16() for k, s in ((n, 2 / (0.25 * math.sqrt(D))), (V, 0.25)))
+    cdf = torch.cumsum(torch.arange(1, V + 1, device="cuda", dtype=torch.float64) ** -1.2, 0)
+    labels = torch.searchsorted(cdf, torch.rand(n, generator=g, device="cuda", dtype=torch.float64) * cdf[-1]).clamp(max=V - 1).int()
+    labels[::16] = -1
+    scale = -1.3 if n % 2 else 0.8
+    d = torch.full((n,), 1.0039 / n, device="cuda") if weights == "mean" else torch.rand(n, generator=g, device="cuda") / n
+    hd, wd = h[:, :D], w[:, :D]
+    ws = torch.empty(B.tensair_softmax_workspace_bytes(n, V, D, w.dtype, True), dtype=torch.uint8, device="cuda")
+    ws.fill_(0xFF)
+    loss, lse = (torch.empty(n, device="cuda") for _ in range(2))
+    B.tensair_softmax_loss(hd, wd, D, labels, loss, lse, ws, scale)
+    ws.fill_(0xFF)
+    dh, dw = torch.empty_like(h), torch.empty_like(w)
+    B.tensair_softmax_grad(hd, wd, D, labels, lse, d, dh[:, :D], dw[:, :D], ws, scale)
+    s = float(torch.tensor(scale, dtype=torch.float32))
+    h64, w64, keep = hd.double(), wd.double(), labels >= 0
+    at, y = keep.nonzero()[:, 0], labels[keep].long()
+    p = torch.softmax(s * (h64 @ w64.t()), 1)
+    p_label = p[at, y]
+    p *= torch.where(keep, d.double(), 0.0)[:, None]
+    rest = p.clone()                                           # dz without the labels' elements
+    rest[at, y] = 0
+    p[at, y] -= d[at].double()
+    # the squares of the labels' errors, in units of 2^-9: of p - 1, or of its product with a factor of a token's own
+    own = d[at].double() ** 2 * (torch.clamp(p_label * 512, max=1.0) if weights == "mean" else 1 - p_label) ** 2
+    for got, value, spread, label in ((dh, s * (p @ w64), (rest ** 2) @ w64 ** 2, 0.0),
+                                      (dw, s * (p.t() @ h64), (rest ** 2).t() @ h64 ** 2, float((own[:, None] * h64[at] ** 2).sum()))):
+        off = float((got[:, :D].double() - value).norm())
+        bound = 2.0 ** -9 * math.sqrt(float(value.norm()) ** 2 + s * s * (float(spread.sum()) + label))
+        assert off <= bound, (off / bound, off / float(value.norm()))
