@@ -468,6 +468,88 @@ int tensair_adamw_step_at(tensair_adamw *h, const double *lr, const int64_t *ste
                           double eps, const float *grad_scale, void *stream);
 int tensair_adamw_destroy(tensair_adamw *h);
 
+/* ------------------------------------------------------------------------------------------------------
+ * What lies between a table's two ends in a model of word sequences, and behind them.  Matrices as above, but an address needs the alignment of
+ * four elements only (16 bytes for fp32, 8 for bfloat16), so that both halves of a product's rows can be passed; a row index times a stride may be
+ * of any size.  Weights, statistics and states: DEVICE fp32, contiguous, 16-byte aligned.  n <= TENSAIR_MAX_ROWS.  Outputs must not overlap
+ * inputs where nothing else is said.  The same call gives the same bits. */
+#define TENSAIR_MAX_ROWS 2147479551LL /* 2^31 - 4097 */
+
+/* Layer norm: out[i] = (x[i] - mean[i]) * rstd[i] * weight + bias, mean[i] = mean of the row, rstd[i] = 1 / sqrt(mean of (x[i] - mean[i])^2 + eps),
+ * all in fp32, rounded once to out's type.  weight, bias: [dim], NULL: 1 and 0.  eps: positive.  mean, rstd: fp32 [n], both NULL: not wanted.
+ * out may be x, with the same type and stride. */
+int tensair_norm(const void *x, int32_t dtype, int64_t x_stride, int64_t n, int32_t dim, const float *weight,
+                 const float *bias, float eps, void *out, int32_t out_dtype, int64_t out_stride, float *mean,
+                 float *rstd, void *stream);
+/* Its gradient.  With y = (x - mean) * rstd and g = d_out * weight, by row
+ *   d_x = d_add + rstd * (g - mean of g - y * (mean of g * y)),   and over the rows   d_weight = sum of d_out * y,   d_bias = sum of d_out.
+ * mean, rstd: what tensair_norm gave.  d_add: of x's type or NULL, the gradient that x has from elsewhere (a residual path); d_x may be d_add,
+ * with the same stride.  d_weight, d_bias: fp32 [dim], overwritten (n = 0: zeros); either may be NULL, with both NULL no workspace is needed.
+ * workspace: DEVICE, 256-byte aligned; holds nothing between calls.  The bytes asked for n rows serve fewer rows, too. */
+size_t tensair_norm_workspace_bytes(int64_t n, int32_t dim);
+int tensair_norm_grad(const void *d_out, int32_t d_dtype, int64_t d_stride, const void *x, int32_t dtype,
+                      int64_t x_stride, int64_t n, int32_t dim, const float *weight, const float *mean,
+                      const float *rstd, const void *d_add, int64_t d_add_stride, void *d_x, int64_t d_x_stride,
+                      float *d_weight, float *d_bias, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Dropout: out[i][j] = residual[i][j] + (kept ? x[i][j] / (1 - p) : 0), 0 <= p < 1; residual: of out's type, NULL: 0.  Element j of row i is
+ * kept if word j mod 4 of Philox4x32-10 with key (seed low, seed high) and counter (c low, c high, step mod 2^32, 0x44524F50 + layer), c = (i * dim + j) / 4,
+ * is at least floor(p * 2^32); the mask is never stored, and hangs on no stride.  x / (1 - p) is the product with 1 / (1 - p) rounded to fp32, in fp32; the sum
+ * too; rounded once more to out's type.  The gradient with respect to x is the same call on that of out without a residual, that of residual is out's own.
+ * step_at: DEVICE int64, 8-byte aligned, read when the work runs and added to step, for calls that are recorded into a graph; NULL: 0.
+ * out may be x or residual, with the same type and stride. */
+int tensair_dropout(const void *x, int32_t dtype, int64_t x_stride, int64_t n, int32_t dim, double p, uint64_t seed,
+                    uint32_t layer, int64_t step, const int64_t *step_at, const void *residual,
+                    int64_t residual_stride, void *out, int32_t out_dtype, int64_t out_stride, void *stream);
+
+/* A gated linear recurrence over the sequences of a packed mini-batch: for the tokens t of sequence s, offsets[s] <= t < offsets[s + 1], and every channel
+ *   h[t] = a[t] h[t - 1] + (1 - a[t]) x[t],   a[t] = 1 / (1 + exp(-gate[t])),
+ * with h0[s] before a sequence's first token (h0: fp32 [n_seq][dim], NULL: 0), in fp32; out[t] is h[t] rounded to x's type, h_last[s] (fp32 [n_seq][dim], NULL: not
+ * wanted) the last h of the sequence, h0[s] if it has no token.  x, gate and out have one type; n: rows that they have.  offsets: DEVICE int32 [n_seq + 1],
+ * ascending (equal ones: an empty sequence), 0 <= offsets[0], offsets[n_seq] <= n; rows outside [offsets[0], offsets[n_seq]) are neither read for
+ * a result nor written.  Offsets out of this order never fault: bit 2 is OR-ed into *status, and no output of the call is to be used.
+ * states: fp32 [tensair_recur_state_rows(n)][dim], what the gradient needs of the states; NULL: no gradient is wanted.
+ * workspace: DEVICE, 256-byte aligned, of tensair_recur_workspace_bytes; holds nothing between calls; serves both calls and fewer rows, too. */
+int64_t tensair_recur_state_rows(int64_t n);
+size_t tensair_recur_workspace_bytes(int64_t n, int32_t dim);
+int tensair_recur(const void *x, int64_t x_stride, const void *gate, int64_t gate_stride, int32_t dtype, int64_t n,
+                  int32_t dim, const int32_t *offsets, int64_t n_seq, const float *h0, void *out, int64_t out_stride,
+                  float *h_last, float *states, void *workspace, size_t workspace_bytes, int32_t *status, void *stream);
+/* Its gradient, from those of out (d_out, of x's type) and of h_last (d_last: fp32 [n_seq][dim], NULL: 0); states as tensair_recur gave them for the same inputs.
+ *   l[t] = d_out[t] + a[t + 1] l[t + 1] (d_last[s] instead of the last term at a sequence's last token),
+ *   d_x[t] = (1 - a[t]) l[t],   d_gate[t] = l[t] (h[t - 1] - x[t]) a[t] (1 - a[t]),   d_h0[s] = a l of the first token (d_last[s] if there is none).
+ * The h are made again in fp32, not taken from out.  d_h0: fp32 [n_seq][dim], NULL: not wanted. */
+int tensair_recur_grad(const void *x, int64_t x_stride, const void *gate, int64_t gate_stride, int32_t dtype, int64_t n,
+                       int32_t dim, const int32_t *offsets, int64_t n_seq, const float *h0, const float *states,
+                       const void *d_out, int64_t d_stride, const float *d_last, void *d_x, int64_t d_x_stride,
+                       void *d_gate, int64_t d_gate_stride, float *d_h0, void *workspace, size_t workspace_bytes,
+                       int32_t *status, void *stream);
+/* The recurrence for single tokens, as a server has them: row i of x and gate is the next token of the sequence whose state is row slots[i] of state (fp32
+ * [n_slots][state_stride], updated in place); slots NULL: row i, n <= n_slots.  Rows of the same slot are tokens that follow one another.  out: like x, NULL: not wanted.
+ * A slot outside [0, n_slots) changes no state, gives a row of zeros and sets bit 1 of *status.  With slots n <= TENSAIR_MAX_STEP_ROWS. */
+#define TENSAIR_MAX_STEP_ROWS 65536
+int tensair_recur_step(const void *x, int64_t x_stride, const void *gate, int64_t gate_stride, int32_t dtype, int64_t n,
+                       int32_t dim, const int32_t *slots, int64_t n_slots, float *state, int64_t state_stride,
+                       void *out, int64_t out_stride, int32_t *status, void *stream);
+
+/* One word for every row of logits, drawn by the row's own random number.  logits: [n][stride] of TENSAIR_F32 or TENSAIR_BF16 with the alignment of an element,
+ * stride >= vocab; 1 <= vocab <= TENSAIR_MAX_SAMPLE_VOCAB.  With z the row and w[v] = exp((z[v] - max z) / temperature), in 64 bits:
+ *   of the words in the order of falling z, equal ones in the order of their numbers, the first top_k are left (top_k < 1: all); of those the first ones, a word being left
+ *   if the words before it have less than top_p of the weight of what top_k left (top_p >= 1: all); of those the ones with w[v] >= min_p;
+ *   words[i] is the first word of those that are left, in the order of their numbers, at which their running sum of weights exceeds u[i] times the sum; prob[i] (NULL: not
+ *   wanted) its weight over that sum.
+ * temperature (not above 0, or NaN: the largest logit is taken, prob 1; NULL: 1), top_p (not above 0, or NaN: the first word; NULL: 1), min_p (above 1: 1; NaN, NULL: 0), u (below 0,
+ * or NaN: 0; 1 or above: the last word that is left): DEVICE fp32 [n]; top_k: DEVICE int32 [n], NULL: 0.  A NaN among the logits counts as minus infinity, and a word of minus infinity has no weight; where
+ * the largest is plus infinity, words of plus infinity share all weight.  A row without a word above minus infinity gives -1 and probability 0 and sets bit 1 of *status.
+ * workspace: DEVICE, 256-byte aligned; holds nothing between calls; serves fewer rows and words, too. */
+#define TENSAIR_MAX_SAMPLE_ROWS 65536
+#define TENSAIR_MAX_SAMPLE_VOCAB 16777216 /* 2^24 */
+size_t tensair_sample_workspace_bytes(int64_t n, int64_t vocab);
+int tensair_sample(const void *logits, int32_t dtype, int64_t stride, int64_t n, int64_t vocab,
+                   const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                   const float *u, int32_t *words, float *prob, void *workspace, size_t workspace_bytes,
+                   int32_t *status, void *stream);
+
 /* Waits for the library's own stream (a pending prefetch), then frees the host handle. */
 int tensair_model_destroy(tensair_model *m);
 

@@ -37,6 +37,9 @@ SYMBOLS = [
     "tensair_embed", "tensair_embed_workspace_bytes", "tensair_embed_grad", "tensair_embed_grad_dense",
     "tensair_softmax_workspace_bytes", "tensair_softmax_loss", "tensair_softmax_grad",
     "tensair_adamw_workspace_bytes", "tensair_adamw_init", "tensair_adamw_step", "tensair_adamw_step_at", "tensair_adamw_destroy",
+    "tensair_norm", "tensair_norm_workspace_bytes", "tensair_norm_grad", "tensair_dropout",
+    "tensair_recur_state_rows", "tensair_recur_workspace_bytes", "tensair_recur", "tensair_recur_grad", "tensair_recur_step",
+    "tensair_sample_workspace_bytes", "tensair_sample",
 ]
 
 PROFILE_TAGS = {1: "keys", 2: "forward", 3: "sort", 4: "segments", 5: "reduce_in", 6: "reduce_out",
@@ -168,6 +171,29 @@ def lib():
         L.tensair_adamw_step_at.restype = C.c_int
         L.tensair_adamw_destroy.argtypes = [vp]
         L.tensair_adamw_destroy.restype = C.c_int
+        u64, f64 = C.c_uint64, C.c_double
+        L.tensair_norm.argtypes = [vp, i32, i64, i64, i32, vp, vp, f32, vp, i32, i64, vp, vp, vp]
+        L.tensair_norm.restype = C.c_int
+        L.tensair_norm_workspace_bytes.argtypes = [i64, i32]
+        L.tensair_norm_workspace_bytes.restype = sz
+        L.tensair_norm_grad.argtypes = [vp, i32, i64, vp, i32, i64, i64, i32, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+        L.tensair_norm_grad.restype = C.c_int
+        L.tensair_dropout.argtypes = [vp, i32, i64, i64, i32, f64, u64, u32, i64, vp, vp, i64, vp, i32, i64, vp]
+        L.tensair_dropout.restype = C.c_int
+        L.tensair_recur_state_rows.argtypes = [i64]
+        L.tensair_recur_state_rows.restype = i64
+        L.tensair_recur_workspace_bytes.argtypes = [i64, i32]
+        L.tensair_recur_workspace_bytes.restype = sz
+        L.tensair_recur.argtypes = [vp, i64, vp, i64, i32, i64, i32, vp, i64, vp, vp, i64, vp, vp, vp, sz, vp, vp]
+        L.tensair_recur.restype = C.c_int
+        L.tensair_recur_grad.argtypes = [vp, i64, vp, i64, i32, i64, i32, vp, i64, vp, vp, vp, i64, vp, vp, i64, vp, i64, vp, vp, sz, vp, vp]
+        L.tensair_recur_grad.restype = C.c_int
+        L.tensair_recur_step.argtypes = [vp, i64, vp, i64, i32, i64, i32, vp, i64, vp, i64, vp, i64, vp, vp]
+        L.tensair_recur_step.restype = C.c_int
+        L.tensair_sample_workspace_bytes.argtypes = [i64, i64]
+        L.tensair_sample_workspace_bytes.restype = sz
+        L.tensair_sample.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp]
+        L.tensair_sample.restype = C.c_int
         L.tensair_last_error.argtypes = []
         L.tensair_last_error.restype = C.c_char_p
         _lib = L
@@ -663,6 +689,158 @@ class AdamW:
             self.close()
         except Exception:
             pass
+
+
+# ---- what lies between a table's two ends in a model of word sequences, and behind them
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _launch(dev, call, *args):
+    """A call whose kernels go to the GPU of that number, whichever is the current one."""
+    if _current_device() == dev:
+        rc = call(*args)
+    else:
+        with torch.cuda.device(dev):
+            rc = call(*args)
+    if rc:
+        _check(rc)
+
+
+def _floats(t, shape, what):
+    """The address of contiguous float32 elements of that shape, or None."""
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or t.shape != shape or not t.is_contiguous():
+        raise TensairError(EINVAL, f"{what}: expected contiguous float32 elements of shape {shape}")
+    return t.data_ptr()
+
+
+def tensair_norm(x, dim: int, weight, bias, out, mean=None, rstd=None, eps=1e-5, stream=None):
+    """x, out: [n, >= dim] float32 or bfloat16; weight, bias: float32 [dim] or None; mean, rstd: float32 [n] or both None."""
+    n, dev = x.shape[0], _device(x, weight, bias, out, mean, rstd)
+    xp, xd, xs = _matrix(x, n, dim, "x")
+    op, od, os_ = _matrix(out, n, dim, "out")
+    _launch(dev, (_lib or lib()).tensair_norm, xp, xd, xs, n, dim, _floats(weight, (dim,), "weight"), _floats(bias, (dim,), "bias"), eps, op, od, os_,
+            _floats(mean, (n,), "mean"), _floats(rstd, (n,), "rstd"), _on(dev, stream))
+
+
+def tensair_norm_workspace_bytes(n: int, dim: int) -> int:
+    nbytes = lib().tensair_norm_workspace_bytes(n, dim)
+    if nbytes == 0:
+        raise TensairError(EINVAL, lib().tensair_last_error().decode())
+    return nbytes
+
+
+def tensair_norm_grad(d_out, x, dim: int, weight, mean, rstd, d_x, d_weight=None, d_bias=None, workspace=None, d_add=None, stream=None):
+    """d_out: [n, >= dim]; x, d_x, d_add (or None): of one type; mean, rstd: as tensair_norm gave them; d_weight, d_bias: float32 [dim] or None (not
+    wanted; with neither no workspace is needed)."""
+    n, dev = x.shape[0], _device(x, d_out, weight, mean, rstd, d_x, d_weight, d_bias, workspace, d_add)
+    dp, dd, ds = _matrix(d_out, n, dim, "d_out")
+    xp, xd, xs = _matrix(x, n, dim, "x")
+    dxp, dxd, dxs = _matrix(d_x, n, dim, "d_x")
+    ap, ad, as_ = _matrix(d_add, n, dim, "d_add") if d_add is not None else (None, xd, dim)
+    if not xd == dxd == ad:
+        raise TensairError(EINVAL, "x, d_x and d_add must have one type")
+    ws = (workspace.data_ptr(), _bytes(workspace)) if workspace is not None else (None, 0)
+    _launch(dev, (_lib or lib()).tensair_norm_grad, dp, dd, ds, xp, xd, xs, n, dim, _floats(weight, (dim,), "weight"), _vector(mean, n, torch.float32, "mean"),
+            _vector(rstd, n, torch.float32, "rstd"), ap, as_, dxp, dxs, _floats(d_weight, (dim,), "d_weight"), _floats(d_bias, (dim,), "d_bias"), *ws,
+            _on(dev, stream))
+
+
+def tensair_dropout(x, dim: int, out, p: float, seed: int, layer=0, step=0, residual=None, stream=None):
+    """x, out: [n, >= dim] float32 or bfloat16; residual: like out, or None; step: a number or, for a call that is recorded into a graph, an int64 tensor
+    of one element on the GPU."""
+    n, at = x.shape[0], step if isinstance(step, torch.Tensor) else None
+    dev = _device(x, out, residual, at)
+    xp, xd, xs = _matrix(x, n, dim, "x")
+    op, od, os_ = _matrix(out, n, dim, "out")
+    rp, rd, rs = _matrix(residual, n, dim, "residual") if residual is not None else (None, od, dim)
+    if rd != od:
+        raise TensairError(EINVAL, "residual and out must have one type")
+    _launch(dev, (_lib or lib()).tensair_dropout, xp, xd, xs, n, dim, p, seed, layer, 0 if at is not None else step, _word(at, torch.int64, "step"), rp, rs, op, od,
+            os_, _on(dev, stream))
+
+
+def tensair_recur_state_rows(n: int) -> int:
+    rows = lib().tensair_recur_state_rows(n)
+    if rows < 0:
+        raise TensairError(EINVAL, lib().tensair_last_error().decode())
+    return rows
+
+
+def tensair_recur_workspace_bytes(n: int, dim: int) -> int:
+    nbytes = lib().tensair_recur_workspace_bytes(n, dim)
+    if nbytes == 0:
+        raise TensairError(EINVAL, lib().tensair_last_error().decode())
+    return nbytes
+
+
+def _recur_inputs(x, gate, dim, offsets, states):
+    n, n_seq = x.shape[0], offsets.numel() - 1
+    xp, xd, xs = _matrix(x, n, dim, "x")
+    gp, gd, gs = _matrix(gate, n, dim, "gate")
+    if xd != gd:
+        raise TensairError(EINVAL, "x and gate must have one type")
+    if n_seq < 0:
+        raise TensairError(EINVAL, "offsets: expected one more than there are sequences")
+    rows = max(1, -(-n // 256))
+    return n, n_seq, xd, (xp, xs, gp, gs, xd, n, dim, _ids(offsets, "offsets"), n_seq), _floats(states, (rows, dim), "states")
+
+
+def tensair_recur(x, gate, dim: int, offsets, out, workspace, h0=None, h_last=None, states=None, status=None, stream=None):
+    """x, gate, out: [n, >= dim] of one type; offsets: int32 [sequences + 1]; h0, h_last: float32 [sequences, dim] or None; states: float32
+    [tensair_recur_state_rows(n), dim] or None (no gradient is wanted)."""
+    dev = _device(x, gate, offsets, out, workspace, h0, h_last, states, status)
+    n, n_seq, code, head, sp = _recur_inputs(x, gate, dim, offsets, states)
+    op, od, os_ = _matrix(out, n, dim, "out")
+    if od != code:
+        raise TensairError(EINVAL, "x, gate and out must have one type")
+    _launch(dev, (_lib or lib()).tensair_recur, *head, _floats(h0, (n_seq, dim), "h0"), op, os_, _floats(h_last, (n_seq, dim), "h_last"), sp,
+            workspace.data_ptr(), _bytes(workspace), _word(status), _on(dev, stream))
+
+
+def tensair_recur_grad(x, gate, dim: int, offsets, states, d_out, d_x, d_gate, workspace, h0=None, d_last=None, d_h0=None, status=None, stream=None):
+    """states: as tensair_recur gave them; d_out, d_x, d_gate: like x; d_last, d_h0: float32 [sequences, dim] or None."""
+    dev = _device(x, gate, offsets, states, d_out, d_x, d_gate, workspace, h0, d_last, d_h0, status)
+    n, n_seq, code, head, sp = _recur_inputs(x, gate, dim, offsets, states)
+    dp, dd, ds = _matrix(d_out, n, dim, "d_out")
+    xp, xd, xs = _matrix(d_x, n, dim, "d_x")
+    gp, gd, gs = _matrix(d_gate, n, dim, "d_gate")
+    if not code == dd == xd == gd:
+        raise TensairError(EINVAL, "x, gate and their gradients must have one type")
+    _launch(dev, (_lib or lib()).tensair_recur_grad, *head, _floats(h0, (n_seq, dim), "h0"), sp, dp, ds, _floats(d_last, (n_seq, dim), "d_last"), xp, xs, gp, gs,
+            _floats(d_h0, (n_seq, dim), "d_h0"), workspace.data_ptr(), _bytes(workspace), _word(status), _on(dev, stream))
+
+
+def tensair_recur_step(x, gate, dim: int, state, out=None, slots=None, status=None, stream=None):
+    """x, gate, out (or None): [n, >= dim] of one type; state: float32 [slots, >= dim], updated; slots: int32 [n], the rows of state, or None (row i)."""
+    n, dev = x.shape[0], _device(x, gate, state, out, slots, status)
+    xp, xd, xs = _matrix(x, n, dim, "x")
+    gp, gd, gs = _matrix(gate, n, dim, "gate")
+    sp, sd, ss = _matrix(state, state.shape[0], dim, "state")
+    op, od, os_ = _matrix(out, n, dim, "out") if out is not None else (None, xd, dim)
+    if not xd == gd == od or sd != F32:
+        raise TensairError(EINVAL, "x, gate and out must have one type, state float32")
+    _launch(dev, (_lib or lib()).tensair_recur_step, xp, xs, gp, gs, xd, n, dim, _vector(slots, n, torch.int32, "slots") if slots is not None else None,
+            state.shape[0], sp, ss, op, os_, _word(status), _on(dev, stream))
+
+
+def tensair_sample_workspace_bytes(n: int, vocab: int) -> int:
+    nbytes = lib().tensair_sample_workspace_bytes(n, vocab)
+    if nbytes == 0:
+        raise TensairError(EINVAL, lib().tensair_last_error().decode())
+    return nbytes
+
+
+def tensair_sample(logits, vocab: int, u, words, workspace, temperature=None, top_k=None, top_p=None, min_p=None, prob=None, status=None, stream=None):
+    """logits: [n, >= vocab] float32 or bfloat16; u: float32 [n]; words: int32 [n]; temperature, top_p, min_p: float32 [n], top_k: int32 [n], each or None;
+    prob: float32 [n] or None."""
+    n, dev = logits.shape[0], _device(logits, u, words, workspace, temperature, top_k, top_p, min_p, prob, status)
+    zp, zd, zs = _matrix(logits, n, vocab, "logits")
+    _launch(dev, (_lib or lib()).tensair_sample, zp, zd, zs, n, vocab, _floats(temperature, (n,), "temperature"),
+            _vector(top_k, n, torch.int32, "top_k") if top_k is not None else None, _floats(top_p, (n,), "top_p"), _floats(min_p, (n,), "min_p"),
+            _vector(u, n, torch.float32, "u"), _vector(words, n, torch.int32, "words"), _floats(prob, (n,), "prob"), workspace.data_ptr(), _bytes(workspace),
+            _word(status), _on(dev, stream))
 
 
 def tensair_status(h, stream=None):

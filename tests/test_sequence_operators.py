@@ -1,0 +1,658 @@
+"""The operators of a model of word sequences -- layer norm, dropout, the gated linear recurrence, drawing words -- on the GPU through the C ABI, against
+plain implementations in 64 bits.  Tolerances are worked out from the number of roundings (U32 and U16: half a unit in the last place of fp32 and
+bfloat16, relative to the value)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2211_10280_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+U32, U16 = 2.0 ** -24, 2.0 ** -8
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+UNIT = {"f32": U32, "bf16": U16}
+MARK = 7.0                # what outputs hold beside and behind what a call writes
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _rows(g, n, D, dtype, pad=0, std=1.0, fill=float("nan")):
+    """[n, D] random rows inside [n, D + pad], `fill` beside them."""
+    t = torch.full((n, D + pad), fill, dtype=DT[dtype], device="cuda")
+    t[:, :D] = torch.randn((n, D), generator=g, device="cuda") * std
+    return t
+
+
+def _empty(n, D, dtype, pad=0):
+    return torch.full((n, D + pad), MARK, dtype=DT[dtype], device="cuda")
+
+
+def _status():
+    return torch.zeros(1, dtype=torch.int32, device="cuda")
+
+
+def _near(got, want, tol, what=""):
+    off = (got.double() - want).abs()
+    assert bool((off <= tol).all()), (what, float((off / tol.clamp(min=1e-300)).max()))
+
+
+def _bytes(nbytes):
+    return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+
+
+# ---------------------------------------------------------------- layer norm
+NORMS = [(1, 4, "f32", "f32", 0), (64, 32, "f32", "f32", 0), (33, 36, "bf16", "f32", 4), (257, 64, "f32", "bf16", 0), (1_023, 128, "bf16", "bf16", 12),
+         (515, 132, "f32", "f32", 4), (777, 300, "f32", "bf16", 20), (129, 512, "bf16", "bf16", 0), (65, 772, "bf16", "f32", 4), (31, 1_024, "f32", "f32", 0),
+         (40_001, 8, "bf16", "bf16", 0), (20_011, 256, "f32", "f32", 0)]
+
+
+def _norm_inputs(n, D, dtype, pad, seed):
+    g = _gen(seed)
+    x = _rows(g, n, D, dtype, pad)
+    x[:, :D] = x[:, :D] * torch.exp(torch.randn((n, 1), generator=g, device="cuda")) + 10 * torch.randn((n, 1), generator=g, device="cuda")
+    x[0, :D] = 3.0                                             # a row without variance
+    return g, x, 1 + torch.randn(D, generator=g, device="cuda"), torch.randn(D, generator=g, device="cuda")
+
+
+@pytest.mark.parametrize("n,D,dtype,out,pad", NORMS)
+@pytest.mark.parametrize("affine", [True, False])
+def test_norm(n, D, dtype, out, pad, affine):
+    g, x, w, b = _norm_inputs(n, D, dtype, pad, n + D)
+    if not affine:
+        w = b = None
+    got, mean, rstd, eps = _empty(n, D, out, pad), torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), 1e-5
+    B.tensair_norm(x, D, w, b, got, mean, rstd, eps)
+    v = x[:, :D].double()
+    m = v.mean(1, keepdim=True)
+    r = (((v - m) ** 2).mean(1, keepdim=True) + eps) ** -0.5
+    y = (v - m) * r
+    W, A = (w.double(), b.double()) if affine else (torch.ones(D, device="cuda").double(), torch.zeros(D, device="cuda").double())
+    want = y * W + A
+    # a row's sum: 3 additions a chunk, up to 4 chunks and 6 steps over the lanes, then the product with 1 / dim: 14 roundings with room
+    size = v.abs().mean(1, keepdim=True)
+    e_mean = 14 * U32 * size
+    # variance: 2 roundings a square and a sum; the error of the mean enters squared; (1 - eps rounding) root and quotient: half of 16 units and 3
+    e_rstd = 12 * U32 + 0.5 * (r * e_mean) ** 2
+    _near(mean, m[:, 0], e_mean[:, 0] + 1e-30, "mean")
+    _near(rstd, r[:, 0], (e_rstd * r)[:, 0], "rstd")
+    tol = W.abs() * (r * (e_mean + U32 * (v - m).abs()) + y.abs() * (e_rstd + 2 * U32)) * (1 + 1e-3) + 2 * U32 * (want.abs() + A.abs()) + UNIT[out] * want.abs() * (1 + 1e-2) + 1e-30
+    _near(got[:, :D], want, tol + UNIT[out] * tol, "out")
+    assert bool((got[:, D:] == MARK).all())
+    again = _empty(n, D, out, pad)
+    B.tensair_norm(x, D, w, b, again, eps=eps)                 # without statistics
+    assert torch.equal(got, again)
+    if dtype == out:
+        B.tensair_norm(x, D, w, b, x, eps=eps)                 # in place
+        assert torch.equal(x[:, :D], got[:, :D])
+
+
+@pytest.mark.parametrize("n,D,dtype,out,pad", NORMS)
+@pytest.mark.parametrize("affine,add", [(True, True), (False, False), (True, False)])
+def test_norm_grad(n, D, dtype, out, pad, affine, add):
+    g, x, w, _ = _norm_inputs(n, D, dtype, pad, 3 * n + D)
+    if not affine:
+        w = None
+    mean, rstd = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    B.tensair_norm(x, D, w, None, _empty(n, D, out), mean, rstd)
+    d = _rows(g, n, D, out, pad)
+    res = _rows(g, n, D, dtype, pad) if add else None
+    dx, dw, db = _empty(n, D, dtype, pad), torch.full((D,), MARK, device="cuda"), torch.full((D,), MARK, device="cuda")
+    ws = _bytes(B.tensair_norm_workspace_bytes(n, D))
+    B.tensair_norm_grad(d, x, D, w, mean, rstd, dx, dw, db, ws, res)
+    W = w.double() if affine else torch.ones(D, device="cuda").double()
+    r = rstd.double()[:, None]
+    y, e = (x[:, :D].double() - mean.double()[:, None]) * r, d[:, :D].double() * W
+    s1, s2 = e.mean(1, keepdim=True), (e * y).mean(1, keepdim=True)
+    R = res[:, :D].double() if add else torch.zeros_like(y)
+    want = R + r * (e - s1 - y * s2)
+    # row sums: 14 roundings as above and one (e) or four (e y, y being off by 2) in each term
+    a1, a2 = e.abs().mean(1, keepdim=True), (e * y).abs().mean(1, keepdim=True)
+    tol = r * U32 * (4 * e.abs() + 18 * a1 + y.abs() * (24 * a2)) + 2 * U32 * (want.abs() + R.abs()) + UNIT[dtype] * want.abs()
+    _near(dx[:, :D], want, tol * (1 + 2 * U16) + 1e-30, "d_x")
+    # columns: at most 256 additions in fp32 in a lane, 31 over a workgroup's lanes, the rest in 64 bits; a term is off by 3 (d y), once rounded at the end
+    groups = 256 // (8 if D <= 32 else 16 if D <= 64 else 32 if D <= 128 else 64)
+    adds = min(256, math.ceil(n / (1024 * groups))) + 32
+    dd = d[:, :D].double()
+    _near(dw, (dd * y).sum(0), ((adds + 4) * U32 * (dd * y).abs().sum(0)) + 1e-30, "d_weight")
+    _near(db, dd.sum(0), ((adds + 1) * U32 * dd.abs().sum(0)) + 1e-30, "d_bias")
+    assert bool((dx[:, D:] == MARK).all())
+    # each result without the others; the same bits
+    dx2, db2 = _empty(n, D, dtype, pad), torch.empty(D, device="cuda")
+    B.tensair_norm_grad(d, x, D, w, mean, rstd, dx2, None, db2, ws, res)
+    assert torch.equal(dx2, dx) and torch.equal(db2, db)
+    B.tensair_norm_grad(d, x, D, w, mean, rstd, dx2, d_add=res)
+    assert torch.equal(dx2, dx)
+    if add:
+        B.tensair_norm_grad(d, x, D, w, mean, rstd, res, dw, db, ws, res)      # the sum where one of its terms was
+        assert torch.equal(res[:, :D], dx[:, :D])
+
+
+def test_norm_grad_against_differences():
+    """The directional derivative of a sum of outputs, by central differences of two widths (their error of the second order taken out) of the
+    operator's own outputs, summed in 64 bits."""
+    n, D = 40, 48
+    g, x, w, b = _norm_inputs(n, D, "f32", 0, 5)
+    x = torch.randn((n, D), generator=g, device="cuda") + 0.5
+    c, v = (torch.randn((n, D), generator=g, device="cuda") for _ in range(2))
+    vw, vb = torch.randn(D, generator=g, device="cuda"), torch.randn(D, generator=g, device="cuda")
+
+    def f(h):
+        out = _empty(n, D, "f32")
+        B.tensair_norm(x + h * v, D, w + h * vw, b + h * vb, out)
+        return float((out.double() * c.double()).sum())
+
+    def slope(h):
+        return (f(h) - f(-h)) / (2 * h)
+
+    h = 2.0 ** -5
+    got = (4 * slope(h / 2) - slope(h)) / 3
+    mean, rstd, dx, dw, db = torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), _empty(n, D, "f32"), torch.empty(D, device="cuda"), torch.empty(D, device="cuda")
+    B.tensair_norm(x, D, w, b, _empty(n, D, "f32"), mean, rstd)
+    B.tensair_norm_grad(c, x, D, w, mean, rstd, dx, dw, db, _bytes(B.tensair_norm_workspace_bytes(n, D)))
+    want = float((dx.double() * v.double()).sum() + (dw.double() * vw.double()).sum() + (db.double() * vb.double()).sum())
+    # rounding: 1 920 outputs of size up to 10, each off by some 20 units at random, over h / 2; what is left of the truncation: h^4 times a fifth derivative
+    # of the order of 5! in every one of 40 rows
+    tol = 20 * U32 * 10 * math.sqrt(n * D) * 4 / h + 40 * 120 * h ** 4
+    assert abs(got - want) <= tol and abs(want) > 10 * tol
+
+
+def test_norm_without_rows_and_with_far_rows():
+    e = torch.empty((0, 8), device="cuda")
+    dw, db = torch.ones(8, device="cuda"), torch.ones(8, device="cuda")
+    B.tensair_norm(e, 8, None, None, e, e[:, 0], e[:, 0])
+    B.tensair_norm_grad(e, e, 8, None, torch.empty(0, device="cuda"), torch.empty(0, device="cuda"), e, dw, db, _bytes(B.tensair_norm_workspace_bytes(0, 8)))
+    assert bool((dw == 0).all()) and bool((db == 0).all())
+    # a row of NaN or infinity is a row of NaN, and no other
+    x = torch.randn((9, 64), generator=_gen(1), device="cuda")
+    x[2, 5], x[7, 0] = float("nan"), float("inf")
+    out = torch.empty_like(x)
+    B.tensair_norm(x, 64, None, None, out)
+    bad = torch.zeros(9, dtype=torch.bool, device="cuda")
+    bad[[2, 7]] = True
+    assert torch.equal(out.isnan().any(1), bad) and bool(out[~bad].isfinite().all())
+
+
+def test_norm_rows_far_apart():
+    """Rows whose last offset passes 2^32 bytes, as views of a buffer of 4.3 GB."""
+    n, D, stride = 5, 64, 1 << 28
+    buf = torch.empty((n - 1) * stride + D, dtype=torch.float32, device="cuda")
+    x = buf.as_strided((n, D), (stride, 1))
+    x.copy_(torch.randn((n, D), generator=_gen(4), device="cuda"))
+    near, out = x.contiguous(), torch.empty((n, D), device="cuda")
+    mean, rstd, dx, dx2 = torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), torch.empty((n, D), device="cuda"), torch.empty((n, D), device="cuda")
+    B.tensair_norm(near, D, None, None, out, mean, rstd)
+    got = torch.empty_like(out)
+    B.tensair_norm(x, D, None, None, got)
+    assert torch.equal(got, out)
+    B.tensair_norm_grad(out, near, D, None, mean, rstd, dx)
+    B.tensair_norm_grad(out, x, D, None, mean, rstd, dx2)
+    assert torch.equal(dx, dx2)
+    drop, far = torch.empty((n, D), device="cuda"), x
+    B.tensair_dropout(near, D, drop, 0.5, 1)
+    B.tensair_dropout(far, D, got, 0.5, 1)
+    assert torch.equal(drop, got)
+    B.tensair_norm(near, D, None, None, x)
+    assert torch.equal(x.contiguous(), out)
+
+
+# ---------------------------------------------------------------- dropout
+def _philox(c, step, tag, seed):
+    """Words of Philox4x32-10 (Salmon et al., 2011), by whole 64-bit products on the host."""
+    c = c.astype(np.uint64)
+    low = np.uint64(0xFFFFFFFF)
+    a = [c & low, c >> np.uint64(32), np.full_like(c, step & 0xFFFFFFFF), np.full_like(c, tag & 0xFFFFFFFF)]
+    k0, k1 = seed & 0xFFFFFFFF, seed >> 32
+    for _ in range(10):
+        p, q = a[0] * np.uint64(0xD2511F53), a[2] * np.uint64(0xCD9E8D57)
+        a = [(q >> np.uint64(32)) ^ a[1] ^ np.uint64(k0), q & low, (p >> np.uint64(32)) ^ a[3] ^ np.uint64(k1), p & low]
+        k0, k1 = (k0 + 0x9E3779B9) & 0xFFFFFFFF, (k1 + 0xBB67AE85) & 0xFFFFFFFF
+    return np.stack(a, 1)
+
+
+def _kept(n, D, p, seed, layer, step):
+    words = _philox(np.arange(n * D // 4), step, 0x44524F50 + layer, seed).reshape(n, D)
+    return torch.from_numpy(words >= np.uint64(math.floor(p * 2.0 ** 32))).cuda()
+
+
+def _dropped(x, keep, p, residual, dtype):
+    """In the order of the definition: every operation rounded by itself."""
+    y = torch.where(keep, x.float() * torch.tensor(np.float32(1 / (1 - p)), device="cuda"), 0.0)
+    return (y if residual is None else residual.float() + y).to(dtype)
+
+
+@pytest.mark.parametrize("n,D,dtype,out,pad,p", [(1, 4, "f32", "f32", 0, 0.5), (1_024, 128, "f32", "f32", 0, 0.1), (777, 300, "bf16", "f32", 20, 0.3),
+                                                 (1_000, 20, "f32", "bf16", 4, 0.75), (333, 1_024, "bf16", "bf16", 0, 0.9), (5_001, 4, "bf16", "bf16", 0, 0.0),
+                                                 (50, 260, "f32", "f32", 8, 1 - 2.0 ** -30)])
+@pytest.mark.parametrize("add", [True, False])
+def test_dropout(n, D, dtype, out, pad, p, add):
+    g, seed, layer, step = _gen(n + D), 0xFEDCBA9876543210, 3, 2 ** 40 + 17
+    x, residual, got = _rows(g, n, D, dtype, pad), _rows(g, n, D, out, pad) if add else None, _empty(n, D, out, pad)
+    B.tensair_dropout(x, D, got, p, seed, layer, step, residual)
+    keep = _kept(n, D, p, seed, layer, step)
+    want = _dropped(x[:, :D], keep, p, residual[:, :D] if add else None, DT[out])
+    assert torch.equal(got[:, :D], want) and bool((got[:, D:] == MARK).all())
+    if dtype == out:
+        B.tensair_dropout(x, D, x, p, seed, layer, step, residual)                 # in place
+        assert torch.equal(x[:, :D], want)
+    if add:
+        B.tensair_dropout(_rows(_gen(n + D), n, D, dtype, pad), D, residual, p, seed, layer, step, residual)
+        assert torch.equal(residual[:, :D], want)
+
+
+def test_dropout_masks():
+    """Dropped elements are 0 whatever they hold; masks of other steps, layers and seeds are others; about p of the elements are dropped."""
+    n, D, p = 2_000, 64, 0.3
+    x = torch.full((n, D), float("nan"), device="cuda")
+    got = torch.empty_like(x)
+    B.tensair_dropout(x, D, got, p, 1)
+    share = 1 - float(got.isnan().float().mean())
+    assert bool((got[~got.isnan()] == 0).all()) and abs(share - p) < 5 * math.sqrt(p * (1 - p) / (n * D))
+    x.fill_(1.0)
+    masks = []
+    for seed, layer, step in ((1, 0, 0), (1, 0, 1), (1, 1, 0), (2, 0, 0), (1 + 2 ** 32, 0, 0)):
+        B.tensair_dropout(x, D, got, p, seed, layer, step)
+        masks.append(got > 0)
+    for i in range(5):
+        for j in range(i):
+            # two independent masks agree in a share 1 - 2 p (1 - p) of the elements
+            assert abs(float((masks[i] == masks[j]).float().mean()) - (1 - 2 * p * (1 - p))) < 5 * 0.5 / math.sqrt(n * D)
+    B.tensair_dropout(x[:0], D, got[:0], p, 1)
+
+
+def test_dropout_gradient_is_the_same_mask():
+    n, D, p = 300, 36, 0.4
+    g = _gen(2)
+    x, d = _rows(g, n, D, "f32"), _rows(g, n, D, "f32")
+    out, dx, r = _empty(n, D, "f32"), _empty(n, D, "f32"), _rows(g, n, D, "f32")
+    B.tensair_dropout(x, D, out, p, 9, 1, 5, r)
+    B.tensair_dropout(d, D, dx, p, 9, 1, 5)
+    # linear in x: <d, out(x) - r> = <dx, x>, both sums of n D products that are off by three roundings each; out carries those of the sum with r
+    lhs, rhs = (d.double() * (out.double() - r.double())).sum(), (dx.double() * x.double()).sum()
+    tol = 3 * U32 * ((d.double() * out.double()).abs().sum() + (d.double() * r.double()).abs().sum() + (dx.double() * x.double()).abs().sum())
+    assert abs(float(lhs - rhs)) <= float(tol)
+
+
+# ---------------------------------------------------------------- recurrence
+def _recur_reference(x, gate, offsets, h0, d=None, d_last=None):
+    """Token by token in 64 bits: (h, h_last, what h may be off by) and, with d, (d_x, d_gate, d_h0, what they may be off by).  A step of the operator
+    rounds a by at most 2 units of its own and (1.5 |gate| + 4) units of exp(-gate), b = 1 - a by 3 and as many, the product and the sum by one each; errors
+    of h go on as h does.  Four times that: tokens are put together tile by tile, with products of the a."""
+    n, D = x.shape
+    S = len(offsets) - 1
+    x, gate = x.double(), gate.double().clamp(-87, None)
+    a = torch.sigmoid(gate)
+    b = torch.sigmoid(-gate)
+    ue = U32 * (1.5 * gate.abs().clamp(max=104) + 4)                # beyond, exp(-gate) is zero, and b with it
+    ua, ub = 2 * U32 + b * ue, 3 * U32 + ue
+    h, eh = torch.zeros_like(x), torch.zeros_like(x)
+    prev = torch.zeros_like(x)
+    eprev = torch.zeros_like(x)
+    last = torch.zeros((S, D), dtype=torch.float64, device="cuda")
+    elast = torch.zeros_like(last)
+    for s in range(S):
+        now = h0[s].double() if h0 is not None else torch.zeros(D, dtype=torch.float64, device="cuda")
+        err = torch.zeros_like(now)
+        for t in range(offsets[s], offsets[s + 1]):
+            prev[t], eprev[t] = now, err
+            new = a[t] * now + b[t] * x[t]
+            err = a[t] * err + (a[t] * now).abs() * ua[t] + (b[t] * x[t]).abs() * (ub[t] + U32) + U32 * new.abs()
+            now = new
+            h[t], eh[t] = now, err
+        last[s], elast[s] = now, err
+    if d is None:
+        return h, last, 4 * eh, 4 * elast
+    l, el = torch.zeros_like(x), torch.zeros_like(x)
+    dh0, edh0 = torch.zeros_like(last), torch.zeros_like(last)
+    for s in range(S):
+        c = d_last[s].double() if d_last is not None else torch.zeros(D, dtype=torch.float64, device="cuda")
+        err = torch.zeros_like(c)
+        for t in range(offsets[s + 1] - 1, offsets[s] - 1, -1):
+            l[t] = d[t].double() + c
+            el[t] = err + U32 * l[t].abs()
+            c = a[t] * l[t]
+            err = a[t] * el[t] + c.abs() * (ua[t] + U32)
+        dh0[s], edh0[s] = c, err
+    dx, e_dx = b * l, b * el + (b * l).abs() * (ub + U32)
+    gap = prev - x
+    dg = l * gap * a * b
+    e_dg = a * b * (gap.abs() * el + l.abs() * (eprev + U32 * gap.abs())) + dg.abs() * (ua + ub + 4 * U32)
+    return dx, dg, dh0, 4 * e_dx, 4 * e_dg, 4 * edh0
+
+
+def _offsets(lengths, first=0):
+    return np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32) + first
+
+
+RECURS = [  # lengths, first row, rows behind, dim, type, pad
+    ([1], 0, 0, 4, "f32", 0), ([255], 0, 0, 36, "bf16", 0), ([256], 0, 0, 64, "f32", 4), ([257], 0, 3, 300, "bf16", 0), ([0, 0, 5, 0, 1, 1, 0], 0, 0, 32, "f32", 0),
+    ([511, 1, 513], 2, 7, 68, "f32", 8), ([1_300], 0, 0, 132, "bf16", 4), ([3] * 100 + [0] * 300 + [2] * 50, 1, 0, 20, "f32", 0), ([256, 256, 0, 256], 0, 0, 128, "bf16", 0),
+    ([700, 0, 30, 1_000], 5, 300, 1_024, "bf16", 0), ([2_900], 100, 1, 8, "f32", 0), ([0, 0], 0, 9, 12, "bf16", 0), ([40, 600], 256, 256, 260, "f32", 0)]
+
+
+def _recur_case(lengths, first, behind, D, dtype, pad, seed, carry=True, slow=True):
+    g = _gen(seed)
+    off = _offsets(lengths, first)
+    n = int(off[-1]) + behind
+    both = _rows(g, n, 2 * D, dtype, pad, 1.5)
+    x, gate = both[:, :D], both[:, D:2 * D]
+    if slow:
+        gate[:, ::3] += 6                                     # channels that remember for hundreds of tokens
+        gate[:, 1::7] -= 20
+    dead = np.ones(n, bool)
+    dead[first:int(off[-1])] = False
+    both[torch.from_numpy(dead).cuda()] = float("nan")        # rows of no sequence must not matter
+    h0 = torch.randn((len(lengths), D), generator=g, device="cuda") if carry else None
+    return g, off, n, x, gate, h0, torch.from_numpy(dead).cuda()
+
+
+@pytest.mark.parametrize("case", RECURS)
+@pytest.mark.parametrize("carry", [True, False])
+def test_recur(case, carry):
+    lengths, first, behind, D, dtype, pad = case
+    g, off, n, x, gate, h0, dead = _recur_case(*case, seed=n_seed(case), carry=carry)
+    S = len(lengths)
+    out, last, status = _empty(n, D, dtype, pad), torch.full((S, D), MARK, device="cuda"), _status()
+    states = torch.full((B.tensair_recur_state_rows(n), D), float("nan"), device="cuda")
+    ws, offsets = _bytes(B.tensair_recur_workspace_bytes(n, D)), torch.from_numpy(off).cuda()
+    B.tensair_recur(x, gate, D, offsets, out, ws, h0, last, states, status)
+    h, want, eh, elast = _recur_reference(x, gate, off.tolist(), h0)
+    live = ~dead
+    _near(out[live][:, :D], h[live], (eh + UNIT[dtype] * (h.abs() + eh))[live], "out")
+    _near(last, want, elast + 1e-30, "h_last")
+    assert bool((out[dead] == MARK).all()) and bool((out[:, D:] == MARK).all()) and int(status) == 0
+    # without what is not wanted: the same bits
+    again = _empty(n, D, dtype, pad)
+    B.tensair_recur(x, gate, D, offsets, again, ws, h0)
+    assert torch.equal(again, out)
+    # gradient
+    d, d_last = _rows(g, n, D, dtype, pad), torch.randn((S, D), generator=g, device="cuda") if carry else None
+    d[dead] = float("nan")
+    d_both, dh0 = _empty(n, 2 * D, dtype, pad), torch.full((S, D), MARK, device="cuda")
+    B.tensair_recur_grad(x, gate, D, offsets, states, d, d_both[:, :D], d_both[:, D:2 * D], ws, h0, d_last, dh0, status)
+    dx, dg, wh, ex, eg, e0 = _recur_reference(x, gate, off.tolist(), h0, d[:, :D], d_last)
+    for got, ref, tol, what in ((d_both[:, :D], dx, ex, "d_x"), (d_both[:, D:2 * D], dg, eg, "d_gate")):
+        _near(got[live], ref[live], (tol + UNIT[dtype] * (ref.abs() + tol))[live] + 1e-37, what)
+    _near(dh0, wh, e0 + 1e-37, "d_h0")
+    assert bool((d_both[dead] == MARK).all()) and bool((d_both[:, 2 * D:] == MARK).all()) and int(status) == 0
+    d2 = _empty(n, 2 * D, dtype, pad)
+    B.tensair_recur_grad(x, gate, D, offsets, states, d, d2[:, :D], d2[:, D:2 * D], ws, h0, d_last)
+    assert torch.equal(d2, d_both)
+
+
+def n_seed(case):
+    return sum(case[0]) + case[3]
+
+
+def test_recur_long_sequence_is_its_parts():
+    """A sequence of 70 000 tokens against the same in parts whose states are handed on, and its gradient against the parts' from behind."""
+    n, D, cuts = 70_000, 40, [0, 1, 300, 20_000, 20_001, 45_555, 70_000]
+    g, off, _, x, gate, h0, _ = _recur_case([n], 0, 0, D, "f32", 0, 11)
+    d, d_last = _rows(g, n, D, "f32", std=1e-2), torch.randn((1, D), generator=g, device="cuda")
+    ws = _bytes(B.tensair_recur_workspace_bytes(n, D))
+
+    def forward(lo, hi, h):
+        o, last, st = _empty(hi - lo, D, "f32"), torch.empty((1, D), device="cuda"), torch.empty((B.tensair_recur_state_rows(hi - lo), D), device="cuda")
+        at = torch.tensor([0, hi - lo], dtype=torch.int32, device="cuda")
+        B.tensair_recur(x[lo:hi], gate[lo:hi], D, at, o, ws, h, last, st)
+        return o, last, st, at
+
+    whole, last, st, at = forward(0, n, h0)
+    dx, dg, dh = (_empty(n, D, "f32") for _ in range(3))
+    dh = torch.empty((1, D), device="cuda")
+    B.tensair_recur_grad(x, gate, D, at, st, d, dx, dg, ws, h0, d_last, dh)
+    h, parts = h0, []
+    for lo, hi in zip(cuts, cuts[1:]):
+        o, nxt, pst, pat = forward(lo, hi, h)
+        parts.append((lo, hi, h, pst, pat, o))
+        h = nxt
+    # states are averages of x and h0 of size about 1; roundings of a remembered for up to 1 / (1 - a) = 3 000 tokens, of random sign; 2^-24 each
+    big = 4 * 3_000 * U32 * float(x.abs().max())
+    assert bool(((torch.cat([p[5] for p in parts]) - whole).abs() <= big).all()) and bool(((h - last).abs() <= big).all())
+    c = d_last
+    for lo, hi, h, pst, pat, _ in reversed(parts):
+        px, pg, ph = _empty(hi - lo, D, "f32"), _empty(hi - lo, D, "f32"), torch.empty((1, D), device="cuda")
+        B.tensair_recur_grad(x[lo:hi], gate[lo:hi], D, pat, pst, d[lo:hi], px, pg, ws, h, c, ph)
+        size = 3_000 * 4 * U32 * 40          # l: sums of up to 3 000 terms of 1e-2, about 10 and less in size
+        assert bool(((px - dx[lo:hi]).abs() <= size).all()) and bool(((pg - dg[lo:hi]).abs() <= size * 8).all())
+        c = ph
+    assert bool(((c - dh).abs() <= size).all())
+
+
+def test_recur_grad_against_differences():
+    n, D, S = 300, 12, 3
+    g, off, _, x, gate, h0, _ = _recur_case([100, 0, 200], 0, 0, D, "f32", 0, 3, slow=False)
+    offsets, ws = torch.from_numpy(off).cuda(), _bytes(B.tensair_recur_workspace_bytes(n, D))
+    c, vx, vg = (torch.randn((n, D), generator=g, device="cuda") for _ in range(3))
+    cl, vh = (torch.randn((S, D), generator=g, device="cuda") for _ in range(2))
+
+    def f(h):
+        out, last = _empty(n, D, "f32"), torch.empty((S, D), device="cuda")
+        B.tensair_recur((x + h * vx).contiguous(), (gate + h * vg).contiguous(), D, offsets, out, ws, h0 + h * vh, last)
+        return float((out.double() * c.double()).sum() + (last.double() * cl.double()).sum())
+
+    def slope(h):
+        return (f(h) - f(-h)) / (2 * h)
+
+    h = 2.0 ** -6
+    got = (4 * slope(h / 2) - slope(h)) / 3
+    states = torch.empty((B.tensair_recur_state_rows(n), D), device="cuda")
+    B.tensair_recur(x, gate, D, offsets, _empty(n, D, "f32"), ws, h0, None, states)
+    dx, dg, dh = _empty(n, D, "f32"), _empty(n, D, "f32"), torch.empty((S, D), device="cuda")
+    B.tensair_recur_grad(x, gate, D, offsets, states, c, dx, dg, ws, h0, cl, dh)
+    want = float((dx.double() * vx.double()).sum() + (dg.double() * vg.double()).sum() + (dh.double() * vh.double()).sum())
+    # 3 600 outputs off by some 20 units of 3, over h / 2; truncation: h^4 times fifth derivatives of at most about 100 in 3 600 outputs at random
+    tol = 20 * U32 * 3 * math.sqrt(n * D) * 4 / h + 100 * math.sqrt(n * D) * h ** 4 * 10
+    assert abs(got - want) <= tol and abs(want) > 10 * tol
+
+
+def test_recur_gates_at_the_ends_and_neighbours_of_nan():
+    """gate = +inf keeps the state, -inf replaces it; NaN stays in its own sequence and behind it."""
+    D, lengths = 16, [300, 400, 290, 0, 300]
+    g, off, n, x, gate, h0, _ = _recur_case(lengths, 0, 0, D, "f32", 0, 8)
+    gate[10], x[10] = float("inf"), 0.0
+    gate[20] = -float("inf")
+    bad = off[1] + 30
+    x[bad, 3] = float("nan")
+    gate[off[2] + 5, 7] = float("nan")
+    out, last, states = _empty(n, D, "f32"), torch.empty((5, D), device="cuda"), torch.empty((B.tensair_recur_state_rows(n), D), device="cuda")
+    ws, offsets = _bytes(B.tensair_recur_workspace_bytes(n, D)), torch.from_numpy(off).cuda()
+    B.tensair_recur(x, gate, D, offsets, out, ws, h0, last, states)
+    assert torch.equal(out[10], out[9])
+    _near(out[20], x[20].double(), 4 * U32 * x[20].double().abs() + 1e-30)
+    want = torch.zeros((n, D), dtype=torch.bool, device="cuda")
+    want[bad:off[2], 3] = True
+    want[off[2] + 5:off[3], 7] = True
+    assert torch.equal(out.isnan(), want)
+    assert last.isnan().nonzero().tolist() == [[1, 3], [2, 7]]
+    d = _rows(g, n, D, "f32")
+    d[off[4] + 10, 2] = float("nan")
+    dx, dg, dh = _empty(n, D, "f32"), _empty(n, D, "f32"), torch.empty((5, D), device="cuda")
+    B.tensair_recur_grad(x, gate, D, offsets, states, d, dx, dg, ws, h0, None, dh)
+    want = torch.zeros((n, D), dtype=torch.bool, device="cuda")
+    want[off[4]:off[4] + 11, 2] = True
+    want[off[2]:off[2] + 6, 7] = True                             # l before the NaN of a gate
+    assert torch.equal(dx.isnan(), want)
+
+
+def test_recur_offsets_out_of_order():
+    """Reported, and no fault: nothing outside the buffers is read or written."""
+    D, n = 8, 600
+    g, _, _, x, gate, _, _ = _recur_case([n], 0, 0, D, "f32", 0, 1)
+    ws, states = _bytes(B.tensair_recur_workspace_bytes(n, D)), torch.zeros((B.tensair_recur_state_rows(n), D), device="cuda")
+    for bad in ([0, 400, 300, 600], [-5, 10, 20, 600], [0, 10, 20, 601], [0, 2**31 - 1, -2**31, 600], [600, 0, 0, 0], [-1, -1, -1, -1]):
+        offsets, status = torch.tensor(bad, dtype=torch.int32, device="cuda"), _status()
+        guard = torch.full((3 + 2, D), MARK, device="cuda")
+        out = torch.full((n + 2, D), MARK, device="cuda")
+        B.tensair_recur(x, gate, D, offsets, out[1:-1], ws, None, guard[1:-1], states, status)
+        assert int(status) == 2 and bool((guard[[0, -1]] == MARK).all()) and bool((out[[0, -1]] == MARK).all()), bad
+        status.zero_()
+        dx, dg = out.clone(), out.clone()
+        B.tensair_recur_grad(x, gate, D, offsets, states, x.contiguous(), dx[1:-1], dg[1:-1], ws, None, None, guard[1:-1], status)
+        assert int(status) == 2 and bool((dx[[0, -1]] == MARK).all()) and bool((dg[[0, -1]] == MARK).all()), bad
+
+
+def test_recur_nothing():
+    e = torch.empty((0, 8), device="cuda")
+    ws = _bytes(B.tensair_recur_workspace_bytes(0, 8))
+    h0, last = torch.randn((2, 8), generator=_gen(1), device="cuda"), torch.empty((2, 8), device="cuda")
+    B.tensair_recur(e, e, 8, torch.zeros(3, dtype=torch.int32, device="cuda"), e, ws, h0, last)
+    assert torch.equal(last, h0)
+    dh = torch.empty((2, 8), device="cuda")
+    B.tensair_recur_grad(e, e, 8, torch.zeros(3, dtype=torch.int32, device="cuda"), torch.empty((1, 8), device="cuda"), e, e, e, ws, h0, last, dh)
+    assert torch.equal(dh, last)
+    B.tensair_recur(e, e, 8, torch.zeros(1, dtype=torch.int32, device="cuda"), e, ws)
+
+
+@pytest.mark.parametrize("n,D,dtype,slots", [(1, 4, "f32", 1), (64, 256, "bf16", 256), (33, 300, "f32", 100), (500, 20, "bf16", 7), (3, 1_024, "f32", None), (700, 64, "bf16", None)])
+def test_recur_step(n, D, dtype, slots):
+    """Rows of the same slot follow one another (500 rows of 7 slots); slots out of range; the same against the recurrence over whole sequences."""
+    g, _, _, x, gate, _, _ = _recur_case([n], 0, 0, D, dtype, 0, n)
+    total = slots or n + 2
+    state = torch.randn((total, D + 4), generator=g, device="cuda")
+    before = state.clone()
+    at = torch.randint(0, slots, (n,), generator=g, device="cuda", dtype=torch.int32) if slots else None
+    if slots and n > 20:
+        at[5], at[20] = -1, slots
+    out, status = _empty(n, D, dtype), _status()
+    B.tensair_recur_step(x, gate, D, state, out, at, status)
+    where = at.tolist() if slots else list(range(n))
+    by = {}
+    for i, s in enumerate(where):
+        by.setdefault(s, []).append(i)
+    want_state = before.clone().double()
+    for s, rows in by.items():
+        if not 0 <= s < total:
+            assert bool((out[rows] == 0).all())
+            continue
+        h, last, eh, elast = _recur_reference(x[rows], gate[rows], [0, len(rows)], before[s:s + 1, :D])
+        _near(out[rows], h, eh + UNIT[dtype] * (h.abs() + eh), "out")
+        _near(state[s, :D], last[0], elast[0] + 1e-30, "state")
+        want_state[s] = state[s].double()
+    assert torch.equal(state.double(), want_state) and torch.equal(state[:, D:], before[:, D:])     # other states and what lies beside them
+    assert int(status) == (1 if slots and n > 20 else 0)
+    state2 = before.clone()
+    B.tensair_recur_step(x, gate, D, state2, None, at)
+    assert torch.equal(state2, state)
+
+
+# ---------------------------------------------------------------- drawing words
+def _draw_reference(z, T, k, p, m, u):
+    """One row in 64 bits, from the definition."""
+    V = len(z)
+    z = np.where(np.isnan(z), -np.inf, z.astype(np.float64))
+    order = np.argsort(-z, kind="stable")
+    if z[order[0]] == -np.inf:
+        return -1, 0.0
+    if not T > 0:
+        return int(order[0]), 1.0
+    with np.errstate(all="ignore"):
+        w = np.exp((z[order] - z[order[0]]) / T)
+    w = np.where(z[order] == z[order[0]], 1.0, np.where(z[order] == -np.inf, 0.0, np.where(np.isnan(w), 0.0, w)))
+    keep = np.arange(V) < (k if k >= 1 else V)
+    if p < 1 or p != p:
+        mass = np.concatenate([[0.0], np.cumsum(np.where(keep, w, 0.0))])
+        keep &= mass[:-1] < (p if p > 0 else 0.0) * mass[-1]
+        keep[0] = True
+    m = min(m, 1.0) if m == m else 0.0
+    keep &= w >= m
+    back = np.zeros(V)
+    back[order] = np.where(keep, w, 0.0)
+    run = np.cumsum(back)
+    target = min(max(u, 0.0), 1.0) * run[-1] if u == u else 0.0
+    above = np.nonzero((run > target) & (back > 0))[0]
+    v = int(above[0]) if len(above) else int(np.nonzero(back)[0][-1])
+    return v, back[v] / run[-1]
+
+
+def _draw(logits, V, **rows):
+    n = logits.shape[0]
+    words, prob, status = torch.full((n,), -7, dtype=torch.int32, device="cuda"), torch.full((n,), -7.0, device="cuda"), _status()
+    args = {k: torch.tensor(v, dtype=torch.int32 if k == "top_k" else torch.float32, device="cuda") for k, v in rows.items()}
+    B.tensair_sample(logits, V, args.pop("u"), words, _bytes(B.tensair_sample_workspace_bytes(n, V)), prob=prob, status=status, **args)
+    return words, prob, status
+
+
+def _check_draw(logits, V, T, k, p, m, u, status=0):
+    words, prob, st = _draw(logits, V, temperature=T, top_k=k, top_p=p, min_p=m, u=u)
+    z = logits[:, :V].float().cpu().numpy()
+    f = np.float32
+    for i in range(len(u)):
+        v, q = _draw_reference(z[i], float(f(T[i])), int(k[i]), float(f(p[i])), float(f(m[i])), float(f(u[i])))
+        assert int(words[i]) == v, (i, V, T[i], k[i], p[i], m[i], u[i], int(words[i]), v)
+        # the weight and the sum are in 64 bits; one rounding to fp32
+        assert abs(float(prob[i]) - q) <= 2 * U32 * q, (i, float(prob[i]), q)
+    assert int(st) == status
+
+
+@pytest.mark.parametrize("V,n,dtype,pad", [(1, 3, "f32", 0), (2, 40, "bf16", 1), (7, 60, "f32", 0), (1_000, 60, "bf16", 24), (4_099, 40, "f32", 0), (50_001, 30, "bf16", 0),
+                                           (100_003, 24, "f32", 5), (262_147, 6, "bf16", 0)])
+def test_sample(V, n, dtype, pad):
+    """Rows with filters of their own, in every combination; logits that spread by two, and by one hundredth."""
+    g, r = _gen(V), np.random.RandomState(V)
+    z = _rows(g, n, V, dtype, pad, 2.0)
+    z[n // 2:] *= 5e-3
+    pick = lambda *v: np.array([v[j] for j in r.randint(0, len(v), n)])      # noqa: E731
+    _check_draw(z, V, pick(0.0, 0.5, 1.0, 1.7), pick(0, 1, 5, 50, 3_000, V), pick(1.0, 0.9, 0.5, 0.05), pick(0.0, 0.0, 0.1, 0.9), r.rand(n))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [9, 5_000, 70_000])
+def test_sample_equal_logits(V, dtype):
+    """Rows of one value, of two, and of few: the border falls among equal words, and the first ones are in."""
+    r = np.random.RandomState(1)
+    z = torch.zeros((12, V), dtype=DT[dtype], device="cuda")
+    z[1] = -3.0
+    z[2, V // 2:] = 1.0
+    z[3, ::3] = 2.0
+    z[4] = torch.from_numpy(r.randint(0, 3, V)).cuda().to(DT[dtype])
+    z[5, V - 1] = 9.0
+    z[6, 0] = -0.0
+    z[7] = torch.from_numpy(r.randint(0, 3, V)).cuda().to(DT[dtype]) * 1e-3
+    z[8] = 1e30
+    z[9] = -1e30
+    z[10] = torch.arange(V, device="cuda").to(DT[dtype]) * -1e-3
+    z[11] = torch.from_numpy(r.randint(0, 3, V)).cuda().to(DT[dtype]) * 1e20
+    for k, p in ((0, 1.0), (5, 1.0), (V // 2 + 1, 1.0), (0, 0.25), (7, 0.5), (V - 1, 0.75)):
+        _check_draw(z, V, np.ones(12), np.full(12, k), np.full(12, p), np.zeros(12), r.rand(12))
+
+
+def test_sample_masked_rows_and_ends():
+    inf, nan = float("inf"), float("nan")
+    V, low = 6_000, float(torch.finfo(torch.float32).min)
+    z = torch.randn((11, V), generator=_gen(3), device="cuda")
+    z[0] = -inf                                   # nothing is left
+    z[1] = nan
+    z[2, :] = -inf
+    z[2, 4_321] = -50.0                           # one word is left
+    z[3, ::2] = nan
+    z[4, 100] = z[4, 5_000] = inf                 # these two share all weight
+    z[5] = low                                    # a mask of the lowest value everywhere: all words are equal
+    z[6, :V - 3] = low
+    z[7] = -inf
+    z[7, 0] = z[7, V - 1] = 0.0
+    r = np.random.RandomState(0)
+    for T, k, p, m in ((1.0, 0, 1.0, 0.0), (0.7, 3, 0.9, 0.0), (2.0, 0, 0.5, 0.3), (0.0, 9, 0.1, 1.0), (1e-30, 0, 0.9, 0.0), (1e30, 0, 0.5, 0.0), (1.0, 0, 0.9, 2.0), (inf, 0, 0.3, 0.0),
+                       (nan, 4, nan, nan), (1.0, -3, 7.0, -1.0), (1.0, 0, 0.0, 0.0), (1.0, 10 ** 9, -1.0, 0.0)):
+        for u in (r.rand(11), np.zeros(11), np.ones(11), np.full(11, 1 - 2.0 ** -24), np.full(11, -1.0), np.full(11, nan)):
+            _check_draw(z, V, np.full(11, T), np.full(11, k), np.full(11, p), np.full(11, m), u, status=1)
+    words, prob, status = _draw(z[2:], V, u=r.rand(9))             # nothing but the random numbers
+    ref = [_draw_reference(z[i].cpu().numpy(), 1.0, 0, 1.0, 0.0, 0.0) for i in range(2, 11)]
+    assert int(status) == 0 and len(ref) == 9
+    _draw(z[:0], V, u=np.zeros(0))
+
+
+def test_sample_frequencies():
+    """Draws at evenly spaced u give every word its probability to within a draw, in the words' order."""
+    V, n = 500, 20_000
+    row = torch.randn(V, generator=_gen(9), device="cuda") * 2
+    z = row[None].expand(n, V).contiguous()
+    words, prob, _ = _draw(z, V, u=(np.arange(n) + 0.5) / n)
+    p = torch.softmax(row.double(), 0)
+    count = torch.bincount(words.long(), minlength=V).double()
+    assert bool(((count - n * p).abs() <= 1.01).all()) and bool((words[1:] >= words[:-1]).all())      # u is rounded to fp32
+    _near(prob, p[words.long()], 2 * U32 * p[words.long()])
