@@ -510,6 +510,7 @@ int tensair_dropout(const void *x, int32_t dtype, int64_t x_stride, int64_t n, i
  * a result nor written.  Offsets out of this order never fault: bit 2 is OR-ed into *status, and no output of the call is to be used.
  * states: fp32 [tensair_recur_state_rows(n)][dim], what the gradient needs of the states; NULL: no gradient is wanted.
  * workspace: DEVICE, 256-byte aligned, of tensair_recur_workspace_bytes; holds nothing between calls; serves both calls and fewer rows, too. */
+#define TENSAIR_MAX_RECUR_STRIDE 1048576 /* 2^20, of the matrices of tensair_recur and tensair_recur_grad */
 int64_t tensair_recur_state_rows(int64_t n);
 size_t tensair_recur_workspace_bytes(int64_t n, int32_t dim);
 int tensair_recur(const void *x, int64_t x_stride, const void *gate, int64_t gate_stride, int32_t dtype, int64_t n,

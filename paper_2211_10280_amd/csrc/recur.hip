@@ -26,21 +26,39 @@ struct RecurArgs {
     int *status;
 };
 
-// a = 1 / (1 + exp(-g)) and b = 1 - a without the difference
-__device__ __forceinline__ void gate2(float g, float &a, float &b)
+// a = 1 / (1 + exp(-g)) and b = 1 - a as one number: the smaller of the two, e / (1 + e) with e = exp(-|g|), with g's sign, which says which of them it is.  The larger is
+// 1 - that, within half a unit whatever the smaller one's last places are.
+__device__ __forceinline__ float gate1(float g)
 {
-    const float e = __expf(-(g < -87.f ? -87.f : g)), d = 1.0f + e, r = __builtin_amdgcn_rcpf(d);
-    a = fmaf(r, fmaf(-d, r, 1.0f), r);           // the reciprocal to half a unit: a is multiplied by itself for thousands of tokens
-    b = e * a;
+    const float e = __builtin_amdgcn_exp2f(fabsf(g) * -1.44269504f);
+    return copysignf(e * __builtin_amdgcn_rcpf(1.0f + e), g);
 }
-__device__ __forceinline__ void gate4(float4 g, float4 &a, float4 &b)
+__device__ __forceinline__ void open2(float s, float &a, float &b)
 {
-    gate2(g.x, a.x, b.x);
-    gate2(g.y, a.y, b.y);
-    gate2(g.z, a.z, b.z);
-    gate2(g.w, a.w, b.w);
+    const float small = fabsf(s), large = 1.0f - small;
+    const bool low = __float_as_int(s) < 0;
+    a = low ? small : large;
+    b = low ? large : small;
 }
+__device__ __forceinline__ float4 gate4(float4 g) { return make_float4(gate1(g.x), gate1(g.y), gate1(g.z), gate1(g.w)); }
+__device__ __forceinline__ void open4(float4 s, float4 &a, float4 &b)
+{
+    open2(s.x, a.x, b.x);
+    open2(s.y, a.y, b.y);
+    open2(s.z, a.z, b.z);
+    open2(s.w, a.w, b.w);
+}
+__device__ __forceinline__ void gate4(float4 g, float4 &a, float4 &b) { open4(gate4(g), a, b); }
 __device__ __forceinline__ float4 fma4(float4 a, float4 b, float4 c) { return make_float4(fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y), fmaf(a.z, b.z, c.z), fmaf(a.w, b.w, c.w)); }
+
+// rounded to nearest even by the hardware's conversion of two
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void put4(float *p, float4 v) { st4(p, v); }
+__device__ __forceinline__ void put4(bf16_t *p, float4 v)
+{
+    const bf16x2 lo = {(__bf16)v.x, (__bf16)v.y}, hi = {(__bf16)v.z, (__bf16)v.w};
+    *reinterpret_cast<uint2 *>(p) = make_uint2(__builtin_bit_cast(u32, lo), __builtin_bit_cast(u32, hi));
+}
 
 // ---- tiles.  The tokens are cut into tiles of RECUR_TILE whatever the sequences are: a sequence's first token resets the state, which is all that a tile has to know of
 // them.  A workgroup has a tile's 4 * G channels; a thread has RECUR_RUN tokens that follow one another (a strand of G threads has their channels), in registers from load to
@@ -84,12 +102,14 @@ struct TileLds {
     static constexpr int WAVES = RECUR_STRANDS * G / WAVE;
     float4 p[WAVES][G], q[WAVES][G];
     int reset[WAVES][G];
-    float4 carry[G];
-    int head[RECUR_TILE], tail[RECUR_TILE];      // the sequence whose first / last token this is, or -1
+    float4 carry[G], own_p[G], own_q[G];
+    int said[G];
+    int head[RECUR_TILE], tail[RECUR_TILE];      // the sequence whose first / last token this is
+    u32 heads[RECUR_STRANDS], tails[RECUR_STRANDS];   // the strands' tokens that are one, as bits; only there the above holds
     int tile;
 };
 
-// The map of all strands before a thread's own (REV: behind it, put together from behind), and of all strands.
+// The map of all strands before a thread's own (REV: behind it, put together from behind); `all`: with its own, so the last strand's is that of the tile.
 template <int G, bool REV>
 __device__ __forceinline__ Map strands_before(Map m, TileLds<G> &lds, Map &all)
 {
@@ -109,15 +129,13 @@ __device__ __forceinline__ Map strands_before(Map m, TileLds<G> &lds, Map &all)
         lds.reset[wave][l] = m.reset;
     }
     __syncthreads();
-    Map run = map_none(), mine = map_none();
-#pragma unroll
-    for (int k = 0; k < WAVES; ++k) {
+    Map run = map_none();
+    for (int k = 0; k < (REV ? WAVES - 1 - wave : wave); ++k) {
         const int w = REV ? WAVES - 1 - k : k;
-        if (w == wave) mine = run;
         run = then(run, Map{lds.p[w][l], lds.q[w][l], lds.reset[w][l]});
     }
-    all = run;
-    return then(mine, before);
+    all = then(run, m);
+    return then(run, before);
 }
 
 // ---- the chain of tiles: every tile publishes its map, the last of every RECUR_GROUP its state, each word with its value in it (0: not yet), so that no order of two
@@ -147,24 +165,34 @@ __device__ __forceinline__ void put_state(u64 *at, float4 h)
 }
 __device__ __forceinline__ float low_float(u64 w) { return __uint_as_float((u32)w); }
 
-// The state that comes into the v'th tile (from the left, or, for the gradient, from the right), where it is `wanted`; `own`: the tile's map.
-template <int G>
-__device__ __forceinline__ float4 chain_state(const Chain &ch, int v, const Map &own, bool wanted, int col, int C4, TileLds<G> &lds)
+// The v'th tile's map, which its last strand has, to the others; its state too where nothing is waited for.
+template <int G, bool REV>
+__device__ __forceinline__ void chain_say(const Chain &ch, int v, const Map &own, bool wanted, int col, int C4, TileLds<G> &lds)
 {
-    const int strand = (int)threadIdx.x / G, l = (int)threadIdx.x % G, D = 4 * C4, first = v / RECUR_GROUP * RECUR_GROUP;
-    const bool last = v % RECUR_GROUP == RECUR_GROUP - 1, live = col < C4;
-    wanted = wanted && v > 0;
-    if (strand == 0 && live) {
-        u64 *at = ch.maps + (size_t)v * D + 4 * col;
-        put_word(at, map_word(own.p.x, own.reset), own.q.x);
-        put_word(at + 1, map_word(own.p.y, own.reset), own.q.y);
-        put_word(at + 2, map_word(own.p.z, own.reset), own.q.z);
-        put_word(at + 3, map_word(own.p.w, own.reset), own.q.w);
-        if (last && (own.reset || !wanted)) put_state(ch.states + (size_t)(v / RECUR_GROUP) * D + 4 * col, own.q);
+    const int strand = REV ? RECUR_STRANDS - 1 - (int)threadIdx.x / G : (int)threadIdx.x / G, l = (int)threadIdx.x % G, D = 4 * C4;
+    if (strand < RECUR_STRANDS - 1 || col >= C4) return;
+    u64 *at = ch.maps + (size_t)v * D + 4 * col;
+    put_word(at, map_word(own.p.x, own.reset), own.q.x);
+    put_word(at + 1, map_word(own.p.y, own.reset), own.q.y);
+    put_word(at + 2, map_word(own.p.z, own.reset), own.q.z);
+    put_word(at + 3, map_word(own.p.w, own.reset), own.q.w);
+    if (v % RECUR_GROUP < RECUR_GROUP - 1) return;
+    if (own.reset || !wanted || v == 0) {
+        put_state(ch.states + (size_t)(v / RECUR_GROUP) * D + 4 * col, own.q);
+    } else {                                     // a thread's own words, for itself
+        lds.own_p[l] = own.p;
+        lds.own_q[l] = own.q;
     }
-    if (!wanted) return make_float4(0.f, 0.f, 0.f, 0.f);
+    lds.said[l] = own.reset || !wanted || v == 0;
+}
+// The state that comes into the v'th tile (from the left, or, for the gradient, from the right), where it is `wanted`.
+template <int G, bool REV>
+__device__ __forceinline__ float4 chain_state(const Chain &ch, int v, bool wanted, int col, int C4, TileLds<G> &lds)
+{
+    const int strand = REV ? RECUR_STRANDS - 1 - (int)threadIdx.x / G : (int)threadIdx.x / G, l = (int)threadIdx.x % G, D = 4 * C4, first = v / RECUR_GROUP * RECUR_GROUP;
+    if (!wanted || v == 0) return make_float4(0.f, 0.f, 0.f, 0.f);
     Map m = map_none(), all;
-    if (strand < v - first && live) {
+    if (strand < v - first && col < C4) {
         const u64 *at = ch.maps + (size_t)(first + strand) * D + 4 * col;
         const u64 a = wait_word(at), b = wait_word(at + 1), c = wait_word(at + 2), d = wait_word(at + 3);
         m.reset = (u32)(a >> 32) == MAP_RESET;
@@ -172,15 +200,15 @@ __device__ __forceinline__ float4 chain_state(const Chain &ch, int v, const Map 
                           __uint_as_float((u32)(d >> 32) & 0x7FFFFFFFu));
         m.q = make_float4(low_float(a), low_float(b), low_float(c), low_float(d));
     }
-    strands_before<G, false>(m, lds, all);
-    if (strand == 0 && live) {
+    strands_before<G, REV>(m, lds, all);
+    if (strand == RECUR_STRANDS - 1 && col < C4) {
         float4 h = make_float4(0.f, 0.f, 0.f, 0.f);
         if (first > 0 && !all.reset) {
             const u64 *at = ch.states + (size_t)(first / RECUR_GROUP - 1) * D + 4 * col;
             h = make_float4(low_float(wait_word(at)), low_float(wait_word(at + 1)), low_float(wait_word(at + 2)), low_float(wait_word(at + 3)));
         }
         h = apply(all, h);
-        if (last && !own.reset) put_state(ch.states + (size_t)(v / RECUR_GROUP) * D + 4 * col, apply(own, h));
+        if (v % RECUR_GROUP == RECUR_GROUP - 1 && !lds.said[l]) put_state(ch.states + (size_t)(v / RECUR_GROUP) * D + 4 * col, fma4(lds.own_p[l], h, lds.own_q[l]));
         lds.carry[l] = h;
     }
     __syncthreads();
@@ -198,7 +226,7 @@ __device__ __forceinline__ void mark_tile(const RecurArgs &a, i64 t0, int tile, 
 {
     constexpr int THREADS = RECUR_STRANDS * G;
     const int t = (int)threadIdx.x;
-    for (int i = t; i < RECUR_TILE; i += THREADS) lds.head[i] = lds.tail[i] = -1;
+    if (t < RECUR_STRANDS) lds.heads[t] = lds.tails[t] = 0;
     if (side == 0 && a.status)
         for (i64 s = (i64)tile * THREADS + t; s < a.n_seq; s += (i64)tiles * THREADS) {
             const int lo = a.offsets[s], hi = a.offsets[s + 1];
@@ -221,8 +249,16 @@ __device__ __forceinline__ void mark_tile(const RecurArgs &a, i64 t0, int tile, 
             const i64 b = a.offsets[s], e = a.offsets[s + 1];
             more = b < t0 + RECUR_TILE;
             if (b < e) {
-                if (b >= t0 && b < t0 + RECUR_TILE) lds.head[b - t0] = (int)s;
-                if (e > t0 && e <= t0 + RECUR_TILE) lds.tail[e - 1 - t0] = (int)s;
+                if (b >= t0 && b < t0 + RECUR_TILE) {
+                    const int at = (int)(b - t0);
+                    lds.head[at] = (int)s;
+                    atomicOr(&lds.heads[at / RECUR_RUN], 1u << at % RECUR_RUN);
+                }
+                if (e > t0 && e <= t0 + RECUR_TILE) {
+                    const int at = (int)(e - 1 - t0);
+                    lds.tail[at] = (int)s;
+                    atomicOr(&lds.tails[at / RECUR_RUN], 1u << at % RECUR_RUN);
+                }
             } else if (b >= t0 && (end || b < t0 + RECUR_TILE)) {            // no tokens: its state goes through
                 float *to = a.dh0 ? a.dh0 : a.h_last;
                 const float *from = a.dh0 ? a.d_last : a.h0;
@@ -238,167 +274,209 @@ __device__ __forceinline__ void mark_tile(const RecurArgs &a, i64 t0, int tile, 
     __syncthreads();
 }
 
-template <typename T> __device__ __forceinline__ typename Raw4<T>::type raw_shut();      // gates that keep the state as it is
-template <> __device__ __forceinline__ float4 raw_shut<float>() { const float inf = __uint_as_float(0x7F800000u); return make_float4(inf, inf, inf, inf); }
-template <> __device__ __forceinline__ uint2 raw_shut<bf16_t>() { return make_uint2(0x7F807F80u, 0x7F807F80u); }
+// Tokens of a tile in a matrix: an address that all threads share and, in 32 bits, places from there.
+struct TileOf {
+    char *p;
+    u32 stride;                  // bytes from token to token
+};
+template <typename T>
+__device__ __forceinline__ TileOf tile_of(const void *p, i64 stride, i64 t0) { return TileOf{(char *)p + t0 * stride * (i64)sizeof(T), (u32)stride * (u32)sizeof(T)}; }
+// A thread's run of tokens, those of no sequence (first..last are of some) as the nearest that is of one: what they hold does not matter, since the sequences' first and last tokens reset what
+// comes before or behind them.  The same for the columns, up to `col`.
+template <typename T>
+__device__ __forceinline__ void load_run(typename Raw4<T>::type (&r)[RECUR_RUN], const TileOf &m, int token, int col, int first, int last)
+{
+#pragma unroll
+    for (int i = 0; i < RECUR_RUN; ++i) r[i] = ldraw((const T *)(m.p + (size_t)((u32)min(max(token + i, first), last) * m.stride + (u32)(4 * sizeof(T)) * (u32)col)));
+}
+template <typename T>
+__device__ __forceinline__ void store_at(const TileOf &m, int token, int col, float4 v) { put4((T *)(m.p + (size_t)((u32)token * m.stride + (u32)(4 * sizeof(T)) * (u32)col)), v); }
+// From here on the compiler takes the values for new ones: it widens and multiplies them again instead of keeping what it has made of them in registers.
+__device__ __forceinline__ void forget(uint2 &v) { asm volatile("" : "+v"(v.x), "+v"(v.y)); }
+__device__ __forceinline__ void forget(float4 &v) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
+__device__ __forceinline__ float4 row_or_zero(const float *p, i64 row, int C4, int col)
+{
+    return p && col < C4 ? ld4(p + row * 4 * C4 + 4 * col) : make_float4(0.f, 0.f, 0.f, 0.f);
+}
 
 template <typename T, int G, bool CHAINED>
-__global__ void __launch_bounds__(RECUR_STRANDS *G) k_recur(RecurArgs a, Chain ch)
+__device__ __forceinline__ void k_recur_tile(const RecurArgs &a, const Chain &ch, int k, int sides, i64 begin, i64 end, TileLds<G> &lds)
 {
-    __shared__ TileLds<G> lds;
-    const int strand = (int)threadIdx.x / G, l = (int)threadIdx.x % G, D = 4 * a.C4;
-    int tile = 0, side = (int)blockIdx.x;
-    if (CHAINED) {
-        if (threadIdx.x == 0) lds.tile = (int)atomicAdd(ch.ticket, 1u);
-        __syncthreads();
-        const int sides = (a.C4 + G - 1) / G;
-        tile = lds.tile / sides;
-        side = lds.tile - tile * sides;
-    }
+    const int strand = (int)threadIdx.x / G, l = (int)threadIdx.x % G;
+    const int tile = CHAINED ? k / sides : 0, side = k - tile * sides;
     const int col = side * G + l;
-    const i64 t0 = (i64)tile * RECUR_TILE, run = t0 + strand * RECUR_RUN;
-    const i64 begin = std::max(0, a.offsets[0]), end = std::min<i64>(a.n, a.offsets[a.n_seq]);
+    const i64 t0 = (i64)tile * RECUR_TILE;
+    const bool mine = col < a.C4;
+    // the tile's tokens that sequences have; where there are none nothing comes through
+    const int from = (int)std::min<i64>(RECUR_TILE, std::max<i64>(0, begin - t0)), to = (int)std::max<i64>(0, std::min<i64>(RECUR_TILE, end - t0));
+    const int token = strand * RECUR_RUN, lo = from - token, hi = to - token, near = min(col, a.C4 - 1);
     typename Raw4<T>::type x[RECUR_RUN], g[RECUR_RUN];
-#pragma unroll
-    for (int i = 0; i < RECUR_RUN; ++i) {
-        const i64 t = run + i;
-        zero_raw(x[i]);
-        g[i] = raw_shut<T>();
-        if (t >= begin && t < end && col < a.C4) {
-            x[i] = ldraw((const T *)a.x + t * a.x_stride + 4 * col);
-            g[i] = ldraw((const T *)a.gate + t * a.g_stride + 4 * col);
-        }
+    if (from < to) {
+        load_run<T>(x, tile_of<T>(a.x, a.x_stride, t0), token, near, from, to - 1);
+        load_run<T>(g, tile_of<T>(a.gate, a.g_stride, t0), token, near, from, to - 1);
     }
     mark_tile<G>(a, t0, tile, ch.tiles, side, lds);
+    if (from >= to) {
+        if (CHAINED) chain_say<G, false>(ch, tile, Map{make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f), 1}, false, col, a.C4, lds);
+        return;
+    }
+    const u32 heads = lds.heads[strand], tails = lds.tails[strand];
+    const bool ends = __any(heads | tails), full = mine && from == 0 && to == RECUR_TILE;
+    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
     float4 f[RECUR_RUN], q[RECUR_RUN];
-    Map m = map_none();
+    Map m = map_none(), all;
+    m.q = zero;
 #pragma unroll
     for (int i = 0; i < RECUR_RUN; ++i) {
         float4 b;
         gate4(widen4(g[i]), f[i], b);
         q[i] = mul4(b, widen4(x[i]));
-        const int s = lds.head[strand * RECUR_RUN + i];
-        if (s >= 0) {
-            if (a.h0 && col < a.C4) q[i] = fma4(f[i], ld4(a.h0 + (i64)s * D + 4 * col), q[i]);
+        if (ends && heads >> i & 1) {
+            q[i] = fma4(f[i], row_or_zero(a.h0, lds.head[strand * RECUR_RUN + i], a.C4, col), q[i]);
             m.reset = 1;
-            m.q = q[i];
-        } else {
-            m.q = fma4(f[i], m.q, q[i]);
-            m.p = mul4(m.p, f[i]);
+            m.q = zero;
         }
+        m.q = fma4(f[i], m.q, q[i]);
+        m.p = mul4(m.p, f[i]);
     }
-    Map all;
     const Map before = strands_before<G, false>(m, lds, all);
     float4 carry = make_float4(0.f, 0.f, 0.f, 0.f);
     if (CHAINED) {
-        const bool wanted = t0 >= begin && t0 < end && lds.head[0] < 0;
-        carry = chain_state<G>(ch, tile, all, wanted, col, a.C4, lds);
-        if (a.states && wanted && strand == 0 && col < a.C4) st4(a.states + (i64)tile * D + 4 * col, carry);
+        const bool wanted = from == 0 && !(lds.heads[0] & 1);
+        chain_say<G, false>(ch, tile, all, wanted, col, a.C4, lds);
+        carry = chain_state<G, false>(ch, tile, wanted, col, a.C4, lds);
+        if (a.states && wanted && strand == 0 && mine) st4(a.states + ((i64)tile * a.C4 + col) * 4, carry);
     }
     float4 h = apply(before, carry);
-    if (col >= a.C4) return;
+    const TileOf out = tile_of<T>(a.out, a.out_stride, t0);
 #pragma unroll
     for (int i = 0; i < RECUR_RUN; ++i) {
-        const i64 t = run + i;
-        if (t < begin || t >= end) continue;
-        h = lds.head[strand * RECUR_RUN + i] >= 0 ? q[i] : fma4(f[i], h, q[i]);
-        st4((T *)a.out + t * a.out_stride + 4 * col, h);
-        const int s = lds.tail[strand * RECUR_RUN + i];
-        if (a.h_last && s >= 0) st4(a.h_last + (i64)s * D + 4 * col, h);
+        if (ends && heads >> i & 1) h = zero;
+        h = fma4(f[i], h, q[i]);
+        if (full || (mine && i >= lo && i < hi)) {
+            store_at<T>(out, token + i, col, h);
+            if (ends && a.h_last && tails >> i & 1) st4(a.h_last + ((i64)lds.tail[strand * RECUR_RUN + i] * a.C4 + col) * 4, h);
+        }
     }
 }
 
 template <typename T, int G, bool CHAINED>
-__global__ void __launch_bounds__(RECUR_STRANDS *G) k_recur_grad(RecurArgs a, Chain ch)
+__global__ void __launch_bounds__(RECUR_STRANDS *G, 4) k_recur(RecurArgs a, Chain ch)
 {
     __shared__ TileLds<G> lds;
-    const int strand = (int)threadIdx.x / G, l = (int)threadIdx.x % G, D = 4 * a.C4;
-    int v = 0, side = (int)blockIdx.x;                         // tiles are taken from behind
+    const i64 begin = std::max(0, a.offsets[0]), end = std::min<i64>(a.n, a.offsets[a.n_seq]);
+    int k = (int)blockIdx.x;
     if (CHAINED) {
         if (threadIdx.x == 0) lds.tile = (int)atomicAdd(ch.ticket, 1u);
         __syncthreads();
-        const int sides = (a.C4 + G - 1) / G;
-        v = lds.tile / sides;
-        side = lds.tile - v * sides;
+        k = uniform(lds.tile);
     }
+    k_recur_tile<T, G, CHAINED>(a, ch, k, (a.C4 + G - 1) / G, begin, end, lds);
+}
+
+template <typename T, int G, bool CHAINED>
+__device__ __forceinline__ void k_recur_grad_tile(const RecurArgs &a, const Chain &ch, int k, int sides, i64 begin, i64 end, TileLds<G> &lds, typename Raw4<T>::type (&kept_d)[RECUR_RUN][RECUR_STRANDS * G])
+{
+    const int strand = (int)threadIdx.x / G, l = (int)threadIdx.x % G;
+    const int v = CHAINED ? k / sides : 0, side = k - v * sides;                         // tiles are taken from behind
     const int tile = ch.tiles - 1 - v, col = side * G + l;
-    const i64 t0 = (i64)tile * RECUR_TILE, run = t0 + strand * RECUR_RUN;
-    const i64 begin = std::max(0, a.offsets[0]), end = std::min<i64>(a.n, a.offsets[a.n_seq]);
+    const i64 t0 = (i64)tile * RECUR_TILE;
+    const bool mine = col < a.C4;
+    // the tile's tokens that sequences have; where there are none nothing comes through
+    const int from = (int)std::min<i64>(RECUR_TILE, std::max<i64>(0, begin - t0)), to = (int)std::max<i64>(0, std::min<i64>(RECUR_TILE, end - t0));
+    const int token = strand * RECUR_RUN, lo = from - token, hi = to - token, near = min(col, a.C4 - 1);
     typename Raw4<T>::type x[RECUR_RUN], g[RECUR_RUN], d[RECUR_RUN];
-#pragma unroll
-    for (int i = 0; i < RECUR_RUN; ++i) {
-        const i64 t = run + i;
-        zero_raw(x[i]);
-        zero_raw(d[i]);
-        g[i] = raw_shut<T>();
-        if (t >= begin && t < end && col < a.C4) {
-            x[i] = ldraw((const T *)a.x + t * a.x_stride + 4 * col);
-            g[i] = ldraw((const T *)a.gate + t * a.g_stride + 4 * col);
-            d[i] = ldraw((const T *)a.d + t * a.d_stride + 4 * col);
-        }
+    if (from < to) {
+        load_run<T>(x, tile_of<T>(a.x, a.x_stride, t0), token, near, from, to - 1);
+        load_run<T>(g, tile_of<T>(a.gate, a.g_stride, t0), token, near, from, to - 1);
+        load_run<T>(d, tile_of<T>(a.d, a.d_stride, t0), token, near, from, to - 1);
     }
     mark_tile<G>(a, t0, tile, ch.tiles, side, lds);
-    // the states again: from the one that the forward pass left before the tile
-    float4 f[RECUR_RUN], b[RECUR_RUN], w[RECUR_RUN];
-    Map m = map_none(), all;
+    if (from >= to) {
+        if (CHAINED) chain_say<G, true>(ch, v, Map{make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f), 1}, false, col, a.C4, lds);
+        return;
+    }
+    const u32 heads = lds.heads[strand], tails = lds.tails[strand];
+    const bool ends = __any(heads | tails), full = mine && from == 0 && to == RECUR_TILE;
+#pragma unroll
+    for (int i = 0; i < RECUR_RUN; ++i) kept_d[i][threadIdx.x] = d[i];
+    // two maps of the run: of the state, from the left, and of c = a l, which a token hands on to the one before, from the right
+    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+    float4 s[RECUR_RUN], w[RECUR_RUN], f, b;
+    Map m = map_none(), n = map_none(), all;
 #pragma unroll
     for (int i = 0; i < RECUR_RUN; ++i) {
-        gate4(widen4(g[i]), f[i], b[i]);
-        float4 q = mul4(b[i], widen4(x[i]));
-        const int s = lds.head[strand * RECUR_RUN + i];
-        if (s >= 0) {
-            if (a.h0 && col < a.C4) q = fma4(f[i], ld4(a.h0 + (i64)s * D + 4 * col), q);
+        s[i] = gate4(widen4(g[i]));
+        open4(s[i], f, b);
+        if (ends && heads >> i & 1) {
             m.reset = 1;
-            m.q = q;
-        } else {
-            m.q = fma4(f[i], m.q, q);
-            m.p = mul4(m.p, f[i]);
+            m.q = row_or_zero(a.h0, lds.head[strand * RECUR_RUN + i], a.C4, col);
         }
+        m.q = fma4(f, m.q, mul4(b, widen4(x[i])));
+        m.p = mul4(m.p, f);
     }
-    const Map before = strands_before<G, false>(m, lds, all);
-    float4 h = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (CHAINED && t0 >= begin && t0 < end && lds.head[0] < 0 && col < a.C4) h = ld4(a.kept + (i64)tile * D + 4 * col);
-    h = apply(before, h);
+#pragma unroll
+    for (int i = RECUR_RUN - 1; i >= 0; --i) {
+        forget(s[i]);
+        open4(s[i], f, b);
+        if (ends && tails >> i & 1) {
+            n.reset = 1;
+            n.q = row_or_zero(a.d_last, lds.tail[strand * RECUR_RUN + i], a.C4, col);
+        }
+        n.q = mul4(f, plus4(widen4(kept_d[i][threadIdx.x]), n.q));
+    }
+    n.p = m.p;
+#pragma unroll
+    for (int i = 0; i < RECUR_RUN; ++i) {
+        forget(s[i]);
+        forget(x[i]);
+    }
+    float4 h = zero, c = zero;
+    if (CHAINED && from == 0 && !(lds.heads[0] & 1) && mine) h = ld4(a.kept + ((i64)tile * a.C4 + col) * 4);
+    h = apply(strands_before<G, false>(m, lds, all), h);
+    const Map behind = strands_before<G, true>(n, lds, all);
+    const bool wanted = to == RECUR_TILE && t0 + RECUR_TILE < end && !(lds.tails[RECUR_STRANDS - 1] >> (RECUR_RUN - 1));
+    if (CHAINED) chain_say<G, true>(ch, v, all, wanted, col, a.C4, lds);
 #pragma unroll
     for (int i = 0; i < RECUR_RUN; ++i) {                      // w = (h[t - 1] - x) a
-        const int s = lds.head[strand * RECUR_RUN + i];
         const float4 in = widen4(x[i]);
-        if (s >= 0) h = a.h0 && col < a.C4 ? ld4(a.h0 + (i64)s * D + 4 * col) : make_float4(0.f, 0.f, 0.f, 0.f);
-        w[i] = mul4(f[i], make_float4(h.x - in.x, h.y - in.y, h.z - in.z, h.w - in.w));
-        h = fma4(f[i], h, mul4(b[i], in));
+        if (ends && heads >> i & 1) h = row_or_zero(a.h0, lds.head[strand * RECUR_RUN + i], a.C4, col);
+        open4(s[i], f, b);
+        w[i] = mul4(f, make_float4(h.x - in.x, h.y - in.y, h.z - in.z, h.w - in.w));
+        h = fma4(f, h, mul4(b, in));
+        forget(s[i]);
+        forget(w[i]);
     }
-    // c = a l, handed on to the token before
-    m = map_none();
-#pragma unroll
-    for (int i = RECUR_RUN - 1; i >= 0; --i) {
-        const int s = lds.tail[strand * RECUR_RUN + i];
-        if (s >= 0) {
-            m.reset = 1;
-            m.q = a.d_last && col < a.C4 ? ld4(a.d_last + (i64)s * D + 4 * col) : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-        m.q = mul4(f[i], plus4(widen4(d[i]), m.q));
-        m.p = mul4(m.p, f[i]);
-    }
-    const Map behind = strands_before<G, true>(m, lds, all);
-    float4 c = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (CHAINED) {
-        const i64 t1 = t0 + RECUR_TILE;
-        c = chain_state<G>(ch, v, all, t1 > begin && t1 < end && lds.tail[RECUR_TILE - 1] < 0, col, a.C4, lds);
-    }
+    if (CHAINED) c = chain_state<G, true>(ch, v, wanted, col, a.C4, lds);
     c = apply(behind, c);
-    if (col >= a.C4) return;
+    const TileOf dx = tile_of<T>(a.dx, a.dx_stride, t0), dg = tile_of<T>(a.dg, a.dg_stride, t0);
 #pragma unroll
     for (int i = RECUR_RUN - 1; i >= 0; --i) {
-        const i64 t = run + i;
-        if (t < begin || t >= end) continue;
-        const int tail = lds.tail[strand * RECUR_RUN + i], head = lds.head[strand * RECUR_RUN + i];
-        if (tail >= 0) c = a.d_last ? ld4(a.d_last + (i64)tail * D + 4 * col) : make_float4(0.f, 0.f, 0.f, 0.f);
-        const float4 lam = plus4(widen4(d[i]), c), dx = mul4(b[i], lam);
-        st4((T *)a.dx + t * a.dx_stride + 4 * col, dx);
-        st4((T *)a.dg + t * a.dg_stride + 4 * col, mul4(dx, w[i]));
-        c = mul4(f[i], lam);
-        if (a.dh0 && head >= 0) st4(a.dh0 + (i64)head * D + 4 * col, c);
+        if (ends && tails >> i & 1) c = row_or_zero(a.d_last, lds.tail[strand * RECUR_RUN + i], a.C4, col);
+        open4(s[i], f, b);
+        const float4 lam = plus4(widen4(kept_d[i][threadIdx.x]), c), o = mul4(b, lam);
+        c = mul4(f, lam);
+        if (full || (mine && i >= lo && i < hi)) {
+            store_at<T>(dx, token + i, col, o);
+            store_at<T>(dg, token + i, col, mul4(o, w[i]));
+            if (ends && a.dh0 && heads >> i & 1) st4(a.dh0 + ((i64)lds.head[strand * RECUR_RUN + i] * a.C4 + col) * 4, c);
+        }
     }
+}
+
+template <typename T, int G, bool CHAINED>
+__global__ void __launch_bounds__(RECUR_STRANDS *G, sizeof(T) == 2 ? 4 : 3) k_recur_grad(RecurArgs a, Chain ch)
+{
+    __shared__ TileLds<G> lds;
+    __shared__ typename Raw4<T>::type kept_d[RECUR_RUN][RECUR_STRANDS * G];   // a thread's own, out of its registers' way until they are used again
+    const i64 begin = std::max(0, a.offsets[0]), end = std::min<i64>(a.n, a.offsets[a.n_seq]);
+    int k = (int)blockIdx.x;
+    if (CHAINED) {
+        if (threadIdx.x == 0) lds.tile = (int)atomicAdd(ch.ticket, 1u);
+        __syncthreads();
+        k = uniform(lds.tile);
+    }
+    k_recur_grad_tile<T, G, CHAINED>(a, ch, k, (a.C4 + G - 1) / G, begin, end, lds, kept_d);
 }
 
 struct StepArgs {
@@ -468,15 +546,22 @@ int launch_recur(const RecurArgs &a, void *workspace, hipStream_t st)
         return TENSAIR_OK;
     }
     hipLaunchKernelGGL(k_recur_clear, dim3((unsigned)std::min<size_t>(1024, (bytes / 8 + BLOCK - 1) / BLOCK)), dim3(BLOCK), 0, st, (u64 *)workspace, bytes / 8);
-    const dim3 grid((unsigned)((i64)ch.tiles * sides));
+    const dim3 grid((unsigned)(ch.tiles * sides));
     if (grad) hipLaunchKernelGGL((k_recur_grad<T, G, true>), grid, blk, 0, st, a, ch);
     else hipLaunchKernelGGL((k_recur<T, G, true>), grid, blk, 0, st, a, ch);
     return TENSAIR_OK;
 }
 int launch_recur(const RecurArgs &a, int32_t dtype, void *workspace, hipStream_t st)
 {
-    if (dtype == TENSAIR_F32) return a.C4 <= 8 ? launch_recur<float, 8>(a, workspace, st) : launch_recur<float, 16>(a, workspace, st);
+    if (dtype == TENSAIR_F32) return launch_recur<float, 8>(a, workspace, st);          // a line of memory to a token and strand
     return a.C4 <= 8 ? launch_recur<bf16_t, 8>(a, workspace, st) : launch_recur<bf16_t, 16>(a, workspace, st);
+}
+
+// a tile's places are kept in 32 bits
+int recur_matrix(const void *p, i64 rows, i64 stride, int32_t dim, int32_t dtype, const char *what)
+{
+    if (stride > TENSAIR_MAX_RECUR_STRIDE) return tn_fail(TENSAIR_EINVAL, "%s: the row stride must be at most TENSAIR_MAX_RECUR_STRIDE", what);
+    return layer_matrix(p, rows, stride, dim, dtype, what);
 }
 
 int check_recur(const void *x, i64 x_stride, const void *gate, i64 gate_stride, int32_t dtype, i64 n, int32_t dim, const int32_t *offsets, i64 n_seq,
@@ -484,7 +569,7 @@ int check_recur(const void *x, i64 x_stride, const void *gate, i64 gate_stride, 
 {
     int rc;
     if ((rc = layer_sizes(n, dim))) return rc;
-    if ((rc = layer_matrix(x, n, x_stride, dim, dtype, "x")) || (rc = layer_matrix(gate, n, gate_stride, dim, dtype, "gate"))) return rc;
+    if ((rc = recur_matrix(x, n, x_stride, dim, dtype, "x")) || (rc = recur_matrix(gate, n, gate_stride, dim, dtype, "gate"))) return rc;
     if (n_seq < 0 || n_seq > TENSAIR_MAX_ROWS) return tn_fail(TENSAIR_EINVAL, "n_seq must be in 0..TENSAIR_MAX_ROWS");
     if (!offsets || ((uintptr_t)offsets & 3)) return tn_fail(TENSAIR_EINVAL, "offsets must be 4-byte aligned and not NULL");
     if ((uintptr_t)status & 3) return tn_fail(TENSAIR_EINVAL, "status must be 4-byte aligned");
@@ -513,7 +598,7 @@ int tensair_recur(const void *x, int64_t x_stride, const void *gate, int64_t gat
 {
     int rc;
     if ((rc = check_recur(x, x_stride, gate, gate_stride, dtype, n, dim, offsets, n_seq, workspace, workspace_bytes, status))) return rc;
-    if ((rc = layer_matrix(out, n, out_stride, dim, dtype, "out"))) return rc;
+    if ((rc = recur_matrix(out, n, out_stride, dim, dtype, "out"))) return rc;
     if ((rc = layer_floats(h0, "h0")) || (rc = layer_floats(h_last, "h_last")) || (rc = layer_floats(states, "states"))) return rc;
     if (n_seq == 0) return TENSAIR_OK;
     RecurArgs a;
@@ -543,8 +628,8 @@ int tensair_recur_grad(const void *x, int64_t x_stride, const void *gate, int64_
 {
     int rc;
     if ((rc = check_recur(x, x_stride, gate, gate_stride, dtype, n, dim, offsets, n_seq, workspace, workspace_bytes, status))) return rc;
-    if ((rc = layer_matrix(d_out, n, d_stride, dim, dtype, "d_out")) || (rc = layer_matrix(d_x, n, d_x_stride, dim, dtype, "d_x")) ||
-        (rc = layer_matrix(d_gate, n, d_gate_stride, dim, dtype, "d_gate")))
+    if ((rc = recur_matrix(d_out, n, d_stride, dim, dtype, "d_out")) || (rc = recur_matrix(d_x, n, d_x_stride, dim, dtype, "d_x")) ||
+        (rc = recur_matrix(d_gate, n, d_gate_stride, dim, dtype, "d_gate")))
         return rc;
     if ((rc = layer_floats(h0, "h0")) || (rc = layer_floats(states, "states")) || (rc = layer_floats(d_last, "d_last")) || (rc = layer_floats(d_h0, "d_h0"))) return rc;
     if (!states) return tn_fail(TENSAIR_EINVAL, "states is NULL");
