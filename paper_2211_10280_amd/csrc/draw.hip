@@ -1,17 +1,31 @@
 // One word for every row of logits: temperature, top-k, top-p, min-p and the draw by a given random number.  With w[v] = exp((z[v] - max z) / T) in 64 bits, what the
-// filters leave is a head of the words in the order of falling logits (equal ones by their numbers), so a row comes down to one border: a logit and how many of
-// the words equal to it are in.  The border's place and the draw are decided by sums of weights, which are taken in 64 bits and in an order that is a function of
-// the sizes alone: a sum in 32 bits would move the border by whole words.
+// filters leave is a head of the words in the order of falling logits (equal ones by their numbers), so a row comes down to one border in that order.  The border's place and the
+// draw are decided by sums of weights: they are taken in 64 bits, or as whole numbers of 2^-62, so that they hang on no order (in 32 bits they would move the border by whole words).
+//   k_draw_top      the largest logit of every part of a row
+//   k_draw_bins     words and weights by their distance from the row's largest logit, in bins; so the border's bin is known
+//   k_draw_gather   the words that may be in (those of the border's bin and, where they are few, all of the bins above) as a list, else the parts' weights above it
+//   k_draw          the border among the list, the part that the draw falls into, the word in it
+// A row without top-k and top-p needs no bins, a row of few words only the last of these, which then takes the row itself for the list; so it does where a list is too short
+// (thousands of words within a 128th of each other's logits at the border).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cmath>
+#include <cstring>
 
 #include "layers.h"
 
 namespace {
 
-#define DRAW_THREADS 1024
+#define DRAW_THREADS 1024        // of k_draw
+#define PART_THREADS 512         // of the other kernels: a workgroup to a part of a row
+#define DRAW_SOLO 8192           // words of a row that k_draw alone takes
+#define DRAW_PART 4096           // fewest words of a part
+#define DRAW_PARTS 1024          // most parts of a row
+#define DRAW_WORKGROUPS 2048     // parts of all rows that are aimed at
+#define DRAW_BINS 2048
+#define DRAW_LIST 16384          // most words of a row's list
+#define DRAW_ROWS 512            // rows at a time, so that the lists take 92 MB at most
 
 struct DrawArgs {
     const void *z;
@@ -21,6 +35,14 @@ struct DrawArgs {
     const int *top_k;
     int *words, *status;
     float *prob;
+    int part, parts;             // words of a part, parts of a row; 0 parts: k_draw alone
+    // in the workspace
+    u32 *tops;                   // [n][parts]
+    u32 *counts;                 // [n][DRAW_BINS]
+    u64 *hi, *lo;                // [n][DRAW_BINS] weights in 2^-30, what is below in 2^-62
+    u32 *listed;                 // [n]
+    u64 *list;                   // [n][DRAW_LIST] places in the order: ~key, word
+    double *mass;                // [n][parts]
 };
 
 // fp32 numbers in their order as unsigned ones; NaN as minus infinity
@@ -42,36 +64,443 @@ __device__ __forceinline__ double weight_of(u32 key, u32 top, double T)
     return w == w ? w : 0.0;
 }
 
-template <typename S>
+// what a row asks for
+struct Row {
+    double T, p, least;
+    int k;                       // 0: all
+    bool first;                  // the first word in the order
+};
+__device__ __forceinline__ Row row_of(const DrawArgs &a, int i)
+{
+    Row r;
+    const double T = a.temperature ? (double)a.temperature[i] : 1.0;
+    r.p = a.top_p ? (double)a.top_p[i] : 1.0;
+    r.least = a.min_p && a.min_p[i] == a.min_p[i] ? fmin((double)a.min_p[i], 1.0) : 0.0;
+    r.k = a.top_k ? a.top_k[i] : 0;
+    if (r.k < 1 || r.k >= a.V) r.k = 0;
+    r.first = !(T > 0.0) || !(r.p > 0.0) || r.k == 1;
+    r.T = T > 0.0 ? T : 1.0;
+    return r;
+}
+// The bin of a word: its distance below the largest logit, plus 1, with 7 bits behind the leading one.  Falls with the logit.
+__device__ __forceinline__ int bin_of(u32 key, u32 top)
+{
+    if (key == top) return 0;
+    const float d = of_key(top) - of_key(key);
+    return (int)min((u32)(DRAW_BINS - 1), (__float_as_uint(d + 1.0f) - 0x3F800000u) >> 16);
+}
+__device__ __forceinline__ u64 place_of(u32 key, u32 word) { return ((u64)~key << 32) | word; }
+__device__ __forceinline__ u64 fixed_of(double w) { return (u64)(w * 0x1p62); }
+__device__ __forceinline__ double mass_of(u64 hi, u64 lo) { return (double)hi * 0x1p-30 + (double)lo * 0x1p-62; }
+
+// f(word, logit) for the words lo..hi of a row, 16 bytes at a time where they are aligned
+template <int THREADS, typename F>
+__device__ __forceinline__ void each_word(const float *z, int lo, int hi, F f)
+{
+    const int t = (int)threadIdx.x;
+    const int head = min(hi - lo, (int)(-((uintptr_t)(z + lo) >> 2) & 3));
+    if (t < head) f(lo + t, z[lo + t]);
+    lo += head;
+    const int chunks = (hi - lo) / 4;
+    for (int c = t; c < chunks; c += 4 * THREADS) {
+        float4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (c + k * THREADS < chunks) v[k] = ld4(z + lo + 4 * (c + k * THREADS));
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (c + k * THREADS < chunks) {
+                const int at = lo + 4 * (c + k * THREADS);
+                f(at, v[k].x);
+                f(at + 1, v[k].y);
+                f(at + 2, v[k].z);
+                f(at + 3, v[k].w);
+            }
+    }
+    if (t < (hi - lo) % 4) f(lo + 4 * chunks + t, z[lo + 4 * chunks + t]);
+}
+template <int THREADS, typename F>
+__device__ __forceinline__ void each_word(const bf16_t *z, int lo, int hi, F f)
+{
+    const int t = (int)threadIdx.x;
+    const int head = min(hi - lo, (int)(-((uintptr_t)(z + lo) >> 1) & 7));
+    if (t < head) f(lo + t, bf16_to_f32(z[lo + t]));
+    lo += head;
+    const int chunks = (hi - lo) / 8;
+    for (int c = t; c < chunks; c += 2 * THREADS) {
+        uint4 v[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (c + k * THREADS < chunks) v[k] = *reinterpret_cast<const uint4 *>(z + lo + 8 * (c + k * THREADS));
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (c + k * THREADS < chunks) {
+                const int at = lo + 8 * (c + k * THREADS);
+                const u32 w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    f(at + 2 * q, __uint_as_float(w[q] << 16));
+                    f(at + 2 * q + 1, __uint_as_float(w[q] & 0xFFFF0000u));
+                }
+            }
+    }
+    if (t < (hi - lo) % 8) f(lo + 8 * chunks + t, bf16_to_f32(z[lo + 8 * chunks + t]));
+}
+
+__device__ __forceinline__ u32 shfl_add(u32 x, int o) { return x + (u32)__shfl_xor((int)x, o, WAVE); }
+__device__ __forceinline__ u64 shfl_add(u64 x, int o) { return x + (u64)__shfl_xor((unsigned long long)x, o, WAVE); }
+__device__ __forceinline__ double shfl_add(double x, int o) { return x + __shfl_xor(x, o, WAVE); }
+template <int THREADS, typename S>
 __device__ __forceinline__ S block_sum(S x, S *lds)
 {
-    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, WAVE);
+    for (int o = 32; o > 0; o >>= 1) x = shfl_add(x, o);
     __syncthreads();
     if (lane_id() == 0) lds[threadIdx.x >> 6] = x;
     __syncthreads();
-    x = 0;
-    for (int k = 0; k < DRAW_THREADS / WAVE; ++k) x += lds[k];
+    x = lds[0];
+    for (int k = 1; k < THREADS / WAVE; ++k) x += lds[k];
     return x;
 }
+template <int THREADS>
+__device__ __forceinline__ u32 block_max(u32 x, u32 *lds)
+{
+    for (int o = 32; o > 0; o >>= 1) x = max(x, (u32)__shfl_xor((int)x, o, WAVE));
+    __syncthreads();
+    if (lane_id() == 0) lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = lds[0];
+    for (int k = 1; k < THREADS / WAVE; ++k) x = max(x, lds[k]);
+    return x;
+}
+// sum of what the threads before have
+template <int THREADS, typename S>
+__device__ __forceinline__ S block_before(S x, S *lds, S &all)
+{
+    S run = x;
+    for (int o = 1; o < WAVE; o *= 2) {
+        const S y = __shfl_up(run, o, WAVE);
+        if (lane_id() >= o) run += y;
+    }
+    S before = __shfl_up(run, 1, WAVE);
+    if (lane_id() == 0) before = 0;
+    __syncthreads();
+    if (lane_id() == WAVE - 1) lds[threadIdx.x >> 6] = run;
+    __syncthreads();
+    S base = 0;
+    all = 0;
+    for (int k = 0; k < THREADS / WAVE; ++k) {
+        if (k == (int)(threadIdx.x >> 6)) base = all;
+        all += lds[k];
+    }
+    return base + before;
+}
+__device__ __forceinline__ unsigned long long *atom(u64 *p) { return (unsigned long long *)p; }
 
-// A workgroup to a row, and a pass over the row for every bit of the borders.
+template <int THREADS>
+__device__ __forceinline__ u32 row_top(const DrawArgs &a, int i, u32 *lds)
+{
+    u32 top = 0;
+    for (int c = (int)threadIdx.x; c < a.parts; c += THREADS) top = max(top, a.tops[(i64)i * a.parts + c]);
+    return block_max<THREADS>(top, lds);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(PART_THREADS) k_draw_top(DrawArgs a)
+{
+    __shared__ u32 lds[PART_THREADS / WAVE];
+    const int i = (int)blockIdx.x / a.parts, c = (int)blockIdx.x - i * a.parts, t = (int)threadIdx.x;
+    for (int b = c * PART_THREADS + t; b < DRAW_BINS; b += a.parts * PART_THREADS) {
+        a.counts[(i64)i * DRAW_BINS + b] = 0;
+        a.hi[(i64)i * DRAW_BINS + b] = a.lo[(i64)i * DRAW_BINS + b] = 0;
+    }
+    if (c == 0 && t == 0) a.listed[i] = 0;
+    u32 top = 0;
+    each_word<PART_THREADS>((const T *)a.z + (i64)i * a.stride, c * a.part, min(a.V, (c + 1) * a.part), [&](int, float z) { top = max(top, key_of(z)); });
+    top = block_max<PART_THREADS>(top, lds);
+    if (t == 0) a.tops[(i64)i * a.parts + c] = top;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(PART_THREADS) k_draw_bins(DrawArgs a)
+{
+    __shared__ u32 counts[DRAW_BINS], tops[PART_THREADS / WAVE];
+    __shared__ u64 hi[DRAW_BINS], lo[DRAW_BINS];
+    const int i = (int)blockIdx.x / a.parts, c = (int)blockIdx.x - i * a.parts, t = (int)threadIdx.x;
+    const Row r = row_of(a, i);
+    if (r.first || (r.k == 0 && r.p >= 1.0)) return;
+    const bool weigh = r.k == 0;                 // else top-p looks at what top-k left, which is listed
+    for (int b = t; b < DRAW_BINS; b += PART_THREADS) {
+        counts[b] = 0;
+        hi[b] = lo[b] = 0;
+    }
+    const u32 top = row_top<PART_THREADS>(a, i, tops);           // waits for all threads
+    each_word<PART_THREADS>((const T *)a.z + (i64)i * a.stride, c * a.part, min(a.V, (c + 1) * a.part), [&](int, float z) {
+        const u32 key = key_of(z);
+        const int b = bin_of(key, top);
+        atomicAdd(&counts[b], 1u);
+        if (weigh) {
+            const u64 w = fixed_of(weight_of(key, top, r.T));
+            atomicAdd(atom(&hi[b]), w >> 32);
+            atomicAdd(atom(&lo[b]), w & 0xFFFFFFFFull);
+        }
+    });
+    __syncthreads();
+    for (int b = t; b < DRAW_BINS; b += PART_THREADS) {
+        if (!counts[b]) continue;
+        const i64 at = (i64)i * DRAW_BINS + b;
+        atomicAdd(&a.counts[at], counts[b]);
+        if (!weigh) continue;
+        atomicAdd(atom(&a.hi[at]), hi[b]);
+        atomicAdd(atom(&a.lo[at]), lo[b]);
+    }
+}
+
+// Where a row's border lies, as far as the bins tell.
+struct Border {
+    int bin;                     // the bin that it falls into; all bins above it are in
+    u32 above, in;               // words of the bins above, of this bin
+    double above_mass, whole;    // weight of the bins above and of the row, where that is needed
+    int how;
+};
+enum { BORDER_NONE, BORDER_ALL_LISTED, BORDER_BIN_LISTED, BORDER_ROW };
+template <int THREADS>
+__device__ __forceinline__ Border border_of(const DrawArgs &a, const Row &r, int i, u64 *lds, int *pick)
+{
+    constexpr int PER = DRAW_BINS / THREADS;
+    const int t = (int)threadIdx.x;
+    Border o = {DRAW_BINS, 0, 0, 0.0, 0.0, BORDER_NONE};
+    if (r.k == 0 && r.p >= 1.0) return o;
+    const i64 at = (i64)i * DRAW_BINS + t * PER;
+    u32 n[PER];
+    u64 hi[PER], lo[PER], sn = 0, sh = 0, sl = 0, all, whole_hi = 0, whole_lo = 0, bh = 0, bl = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        n[j] = a.counts[at + j];
+        hi[j] = a.hi[at + j];
+        lo[j] = a.lo[at + j];
+        sn += n[j];
+        sh += hi[j];
+        sl += lo[j];
+    }
+    u64 bn = block_before<THREADS>(sn, lds, all);
+    if (r.k == 0) {
+        bh = block_before<THREADS>(sh, lds, whole_hi);
+        bl = block_before<THREADS>(sl, lds, whole_lo);
+    }
+    o.whole = mass_of(whole_hi, whole_lo);
+    const double want = r.p * o.whole;
+    if (t == 0) *pick = DRAW_BINS - 1;
+    __syncthreads();
+    u64 cn = bn, chi = bh, clo = bl;
+    for (int j = 0; j < PER; ++j) {
+        cn += n[j];
+        chi += hi[j];
+        clo += lo[j];
+        if (n[j] && (r.k ? cn >= (u64)r.k : mass_of(chi, clo) >= want)) {
+            atomicMin(pick, t * PER + j);
+            break;
+        }
+    }
+    __syncthreads();
+    o.bin = *pick;
+    // the one thread that has the bin tells the others
+    if (o.bin / PER == t) {
+        for (int j = 0; j < o.bin % PER; ++j) {
+            bn += n[j];
+            bh += hi[j];
+            bl += lo[j];
+        }
+        lds[0] = bn;
+        lds[1] = n[o.bin % PER];
+        lds[2] = bh;
+        lds[3] = bl;
+    }
+    __syncthreads();
+    o.above = (u32)lds[0];
+    o.in = (u32)lds[1];
+    o.above_mass = mass_of(lds[2], lds[3]);
+    __syncthreads();
+    o.how = o.above + o.in <= DRAW_LIST ? BORDER_ALL_LISTED : o.in <= DRAW_LIST && (r.k == 0 || r.p >= 1.0) ? BORDER_BIN_LISTED : BORDER_ROW;
+    return o;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(PART_THREADS) k_draw_gather(DrawArgs a)
+{
+    __shared__ u64 lds[PART_THREADS / WAVE];
+    __shared__ u32 tops[PART_THREADS / WAVE];
+    __shared__ double sums[PART_THREADS / WAVE];
+    __shared__ int pick;
+    const int i = (int)blockIdx.x / a.parts, c = (int)blockIdx.x - i * a.parts;
+    const Row r = row_of(a, i);
+    if (r.first) return;
+    const u32 top = row_top<PART_THREADS>(a, i, tops);
+    if (top <= KEY_LOWEST) return;
+    const Border o = border_of<PART_THREADS>(a, r, i, lds, &pick);
+    if (o.how == BORDER_ROW) return;
+    const bool weigh = o.how != BORDER_ALL_LISTED;
+    double m = 0.0;
+    each_word<PART_THREADS>((const T *)a.z + (i64)i * a.stride, c * a.part, min(a.V, (c + 1) * a.part), [&](int v, float z) {
+        const u32 key = key_of(z);
+        const int b = o.how == BORDER_NONE ? 0 : bin_of(key, top);
+        if (b > o.bin) return;
+        if (o.how != BORDER_NONE && (b == o.bin || !weigh)) {
+            const u32 at = atomicAdd(&a.listed[i], 1u);
+            if (at < DRAW_LIST) a.list[(i64)i * DRAW_LIST + at] = place_of(key, (u32)v);
+        } else {
+            const double w = weight_of(key, top, r.T);
+            if (w >= r.least) m += w;
+        }
+    });
+    if (!weigh) return;
+    m = block_sum<PART_THREADS>(m, sums);
+    if (threadIdx.x == 0) a.mass[(i64)i * a.parts + c] = m;
+}
+
+struct DrawLds {
+    u32 counts[DRAW_BINS], tops[DRAW_THREADS / WAVE];
+    u64 hi[DRAW_BINS], lo[DRAW_BINS];            // by digits, then by parts
+    u64 sums[DRAW_THREADS / WAVE];
+    double mass[DRAW_THREADS / WAVE];
+    u64 found[4];
+    int pick;
+};
+// The place in the order of the word with which the words up to `limit` (none of items that are behind) reach a number (or, BY_MASS, a weight): digits of 11 bits
+// of the distance from the first place, until one word is left.  each(f): calls f(place) for the items, every thread for its own.
+template <bool BY_MASS, typename Each, typename Weigh>
+__device__ __forceinline__ u64 place_at(Each each, Weigh weigh, u64 limit, u64 number, double mass, DrawLds &lds)
+{
+    constexpr int PER = DRAW_BINS / DRAW_THREADS;
+    const int t = (int)threadIdx.x;
+    u64 first = ~0ull, last = 0;
+    each([&](u64 x) {
+        if (x > limit) return;
+        first = x < first ? x : first;
+        last = x > last ? x : last;
+    });
+    for (int o = 32; o > 0; o >>= 1) {
+        const u64 x = (u64)__shfl_xor((unsigned long long)first, o, WAVE), y = (u64)__shfl_xor((unsigned long long)last, o, WAVE);
+        first = x < first ? x : first;
+        last = y > last ? y : last;
+    }
+    __syncthreads();
+    if (t == 0) {
+        lds.found[0] = ~0ull;
+        lds.found[1] = 0;
+    }
+    __syncthreads();
+    if (lane_id() == 0) {
+        atomicMin(atom(&lds.found[0]), first);
+        atomicMax(atom(&lds.found[1]), last);
+    }
+    __syncthreads();
+    first = lds.found[0];
+    last = lds.found[1];
+    double before = 0.0;                         // weight of what is in for sure
+    while (first < last) {
+        const int bits = 64 - __clzll((long long)(last - first)), shift = bits > 11 ? bits - 11 : 0;
+        __syncthreads();
+        for (int b = t; b < DRAW_BINS; b += DRAW_THREADS) {
+            lds.counts[b] = 0;
+            if (BY_MASS) lds.hi[b] = lds.lo[b] = 0;
+        }
+        if (t == 0) lds.pick = DRAW_BINS;
+        __syncthreads();
+        each([&](u64 x) {
+            if (x < first || x > last) return;
+            const int b = (int)((x - first) >> shift);
+            atomicAdd(&lds.counts[b], 1u);
+            if (BY_MASS) {
+                const u64 w = fixed_of(weigh(x));
+                atomicAdd(atom(&lds.hi[b]), w >> 32);
+                atomicAdd(atom(&lds.lo[b]), w & 0xFFFFFFFFull);
+            }
+        });
+        __syncthreads();
+        u32 n[PER];
+        u64 sn = 0, sh = 0, sl = 0, all, h0 = 0, l0 = 0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            n[j] = lds.counts[t * PER + j];
+            sn += n[j];
+            if (BY_MASS) {
+                sh += lds.hi[t * PER + j];
+                sl += lds.lo[t * PER + j];
+            }
+        }
+        u64 bn = block_before<DRAW_THREADS>(sn, lds.sums, all);
+        if (BY_MASS) {
+            h0 = block_before<DRAW_THREADS>(sh, lds.sums, all);
+            l0 = block_before<DRAW_THREADS>(sl, lds.sums, all);
+        }
+        int mine = DRAW_BINS, filled = -1;
+        u64 cn = bn, chi = h0, clo = l0;
+        for (int j = 0; j < PER; ++j) {
+            cn += n[j];
+            if (BY_MASS) {
+                chi += lds.hi[t * PER + j];
+                clo += lds.lo[t * PER + j];
+            }
+            if (n[j]) filled = t * PER + j;
+            if (n[j] && mine == DRAW_BINS && (BY_MASS ? before + mass_of(chi, clo) >= mass : cn >= number)) mine = t * PER + j;
+        }
+        if (mine < DRAW_BINS) atomicMin(&lds.pick, mine);
+        __syncthreads();
+        if (lds.pick == DRAW_BINS) {             // a weight that rounding put out of reach: the last word
+            __syncthreads();
+            if (t == 0) lds.pick = -1;
+            __syncthreads();
+            if (filled >= 0) atomicMax(&lds.pick, filled);
+            __syncthreads();
+        }
+        const int b = lds.pick;
+        if (b / PER == t) {
+            for (int j = 0; j < b % PER; ++j) {
+                bn += n[j];
+                if (BY_MASS) {
+                    h0 += lds.hi[t * PER + j];
+                    l0 += lds.lo[t * PER + j];
+                }
+            }
+            lds.found[0] = bn;
+            lds.found[1] = h0;
+            lds.found[2] = l0;
+        }
+        __syncthreads();
+        number -= BY_MASS ? 0 : lds.found[0];
+        if (BY_MASS) before += mass_of(lds.found[1], lds.found[2]);
+        const u64 low = first + ((u64)b << shift);
+        const u64 high = low + (((u64)1 << shift) - 1);
+        last = high < last ? high : last;
+        first = low;
+        if (lds.counts[b] == 1 && shift) {       // one word: its place
+            __syncthreads();
+            each([&](u64 x) {
+                if (x >= first && x <= last) lds.found[3] = x;
+            });
+            __syncthreads();
+            first = last = lds.found[3];
+        }
+    }
+    return first;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
 {
-    __shared__ double sums[DRAW_THREADS / WAVE];
-    __shared__ u64 counts[DRAW_THREADS / WAVE];
-    __shared__ int answer;
-    const int i = (int)blockIdx.x, t = (int)threadIdx.x;
+    __shared__ DrawLds lds;
+    const int i = (int)blockIdx.x, t = (int)threadIdx.x, V = a.V;
     const T *z = (const T *)a.z + (i64)i * a.stride;
-    const int V = a.V;
-    auto key = [&](int v) { return key_of(widen1(z[v])); };
+    const Row r = row_of(a, i);
+    const bool solo = a.parts == 0;
+    const int part = solo ? (V + DRAW_THREADS - 1) / DRAW_THREADS * DRAW_THREADS : a.part, parts = solo ? 1 : a.parts;
     u32 top = 0;
-    for (int v = t; v < V; v += DRAW_THREADS) top = max(top, key(v));
-    for (int o = 32; o > 0; o >>= 1) top = max(top, (u32)__shfl_xor((int)top, o, WAVE));
-    if (lane_id() == 0) counts[t >> 6] = top;
-    __syncthreads();
-    for (int k = 0; k < DRAW_THREADS / WAVE; ++k) top = max(top, (u32)counts[k]);
-    __syncthreads();
+    if (solo) {
+        each_word<DRAW_THREADS>(z, 0, V, [&](int, float x) { top = max(top, key_of(x)); });
+        top = block_max<DRAW_THREADS>(top, lds.tops);
+    } else {
+        top = row_top<DRAW_THREADS>(a, i, lds.tops);
+    }
     if (top <= KEY_LOWEST) {
         if (t == 0) {
             a.words[i] = -1;
@@ -80,123 +509,210 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
         }
         return;
     }
-    const double T0 = a.temperature ? (double)a.temperature[i] : 1.0, p = a.top_p ? (double)a.top_p[i] : 1.0;
-    const bool greedy = !(T0 > 0.0), first = !(p > 0.0);
-    const double Tq = greedy ? 1.0 : T0;
-    int k = a.top_k ? a.top_k[i] : 0;
-    if (k < 1 || k > V) k = V;
-    if (greedy || first) k = 1;
-    // the border: words above key `low` are in, of those equal to it the first `ties`
-    u32 low = 0;
-    int ties = V;
-    double above = 0.0;                                        // weight above the border
-    auto weight = [&](u32 x) { return weight_of(x, top, Tq); };
-    auto at_least = [&](u64 b, double &m, u64 &c) {            // weight and number of the words of keys >= b, as far as top-k left them
-        m = 0.0;
-        c = 0;
-        for (int v = t; v < V; v += DRAW_THREADS) {
-            const u32 x = key(v);
-            if ((u64)x >= b) {
-                m += weight(x);
-                ++c;
-            }
-        }
-        m = block_sum<double>(m, sums);
-        c = block_sum<u64>(c, counts);
+    u64 limit = ~0ull;                           // the last place that is in
+    double total = 0.0, before = 0.0, want = 0.0;
+    int c = 0;                                   // the part that the word is in
+    bool end = false;                            // the last word of it that is in
+    auto weigh = [&](u64 x) { return weight_of(~(u32)(x >> 32), top, r.T); };
+    auto weight_in = [&](u64 x) {
+        if (x > limit) return 0.0;
+        const double w = weigh(x);
+        return w >= r.least ? w : 0.0;
     };
-    double m;
-    u64 c;
-    if (k < V) {
-        for (int bit = 31; bit >= 0; --bit) {                  // the largest key that k words reach
-            at_least((u64)low | (1ull << bit), m, c);
-            if (c >= (u64)k) low |= 1u << bit;
+    if (r.first) {
+        // the first part that has the largest logit
+        if (t == 0) lds.pick = parts;
+        __syncthreads();
+        if (!solo)
+            for (int q = t; q < parts; q += DRAW_THREADS)
+                if (a.tops[(i64)i * parts + q] == top) atomicMin(&lds.pick, q);
+        __syncthreads();
+        c = solo ? 0 : lds.pick;
+        limit = place_of(top, 0xFFFFFFFFu);      // the first word of that logit: nothing is drawn
+    } else {
+        Border o = {DRAW_BINS, 0, 0, 0.0, 0.0, r.k == 0 && r.p >= 1.0 ? BORDER_NONE : BORDER_ROW};
+        if (!solo) o = border_of<DRAW_THREADS>(a, r, i, lds.sums, &lds.pick);
+        const bool listed = o.how == BORDER_ALL_LISTED || o.how == BORDER_BIN_LISTED;
+        const int items = listed ? (int)min(a.listed[i], (u32)DRAW_LIST) : 0;
+        auto each = [&](auto f) {
+            if (listed)
+                for (int q = t; q < items; q += DRAW_THREADS) f(a.list[(i64)i * DRAW_LIST + q]);
+            else
+                each_word<DRAW_THREADS>(z, 0, V, [&](int v, float x) { f(place_of(key_of(x), (u32)v)); });
+        };
+        // integers: what the threads put in does not hang on the order
+        auto mass_within = [&](u64 up_to) {
+            u64 h = 0, l = 0;
+            each([&](u64 x) {
+                if (x > up_to) return;
+                const u64 w = fixed_of(weigh(x));
+                h += w >> 32;
+                l += w & 0xFFFFFFFFull;
+            });
+            h = block_sum<DRAW_THREADS>(h, lds.sums);
+            l = block_sum<DRAW_THREADS>(l, lds.sums);
+            return mass_of(h, l);
+        };
+        if (r.k) limit = place_at<false>(each, weigh, ~0ull, (u64)r.k - (o.how == BORDER_BIN_LISTED ? o.above : 0), 0.0, lds);
+        if (r.p < 1.0) {
+            const bool bin = o.how == BORDER_BIN_LISTED;
+            const double whole = r.k || !listed ? mass_within(limit) : o.whole;
+            limit = place_at<true>(each, weigh, limit, 0, r.p * whole - (bin ? o.above_mass : 0.0), lds);
         }
-        at_least((u64)low + 1, above, c);
-        ties = k - (int)c;
-    }
-    if (p < 1.0 && !first) {
-        at_least(0, m, c);
-        const double whole = k < V ? above + ties * weight(low) : m;
-        const double want = p * whole;
-        u32 b = 0;
-        for (int bit = 31; bit >= 0; --bit) {                  // the largest key whose words and those above have `want`
-            const u32 next = b | (1u << bit);
-            if (k < V && next <= low) {
-                b = next;
-                continue;
+        // weights of the parts
+        __syncthreads();
+        for (int q = t; q < parts; q += DRAW_THREADS) lds.hi[q] = lds.lo[q] = 0;
+        __syncthreads();
+        if (solo || o.how == BORDER_ROW) {
+            // one part after the other; a part's words in 64 bits, in the threads' order
+            for (int q = 0; q < parts; ++q) {
+                u64 h = 0, l = 0;
+                each_word<DRAW_THREADS>(z, q * part, min(V, (q + 1) * part), [&](int v, float x) {
+                    const u64 w = fixed_of(weight_in(place_of(key_of(x), (u32)v)));
+                    h += w >> 32;
+                    l += w & 0xFFFFFFFFull;
+                });
+                h = block_sum<DRAW_THREADS>(h, lds.sums);
+                l = block_sum<DRAW_THREADS>(l, lds.sums);
+                if (t == 0) {
+                    lds.hi[q] = h;
+                    lds.lo[q] = l;
+                }
             }
-            at_least((u64)next, m, c);
-            if (m >= want) b = next;
+        } else if (listed) {
+            each([&](u64 x) {
+                const double w = weight_in(x);
+                if (w == 0.0) return;
+                const u64 f = fixed_of(w);
+                const int q = (int)((u32)x / (u32)part);
+                atomicAdd(atom(&lds.hi[q]), f >> 32);
+                atomicAdd(atom(&lds.lo[q]), f & 0xFFFFFFFFull);
+            });
         }
-        at_least((u64)b + 1, m, c);
-        const double w = weight(b);
-        const double more = w > 0.0 ? ceil((want - m) / w) : 1.0;
-        const int some = more > 1.0 ? (more < (double)V ? (int)more : V) : 1;
-        ties = k < V && b == low ? std::min(ties, some) : some;
-        low = b;
+        __syncthreads();
+        double m = 0.0;
+        if (t < parts) {
+            m = mass_of(lds.hi[t], lds.lo[t]);
+            if (!solo && (o.how == BORDER_NONE || o.how == BORDER_BIN_LISTED)) m += a.mass[(i64)i * parts + t];
+        }
+        const double run = block_before<DRAW_THREADS>(m, lds.mass, total);
+        double u = a.u[i];
+        u = u > 0.0 ? fmin(u, 1.0) : 0.0;
+        want = u * total;
+        if (t == 0) lds.pick = parts;
+        __syncthreads();
+        if (m > 0.0 && run + m > want) atomicMin(&lds.pick, t);
+        __syncthreads();
+        c = lds.pick;
+        if (c == parts) {                        // u is 1: the last word
+            end = true;
+            __syncthreads();
+            if (t == 0) lds.pick = 0;
+            __syncthreads();
+            if (m > 0.0) atomicMax(&lds.pick, t);
+            __syncthreads();
+            c = lds.pick;
+        }
+        if (t == c) lds.mass[0] = run;
+        __syncthreads();
+        before = lds.mass[0];
+        __syncthreads();
     }
-    const double floor_ = a.min_p && a.min_p[i] == a.min_p[i] ? std::min((double)a.min_p[i], 1.0) : 0.0;
-    // a run of words to a thread, so that running sums go by the words' numbers
-    const int per = (V + DRAW_THREADS - 1) / DRAW_THREADS, lo = std::min(V, t * per), hi = std::min(V, lo + per);
-    int equal = 0;
-    for (int v = lo; v < hi; ++v) equal += key(v) == low;
-    __shared__ int before[DRAW_THREADS];
-    __shared__ double mass[DRAW_THREADS];
-    before[t] = equal;
-    __syncthreads();
-    int rank = 0;
-    for (int q = 0; q < t; ++q) rank += before[q];
-    const int rank0 = rank;
-    auto kept = [&](u32 x) {
-        if (x < low || (x == low && rank++ >= ties)) return 0.0;
-        const double w = weight(x);
-        return w >= floor_ ? w : 0.0;
-    };
-    m = 0.0;
-    for (int v = lo; v < hi; ++v) m += kept(key(v));
-    mass[t] = m;
-    if (t == 0) answer = V;
-    __syncthreads();
-    double run = 0.0, total = 0.0;
-    for (int q = 0; q < DRAW_THREADS; ++q) {
-        if (q == t) run = total;
-        total += mass[q];
-    }
-    double u = a.u[i];
-    u = u > 0.0 ? std::min(u, 1.0) : 0.0;
-    const double want = u * total;
-    rank = rank0;
-    int mine = V, last = -1;
+    // the word in part c: a run of it to a thread, so that running sums go by the words' numbers
+    const int from = c * part, to = min(V, from + part), per = part / DRAW_THREADS, lo = min(to, from + t * per), hi = min(to, lo + per);
+    double m = 0.0;
+    int mine = -1, last = -1;
     double w_mine = 0.0, w_last = 0.0;
-    for (int v = lo; v < hi; ++v) {
-        const double w = kept(key(v));
-        if (w > 0.0) {
+    if (!r.first) {
+        for (int v = lo; v < hi; ++v) m += weight_in(place_of(key_of(widen1(z[v])), (u32)v));
+        double all;
+        double run = before + block_before<DRAW_THREADS>(m, lds.mass, all);
+        for (int v = lo; v < hi; ++v) {
+            const double w = weight_in(place_of(key_of(widen1(z[v])), (u32)v));
+            if (!(w > 0.0)) continue;
+            run += w;
             last = v;
             w_last = w;
+            if (!end && mine < 0 && run > want) {
+                mine = v;
+                w_mine = w;
+            }
         }
-        run += w;
-        if (w > 0.0 && run > want && mine == V) {
-            mine = v;
-            w_mine = w;
-        }
+    } else {
+        for (int v = hi - 1; v >= lo; --v)
+            if (key_of(widen1(z[v])) == top) mine = v;
     }
-    if (mine < V) atomicMin(&answer, mine);
     __syncthreads();
-    int got = answer;
+    if (t == 0) {
+        lds.pick = V;
+        lds.found[0] = 0;
+    }
     __syncthreads();
-    if (got == V) {                                            // u times the sum is the sum: the last word that is left
-        if (t == 0) answer = -1;
-        __syncthreads();
-        if (last >= 0) atomicMax(&answer, last);
-        __syncthreads();
-        got = answer;
+    if (mine >= 0) atomicMin(&lds.pick, mine);
+    if (last >= 0) atomicMax(atom(&lds.found[0]), (u64)last);
+    __syncthreads();
+    if (lds.pick == V && last >= 0 && (u64)last == lds.found[0]) {       // the sums of a part and of its words differ in their last places
         mine = last;
         w_mine = w_last;
+    } else if (mine != lds.pick) {
+        mine = -1;
     }
-    if (mine == got) {
-        a.words[i] = got;
-        if (a.prob) a.prob[i] = (float)(w_mine / total);
+    if (mine >= 0) {
+        a.words[i] = mine;
+        if (a.prob) a.prob[i] = r.first ? 1.f : (float)(w_mine / total);
     }
+}
+
+// the parts of a row, and where what lies in the workspace
+void draw_plan(i64 n, i64 V, int *part, int *parts)
+{
+    *part = *parts = 0;
+    if (V <= DRAW_SOLO) return;
+    i64 p = DRAW_PART;
+    while ((V + p - 1) / p > DRAW_PARTS || (n * ((V + p - 1) / p) > DRAW_WORKGROUPS && p < V)) p *= 2;
+    *part = (int)p;
+    *parts = (int)((V + p - 1) / p);
+}
+size_t draw_carve(i64 n, i64 V, char *ws, DrawArgs *a)
+{
+    int part, parts;
+    draw_plan(n, V, &part, &parts);
+    if (a) {
+        a->part = part;
+        a->parts = parts;
+    }
+    if (!parts) return 256;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        char *p = ws ? ws + at : nullptr;
+        at += layer_up256(bytes);
+        return p;
+    };
+    const size_t N = (size_t)n;
+    char *tops = take(4 * N * parts), *counts = take(4 * N * DRAW_BINS), *hi = take(8 * N * DRAW_BINS), *lo = take(8 * N * DRAW_BINS), *listed = take(4 * N),
+         *list = take(8 * N * DRAW_LIST), *mass = take(8 * N * parts);
+    if (a) {
+        a->tops = (u32 *)tops;
+        a->counts = (u32 *)counts;
+        a->hi = (u64 *)hi;
+        a->lo = (u64 *)lo;
+        a->listed = (u32 *)listed;
+        a->list = (u64 *)list;
+        a->mass = (double *)mass;
+    }
+    return at;
+}
+
+template <typename T>
+void launch_draw(const DrawArgs &a, hipStream_t st)
+{
+    if (a.parts) {
+        const dim3 grid((unsigned)(a.n * a.parts)), blk(PART_THREADS);
+        hipLaunchKernelGGL(k_draw_top<T>, grid, blk, 0, st, a);
+        if (a.top_k || a.top_p) hipLaunchKernelGGL(k_draw_bins<T>, grid, blk, 0, st, a);
+        hipLaunchKernelGGL(k_draw_gather<T>, grid, blk, 0, st, a);
+    }
+    hipLaunchKernelGGL(k_draw<T>, dim3((unsigned)a.n), dim3(DRAW_THREADS), 0, st, a);
 }
 
 }  // namespace
@@ -209,7 +725,11 @@ size_t tensair_sample_workspace_bytes(int64_t n, int64_t vocab)
         tn_fail(TENSAIR_EINVAL, "n must be in 0..TENSAIR_MAX_SAMPLE_ROWS, vocab in 1..TENSAIR_MAX_SAMPLE_VOCAB");
         return 0;
     }
-    return 256;
+    // the most of all rows up to n and all vocabularies up to vocab: fewer rows have more parts
+    if (vocab <= DRAW_SOLO) return 256;
+    n = std::min<int64_t>(n, DRAW_ROWS);
+    return std::max<size_t>(256, layer_up256((size_t)n * 8 * DRAW_LIST) + 2 * layer_up256((size_t)n * 8 * DRAW_BINS) + layer_up256((size_t)n * 4 * DRAW_BINS) +
+                                     layer_up256((size_t)n * 4) + layer_up256((size_t)n * 4 * DRAW_PARTS) + layer_up256((size_t)n * 8 * DRAW_PARTS));
 }
 
 int tensair_sample(const void *logits, int32_t dtype, int64_t stride, int64_t n, int64_t vocab, const float *temperature, const int32_t *top_k,
@@ -226,11 +746,26 @@ int tensair_sample(const void *logits, int32_t dtype, int64_t stride, int64_t n,
         return tn_fail(TENSAIR_EINVAL, "vectors must be 4-byte aligned");
     if (n == 0) return TENSAIR_OK;
     if (int rc = layer_workspace(workspace, workspace_bytes, need, "tensair_sample_workspace_bytes")) return rc;
-    const DrawArgs a = {logits, stride, (int)n, (int)vocab, temperature, top_p, min_p, u, top_k, words, status, prob};
     hipStream_t st = (hipStream_t)stream;
-    const dim3 grid((unsigned)n), blk(DRAW_THREADS);
-    if (dtype == TENSAIR_F32) hipLaunchKernelGGL(k_draw<float>, grid, blk, 0, st, a);
-    else hipLaunchKernelGGL(k_draw<bf16_t>, grid, blk, 0, st, a);
+    for (int64_t i = 0; i < n; i += DRAW_ROWS) {
+        DrawArgs a;
+        memset(&a, 0, sizeof(a));
+        a.z = (const char *)logits + i * stride * (dtype == TENSAIR_F32 ? 4 : 2);
+        a.stride = stride;
+        a.n = (int)std::min<int64_t>(DRAW_ROWS, n - i);
+        a.V = (int)vocab;
+        a.temperature = temperature ? temperature + i : nullptr;
+        a.top_k = top_k ? top_k + i : nullptr;
+        a.top_p = top_p ? top_p + i : nullptr;
+        a.min_p = min_p ? min_p + i : nullptr;
+        a.u = u + i;
+        a.words = words + i;
+        a.status = status;
+        a.prob = prob ? prob + i : nullptr;
+        draw_carve(a.n, vocab, (char *)workspace, &a);
+        if (dtype == TENSAIR_F32) launch_draw<float>(a, st);
+        else launch_draw<bf16_t>(a, st);
+    }
     return layer_launched("sample");
 }
 
