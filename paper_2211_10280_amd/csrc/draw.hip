@@ -2,11 +2,12 @@
 // filters leave is a head of the words in the order of falling logits (equal ones by their numbers), so a row comes down to one border in that order.  The border's place and the
 // draw are decided by sums of weights: they are taken in 64 bits, or as whole numbers of 2^-62, so that they hang on no order (in 32 bits they would move the border by whole words).
 //   k_draw_top      the largest logit of every part of a row
-//   k_draw_bins     words and weights by their distance from the row's largest logit, in bins; so the border's bin is known
+//   k_draw_bins     words and weights by their distance from the row's largest logit, in bins
+//   k_draw_border   the bin that the border falls into
 //   k_draw_gather   the words that may be in (those of the border's bin and, where they are few, all of the bins above) as a list, else the parts' weights above it
 //   k_draw          the border among the list, the part that the draw falls into, the word in it
 // A row without top-k and top-p needs no bins, a row of few words only the last of these, which then takes the row itself for the list; so it does where a list is too short
-// (thousands of words within a 128th of each other's logits at the border).
+// (thousands of words within a 256th of each other's logits at the border).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -23,9 +24,12 @@ namespace {
 #define DRAW_PART 4096           // fewest words of a part
 #define DRAW_PARTS 1024          // most parts of a row
 #define DRAW_WORKGROUPS 2048     // parts of all rows that are aimed at
-#define DRAW_BINS 2048
+#define DRAW_BINS 4096           // 256 to a doubling of (distance + 1)
+#define DRAW_DIGITS 2048         // of places
 #define DRAW_LIST 16384          // most words of a row's list
-#define DRAW_ROWS 512            // rows at a time, so that the lists take 92 MB at most
+#define DRAW_STAGED 2048         // of a part's words that go to it, most that are put together in LDS before
+#define DRAW_FEW 256             // words of a list that are compared each with each
+#define DRAW_ROWS 256            // rows at a time, so that the lists take 67 MB at most
 
 struct DrawArgs {
     const void *z;
@@ -40,8 +44,9 @@ struct DrawArgs {
     u32 *tops;                   // [n][parts]
     u32 *counts;                 // [n][DRAW_BINS]
     u64 *hi, *lo;                // [n][DRAW_BINS] weights in 2^-30, what is below in 2^-62
+    struct Border *borders;      // [n]
     u32 *listed;                 // [n]
-    u64 *list;                   // [n][DRAW_LIST] places in the order: ~key, word
+    ulong2 *list;                // [n][DRAW_LIST] places in the order (~key, word) and weights in 2^-62
     double *mass;                // [n][parts]
 };
 
@@ -55,18 +60,35 @@ __device__ __forceinline__ u32 key_of(float f)
 }
 __device__ __forceinline__ float of_key(u32 k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
 
-// weight of a logit beside the largest
-__device__ __forceinline__ double weight_of(u32 key, u32 top, double T)
+// 2^t: whole part by the exponent, the rest, at most 1/2, by the series of exp up to the 11th power (the 12th term is below 7e-15 of the sum)
+__device__ __forceinline__ double exp2_of(double t)
 {
-    if (key == KEY_LOWEST) return 0.0;
-    if (key == top) return 1.0;
-    const double w = exp(((double)of_key(key) - (double)of_key(top)) / T);
-    return w == w ? w : 0.0;
+    const double n = rint(t), f = t - n;
+    double p = 4.4455382718708101e-10;           // ln(2)^k / k!, k = 11 .. 0
+    p = fma(p, f, 7.0549116208011209e-09);
+    p = fma(p, f, 1.0178086009239696e-07);
+    p = fma(p, f, 1.3215486790144305e-06);
+    p = fma(p, f, 1.5252733804059838e-05);
+    p = fma(p, f, 1.5403530393381606e-04);
+    p = fma(p, f, 1.3333558146428441e-03);
+    p = fma(p, f, 9.6181291076284769e-03);
+    p = fma(p, f, 5.5504108664821576e-02);
+    p = fma(p, f, 2.4022650695910069e-01);
+    p = fma(p, f, 6.9314718055994529e-01);
+    p = fma(p, f, 1.0);
+    return ldexp(p, (int)n);
+}
+// weight of a logit beside the largest; slope: log2(e) / T
+__device__ __forceinline__ double weight_of(u32 key, u32 top, double slope)
+{
+    const double t = ((double)of_key(key) - (double)of_key(top)) * slope;
+    const double w = t > -1000.0 ? exp2_of(t) : 0.0;             // NaN (minus infinity beside an endless temperature): none
+    return key == top ? 1.0 : key == KEY_LOWEST ? 0.0 : w;
 }
 
 // what a row asks for
 struct Row {
-    double T, p, least;
+    double slope, p, least;
     int k;                       // 0: all
     bool first;                  // the first word in the order
 };
@@ -79,15 +101,15 @@ __device__ __forceinline__ Row row_of(const DrawArgs &a, int i)
     r.k = a.top_k ? a.top_k[i] : 0;
     if (r.k < 1 || r.k >= a.V) r.k = 0;
     r.first = !(T > 0.0) || !(r.p > 0.0) || r.k == 1;
-    r.T = T > 0.0 ? T : 1.0;
+    r.slope = 1.4426950408889634 / (T > 0.0 ? T : 1.0);
     return r;
 }
-// The bin of a word: its distance below the largest logit, plus 1, with 7 bits behind the leading one.  Falls with the logit.
+// The bin of a word: its distance below the largest logit, plus 1, with 8 bits behind the leading one.  Falls with the logit.
 __device__ __forceinline__ int bin_of(u32 key, u32 top)
 {
     if (key == top) return 0;
     const float d = of_key(top) - of_key(key);
-    return (int)min((u32)(DRAW_BINS - 1), (__float_as_uint(d + 1.0f) - 0x3F800000u) >> 16);
+    return (int)min((u32)(DRAW_BINS - 1), (__float_as_uint(d + 1.0f) - 0x3F800000u) >> 15);
 }
 __device__ __forceinline__ u64 place_of(u32 key, u32 word) { return ((u64)~key << 32) | word; }
 __device__ __forceinline__ u64 fixed_of(double w) { return (u64)(w * 0x1p62); }
@@ -194,6 +216,34 @@ __device__ __forceinline__ S block_before(S x, S *lds, S &all)
     }
     return base + before;
 }
+struct Three {
+    u64 n, hi, lo;
+};
+template <int THREADS>
+__device__ __forceinline__ Three block_before(Three x, Three *lds, Three &all)
+{
+    Three run = x;
+    for (int o = 1; o < WAVE; o *= 2) {
+        const u64 a = __shfl_up(run.n, o, WAVE), b = __shfl_up(run.hi, o, WAVE), c = __shfl_up(run.lo, o, WAVE);
+        if (lane_id() >= o) {
+            run.n += a;
+            run.hi += b;
+            run.lo += c;
+        }
+    }
+    __syncthreads();
+    if (lane_id() == WAVE - 1) lds[threadIdx.x >> 6] = run;
+    __syncthreads();
+    Three base = {0, 0, 0};
+    all = base;
+    for (int k = 0; k < THREADS / WAVE; ++k) {
+        if (k == (int)(threadIdx.x >> 6)) base = all;
+        all.n += lds[k].n;
+        all.hi += lds[k].hi;
+        all.lo += lds[k].lo;
+    }
+    return Three{base.n + run.n - x.n, base.hi + run.hi - x.hi, base.lo + run.lo - x.lo};
+}
 __device__ __forceinline__ unsigned long long *atom(u64 *p) { return (unsigned long long *)p; }
 
 template <int THREADS>
@@ -239,7 +289,7 @@ __global__ void __launch_bounds__(PART_THREADS) k_draw_bins(DrawArgs a)
         const int b = bin_of(key, top);
         atomicAdd(&counts[b], 1u);
         if (weigh) {
-            const u64 w = fixed_of(weight_of(key, top, r.T));
+            const u64 w = fixed_of(weight_of(key, top, r.slope));
             atomicAdd(atom(&hi[b]), w >> 32);
             atomicAdd(atom(&lo[b]), w & 0xFFFFFFFFull);
         }
@@ -259,122 +309,130 @@ __global__ void __launch_bounds__(PART_THREADS) k_draw_bins(DrawArgs a)
 struct Border {
     int bin;                     // the bin that it falls into; all bins above it are in
     u32 above, in;               // words of the bins above, of this bin
-    double above_mass, whole;    // weight of the bins above and of the row, where that is needed
     int how;
+    double above_mass, whole;    // weight of the bins above and of the row, where that is needed
 };
 enum { BORDER_NONE, BORDER_ALL_LISTED, BORDER_BIN_LISTED, BORDER_ROW };
-template <int THREADS>
-__device__ __forceinline__ Border border_of(const DrawArgs &a, const Row &r, int i, u64 *lds, int *pick)
+__global__ void __launch_bounds__(DRAW_THREADS) k_draw_border(DrawArgs a)
 {
-    constexpr int PER = DRAW_BINS / THREADS;
-    const int t = (int)threadIdx.x;
-    Border o = {DRAW_BINS, 0, 0, 0.0, 0.0, BORDER_NONE};
-    if (r.k == 0 && r.p >= 1.0) return o;
+    constexpr int PER = DRAW_BINS / DRAW_THREADS;
+    __shared__ Three lds[DRAW_THREADS / WAVE];
+    __shared__ int pick;
+    const int t = (int)threadIdx.x, i = (int)blockIdx.x;
+    const Row r = row_of(a, i);
+    if (r.first || (r.k == 0 && r.p >= 1.0)) return;
     const i64 at = (i64)i * DRAW_BINS + t * PER;
-    u32 n[PER];
-    u64 hi[PER], lo[PER], sn = 0, sh = 0, sl = 0, all, whole_hi = 0, whole_lo = 0, bh = 0, bl = 0;
+    Three x[PER], sum = {0, 0, 0}, all;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-        n[j] = a.counts[at + j];
-        hi[j] = a.hi[at + j];
-        lo[j] = a.lo[at + j];
-        sn += n[j];
-        sh += hi[j];
-        sl += lo[j];
-    }
-    u64 bn = block_before<THREADS>(sn, lds, all);
-    if (r.k == 0) {
-        bh = block_before<THREADS>(sh, lds, whole_hi);
-        bl = block_before<THREADS>(sl, lds, whole_lo);
-    }
-    o.whole = mass_of(whole_hi, whole_lo);
-    const double want = r.p * o.whole;
-    if (t == 0) *pick = DRAW_BINS - 1;
-    __syncthreads();
-    u64 cn = bn, chi = bh, clo = bl;
-    for (int j = 0; j < PER; ++j) {
-        cn += n[j];
-        chi += hi[j];
-        clo += lo[j];
-        if (n[j] && (r.k ? cn >= (u64)r.k : mass_of(chi, clo) >= want)) {
-            atomicMin(pick, t * PER + j);
-            break;
+        x[j] = Three{a.counts[at + j], 0, 0};
+        if (r.k == 0) {
+            x[j].hi = a.hi[at + j];
+            x[j].lo = a.lo[at + j];
         }
+        sum = Three{sum.n + x[j].n, sum.hi + x[j].hi, sum.lo + x[j].lo};
     }
-    __syncthreads();
-    o.bin = *pick;
-    // the one thread that has the bin tells the others
-    if (o.bin / PER == t) {
-        for (int j = 0; j < o.bin % PER; ++j) {
-            bn += n[j];
-            bh += hi[j];
-            bl += lo[j];
+    if (t == 0) pick = DRAW_BINS;
+    Three run = block_before<DRAW_THREADS>(sum, lds, all);
+    const double whole = mass_of(all.hi, all.lo), want = r.p * whole;
+    Border o = {DRAW_BINS, 0, 0, BORDER_ROW, 0.0, whole};
+    for (int j = 0; j < PER && o.bin == DRAW_BINS; ++j) {
+        const Three to = {run.n + x[j].n, run.hi + x[j].hi, run.lo + x[j].lo};
+        if (x[j].n && (r.k ? to.n >= (u64)r.k : mass_of(to.hi, to.lo) >= want)) {
+            o.bin = t * PER + j;
+            o.above = (u32)run.n;
+            o.in = (u32)x[j].n;
+            o.above_mass = mass_of(run.hi, run.lo);
         }
-        lds[0] = bn;
-        lds[1] = n[o.bin % PER];
-        lds[2] = bh;
-        lds[3] = bl;
+        run = to;
     }
+    if (o.bin < DRAW_BINS) atomicMin(&pick, o.bin);
     __syncthreads();
-    o.above = (u32)lds[0];
-    o.in = (u32)lds[1];
-    o.above_mass = mass_of(lds[2], lds[3]);
-    __syncthreads();
-    o.how = o.above + o.in <= DRAW_LIST ? BORDER_ALL_LISTED : o.in <= DRAW_LIST && (r.k == 0 || r.p >= 1.0) ? BORDER_BIN_LISTED : BORDER_ROW;
-    return o;
+    if (o.bin == DRAW_BINS || o.bin != pick) return;             // all words' number and weight are enough: there is one
+    if (o.above + o.in <= DRAW_LIST) o.how = BORDER_ALL_LISTED;
+    else if (o.in <= DRAW_LIST && (r.k == 0 || r.p >= 1.0)) o.how = BORDER_BIN_LISTED;
+    a.borders[i] = o;
+}
+__device__ __forceinline__ Border border_of(const DrawArgs &a, const Row &r, int i)
+{
+    if (r.k == 0 && r.p >= 1.0) return Border{DRAW_BINS, 0, 0, BORDER_NONE, 0.0, 0.0};
+    return a.borders[i];
 }
 
 template <typename T>
 __global__ void __launch_bounds__(PART_THREADS) k_draw_gather(DrawArgs a)
 {
-    __shared__ u64 lds[PART_THREADS / WAVE];
     __shared__ u32 tops[PART_THREADS / WAVE];
     __shared__ double sums[PART_THREADS / WAVE];
-    __shared__ int pick;
-    const int i = (int)blockIdx.x / a.parts, c = (int)blockIdx.x - i * a.parts;
+    __shared__ u64 staged[DRAW_STAGED];
+    __shared__ u32 some, base;
+    const int i = (int)blockIdx.x / a.parts, c = (int)blockIdx.x - i * a.parts, t = (int)threadIdx.x;
     const Row r = row_of(a, i);
     if (r.first) return;
-    const u32 top = row_top<PART_THREADS>(a, i, tops);
-    if (top <= KEY_LOWEST) return;
-    const Border o = border_of<PART_THREADS>(a, r, i, lds, &pick);
+    const Border o = border_of(a, r, i);
     if (o.how == BORDER_ROW) return;
+    if (t == 0) some = 0;
+    const u32 top = row_top<PART_THREADS>(a, i, tops);           // waits for all threads
+    if (top <= KEY_LOWEST) return;
     const bool weigh = o.how != BORDER_ALL_LISTED;
+    ulong2 *list = a.list + (i64)i * DRAW_LIST;
     double m = 0.0;
     each_word<PART_THREADS>((const T *)a.z + (i64)i * a.stride, c * a.part, min(a.V, (c + 1) * a.part), [&](int v, float z) {
         const u32 key = key_of(z);
         const int b = o.how == BORDER_NONE ? 0 : bin_of(key, top);
         if (b > o.bin) return;
         if (o.how != BORDER_NONE && (b == o.bin || !weigh)) {
-            const u32 at = atomicAdd(&a.listed[i], 1u);
-            if (at < DRAW_LIST) a.list[(i64)i * DRAW_LIST + at] = place_of(key, (u32)v);
+            const u32 at = atomicAdd(&some, 1u);
+            if (at < DRAW_STAGED) {
+                staged[at] = place_of(key, (u32)v);
+            } else {                             // more than are put together: one by one
+                const u32 to = atomicAdd(&a.listed[i], 1u);
+                if (to < DRAW_LIST) list[to] = make_ulong2(place_of(key, (u32)v), fixed_of(weight_of(key, top, r.slope)));
+            }
         } else {
-            const double w = weight_of(key, top, r.T);
+            const double w = weight_of(key, top, r.slope);
             if (w >= r.least) m += w;
         }
     });
+    __syncthreads();
+    const u32 n = min(some, (u32)DRAW_STAGED);
+    if (n) {
+        if (t == 0) base = atomicAdd(&a.listed[i], n);
+        __syncthreads();
+        for (u32 q = t; q < n; q += PART_THREADS) {
+            const u64 x = staged[q];
+            if (base + q < DRAW_LIST) list[base + q] = make_ulong2(x, fixed_of(weight_of(~(u32)(x >> 32), top, r.slope)));
+        }
+    }
     if (!weigh) return;
     m = block_sum<PART_THREADS>(m, sums);
-    if (threadIdx.x == 0) a.mass[(i64)i * a.parts + c] = m;
+    if (t == 0) a.mass[(i64)i * a.parts + c] = m;
 }
 
 struct DrawLds {
-    u32 counts[DRAW_BINS], tops[DRAW_THREADS / WAVE];
-    u64 hi[DRAW_BINS], lo[DRAW_BINS];            // by digits, then by parts
+    u32 counts[DRAW_DIGITS], tops[DRAW_THREADS / WAVE];
+    u64 hi[DRAW_DIGITS], lo[DRAW_DIGITS];        // by digits, then by parts
+    Three three[DRAW_THREADS / WAVE];
     u64 sums[DRAW_THREADS / WAVE];
     double mass[DRAW_THREADS / WAVE];
     u64 found[4];
     int pick;
 };
-// The place in the order of the word with which the words up to `limit` (none of items that are behind) reach a number (or, BY_MASS, a weight): digits of 11 bits
-// of the distance from the first place, until one word is left.  each(f): calls f(place) for the items, every thread for its own.
-template <bool BY_MASS, typename Each, typename Weigh>
-__device__ __forceinline__ u64 place_at(Each each, Weigh weigh, u64 limit, u64 number, double mass, DrawLds &lds)
+// The place in the order of the word with which the items, of those for which `among` holds, reach a number (or, BY_MASS, a weight): digits of 11 bits of the
+// distance from the first place, until one word is left.  each(f): calls f(place, weight) for the items, every thread for its own, the weight as a function.
+template <bool BY_MASS, typename Each, typename Among>
+__device__ __forceinline__ u64 place_at(Each each, Among among, u64 number, double mass, DrawLds &lds)
 {
-    constexpr int PER = DRAW_BINS / DRAW_THREADS;
+    constexpr int PER = DRAW_DIGITS / DRAW_THREADS;
     const int t = (int)threadIdx.x;
     u64 first = ~0ull, last = 0;
-    each([&](u64 x) {
-        if (x > limit) return;
+    __syncthreads();
+    if (t == 0) {
+        lds.found[0] = ~0ull;
+        lds.found[1] = 0;
+    }
+    each([&](u64 x, auto) {
+        if (!among(x)) return;
         first = x < first ? x : first;
         last = x > last ? x : last;
     });
@@ -382,11 +440,6 @@ __device__ __forceinline__ u64 place_at(Each each, Weigh weigh, u64 limit, u64 n
         const u64 x = (u64)__shfl_xor((unsigned long long)first, o, WAVE), y = (u64)__shfl_xor((unsigned long long)last, o, WAVE);
         first = x < first ? x : first;
         last = y > last ? y : last;
-    }
-    __syncthreads();
-    if (t == 0) {
-        lds.found[0] = ~0ull;
-        lds.found[1] = 0;
     }
     __syncthreads();
     if (lane_id() == 0) {
@@ -400,89 +453,156 @@ __device__ __forceinline__ u64 place_at(Each each, Weigh weigh, u64 limit, u64 n
     while (first < last) {
         const int bits = 64 - __clzll((long long)(last - first)), shift = bits > 11 ? bits - 11 : 0;
         __syncthreads();
-        for (int b = t; b < DRAW_BINS; b += DRAW_THREADS) {
+        for (int b = t; b < DRAW_DIGITS; b += DRAW_THREADS) {
             lds.counts[b] = 0;
             if (BY_MASS) lds.hi[b] = lds.lo[b] = 0;
         }
-        if (t == 0) lds.pick = DRAW_BINS;
+        if (t == 0) lds.pick = DRAW_DIGITS;
         __syncthreads();
-        each([&](u64 x) {
+        each([&](u64 x, auto weight) {
             if (x < first || x > last) return;
             const int b = (int)((x - first) >> shift);
             atomicAdd(&lds.counts[b], 1u);
             if (BY_MASS) {
-                const u64 w = fixed_of(weigh(x));
+                const u64 w = weight();
                 atomicAdd(atom(&lds.hi[b]), w >> 32);
                 atomicAdd(atom(&lds.lo[b]), w & 0xFFFFFFFFull);
             }
         });
         __syncthreads();
-        u32 n[PER];
-        u64 sn = 0, sh = 0, sl = 0, all, h0 = 0, l0 = 0;
+        Three x[PER], sum = {0, 0, 0}, all;
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
-            n[j] = lds.counts[t * PER + j];
-            sn += n[j];
+            x[j] = Three{lds.counts[t * PER + j], 0, 0};
             if (BY_MASS) {
-                sh += lds.hi[t * PER + j];
-                sl += lds.lo[t * PER + j];
+                x[j].hi = lds.hi[t * PER + j];
+                x[j].lo = lds.lo[t * PER + j];
             }
+            sum = Three{sum.n + x[j].n, sum.hi + x[j].hi, sum.lo + x[j].lo};
         }
-        u64 bn = block_before<DRAW_THREADS>(sn, lds.sums, all);
-        if (BY_MASS) {
-            h0 = block_before<DRAW_THREADS>(sh, lds.sums, all);
-            l0 = block_before<DRAW_THREADS>(sl, lds.sums, all);
-        }
-        int mine = DRAW_BINS, filled = -1;
-        u64 cn = bn, chi = h0, clo = l0;
+        Three run = block_before<DRAW_THREADS>(sum, lds.three, all);
+        int mine = DRAW_DIGITS, filled = -1;
+        Three at = run;
+        u32 there = 0;
+#pragma unroll
         for (int j = 0; j < PER; ++j) {
-            cn += n[j];
-            if (BY_MASS) {
-                chi += lds.hi[t * PER + j];
-                clo += lds.lo[t * PER + j];
+            const Three to = {run.n + x[j].n, run.hi + x[j].hi, run.lo + x[j].lo};
+            if (x[j].n) {
+                if (mine == DRAW_DIGITS) {
+                    at = run;                    // in the end that of the digit that is taken, or of the last one
+                    there = (u32)x[j].n;
+                    filled = t * PER + j;
+                    if (BY_MASS ? before + mass_of(to.hi, to.lo) >= mass : to.n >= number) mine = t * PER + j;
+                }
             }
-            if (n[j]) filled = t * PER + j;
-            if (n[j] && mine == DRAW_BINS && (BY_MASS ? before + mass_of(chi, clo) >= mass : cn >= number)) mine = t * PER + j;
+            run = to;
         }
-        if (mine < DRAW_BINS) atomicMin(&lds.pick, mine);
+        if (mine < DRAW_DIGITS) atomicMin(&lds.pick, mine);
         __syncthreads();
-        if (lds.pick == DRAW_BINS) {             // a weight that rounding put out of reach: the last word
+        int b = lds.pick;
+        if (b == DRAW_DIGITS) {                  // a weight that rounding put out of reach: the last word
             __syncthreads();
             if (t == 0) lds.pick = -1;
             __syncthreads();
             if (filled >= 0) atomicMax(&lds.pick, filled);
             __syncthreads();
+            b = lds.pick;
         }
-        const int b = lds.pick;
-        if (b / PER == t) {
-            for (int j = 0; j < b % PER; ++j) {
-                bn += n[j];
-                if (BY_MASS) {
-                    h0 += lds.hi[t * PER + j];
-                    l0 += lds.lo[t * PER + j];
-                }
-            }
-            lds.found[0] = bn;
-            lds.found[1] = h0;
-            lds.found[2] = l0;
+        if (b == filled) {
+            lds.found[0] = at.n;
+            lds.found[1] = at.hi;
+            lds.found[2] = at.lo;
+            lds.found[3] = there;
         }
         __syncthreads();
-        number -= BY_MASS ? 0 : lds.found[0];
+        if (!BY_MASS) number -= lds.found[0];
         if (BY_MASS) before += mass_of(lds.found[1], lds.found[2]);
-        const u64 low = first + ((u64)b << shift);
-        const u64 high = low + (((u64)1 << shift) - 1);
-        last = high < last ? high : last;
+        const bool one = lds.found[3] == 1;
+        const u64 low = first + ((u64)b << shift), high = low + (((u64)1 << shift) - 1);
         first = low;
-        if (lds.counts[b] == 1 && shift) {       // one word: its place
+        last = high < last ? high : last;
+        if (one && shift) {                      // one word: its place
             __syncthreads();
-            each([&](u64 x) {
-                if (x >= first && x <= last) lds.found[3] = x;
+            each([&](u64 x, auto) {
+                if (x >= first && x <= last) lds.found[0] = x;
             });
             __syncthreads();
-            first = last = lds.found[3];
+            first = last = lds.found[0];
         }
     }
+    __syncthreads();
     return first;
+}
+
+// A list of at most DRAW_FEW words: each compared with each, a word to a thread.  Sums are of whole numbers, so the list's order does not matter.
+__device__ __forceinline__ void draw_few(const DrawArgs &a, const Row &r, int i, const Border &o, int items, DrawLds &lds)
+{
+    const int t = (int)threadIdx.x;
+    ulong2 *list = (ulong2 *)lds.hi;             // DRAW_FEW of them
+    ulong2 x = make_ulong2(~0ull, 0);
+    if (t < items) {
+        x = a.list[(i64)i * DRAW_LIST + t];
+        list[t] = x;
+    }
+    __syncthreads();
+    int rank = 0;
+    u64 hi = 0, lo = 0;
+    if (t < items)
+        for (int q = 0; q < items; ++q) {
+            const ulong2 y = list[q];
+            if (y.x < x.x) {
+                ++rank;
+                hi += y.y >> 32;
+                lo += y.y & 0xFFFFFFFFull;
+            }
+        }
+    bool in = t < items && (r.k == 0 || rank < r.k);
+    double whole = o.whole;
+    if (r.p < 1.0) {
+        if (r.k) {
+            const u64 h = block_sum<DRAW_THREADS, u64>(in ? x.y >> 32 : 0, lds.sums), l = block_sum<DRAW_THREADS, u64>(in ? x.y & 0xFFFFFFFFull : 0, lds.sums);
+            whole = mass_of(h, l);
+        }
+        in = in && (rank == 0 || mass_of(hi, lo) < r.p * whole);
+    }
+    in = in && (double)x.y * 0x1p-62 >= r.least;
+    __syncthreads();
+    if (t < items) {
+        list[t].x = (u32)x.x;                    // by words now
+        list[t].y = in ? x.y : 0;
+    }
+    if (t == 0) lds.found[0] = ~0ull;
+    __syncthreads();
+    hi = lo = 0;
+    u64 all_hi = 0, all_lo = 0;
+    if (t < items)
+        for (int q = 0; q < items; ++q) {
+            const ulong2 y = list[q];
+            all_hi += y.y >> 32;
+            all_lo += y.y & 0xFFFFFFFFull;
+            if (y.x <= (u32)x.x) {
+                hi += y.y >> 32;
+                lo += y.y & 0xFFFFFFFFull;
+            }
+        }
+    const double total = mass_of(all_hi, all_lo);
+    double u = a.u[i];
+    u = u > 0.0 ? fmin(u, 1.0) : 0.0;
+    in = in && x.y > 0;
+    const bool above = in && mass_of(hi, lo) > u * total;
+    if (above) atomicMin(atom(&lds.found[0]), (u64)(u32)x.x);
+    __syncthreads();
+    if (lds.found[0] == ~0ull) {                 // u is 1: the last word
+        __syncthreads();
+        if (t == 0) lds.found[0] = 0;
+        __syncthreads();
+        if (in) atomicMax(atom(&lds.found[0]), (u64)(u32)x.x);
+        __syncthreads();
+    }
+    if (in && (u32)x.x == (u32)lds.found[0]) {
+        a.words[i] = (int)(u32)x.x;
+        if (a.prob) a.prob[i] = (float)((double)x.y * 0x1p-62 / total);
+    }
 }
 
 template <typename T>
@@ -513,7 +633,7 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
     double total = 0.0, before = 0.0, want = 0.0;
     int c = 0;                                   // the part that the word is in
     bool end = false;                            // the last word of it that is in
-    auto weigh = [&](u64 x) { return weight_of(~(u32)(x >> 32), top, r.T); };
+    auto weigh = [&](u64 x) { return weight_of(~(u32)(x >> 32), top, r.slope); };
     auto weight_in = [&](u64 x) {
         if (x > limit) return 0.0;
         const double w = weigh(x);
@@ -530,22 +650,34 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
         c = solo ? 0 : lds.pick;
         limit = place_of(top, 0xFFFFFFFFu);      // the first word of that logit: nothing is drawn
     } else {
-        Border o = {DRAW_BINS, 0, 0, 0.0, 0.0, r.k == 0 && r.p >= 1.0 ? BORDER_NONE : BORDER_ROW};
-        if (!solo) o = border_of<DRAW_THREADS>(a, r, i, lds.sums, &lds.pick);
+        Border o = {DRAW_BINS, 0, 0, r.k == 0 && r.p >= 1.0 ? BORDER_NONE : BORDER_ROW, 0.0, 0.0};
+        if (!solo) o = border_of(a, r, i);
         const bool listed = o.how == BORDER_ALL_LISTED || o.how == BORDER_BIN_LISTED;
         const int items = listed ? (int)min(a.listed[i], (u32)DRAW_LIST) : 0;
+        if (o.how == BORDER_ALL_LISTED && items <= DRAW_FEW) {
+            draw_few(a, r, i, o, items, lds);
+            return;
+        }
         auto each = [&](auto f) {
             if (listed)
-                for (int q = t; q < items; q += DRAW_THREADS) f(a.list[(i64)i * DRAW_LIST + q]);
+                for (int q = t; q < items; q += DRAW_THREADS) {
+                    const ulong2 x = a.list[(i64)i * DRAW_LIST + q];
+                    f((u64)x.x, [&] { return (u64)x.y; });
+                }
             else
-                each_word<DRAW_THREADS>(z, 0, V, [&](int v, float x) { f(place_of(key_of(x), (u32)v)); });
+                each_word<DRAW_THREADS>(z, 0, V, [&](int v, float x) {
+                    const u32 key = key_of(x);
+                    f(place_of(key, (u32)v), [&] { return fixed_of(weight_of(key, top, r.slope)); });
+                });
         };
-        // integers: what the threads put in does not hang on the order
-        auto mass_within = [&](u64 up_to) {
+        // the border is among the words of its bin; where top-p looks at what top-k left, among those
+        auto in_bin = [&](u64 x) { return !listed || bin_of(~(u32)(x >> 32), top) == o.bin; };
+        auto within = [&](u64 x) { return x <= limit; };
+        auto mass_within = [&] {
             u64 h = 0, l = 0;
-            each([&](u64 x) {
-                if (x > up_to) return;
-                const u64 w = fixed_of(weigh(x));
+            each([&](u64 x, auto weight) {
+                if (x > limit) return;
+                const u64 w = weight();
                 h += w >> 32;
                 l += w & 0xFFFFFFFFull;
             });
@@ -553,11 +685,14 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
             l = block_sum<DRAW_THREADS>(l, lds.sums);
             return mass_of(h, l);
         };
-        if (r.k) limit = place_at<false>(each, weigh, ~0ull, (u64)r.k - (o.how == BORDER_BIN_LISTED ? o.above : 0), 0.0, lds);
+        if (r.k) limit = place_at<false>(each, in_bin, (u64)r.k - (listed ? o.above : 0), 0.0, lds);
         if (r.p < 1.0) {
-            const bool bin = o.how == BORDER_BIN_LISTED;
-            const double whole = r.k || !listed ? mass_within(limit) : o.whole;
-            limit = place_at<true>(each, weigh, limit, 0, r.p * whole - (bin ? o.above_mass : 0.0), lds);
+            if (r.k || !listed) {
+                const double whole = mass_within();
+                limit = place_at<true>(each, within, 0, r.p * whole, lds);
+            } else {
+                limit = place_at<true>(each, in_bin, 0, r.p * o.whole - o.above_mass, lds);
+            }
         }
         // weights of the parts
         __syncthreads();
@@ -580,10 +715,9 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
                 }
             }
         } else if (listed) {
-            each([&](u64 x) {
-                const double w = weight_in(x);
-                if (w == 0.0) return;
-                const u64 f = fixed_of(w);
+            each([&](u64 x, auto weight) {
+                const u64 f = weight();
+                if (x > limit || f == 0 || (double)f * 0x1p-62 < r.least) return;
                 const int q = (int)((u32)x / (u32)part);
                 atomicAdd(atom(&lds.hi[q]), f >> 32);
                 atomicAdd(atom(&lds.lo[q]), f & 0xFFFFFFFFull);
@@ -690,14 +824,15 @@ size_t draw_carve(i64 n, i64 V, char *ws, DrawArgs *a)
     };
     const size_t N = (size_t)n;
     char *tops = take(4 * N * parts), *counts = take(4 * N * DRAW_BINS), *hi = take(8 * N * DRAW_BINS), *lo = take(8 * N * DRAW_BINS), *listed = take(4 * N),
-         *list = take(8 * N * DRAW_LIST), *mass = take(8 * N * parts);
+         *borders = take(sizeof(Border) * N), *list = take(16 * N * DRAW_LIST), *mass = take(8 * N * parts);
     if (a) {
         a->tops = (u32 *)tops;
         a->counts = (u32 *)counts;
         a->hi = (u64 *)hi;
         a->lo = (u64 *)lo;
         a->listed = (u32 *)listed;
-        a->list = (u64 *)list;
+        a->borders = (Border *)borders;
+        a->list = (ulong2 *)list;
         a->mass = (double *)mass;
     }
     return at;
@@ -710,6 +845,7 @@ void launch_draw(const DrawArgs &a, hipStream_t st)
         const dim3 grid((unsigned)(a.n * a.parts)), blk(PART_THREADS);
         hipLaunchKernelGGL(k_draw_top<T>, grid, blk, 0, st, a);
         if (a.top_k || a.top_p) hipLaunchKernelGGL(k_draw_bins<T>, grid, blk, 0, st, a);
+        if (a.top_k || a.top_p) hipLaunchKernelGGL(k_draw_border, dim3((unsigned)a.n), dim3(DRAW_THREADS), 0, st, a);
         hipLaunchKernelGGL(k_draw_gather<T>, grid, blk, 0, st, a);
     }
     hipLaunchKernelGGL(k_draw<T>, dim3((unsigned)a.n), dim3(DRAW_THREADS), 0, st, a);
@@ -728,7 +864,7 @@ size_t tensair_sample_workspace_bytes(int64_t n, int64_t vocab)
     // the most of all rows up to n and all vocabularies up to vocab: fewer rows have more parts
     if (vocab <= DRAW_SOLO) return 256;
     n = std::min<int64_t>(n, DRAW_ROWS);
-    return std::max<size_t>(256, layer_up256((size_t)n * 8 * DRAW_LIST) + 2 * layer_up256((size_t)n * 8 * DRAW_BINS) + layer_up256((size_t)n * 4 * DRAW_BINS) +
+    return std::max<size_t>(256, layer_up256((size_t)n * 16 * DRAW_LIST) + layer_up256((size_t)n * sizeof(Border)) + 2 * layer_up256((size_t)n * 8 * DRAW_BINS) + layer_up256((size_t)n * 4 * DRAW_BINS) +
                                      layer_up256((size_t)n * 4) + layer_up256((size_t)n * 4 * DRAW_PARTS) + layer_up256((size_t)n * 8 * DRAW_PARTS));
 }
 
