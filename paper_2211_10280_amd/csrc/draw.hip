@@ -40,6 +40,7 @@ struct DrawArgs {
     int *words, *status;
     float *prob;
     int part, parts;             // words of a part, parts of a row; 0 parts: k_draw alone
+    int unit;                    // a part's weights are whole numbers of 2^-unit in the bins
     // in the workspace
     u32 *tops;                   // [n][parts]
     u32 *counts;                 // [n][DRAW_BINS]
@@ -274,25 +275,22 @@ template <typename T>
 __global__ void __launch_bounds__(PART_THREADS) k_draw_bins(DrawArgs a)
 {
     __shared__ u32 counts[DRAW_BINS], tops[PART_THREADS / WAVE];
-    __shared__ u64 hi[DRAW_BINS], lo[DRAW_BINS];
+    __shared__ u64 mass[DRAW_BINS];              // in 2^-unit, so that a part's words fit
     const int i = (int)blockIdx.x / a.parts, c = (int)blockIdx.x - i * a.parts, t = (int)threadIdx.x;
     const Row r = row_of(a, i);
     if (r.first || (r.k == 0 && r.p >= 1.0)) return;
     const bool weigh = r.k == 0;                 // else top-p looks at what top-k left, which is listed
+    const double unit = (double)(1ull << a.unit);
     for (int b = t; b < DRAW_BINS; b += PART_THREADS) {
         counts[b] = 0;
-        hi[b] = lo[b] = 0;
+        if (weigh) mass[b] = 0;
     }
     const u32 top = row_top<PART_THREADS>(a, i, tops);           // waits for all threads
     each_word<PART_THREADS>((const T *)a.z + (i64)i * a.stride, c * a.part, min(a.V, (c + 1) * a.part), [&](int, float z) {
         const u32 key = key_of(z);
         const int b = bin_of(key, top);
         atomicAdd(&counts[b], 1u);
-        if (weigh) {
-            const u64 w = fixed_of(weight_of(key, top, r.slope));
-            atomicAdd(atom(&hi[b]), w >> 32);
-            atomicAdd(atom(&lo[b]), w & 0xFFFFFFFFull);
-        }
+        if (weigh) atomicAdd(atom(&mass[b]), (u64)(weight_of(key, top, r.slope) * unit));
     });
     __syncthreads();
     for (int b = t; b < DRAW_BINS; b += PART_THREADS) {
@@ -300,8 +298,8 @@ __global__ void __launch_bounds__(PART_THREADS) k_draw_bins(DrawArgs a)
         const i64 at = (i64)i * DRAW_BINS + b;
         atomicAdd(&a.counts[at], counts[b]);
         if (!weigh) continue;
-        atomicAdd(atom(&a.hi[at]), hi[b]);
-        atomicAdd(atom(&a.lo[at]), lo[b]);
+        atomicAdd(atom(&a.hi[at]), mass[b] >> (a.unit - 30));
+        atomicAdd(atom(&a.lo[at]), (mass[b] & ((1ull << (a.unit - 30)) - 1)) << (62 - a.unit));
     }
 }
 
@@ -316,36 +314,36 @@ enum { BORDER_NONE, BORDER_ALL_LISTED, BORDER_BIN_LISTED, BORDER_ROW };
 __global__ void __launch_bounds__(DRAW_THREADS) k_draw_border(DrawArgs a)
 {
     constexpr int PER = DRAW_BINS / DRAW_THREADS;
+    static_assert(PER == 4, "a thread loads its bins at once");
     __shared__ Three lds[DRAW_THREADS / WAVE];
     __shared__ int pick;
     const int t = (int)threadIdx.x, i = (int)blockIdx.x;
     const Row r = row_of(a, i);
-    if (r.first || (r.k == 0 && r.p >= 1.0)) return;
     const i64 at = (i64)i * DRAW_BINS + t * PER;
-    Three x[PER], sum = {0, 0, 0}, all;
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-        x[j] = Three{a.counts[at + j], 0, 0};
-        if (r.k == 0) {
-            x[j].hi = a.hi[at + j];
-            x[j].lo = a.lo[at + j];
-        }
-        sum = Three{sum.n + x[j].n, sum.hi + x[j].hi, sum.lo + x[j].lo};
-    }
+    const uint4 n = *reinterpret_cast<const uint4 *>(a.counts + at);
+    const ulong2 h0 = *reinterpret_cast<const ulong2 *>(a.hi + at), h1 = *reinterpret_cast<const ulong2 *>(a.hi + at + 2);
+    const ulong2 l0 = *reinterpret_cast<const ulong2 *>(a.lo + at), l1 = *reinterpret_cast<const ulong2 *>(a.lo + at + 2);
+    if (r.first || (r.k == 0 && r.p >= 1.0)) return;
+    // sums up to each of the four bins; weights are 0 where top-k decides
+    const Three s0 = {n.x, h0.x, l0.x}, s1 = {s0.n + n.y, s0.hi + h0.y, s0.lo + l0.y}, s2 = {s1.n + n.z, s1.hi + h1.x, s1.lo + l1.x}, s3 = {s2.n + n.w, s2.hi + h1.y, s2.lo + l1.y};
     if (t == 0) pick = DRAW_BINS;
-    Three run = block_before<DRAW_THREADS>(sum, lds, all);
+    Three all;
+    const Three run = block_before<DRAW_THREADS>(s3, lds, all);
     const double whole = mass_of(all.hi, all.lo), want = r.p * whole;
     Border o = {DRAW_BINS, 0, 0, BORDER_ROW, 0.0, whole};
-    for (int j = 0; j < PER && o.bin == DRAW_BINS; ++j) {
-        const Three to = {run.n + x[j].n, run.hi + x[j].hi, run.lo + x[j].lo};
-        if (x[j].n && (r.k ? to.n >= (u64)r.k : mass_of(to.hi, to.lo) >= want)) {
+    auto look = [&](int j, const Three &before, const Three &to) {
+        if (o.bin < DRAW_BINS || to.n == before.n) return;
+        if (r.k ? run.n + to.n >= (u64)r.k : mass_of(run.hi + to.hi, run.lo + to.lo) >= want) {
             o.bin = t * PER + j;
-            o.above = (u32)run.n;
-            o.in = (u32)x[j].n;
-            o.above_mass = mass_of(run.hi, run.lo);
+            o.above = (u32)(run.n + before.n);
+            o.in = (u32)(to.n - before.n);
+            o.above_mass = mass_of(run.hi + before.hi, run.lo + before.lo);
         }
-        run = to;
-    }
+    };
+    look(0, Three{0, 0, 0}, s0);
+    look(1, s0, s1);
+    look(2, s1, s2);
+    look(3, s2, s3);
     if (o.bin < DRAW_BINS) atomicMin(&pick, o.bin);
     __syncthreads();
     if (o.bin == DRAW_BINS || o.bin != pick) return;             // all words' number and weight are enough: there is one
@@ -613,7 +611,7 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
     const T *z = (const T *)a.z + (i64)i * a.stride;
     const Row r = row_of(a, i);
     const bool solo = a.parts == 0;
-    const int part = solo ? (V + DRAW_THREADS - 1) / DRAW_THREADS * DRAW_THREADS : a.part, parts = solo ? 1 : a.parts;
+    const int part = solo ? V : a.part, parts = solo ? 1 : a.parts;
     u32 top = 0;
     if (solo) {
         each_word<DRAW_THREADS>(z, 0, V, [&](int, float x) { top = max(top, key_of(x)); });
@@ -659,20 +657,27 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
             return;
         }
         auto each = [&](auto f) {
-            if (listed)
-                for (int q = t; q < items; q += DRAW_THREADS) {
-                    const ulong2 x = a.list[(i64)i * DRAW_LIST + q];
-                    f((u64)x.x, [&] { return (u64)x.y; });
+            if (listed) {
+                const ulong2 *list = a.list + (i64)i * DRAW_LIST;
+                for (int q = t; q < items; q += 4 * DRAW_THREADS) {          // four in flight at a time
+                    ulong2 x[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (q + k * DRAW_THREADS < items) x[k] = list[q + k * DRAW_THREADS];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (q + k * DRAW_THREADS < items) f((u64)x[k].x, [&] { return (u64)x[k].y; });
                 }
-            else
+            } else {
                 each_word<DRAW_THREADS>(z, 0, V, [&](int v, float x) {
                     const u32 key = key_of(x);
                     f(place_of(key, (u32)v), [&] { return fixed_of(weight_of(key, top, r.slope)); });
                 });
+            }
         };
         // the border is among the words of its bin; where top-p looks at what top-k left, among those
-        auto in_bin = [&](u64 x) { return !listed || bin_of(~(u32)(x >> 32), top) == o.bin; };
-        auto within = [&](u64 x) { return x <= limit; };
+        bool binned = listed;
+        auto among = [&](u64 x) { return x <= limit && (!binned || bin_of(~(u32)(x >> 32), top) == o.bin); };
         auto mass_within = [&] {
             u64 h = 0, l = 0;
             each([&](u64 x, auto weight) {
@@ -685,18 +690,18 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
             l = block_sum<DRAW_THREADS>(l, lds.sums);
             return mass_of(h, l);
         };
-        if (r.k) limit = place_at<false>(each, in_bin, (u64)r.k - (listed ? o.above : 0), 0.0, lds);
+        if (r.k) limit = place_at<false>(each, among, (u64)r.k - (listed ? o.above : 0), 0.0, lds);
         if (r.p < 1.0) {
-            if (r.k || !listed) {
-                const double whole = mass_within();
-                limit = place_at<true>(each, within, 0, r.p * whole, lds);
-            } else {
-                limit = place_at<true>(each, in_bin, 0, r.p * o.whole - o.above_mass, lds);
-            }
+            binned = listed && !r.k;
+            const double want = binned ? r.p * o.whole - o.above_mass : r.p * mass_within();
+            limit = place_at<true>(each, among, 0, want, lds);
         }
         // weights of the parts
         __syncthreads();
-        for (int q = t; q < parts; q += DRAW_THREADS) lds.hi[q] = lds.lo[q] = 0;
+        // the likely words of a vocabulary lie side by side, so that most of a list may be of one part: neighbouring lanes add to copies of their own
+        int copies = 0;
+        while ((parts << (copies + 1)) <= DRAW_DIGITS && copies < 5) ++copies;
+        for (int q = t; q < parts << copies; q += DRAW_THREADS) lds.hi[q] = lds.lo[q] = 0;
         __syncthreads();
         if (solo || o.how == BORDER_ROW) {
             // one part after the other; a part's words in 64 bits, in the threads' order
@@ -710,15 +715,15 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
                 h = block_sum<DRAW_THREADS>(h, lds.sums);
                 l = block_sum<DRAW_THREADS>(l, lds.sums);
                 if (t == 0) {
-                    lds.hi[q] = h;
-                    lds.lo[q] = l;
+                    lds.hi[q << copies] = h;
+                    lds.lo[q << copies] = l;
                 }
             }
         } else if (listed) {
             each([&](u64 x, auto weight) {
                 const u64 f = weight();
                 if (x > limit || f == 0 || (double)f * 0x1p-62 < r.least) return;
-                const int q = (int)((u32)x / (u32)part);
+                const int q = (int)((u32)x / (u32)part) << copies | (t & ((1 << copies) - 1));
                 atomicAdd(atom(&lds.hi[q]), f >> 32);
                 atomicAdd(atom(&lds.lo[q]), f & 0xFFFFFFFFull);
             });
@@ -726,7 +731,12 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
         __syncthreads();
         double m = 0.0;
         if (t < parts) {
-            m = mass_of(lds.hi[t], lds.lo[t]);
+            u64 h = 0, l = 0;
+            for (int q = t << copies; q < (t + 1) << copies; ++q) {
+                h += lds.hi[q];
+                l += lds.lo[q];
+            }
+            m = mass_of(h, l);
             if (!solo && (o.how == BORDER_NONE || o.how == BORDER_BIN_LISTED)) m += a.mass[(i64)i * parts + t];
         }
         const double run = block_before<DRAW_THREADS>(m, lds.mass, total);
@@ -752,40 +762,42 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
         before = lds.mass[0];
         __syncthreads();
     }
-    // the word in part c: a run of it to a thread, so that running sums go by the words' numbers
-    const int from = c * part, to = min(V, from + part), per = part / DRAW_THREADS, lo = min(to, from + t * per), hi = min(to, lo + per);
-    double m = 0.0;
+    // the word in part c: four words to a thread at a time, so that running sums go by the words' numbers
+    const int from = c * part, to = min(V, from + part);
     int mine = -1, last = -1;
     double w_mine = 0.0, w_last = 0.0;
-    if (!r.first) {
-        for (int v = lo; v < hi; ++v) m += weight_in(place_of(key_of(widen1(z[v])), (u32)v));
-        double all;
-        double run = before + block_before<DRAW_THREADS>(m, lds.mass, all);
-        for (int v = lo; v < hi; ++v) {
-            const double w = weight_in(place_of(key_of(widen1(z[v])), (u32)v));
-            if (!(w > 0.0)) continue;
-            run += w;
-            last = v;
-            w_last = w;
-            if (!end && mine < 0 && run > want) {
-                mine = v;
-                w_mine = w;
-            }
-        }
-    } else {
-        for (int v = hi - 1; v >= lo; --v)
-            if (key_of(widen1(z[v])) == top) mine = v;
-    }
     __syncthreads();
     if (t == 0) {
         lds.pick = V;
         lds.found[0] = 0;
     }
-    __syncthreads();
-    if (mine >= 0) atomicMin(&lds.pick, mine);
-    if (last >= 0) atomicMax(atom(&lds.found[0]), (u64)last);
-    __syncthreads();
-    if (lds.pick == V && last >= 0 && (u64)last == lds.found[0]) {       // the sums of a part and of its words differ in their last places
+    for (int block = from; block < to; block += 4 * DRAW_THREADS) {
+        const int v = block + 4 * t;
+        u32 key[4];
+        double w[4], all;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) key[j] = v + j < to ? key_of(widen1(z[v + j])) : KEY_LOWEST;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = r.first ? (key[j] == top ? 1.0 : 0.0) : weight_in(place_of(key[j], (u32)(v + j)));
+        double run = before + block_before<DRAW_THREADS>((w[0] + w[1]) + (w[2] + w[3]), lds.mass, all);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (!(w[j] > 0.0)) continue;
+            run += w[j];
+            last = v + j;
+            w_last = w[j];
+            if (!end && mine < 0 && run > want) {
+                mine = v + j;
+                w_mine = w[j];
+            }
+        }
+        before += all;
+        if (mine >= 0) atomicMin(&lds.pick, mine);
+        if (last >= 0) atomicMax(atom(&lds.found[0]), (u64)last);
+        __syncthreads();
+        if (lds.pick < V) break;
+    }
+    if (lds.pick == V && last >= 0 && (u64)last == lds.found[0]) {       // u is 1, or the sums of a part and of its words differ in their last places
         mine = last;
         w_mine = w_last;
     } else if (mine != lds.pick) {
@@ -814,6 +826,8 @@ size_t draw_carve(i64 n, i64 V, char *ws, DrawArgs *a)
     if (a) {
         a->part = part;
         a->parts = parts;
+        a->unit = 62;
+        while (parts && (1ll << (62 - a->unit)) < part) --a->unit;
     }
     if (!parts) return 256;
     size_t at = 0;
