@@ -18,17 +18,20 @@
 
 namespace {
 
-#define DRAW_THREADS 1024        // of k_draw
+#define DRAW_THREADS 512         // of k_draw; with 1 024 its registers go to memory and back
+#define BORDER_THREADS 1024      // of k_draw_border
 #define PART_THREADS 512         // of the other kernels: a workgroup to a part of a row
 #define DRAW_SOLO 8192           // words of a row that k_draw alone takes
 #define DRAW_PART 4096           // fewest words of a part
-#define DRAW_PARTS 1024          // most parts of a row
+#define DRAW_PARTS 512           // most parts of a row
 #define DRAW_WORKGROUPS 2048     // parts of all rows that are aimed at
 #define DRAW_BINS 4096           // 256 to a doubling of (distance + 1)
 #define DRAW_DIGITS 2048         // of places
 #define DRAW_LIST 16384          // most words of a row's list
 #define DRAW_STAGED 2048         // of a part's words that go to it, most that are put together in LDS before
-#define DRAW_FEW 256             // words of a list that are compared each with each
+#define DRAW_SHORT 512           // most words of a list that need not hold those above the border's bin
+#define DRAW_FEW 128             // words of a list that are compared each with each
+#define DRAW_PAIRS 128           // words of the border's bin that are
 #define DRAW_ROWS 256            // rows at a time, so that the lists take 67 MB at most
 
 struct DrawArgs {
@@ -195,7 +198,7 @@ __device__ __forceinline__ u32 block_max(u32 x, u32 *lds)
     for (int k = 1; k < THREADS / WAVE; ++k) x = max(x, lds[k]);
     return x;
 }
-// sum of what the threads before have
+// sum of what the threads before have.
 template <int THREADS, typename S>
 __device__ __forceinline__ S block_before(S x, S *lds, S &all)
 {
@@ -245,6 +248,13 @@ __device__ __forceinline__ Three block_before(Three x, Three *lds, Three &all)
     }
     return Three{base.n + run.n - x.n, base.hi + run.hi - x.hi, base.lo + run.lo - x.lo};
 }
+__device__ __forceinline__ double wave_sum64(double x)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, WAVE);
+    return x;
+}
+__device__ __forceinline__ double rd_lane(double x, int l) { return __longlong_as_double((long long)rd_lane64((u64)__double_as_longlong(x), l)); }
 __device__ __forceinline__ unsigned long long *atom(u64 *p) { return (unsigned long long *)p; }
 
 template <int THREADS>
@@ -311,11 +321,11 @@ struct Border {
     double above_mass, whole;    // weight of the bins above and of the row, where that is needed
 };
 enum { BORDER_NONE, BORDER_ALL_LISTED, BORDER_BIN_LISTED, BORDER_ROW };
-__global__ void __launch_bounds__(DRAW_THREADS) k_draw_border(DrawArgs a)
+__global__ void __launch_bounds__(BORDER_THREADS) k_draw_border(DrawArgs a)
 {
-    constexpr int PER = DRAW_BINS / DRAW_THREADS;
+    constexpr int PER = DRAW_BINS / BORDER_THREADS;
     static_assert(PER == 4, "a thread loads its bins at once");
-    __shared__ Three lds[DRAW_THREADS / WAVE];
+    __shared__ Three lds[BORDER_THREADS / WAVE];
     __shared__ int pick;
     const int t = (int)threadIdx.x, i = (int)blockIdx.x;
     const Row r = row_of(a, i);
@@ -328,7 +338,7 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw_border(DrawArgs a)
     const Three s0 = {n.x, h0.x, l0.x}, s1 = {s0.n + n.y, s0.hi + h0.y, s0.lo + l0.y}, s2 = {s1.n + n.z, s1.hi + h1.x, s1.lo + l1.x}, s3 = {s2.n + n.w, s2.hi + h1.y, s2.lo + l1.y};
     if (t == 0) pick = DRAW_BINS;
     Three all;
-    const Three run = block_before<DRAW_THREADS>(s3, lds, all);
+    const Three run = block_before<BORDER_THREADS>(s3, lds, all);
     const double whole = mass_of(all.hi, all.lo), want = r.p * whole;
     Border o = {DRAW_BINS, 0, 0, BORDER_ROW, 0.0, whole};
     auto look = [&](int j, const Three &before, const Three &to) {
@@ -347,8 +357,10 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw_border(DrawArgs a)
     if (o.bin < DRAW_BINS) atomicMin(&pick, o.bin);
     __syncthreads();
     if (o.bin == DRAW_BINS || o.bin != pick) return;             // all words' number and weight are enough: there is one
-    if (o.above + o.in <= DRAW_LIST) o.how = BORDER_ALL_LISTED;
-    else if (o.in <= DRAW_LIST && (r.k == 0 || r.p >= 1.0)) o.how = BORDER_BIN_LISTED;
+    // top-p looks at what top-k left; else the words above the border's bin need not be listed, and are not where they are many
+    const bool both = r.k && r.p < 1.0;
+    if (o.above + o.in <= (both ? DRAW_LIST : DRAW_SHORT)) o.how = BORDER_ALL_LISTED;
+    else if (o.in <= DRAW_LIST && !both) o.how = BORDER_BIN_LISTED;
     a.borders[i] = o;
 }
 __device__ __forceinline__ Border border_of(const DrawArgs &a, const Row &r, int i)
@@ -409,7 +421,8 @@ __global__ void __launch_bounds__(PART_THREADS) k_draw_gather(DrawArgs a)
 
 struct DrawLds {
     u32 counts[DRAW_DIGITS], tops[DRAW_THREADS / WAVE];
-    u64 hi[DRAW_DIGITS], lo[DRAW_DIGITS];        // by digits, then by parts
+    alignas(16) u64 hi[DRAW_DIGITS];             // by digits, then by parts
+    u64 lo[DRAW_DIGITS];
     Three three[DRAW_THREADS / WAVE];
     u64 sums[DRAW_THREADS / WAVE];
     double mass[DRAW_THREADS / WAVE];
@@ -532,6 +545,45 @@ __device__ __forceinline__ u64 place_at(Each each, Among among, u64 number, doub
     return first;
 }
 
+// The same where at most DRAW_PAIRS items are in question (else ~0): each is compared with each, an item to a thread.  One word after the other is in while those
+// before it do not reach the number or the weight.
+template <bool BY_MASS, typename Each, typename Among>
+__device__ __forceinline__ u64 place_among_few(Each each, Among among, u64 number, double mass, DrawLds &lds)
+{
+    ulong2 *items = (ulong2 *)lds.hi;
+    const int t = (int)threadIdx.x;
+    __syncthreads();
+    if (t == 0) {
+        lds.pick = 0;
+        lds.found[0] = 0;
+    }
+    __syncthreads();
+    each([&](u64 x, auto weight) {
+        if (!among(x)) return;
+        const int at = atomicAdd(&lds.pick, 1);
+        if (at < DRAW_PAIRS) items[at] = make_ulong2(x, BY_MASS ? weight() : 0);
+    });
+    __syncthreads();
+    const int n = lds.pick;
+    if (n > DRAW_PAIRS) return ~0ull;
+    if (t < n) {
+        const u64 x = items[t].x;
+        u64 rank = 0, hi = 0, lo = 0;
+#pragma unroll 4
+        for (int q = 0; q < n; ++q) {
+            const ulong2 y = items[q];
+            if (y.x < x) {
+                ++rank;
+                hi += y.y >> 32;
+                lo += y.y & 0xFFFFFFFFull;
+            }
+        }
+        if (rank == 0 || (BY_MASS ? mass_of(hi, lo) < mass : rank < number)) atomicMax(atom(&lds.found[0]), x);
+    }
+    __syncthreads();
+    return lds.found[0];
+}
+
 // A list of at most DRAW_FEW words: each compared with each, a word to a thread.  Sums are of whole numbers, so the list's order does not matter.
 __device__ __forceinline__ void draw_few(const DrawArgs &a, const Row &r, int i, const Border &o, int items, DrawLds &lds)
 {
@@ -627,6 +679,8 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
         }
         return;
     }
+    double u = a.u[i];
+    u = u > 0.0 ? fmin(u, 1.0) : 0.0;
     u64 limit = ~0ull;                           // the last place that is in
     double total = 0.0, before = 0.0, want = 0.0;
     int c = 0;                                   // the part that the word is in
@@ -690,11 +744,16 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
             l = block_sum<DRAW_THREADS>(l, lds.sums);
             return mass_of(h, l);
         };
-        if (r.k) limit = place_at<false>(each, among, (u64)r.k - (listed ? o.above : 0), 0.0, lds);
+        if (r.k) {
+            const u64 number = (u64)r.k - (listed ? o.above : 0);
+            if (listed) limit = place_among_few<false>(each, among, number, 0.0, lds);
+            if (limit == ~0ull) limit = place_at<false>(each, among, number, 0.0, lds);
+        }
         if (r.p < 1.0) {
             binned = listed && !r.k;
             const double want = binned ? r.p * o.whole - o.above_mass : r.p * mass_within();
-            limit = place_at<true>(each, among, 0, want, lds);
+            const u64 found = listed ? place_among_few<true>(each, among, 0, want, lds) : ~0ull;
+            limit = found == ~0ull ? place_at<true>(each, among, 0, want, lds) : found;
         }
         // weights of the parts
         __syncthreads();
@@ -740,8 +799,6 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
             if (!solo && (o.how == BORDER_NONE || o.how == BORDER_BIN_LISTED)) m += a.mass[(i64)i * parts + t];
         }
         const double run = block_before<DRAW_THREADS>(m, lds.mass, total);
-        double u = a.u[i];
-        u = u > 0.0 ? fmin(u, 1.0) : 0.0;
         want = u * total;
         if (t == 0) lds.pick = parts;
         __syncthreads();
@@ -762,50 +819,64 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
         before = lds.mass[0];
         __syncthreads();
     }
-    // the word in part c: four words to a thread at a time, so that running sums go by the words' numbers
-    const int from = c * part, to = min(V, from + part);
-    int mine = -1, last = -1;
-    double w_mine = 0.0, w_last = 0.0;
-    __syncthreads();
-    if (t == 0) {
-        lds.pick = V;
-        lds.found[0] = 0;
-    }
-    for (int block = from; block < to; block += 4 * DRAW_THREADS) {
-        const int v = block + 4 * t;
-        u32 key[4];
-        double w[4], all;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) key[j] = v + j < to ? key_of(widen1(z[v + j])) : KEY_LOWEST;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = r.first ? (key[j] == top ? 1.0 : 0.0) : weight_in(place_of(key[j], (u32)(v + j)));
-        double run = before + block_before<DRAW_THREADS>((w[0] + w[1]) + (w[2] + w[3]), lds.mass, all);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (!(w[j] > 0.0)) continue;
-            run += w[j];
-            last = v + j;
-            w_last = w[j];
-            if (!end && mine < 0 && run > want) {
-                mine = v + j;
-                w_mine = w[j];
-            }
-        }
-        before += all;
-        if (mine >= 0) atomicMin(&lds.pick, mine);
-        if (last >= 0) atomicMax(atom(&lds.found[0]), (u64)last);
+    // the word in part c: an eighth of it to a wave, then an eighth of the one that has it, then 64 words at a time
+    constexpr int WAVES = DRAW_THREADS / WAVE;
+    const int lane = lane_id(), wave = t / WAVE;
+    auto weight_at = [&](int v, int to) {
+        if (v >= to) return 0.0;
+        const u32 key = key_of(widen1(z[v]));
+        return r.first ? (key == top ? 1.0 : 0.0) : weight_in(place_of(key, (u32)v));
+    };
+    int from = c * part, len = (min(V - from, part) + WAVES * WAVES * WAVE - 1) / (WAVES * WAVES * WAVE) * (WAVES * WAVES * WAVE);
+    const int stop = min(V, from + part);
+#pragma unroll 1
+    for (int level = 0; level < 2; ++level) {
+        len /= WAVES;
+        const int lo = from + wave * len;
+        double m = 0.0;
+#pragma unroll 4
+        for (int v = lo; v < lo + len; v += WAVE) m += weight_at(v + lane, stop);
+        m = wave_sum64(m);
         __syncthreads();
-        if (lds.pick < V) break;
+        if (lane == 0) lds.mass[wave] = m;
+        __syncthreads();
+        // the first that the draw falls into; the last one that is not empty where u is 1 or sums differ in their last places
+        int got = -1, filled = 0;
+        double run = before, at = before;
+        for (int w = 0; w < WAVES; ++w) {
+            const double x = lds.mass[w];
+            if (x > 0.0 && got < 0) {
+                filled = w;
+                at = run;
+                if (!end && run + x > want) got = w;
+            }
+            run += x;
+        }
+        end = end || got < 0;
+        from += filled * len;
+        before = at;
     }
-    if (lds.pick == V && last >= 0 && (u64)last == lds.found[0]) {       // u is 1, or the sums of a part and of its words differ in their last places
-        mine = last;
-        w_mine = w_last;
-    } else if (mine != lds.pick) {
-        mine = -1;
-    }
-    if (mine >= 0) {
-        a.words[i] = mine;
-        if (a.prob) a.prob[i] = r.first ? 1.f : (float)(w_mine / total);
+    if (wave > 0) return;
+    for (int v = from; v < from + len; v += WAVE) {
+        const double w = weight_at(v + lane, stop);
+        double run = w;
+#pragma unroll
+        for (int o = 1; o < WAVE; o *= 2) {
+            const double x = __shfl_up(run, o, WAVE);
+            if (lane >= o) run += x;
+        }
+        const u64 in = __ballot(w > 0.0), above = end ? 0 : __ballot(w > 0.0 && before + run > want);
+        u64 later = 0;                           // whether a word further on is left
+        if (!above && in)
+            for (int x = v + WAVE; x < from + len && !later; x += WAVE) later = __ballot(weight_at(x + lane, stop) > 0.0);
+        before += rd_lane(run, WAVE - 1);
+        if (!above && (!in || later)) continue;
+        const int got = above ? __ffsll((long long)above) - 1 : 63 - __clzll((long long)in);
+        if (lane == got) {
+            a.words[i] = v + lane;
+            if (a.prob) a.prob[i] = r.first ? 1.f : (float)(w / total);
+        }
+        return;
     }
 }
 
@@ -859,7 +930,7 @@ void launch_draw(const DrawArgs &a, hipStream_t st)
         const dim3 grid((unsigned)(a.n * a.parts)), blk(PART_THREADS);
         hipLaunchKernelGGL(k_draw_top<T>, grid, blk, 0, st, a);
         if (a.top_k || a.top_p) hipLaunchKernelGGL(k_draw_bins<T>, grid, blk, 0, st, a);
-        if (a.top_k || a.top_p) hipLaunchKernelGGL(k_draw_border, dim3((unsigned)a.n), dim3(DRAW_THREADS), 0, st, a);
+        if (a.top_k || a.top_p) hipLaunchKernelGGL(k_draw_border, dim3((unsigned)a.n), dim3(BORDER_THREADS), 0, st, a);
         hipLaunchKernelGGL(k_draw_gather<T>, grid, blk, 0, st, a);
     }
     hipLaunchKernelGGL(k_draw<T>, dim3((unsigned)a.n), dim3(DRAW_THREADS), 0, st, a);
