@@ -54,3 +54,11 @@ __device__ __forceinline__ float lanes_sum(float x)
 __device__ __forceinline__ float4 mul4(float4 a, float4 b) { return make_float4(a.x * b.x, a.y * b.y, a.z * b.z, a.w * b.w); }
 __device__ __forceinline__ float4 plus4(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
 __device__ __forceinline__ float hsum4(float4 a) { return (a.x + a.y) + (a.z + a.w); }
+// rounded to nearest even by the hardware's conversion of two
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void put4(float *p, float4 v) { st4(p, v); }
+__device__ __forceinline__ void put4(bf16_t *p, float4 v)
+{
+    const bf16x2 lo = {(__bf16)v.x, (__bf16)v.y}, hi = {(__bf16)v.z, (__bf16)v.w};
+    *reinterpret_cast<uint2 *>(p) = make_uint2(__builtin_bit_cast(u32, lo), __builtin_bit_cast(u32, hi));
+}

@@ -51,15 +51,6 @@ __device__ __forceinline__ void open4(float4 s, float4 &a, float4 &b)
 __device__ __forceinline__ void gate4(float4 g, float4 &a, float4 &b) { open4(gate4(g), a, b); }
 __device__ __forceinline__ float4 fma4(float4 a, float4 b, float4 c) { return make_float4(fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y), fmaf(a.z, b.z, c.z), fmaf(a.w, b.w, c.w)); }
 
-// rounded to nearest even by the hardware's conversion of two
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ void put4(float *p, float4 v) { st4(p, v); }
-__device__ __forceinline__ void put4(bf16_t *p, float4 v)
-{
-    const bf16x2 lo = {(__bf16)v.x, (__bf16)v.y}, hi = {(__bf16)v.z, (__bf16)v.w};
-    *reinterpret_cast<uint2 *>(p) = make_uint2(__builtin_bit_cast(u32, lo), __builtin_bit_cast(u32, hi));
-}
-
 // ---- tiles.  The tokens are cut into tiles of RECUR_TILE whatever the sequences are: a sequence's first token resets the state, which is all that a tile has to know of
 // them.  A workgroup has a tile's 4 * G channels; a thread has RECUR_RUN tokens that follow one another (a strand of G threads has their channels), in registers from load to
 // store.  A run of tokens is a map h -> p h + q (with a reset in it: h -> q), and maps are put together: threads of a wave by shuffles, waves through LDS, tiles by the chain
@@ -489,33 +480,63 @@ struct StepArgs {
     int *status;
 };
 
-template <typename T>
+// A workgroup to ROWS rows.  Whether another row has the slot of one of them is seen by comparing all slots with theirs, a slot to a thread at a time, while the rows and
+// states are on their way.  A slot's first row takes those that follow, in order; the others leave it.
+template <typename T, int ROWS>
 __global__ void __launch_bounds__(BLOCK) k_recur_step(StepArgs a)
 {
-    const i64 id = (i64)blockIdx.x * BLOCK + threadIdx.x, i = id / a.C4;
-    const int c = 4 * (int)(id - i * a.C4);
-    if (i >= a.n) return;
-    const i64 slot = a.slots ? a.slots[i] : i;
-    if (slot < 0 || slot >= a.n_slots) {
-        if (a.status && c == 0) atomicOr(a.status, ST_BAD_ID);
-        if (a.out) st4((T *)a.out + i * a.out_stride + c, make_float4(0.f, 0.f, 0.f, 0.f));
-        return;
+    __shared__ u32 lds[2];
+    const int t = (int)threadIdx.x, total = ROWS * a.C4;
+    const i64 row0 = (i64)blockIdx.x * ROWS;
+    if (a.slots) {
+        int mine[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) mine[r] = row0 + r < a.n ? a.slots[row0 + r] : 0;
+        if (t < 2) lds[t] = 0;
+        __syncthreads();
+        u32 earlier = 0, later = 0;
+#pragma unroll 8
+        for (int j = t; j < (int)a.n; j += BLOCK) {
+            const int s = a.slots[j];
+            u32 same = 0;
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) same |= s == mine[r] ? 1u << r : 0u;
+            const i64 at = j - row0;                           // rows before this one of the workgroup's come after it, and the other way round
+            const u32 before = at <= 0 ? 0u : at >= ROWS ? ~0u : (1u << at) - 1u, after = at >= ROWS - 1 ? 0u : at < 0 ? ~0u : ~0u << (at + 1);
+            later |= same & before;
+            earlier |= same & after;
+        }
+        earlier = wave_or(earlier);
+        later = wave_or(later);
+        if (lane_id() == 0 && (earlier | later)) {
+            atomicOr(&lds[0], earlier);
+            atomicOr(&lds[1], later);
+        }
+        __syncthreads();
     }
-    if (a.slots)
-        for (i64 j = 0; j < i; ++j)
-            if (a.slots[j] == slot) return;                    // the slot's first row takes them all
-    float4 h = ld4(a.state + slot * a.state_stride + c);
-    for (i64 j = i; j < a.n; ++j) {
-        if (j > i && (!a.slots || a.slots[j] != slot)) {
-            if (!a.slots) break;
+    for (int k = t; k < total; k += BLOCK) {
+        const int r = k / a.C4, c = 4 * (k - r * a.C4);
+        const i64 i = row0 + r;
+        if (i >= a.n) break;
+        const i64 slot = a.slots ? a.slots[i] : i;
+        if (slot < 0 || slot >= a.n_slots) {
+            if (a.status && c == 0) atomicOr(a.status, ST_BAD_ID);
+            if (a.out) st4((T *)a.out + i * a.out_stride + c, make_float4(0.f, 0.f, 0.f, 0.f));
             continue;
         }
-        float4 f, b;
-        gate4(ld4((const T *)a.gate + j * a.g_stride + c), f, b);
-        h = fma4(f, h, mul4(b, ld4((const T *)a.x + j * a.x_stride + c)));
-        if (a.out) st4((T *)a.out + j * a.out_stride + c, h);
+        if (a.slots && lds[0] >> r & 1) continue;
+        const bool more = a.slots && lds[1] >> r & 1;
+        float4 h = ld4(a.state + slot * a.state_stride + c);
+        for (i64 j = i; j < a.n; ++j) {
+            if (j > i && a.slots[j] != slot) continue;
+            float4 f, b;
+            gate4(ld4((const T *)a.gate + j * a.g_stride + c), f, b);
+            h = fma4(f, h, mul4(b, ld4((const T *)a.x + j * a.x_stride + c)));
+            if (a.out) put4((T *)a.out + j * a.out_stride + c, h);
+            if (!more) break;
+        }
+        st4(a.state + slot * a.state_stride + c, h);
     }
-    st4(a.state + slot * a.state_stride + c, h);
 }
 
 // bytes of the chain's words, or, with an address, the chain there and what of it has to be zero
@@ -674,12 +695,16 @@ int tensair_recur_step(const void *x, int64_t x_stride, const void *gate, int64_
     if ((uintptr_t)status & 3) return tn_fail(TENSAIR_EINVAL, "status must be 4-byte aligned");
     if (n == 0) return TENSAIR_OK;
     const StepArgs a = {x, gate, out, x_stride, gate_stride, out_stride, state_stride, n, n_slots, dim / 4, slots, state, status};
-    const u64 blocks = ((u64)n * (u64)a.C4 + BLOCK - 1) / BLOCK;
-    if (blocks > TN_MAX_BLOCKS) return tn_fail(TENSAIR_EINVAL, "n * dim beyond what one launch covers");
+    // few rows to a workgroup where there are few rows, so that each has one chunk of them to a thread; more of them share the look through the slots
+    const int rows = n <= 4096 ? 4 : 16;
+    const u64 blocks = ((u64)n + rows - 1) / rows;
+    if (blocks > TN_MAX_BLOCKS) return tn_fail(TENSAIR_EINVAL, "n beyond what one launch covers");
     const dim3 grid((unsigned)blocks), blk(BLOCK);
     hipStream_t st = (hipStream_t)stream;
-    if (dtype == TENSAIR_F32) hipLaunchKernelGGL(k_recur_step<float>, grid, blk, 0, st, a);
-    else hipLaunchKernelGGL(k_recur_step<bf16_t>, grid, blk, 0, st, a);
+    if (dtype == TENSAIR_F32 && rows == 4) hipLaunchKernelGGL((k_recur_step<float, 4>), grid, blk, 0, st, a);
+    else if (dtype == TENSAIR_F32) hipLaunchKernelGGL((k_recur_step<float, 16>), grid, blk, 0, st, a);
+    else if (rows == 4) hipLaunchKernelGGL((k_recur_step<bf16_t, 4>), grid, blk, 0, st, a);
+    else hipLaunchKernelGGL((k_recur_step<bf16_t, 16>), grid, blk, 0, st, a);
     return layer_launched("recur_step");
 }
 
