@@ -22,43 +22,44 @@ struct NormArgs {
     float *mean, *rstd;
 };
 
+// A row to a group of G lanes.  Memory bounds it: 262 143 rows of 300, fp32 to bfloat16, 97 us (472 MB, 4.9 TB/s); two rows to a group, their loads side by side, 101, four 116.
 template <typename T, typename TO, int G, int ITERS>
 __global__ void __launch_bounds__(BLOCK) k_norm(NormArgs a)
 {
     const int l = (int)threadIdx.x % G;
-    const i64 row = (i64)blockIdx.x * (BLOCK / G) + (int)threadIdx.x / G;
-    if (row >= a.n) return;      // whole groups of G lanes leave
-    const T *src = (const T *)a.x + row * a.x_stride;
-    float4 v[ITERS];
-    float sum = 0.f;
+    for (i64 row = (i64)blockIdx.x * (BLOCK / G) + (int)threadIdx.x / G; row < a.n; row += (i64)gridDim.x * (BLOCK / G)) {
+        const T *src = (const T *)a.x + row * a.x_stride;
+        float4 v[ITERS];
+        float sum = 0.f;
 #pragma unroll
-    for (int it = 0; it < ITERS; ++it) {
-        const int c = l + G * it;
-        v[it] = c < a.C4 ? ld4(src + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
-        sum += hsum4(v[it]);
-    }
-    const float mean = lanes_sum<G>(sum) * a.inv;
-    sum = 0.f;
-#pragma unroll
-    for (int it = 0; it < ITERS; ++it)
-        if (l + G * it < a.C4) {
-            v[it] = make_float4(v[it].x - mean, v[it].y - mean, v[it].z - mean, v[it].w - mean);
-            sum += hsum4(mul4(v[it], v[it]));
+        for (int it = 0; it < ITERS; ++it) {
+            const int c = l + G * it;
+            v[it] = c < a.C4 ? ld4(src + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
+            sum += hsum4(v[it]);
         }
-    const float rstd = 1.0f / sqrtf(lanes_sum<G>(sum) * a.inv + a.eps);
-    if (l == 0 && a.mean) {
-        a.mean[row] = mean;
-        a.rstd[row] = rstd;
-    }
-    TO *dst = (TO *)a.out + row * a.out_stride;
+        const float mean = lanes_sum<G>(sum) * a.inv;
+        sum = 0.f;
 #pragma unroll
-    for (int it = 0; it < ITERS; ++it) {
-        const int c = l + G * it;
-        if (c >= a.C4) continue;
-        float4 y = make_float4(v[it].x * rstd, v[it].y * rstd, v[it].z * rstd, v[it].w * rstd);
-        if (a.w) y = mul4(y, ld4(a.w + 4 * c));
-        if (a.b) y = plus4(y, ld4(a.b + 4 * c));
-        st4(dst + 4 * c, y);
+        for (int it = 0; it < ITERS; ++it)
+            if (l + G * it < a.C4) {
+                v[it] = make_float4(v[it].x - mean, v[it].y - mean, v[it].z - mean, v[it].w - mean);
+                sum += hsum4(mul4(v[it], v[it]));
+            }
+        const float rstd = 1.0f / sqrtf(lanes_sum<G>(sum) * a.inv + a.eps);
+        if (l == 0 && a.mean) {
+            a.mean[row] = mean;
+            a.rstd[row] = rstd;
+        }
+        TO *dst = (TO *)a.out + row * a.out_stride;
+#pragma unroll
+        for (int it = 0; it < ITERS; ++it) {
+            const int c = l + G * it;
+            if (c >= a.C4) continue;
+            float4 y = make_float4(v[it].x * rstd, v[it].y * rstd, v[it].z * rstd, v[it].w * rstd);
+            if (a.w) y = mul4(y, ld4(a.w + 4 * c));
+            if (a.b) y = plus4(y, ld4(a.b + 4 * c));
+            put4(dst + 4 * c, y);
+        }
     }
 }
 
@@ -75,9 +76,12 @@ struct NormGradArgs {
     int blocks;
 };
 #define NORM_MOST_ROWS 256       // that one lane adds up in fp32; their sums are added in 64 bits
-#define NORM_BLOCKS 1024         // workgroups that few rows are spread over
+// Workgroups that few rows are spread over: twice what the card holds at the registers of rows of 300 (262 143 of them, fp32, with a residual's gradient: 1 536 workgroups 244 us,
+// 1 024 295, 2 048 257; 16 384 rows of 512 in bfloat16 14 each, but more shares to put together).
+#define NORM_BLOCKS 1536
 
-// A group of G lanes takes `per` rows of a run that its workgroup has to itself, and holds its columns' sums of d_w and d_b meanwhile.
+// A group of G lanes takes `per` rows of a run that its workgroup has to itself, and holds its columns' sums of d_w and d_b meanwhile.  Memory bounds it: 262 143 rows of 300,
+// fp32 with bfloat16 gradients and a residual's, 244 us (1.1 GB, 4.5 TB/s).
 template <typename T, typename TD, int G, int ITERS>
 __global__ void __launch_bounds__(BLOCK) k_norm_grad(NormGradArgs a)
 {
@@ -98,12 +102,15 @@ __global__ void __launch_bounds__(BLOCK) k_norm_grad(NormGradArgs a)
         if (row >= a.n) break;
         const float mean = a.mean[row], rstd = a.rstd[row];
         float4 d[ITERS], y[ITERS];
+        typename Raw4<T>::type add[ITERS];
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int it = 0; it < ITERS; ++it) {
             const int c = l + G * it;
             d[it] = y[it] = make_float4(0.f, 0.f, 0.f, 0.f);
+            zero_raw(add[it]);
             if (c >= a.C4) continue;
+            if (a.add) add[it] = ldraw((const T *)a.add + row * a.add_stride + 4 * c);
             d[it] = ld4((const TD *)a.d + row * a.d_stride + 4 * c);
             y[it] = ld4((const T *)a.x + row * a.x_stride + 4 * c);
         }
@@ -125,8 +132,8 @@ __global__ void __launch_bounds__(BLOCK) k_norm_grad(NormGradArgs a)
             if (c >= a.C4) continue;
             float4 o = make_float4(rstd * (d[it].x - s1 - y[it].x * s2), rstd * (d[it].y - s1 - y[it].y * s2), rstd * (d[it].z - s1 - y[it].z * s2),
                                    rstd * (d[it].w - s1 - y[it].w * s2));
-            if (a.add) o = plus4(o, ld4((const T *)a.add + row * a.add_stride + 4 * c));
-            st4((T *)a.dx + row * a.dx_stride + 4 * c, o);
+            o = plus4(widen4(add[it]), o);
+            put4((T *)a.dx + row * a.dx_stride + 4 * c, o);
         }
     }
     if (!a.part) return;
@@ -151,16 +158,17 @@ __global__ void __launch_bounds__(BLOCK) k_norm_grad(NormGradArgs a)
     }
 }
 
-// The workgroups' shares put together: 8 chunks of columns and 32 runs of shares to a workgroup, in 64 bits, in order.
-__global__ void __launch_bounds__(BLOCK) k_norm_join(const float *part, int blocks, int C4, float *dw, float *db)
+#define JOIN_THREADS 1024
+// The workgroups' shares put together: 8 chunks of columns and 128 runs of shares to a workgroup, in 64 bits, in an order that hangs on their number alone.
+__global__ void __launch_bounds__(JOIN_THREADS) k_norm_join(const float *part, int blocks, int C4, float *dw, float *db)
 {
-    __shared__ double lds[32][8][4];
+    __shared__ double lds[JOIN_THREADS / WAVE][8][4];
     const int l = (int)threadIdx.x & 7, run = (int)threadIdx.x >> 3, c = (int)blockIdx.x * 8 + l;    // of 2 * C4 chunks
     double s[4] = {0, 0, 0, 0};
     if (c < 2 * C4) {
         const float *p = part + 4 * c;
-#pragma unroll 4
-        for (int b = run; b < blocks; b += 32) {
+#pragma unroll 8
+        for (int b = run; b < blocks; b += JOIN_THREADS / 8) {
             const float4 v = ld4(p + (i64)b * 8 * C4);
             s[0] += v.x;
             s[1] += v.y;
@@ -168,16 +176,20 @@ __global__ void __launch_bounds__(BLOCK) k_norm_join(const float *part, int bloc
             s[3] += v.w;
         }
     }
-    for (int k = 0; k < 4; ++k) lds[run][l][k] = s[k];
+    for (int k = 0; k < 4; ++k) {
+        for (int o = 8; o < WAVE; o *= 2) s[k] += __shfl_xor(s[k], o, WAVE);
+        if (lane_id() < 8) lds[threadIdx.x >> 6][l][k] = s[k];
+    }
     __syncthreads();
     if (run > 0 || c >= 2 * C4) return;
-    for (int r = 1; r < 32; ++r)
+    for (int r = 1; r < JOIN_THREADS / WAVE; ++r)
         for (int k = 0; k < 4; ++k) s[k] += lds[r][l][k];
     float *to = c < C4 ? dw : db;
     if (to) st4(to + 4 * (c < C4 ? c : c - C4), make_float4((float)s[0], (float)s[1], (float)s[2], (float)s[3]));
 }
 
-int norm_lanes(int C4) { return C4 <= 8 ? 8 : C4 <= 16 ? 16 : C4 <= 32 ? 32 : 64; }
+// Lanes to a row, the fewest whose loads stay below 6 a lane: rows of 300 in 16 lanes of 5 chunks leave 6 % of them idle (in 64 of 2: 41 %), and four rows share a wave's sums.
+int norm_lanes(int C4) { return C4 <= 8 ? 8 : C4 <= 80 ? 16 : C4 <= 160 ? 32 : 64; }
 void norm_blocks(i64 n, int dim, int *per, i64 *blocks)
 {
     const i64 groups = BLOCK / norm_lanes(dim / 4);
@@ -186,31 +198,42 @@ void norm_blocks(i64 n, int dim, int *per, i64 *blocks)
     *blocks = (n + groups * rows - 1) / (groups * rows);
 }
 
+// f(lanes, loads of a lane) as constants
+template <int N> struct Int {
+    static constexpr int value = N;
+};
+template <typename F>
+void norm_shape(int C4, F f)
+{
+    const int G = norm_lanes(C4), iters = (C4 + G - 1) / G;
+    if (G == 8) f(Int<8>(), Int<1>());
+    else if (G == 16 && iters == 1) f(Int<16>(), Int<1>());
+    else if (G == 16 && iters == 2) f(Int<16>(), Int<2>());
+    else if (G == 16 && iters == 3) f(Int<16>(), Int<3>());
+    else if (G == 16 && iters == 4) f(Int<16>(), Int<4>());
+    else if (G == 16) f(Int<16>(), Int<5>());
+    else if (G == 32 && iters == 3) f(Int<32>(), Int<3>());
+    else if (G == 32 && iters == 4) f(Int<32>(), Int<4>());
+    else if (G == 32) f(Int<32>(), Int<5>());
+    else if (iters == 3) f(Int<64>(), Int<3>());
+    else f(Int<64>(), Int<4>());
+}
+#define NORM_MOST_BLOCKS 65536   // of k_norm; more rows are taken one after the other
 template <typename T, typename TO>
 void launch_norm(const NormArgs &a, hipStream_t st)
 {
-    const int G = norm_lanes(a.C4);
-    const dim3 grid((unsigned)((a.n + BLOCK / G - 1) / (BLOCK / G))), blk(BLOCK);
-    if (G == 8) hipLaunchKernelGGL((k_norm<T, TO, 8, 1>), grid, blk, 0, st, a);
-    else if (G == 16) hipLaunchKernelGGL((k_norm<T, TO, 16, 1>), grid, blk, 0, st, a);
-    else if (G == 32) hipLaunchKernelGGL((k_norm<T, TO, 32, 1>), grid, blk, 0, st, a);
-    else if (a.C4 <= 64) hipLaunchKernelGGL((k_norm<T, TO, 64, 1>), grid, blk, 0, st, a);
-    else if (a.C4 <= 128) hipLaunchKernelGGL((k_norm<T, TO, 64, 2>), grid, blk, 0, st, a);
-    else if (a.C4 <= 192) hipLaunchKernelGGL((k_norm<T, TO, 64, 3>), grid, blk, 0, st, a);
-    else hipLaunchKernelGGL((k_norm<T, TO, 64, 4>), grid, blk, 0, st, a);
+    norm_shape(a.C4, [&](auto g, auto iters) {
+        constexpr int G = decltype(g)::value, GROUPS = BLOCK / G;
+        const i64 blocks = std::min<i64>((a.n + GROUPS - 1) / GROUPS, NORM_MOST_BLOCKS);
+        hipLaunchKernelGGL((k_norm<T, TO, G, decltype(iters)::value>), dim3((unsigned)blocks), dim3(BLOCK), 0, st, a);
+    });
 }
 template <typename T, typename TD>
 void launch_norm_grad(const NormGradArgs &a, hipStream_t st)
 {
-    const int G = norm_lanes(a.C4);
-    const dim3 grid((unsigned)a.blocks), blk(BLOCK);
-    if (G == 8) hipLaunchKernelGGL((k_norm_grad<T, TD, 8, 1>), grid, blk, 0, st, a);
-    else if (G == 16) hipLaunchKernelGGL((k_norm_grad<T, TD, 16, 1>), grid, blk, 0, st, a);
-    else if (G == 32) hipLaunchKernelGGL((k_norm_grad<T, TD, 32, 1>), grid, blk, 0, st, a);
-    else if (a.C4 <= 64) hipLaunchKernelGGL((k_norm_grad<T, TD, 64, 1>), grid, blk, 0, st, a);
-    else if (a.C4 <= 128) hipLaunchKernelGGL((k_norm_grad<T, TD, 64, 2>), grid, blk, 0, st, a);
-    else if (a.C4 <= 192) hipLaunchKernelGGL((k_norm_grad<T, TD, 64, 3>), grid, blk, 0, st, a);
-    else hipLaunchKernelGGL((k_norm_grad<T, TD, 64, 4>), grid, blk, 0, st, a);
+    norm_shape(a.C4, [&](auto g, auto iters) {
+        hipLaunchKernelGGL((k_norm_grad<T, TD, decltype(g)::value, decltype(iters)::value>), dim3((unsigned)a.blocks), dim3(BLOCK), 0, st, a);
+    });
 }
 
 }  // namespace
@@ -290,7 +313,7 @@ int tensair_norm_grad(const void *d_out, int32_t d_dtype, int64_t d_stride, cons
         else if (d_dtype == TENSAIR_F32) launch_norm_grad<bf16_t, float>(a, st);
         else launch_norm_grad<bf16_t, bf16_t>(a, st);
     }
-    if (sums) hipLaunchKernelGGL(k_norm_join, dim3((unsigned)((2 * a.C4 + 7) / 8)), dim3(BLOCK), 0, st, (const float *)workspace, a.blocks, a.C4, d_weight, d_bias);
+    if (sums) hipLaunchKernelGGL(k_norm_join, dim3((unsigned)((2 * a.C4 + 7) / 8)), dim3(JOIN_THREADS), 0, st, (const float *)workspace, a.blocks, a.C4, d_weight, d_bias);
     return layer_launched("norm_grad");
 }
 
