@@ -552,7 +552,7 @@ size_t recur_carve(i64 n, int dim, char *ws, Chain *ch)
     return 256 + layer_up256(8 * (size_t)(tiles + groups) * (size_t)dim);
 }
 
-template <typename T, int G>
+template <typename T, int G, bool GRAD>
 int launch_recur(const RecurArgs &a, void *workspace, hipStream_t st)
 {
     Chain ch;
@@ -560,22 +560,24 @@ int launch_recur(const RecurArgs &a, void *workspace, hipStream_t st)
     const int sides = (a.C4 + G - 1) / G;
     if ((i64)ch.tiles * sides > (i64)TN_MAX_BLOCKS * BLOCK / (RECUR_STRANDS * G)) return tn_fail(TENSAIR_EINVAL, "n * dim beyond what one launch covers");
     const dim3 blk(RECUR_STRANDS * G);
-    const bool grad = a.dx != nullptr || a.kept != nullptr;
     if (ch.tiles == 1) {
-        if (grad) hipLaunchKernelGGL((k_recur_grad<T, G, false>), dim3(sides), blk, 0, st, a, ch);
+        if constexpr (GRAD) hipLaunchKernelGGL((k_recur_grad<T, G, false>), dim3(sides), blk, 0, st, a, ch);
         else hipLaunchKernelGGL((k_recur<T, G, false>), dim3(sides), blk, 0, st, a, ch);
         return TENSAIR_OK;
     }
     hipLaunchKernelGGL(k_recur_clear, dim3((unsigned)std::min<size_t>(1024, (bytes / 8 + BLOCK - 1) / BLOCK)), dim3(BLOCK), 0, st, (u64 *)workspace, bytes / 8);
     const dim3 grid((unsigned)(ch.tiles * sides));
-    if (grad) hipLaunchKernelGGL((k_recur_grad<T, G, true>), grid, blk, 0, st, a, ch);
+    if constexpr (GRAD) hipLaunchKernelGGL((k_recur_grad<T, G, true>), grid, blk, 0, st, a, ch);
     else hipLaunchKernelGGL((k_recur<T, G, true>), grid, blk, 0, st, a, ch);
     return TENSAIR_OK;
 }
-int launch_recur(const RecurArgs &a, int32_t dtype, void *workspace, hipStream_t st)
+// Lanes to a token: a line of memory for fp32, and for bfloat16 forward; half a line for the gradient in bfloat16, which keeps more than a workgroup of 512 threads has registers for
+// (262 144 tokens of 512: forward with a line 270 us, with half of one 290; gradient 460 and 413; the halves' workgroups on one die, by their order: no difference).
+int launch_recur(const RecurArgs &a, int32_t dtype, bool grad, void *workspace, hipStream_t st)
 {
-    if (dtype == TENSAIR_F32) return launch_recur<float, 8>(a, workspace, st);          // a line of memory to a token and strand
-    return a.C4 <= 8 ? launch_recur<bf16_t, 8>(a, workspace, st) : launch_recur<bf16_t, 16>(a, workspace, st);
+    if (dtype == TENSAIR_F32) return grad ? launch_recur<float, 8, true>(a, workspace, st) : launch_recur<float, 8, false>(a, workspace, st);
+    if (grad) return launch_recur<bf16_t, 8, true>(a, workspace, st);
+    return a.C4 <= 8 ? launch_recur<bf16_t, 8, false>(a, workspace, st) : launch_recur<bf16_t, 16, false>(a, workspace, st);
 }
 
 // a tile's places are kept in 32 bits
@@ -639,7 +641,7 @@ int tensair_recur(const void *x, int64_t x_stride, const void *gate, int64_t gat
     a.states = states;
     a.status = status;
     hipStream_t st = (hipStream_t)stream;
-    if ((rc = launch_recur(a, dtype, workspace, st))) return rc;
+    if ((rc = launch_recur(a, dtype, false, workspace, st))) return rc;
     return layer_launched("recur");
 }
 
@@ -677,7 +679,7 @@ int tensair_recur_grad(const void *x, int64_t x_stride, const void *gate, int64_
     a.kept = states;
     a.status = status;
     hipStream_t st = (hipStream_t)stream;
-    if ((rc = launch_recur(a, dtype, workspace, st))) return rc;
+    if ((rc = launch_recur(a, dtype, true, workspace, st))) return rc;
     return layer_launched("recur_grad");
 }
 
