@@ -86,7 +86,7 @@ __device__ __forceinline__ double exp2_of(double t)
 __device__ __forceinline__ double weight_of(u32 key, u32 top, double slope)
 {
     const double t = ((double)of_key(key) - (double)of_key(top)) * slope;
-    const double w = t > -1000.0 ? exp2_of(t) : 0.0;             // NaN (minus infinity beside an endless temperature): none
+    const double w = t > -1075.0 ? exp2_of(t) : 0.0;             // NaN (minus infinity beside an endless temperature): none
     return key == top ? 1.0 : key == KEY_LOWEST ? 0.0 : w;
 }
 
@@ -116,7 +116,8 @@ __device__ __forceinline__ int bin_of(u32 key, u32 top)
     return (int)min((u32)(DRAW_BINS - 1), (__float_as_uint(d + 1.0f) - 0x3F800000u) >> 15);
 }
 __device__ __forceinline__ u64 place_of(u32 key, u32 word) { return ((u64)~key << 32) | word; }
-__device__ __forceinline__ u64 fixed_of(double w) { return (u64)(w * 0x1p62); }
+// a weight as a whole number, at least 1 where there is one
+__device__ __forceinline__ u64 fixed_of(double w) { return w > 0.0 ? (u64)fmax(w * 0x1p62, 1.0) : 0; }
 __device__ __forceinline__ double mass_of(u64 hi, u64 lo) { return (double)hi * 0x1p-30 + (double)lo * 0x1p-62; }
 
 // f(word, logit) for the words lo..hi of a row, 16 bytes at a time where they are aligned

@@ -423,6 +423,28 @@ def test_recur_long_sequence_is_its_parts():
     assert bool(((c - dh).abs() <= size).all())
 
 
+def test_recur_many_short_sequences():
+    """3 000 sequences of 0 to 3 tokens, then as many empty ones: more than a workgroup looks at once."""
+    r = np.random.RandomState(2)
+    lengths = list(r.randint(0, 4, 3_000)) + [0] * 3_000 + [5]
+    D, S = 8, len(lengths)
+    g, off, n, x, gate, h0, _ = _recur_case(lengths, 3, 0, D, "f32", 0, 4)
+    out, last, states, ws = _empty(n, D, "f32"), torch.empty((S, D), device="cuda"), torch.empty((B.tensair_recur_state_rows(n), D), device="cuda"), _bytes(B.tensair_recur_workspace_bytes(n, D))
+    status, offsets = _status(), torch.from_numpy(off).cuda()
+    B.tensair_recur(x, gate, D, offsets, out, ws, h0, last, states, status)
+    live = slice(3, n)
+    host = _recur_reference(x, gate, off.tolist(), h0)
+    _near(out[live], host[0][live], host[2][live] + U32 * host[0][live].abs(), "out")
+    _near(last, host[1], host[3] + 1e-30, "h_last")
+    d, d_last, dx, dg, dh = _rows(g, n, D, "f32"), torch.randn((S, D), generator=g, device="cuda"), _empty(n, D, "f32"), _empty(n, D, "f32"), torch.empty((S, D), device="cuda")
+    B.tensair_recur_grad(x, gate, D, offsets, states, d, dx, dg, ws, h0, d_last, dh, status)
+    rx, rg, rh, ex, eg, e0 = _recur_reference(x, gate, off.tolist(), h0, d, d_last)
+    _near(dx[live], rx[live], ex[live] + U32 * rx[live].abs() + 1e-37, "d_x")
+    _near(dg[live], rg[live], eg[live] + U32 * rg[live].abs() + 1e-37, "d_gate")
+    _near(dh, rh, e0 + 1e-37, "d_h0")
+    assert int(status) == 0 and bool((out[:3] == MARK).all()) and bool((dx[:3] == MARK).all())
+
+
 def test_recur_grad_against_differences():
     n, D, S = 300, 12, 3
     g, off, _, x, gate, h0, _ = _recur_case([100, 0, 200], 0, 0, D, "f32", 0, 3, slow=False)
@@ -644,6 +666,15 @@ def test_sample_masked_rows_and_ends():
     ref = [_draw_reference(z[i].cpu().numpy(), 1.0, 0, 1.0, 0.0, 0.0) for i in range(2, 11)]
     assert int(status) == 0 and len(ref) == 9
     _draw(z[:0], V, u=np.zeros(0))
+
+
+@pytest.mark.parametrize("V,n,k,p,spread", [(9_000, 300, 0, 0.9, 2.0), (70_000, 3, 20_000, 0.9, 2.0), (70_000, 3, 20_000, 1.0, 2.0), (300_000, 2, 0, 0.97, 0.5), (16_777_216, 1, 0, 0.6, 2.0),
+                                            (200_000, 2, 150_000, 0.5, 1e-4), (60_000, 4, 600, 0.99, 1.0)])
+def test_sample_long_heads(V, n, k, p, spread):
+    """More rows than are taken at a time; borders behind tens of thousands of words, with and without both filters; the largest vocabulary."""
+    z = torch.randn((n, V), generator=_gen(V + k), device="cuda") * spread
+    r = np.random.RandomState(5)
+    _check_draw(z, V, np.full(n, 1.0), np.full(n, k), np.full(n, p), np.full(n, 0.0), r.rand(n))
 
 
 def test_sample_frequencies():
