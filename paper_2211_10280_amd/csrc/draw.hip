@@ -24,7 +24,7 @@ namespace {
 #define DRAW_SOLO 8192           // words of a row that k_draw alone takes
 #define DRAW_PART 4096           // fewest words of a part
 #define DRAW_PARTS 512           // most parts of a row
-#define DRAW_WORKGROUPS 2048     // parts of all rows that are aimed at
+#define DRAW_WORKGROUPS 4096     // parts of all rows that are aimed at
 #define DRAW_BINS 4096           // 256 to a doubling of (distance + 1)
 #define DRAW_DIGITS 2048         // of places
 #define DRAW_LIST 16384          // most words of a row's list
@@ -886,7 +886,9 @@ void draw_plan(i64 n, i64 V, int *part, int *parts)
 {
     *part = *parts = 0;
     if (V <= DRAW_SOLO) return;
-    i64 p = DRAW_PART;
+    // the smallest parts only where larger ones would leave compute units without: one row of a million, parts of 4 096 / 8 192 59 / 62 us, 64 rows of 50 000 45 / 40; more than 2 048
+    // workgroups to 256 rows of 100 003 140 -> 127
+    i64 p = n * ((V + 2 * DRAW_PART - 1) / (2 * DRAW_PART)) >= 256 ? 2 * DRAW_PART : DRAW_PART;
     while ((V + p - 1) / p > DRAW_PARTS || (n * ((V + p - 1) / p) > DRAW_WORKGROUPS && p < V)) p *= 2;
     *part = (int)p;
     *parts = (int)((V + p - 1) / p);

@@ -57,7 +57,6 @@ __device__ __forceinline__ float4 fma4(float4 a, float4 b, float4 c) { return ma
 // below.  What is put together with what, and in which order, hangs on the sizes and offsets alone.
 #define RECUR_RUN 8
 #define RECUR_STRANDS (RECUR_TILE / RECUR_RUN)
-#define RECUR_GROUP 32           // tiles whose maps are put together by every tile of them; their last ones hand states on
 
 struct Map {
     float4 p, q;
@@ -129,13 +128,14 @@ __device__ __forceinline__ Map strands_before(Map m, TileLds<G> &lds, Map &all)
     return then(run, before);
 }
 
-// ---- the chain of tiles: every tile publishes its map, the last of every RECUR_GROUP its state, each word with its value in it (0: not yet), so that no order of two
+// ---- the chain of tiles: every tile publishes its map, the last of every group its state, each word with its value in it (0: not yet), so that no order of two
 // stores matters.  A tile's state is the state handed on by the group before, then the maps of the group's tiles up to it.  Workgroups take tiles in order from a
 // counter, so those that a tile waits for run already, and wait for none behind them.
 struct Chain {
     u32 *ticket;
     u64 *maps, *states;          // [tiles][4 * C4], [groups][4 * C4]; zero at the start
     int tiles;
+    int group;                   // tiles whose maps are put together by every tile of them; the last of a group hands the state on
 };
 #define MAP_RESET 0xC0000000u
 __device__ __forceinline__ void put_word(u64 *at, u32 hi, float v) { __hip_atomic_store(at, ((u64)hi << 32) | __float_as_uint(v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
@@ -167,9 +167,9 @@ __device__ __forceinline__ void chain_say(const Chain &ch, int v, const Map &own
     put_word(at + 1, map_word(own.p.y, own.reset), own.q.y);
     put_word(at + 2, map_word(own.p.z, own.reset), own.q.z);
     put_word(at + 3, map_word(own.p.w, own.reset), own.q.w);
-    if (v % RECUR_GROUP < RECUR_GROUP - 1) return;
+    if (v % ch.group < ch.group - 1) return;
     if (own.reset || !wanted || v == 0) {
-        put_state(ch.states + (size_t)(v / RECUR_GROUP) * D + 4 * col, own.q);
+        put_state(ch.states + (size_t)(v / ch.group) * D + 4 * col, own.q);
     } else {                                     // a thread's own words, for itself
         lds.own_p[l] = own.p;
         lds.own_q[l] = own.q;
@@ -180,26 +180,27 @@ __device__ __forceinline__ void chain_say(const Chain &ch, int v, const Map &own
 template <int G, bool REV>
 __device__ __forceinline__ float4 chain_state(const Chain &ch, int v, bool wanted, int col, int C4, TileLds<G> &lds)
 {
-    const int strand = REV ? RECUR_STRANDS - 1 - (int)threadIdx.x / G : (int)threadIdx.x / G, l = (int)threadIdx.x % G, D = 4 * C4, first = v / RECUR_GROUP * RECUR_GROUP;
+    const int strand = REV ? RECUR_STRANDS - 1 - (int)threadIdx.x / G : (int)threadIdx.x / G, l = (int)threadIdx.x % G, D = 4 * C4, first = v / ch.group * ch.group;
     if (!wanted || v == 0) return make_float4(0.f, 0.f, 0.f, 0.f);
     Map m = map_none(), all;
-    if (strand < v - first && col < C4) {
-        const u64 *at = ch.maps + (size_t)(first + strand) * D + 4 * col;
+    const int per = (ch.group + RECUR_STRANDS - 1) / RECUR_STRANDS;      // tiles that follow one another to a strand
+    for (int tile = first + strand * per; tile < min(v, first + (strand + 1) * per) && col < C4; ++tile) {
+        const u64 *at = ch.maps + (size_t)tile * D + 4 * col;
         const u64 a = wait_word(at), b = wait_word(at + 1), c = wait_word(at + 2), d = wait_word(at + 3);
-        m.reset = (u32)(a >> 32) == MAP_RESET;
-        m.p = make_float4(__uint_as_float((u32)(a >> 32) & 0x7FFFFFFFu), __uint_as_float((u32)(b >> 32) & 0x7FFFFFFFu), __uint_as_float((u32)(c >> 32) & 0x7FFFFFFFu),
-                          __uint_as_float((u32)(d >> 32) & 0x7FFFFFFFu));
-        m.q = make_float4(low_float(a), low_float(b), low_float(c), low_float(d));
+        const Map x = {make_float4(__uint_as_float((u32)(a >> 32) & 0x7FFFFFFFu), __uint_as_float((u32)(b >> 32) & 0x7FFFFFFFu), __uint_as_float((u32)(c >> 32) & 0x7FFFFFFFu),
+                                   __uint_as_float((u32)(d >> 32) & 0x7FFFFFFFu)),
+                       make_float4(low_float(a), low_float(b), low_float(c), low_float(d)), (u32)(a >> 32) == MAP_RESET};
+        m = then(m, x);
     }
     strands_before<G, REV>(m, lds, all);
     if (strand == RECUR_STRANDS - 1 && col < C4) {
         float4 h = make_float4(0.f, 0.f, 0.f, 0.f);
         if (first > 0 && !all.reset) {
-            const u64 *at = ch.states + (size_t)(first / RECUR_GROUP - 1) * D + 4 * col;
+            const u64 *at = ch.states + (size_t)(first / ch.group - 1) * D + 4 * col;
             h = make_float4(low_float(wait_word(at)), low_float(wait_word(at + 1)), low_float(wait_word(at + 2)), low_float(wait_word(at + 3)));
         }
         h = apply(all, h);
-        if (v % RECUR_GROUP == RECUR_GROUP - 1 && !lds.said[l]) put_state(ch.states + (size_t)(v / RECUR_GROUP) * D + 4 * col, fma4(lds.own_p[l], h, lds.own_q[l]));
+        if (v % ch.group == ch.group - 1 && !lds.said[l]) put_state(ch.states + (size_t)(v / ch.group) * D + 4 * col, fma4(lds.own_p[l], h, lds.own_q[l]));
         lds.carry[l] = h;
     }
     __syncthreads();
@@ -539,15 +540,17 @@ __global__ void __launch_bounds__(BLOCK) k_recur_step(StepArgs a)
     }
 }
 
+#define RECUR_LEAST_GROUP 32
 // bytes of the chain's words, or, with an address, the chain there and what of it has to be zero
 size_t recur_carve(i64 n, int dim, char *ws, Chain *ch)
 {
-    const i64 tiles = std::max<i64>(1, (n + RECUR_TILE - 1) / RECUR_TILE), groups = (tiles + RECUR_GROUP - 1) / RECUR_GROUP;
+    const i64 tiles = std::max<i64>(1, (n + RECUR_TILE - 1) / RECUR_TILE), groups = (tiles + RECUR_LEAST_GROUP - 1) / RECUR_LEAST_GROUP;
     if (ch) {
         ch->ticket = (u32 *)ws;
         ch->maps = (u64 *)(ws + 256);
         ch->states = ch->maps + (size_t)tiles * dim;
         ch->tiles = (int)tiles;
+        ch->group = RECUR_LEAST_GROUP;
     }
     return 256 + layer_up256(8 * (size_t)(tiles + groups) * (size_t)dim);
 }
@@ -558,6 +561,9 @@ int launch_recur(const RecurArgs &a, void *workspace, hipStream_t st)
     Chain ch;
     const size_t bytes = recur_carve(a.n, 4 * a.C4, (char *)workspace, &ch);
     const int sides = (a.C4 + G - 1) / G;
+    // Larger groups hand the state on less often, and read more maps to every tile of them: 131 072 tokens in one sequence, forward, groups of 16 / 32 / 64: 32 channels 53 / 36 / 28 us,
+    // 64 61 / 44 / 36, 128 65 / 55 / 54, 256 82 / 80 / 82; 262 144 tokens of 512 257 / 259 / 266.
+    if (sides <= 2) ch.group = 2 * RECUR_LEAST_GROUP;
     if ((i64)ch.tiles * sides > (i64)TN_MAX_BLOCKS * BLOCK / (RECUR_STRANDS * G)) return tn_fail(TENSAIR_EINVAL, "n * dim beyond what one launch covers");
     const dim3 blk(RECUR_STRANDS * G);
     if (ch.tiles == 1) {
