@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(BLOCK) k_dropout(DropArgs a)
     const u64 chunk = (u64)blockIdx.x * (BLOCK * DROP_CHUNKS);
     const u64 row0 = chunk / (u32)a.C4;
     const u32 first = (u32)(chunk - row0 * (u32)a.C4);
-    const u32 step = (u32)(a.step_at ? a.step + *a.step_at : a.step);
+    const u32 step = (u32)a.step + (a.step_at ? (u32)*a.step_at : 0u);
     typename Raw4<T>::type v[DROP_CHUNKS];
     typename Raw4<TO>::type add[DROP_CHUNKS];
     i64 row[DROP_CHUNKS];

@@ -177,6 +177,28 @@ def test_norm_without_rows_and_with_far_rows():
     assert torch.equal(out.isnan().any(1), bad) and bool(out[~bad].isfinite().all())
 
 
+@pytest.mark.parametrize("n", [2_200_001, 13_000_003])
+def test_norm_many_rows(n):
+    """More rows than a launch has groups of lanes for, and than are spread over few workgroups."""
+    D, g = 4, _gen(n)
+    x, d, w = torch.randn((n, D), generator=g, device="cuda"), torch.randn((n, D), generator=g, device="cuda"), torch.rand(D, generator=g, device="cuda")
+    out, mean, rstd, dx, dw, db = torch.empty_like(x), torch.empty(n, device="cuda"), torch.empty(n, device="cuda"), torch.empty_like(x), torch.empty(D, device="cuda"), torch.empty(D, device="cuda")
+    B.tensair_norm(x, D, w, None, out, mean, rstd)
+    v = x.double()
+    m, r = v.mean(1, keepdim=True), (v.var(1, unbiased=False, keepdim=True) + 1e-5) ** -0.5
+    y = (v - m) * r
+    e_mean = 4 * U32 * v.abs().mean(1, keepdim=True)
+    _near(out, y * w.double(), w.double() * (r * (e_mean + U32 * (v - m).abs()) + y.abs() * (8 * U32 + (r * e_mean) ** 2)) + 2 * U32 * y.abs() + 1e-30, "out")
+    B.tensair_norm_grad(d, x, D, w, mean, rstd, dx, dw, db, _bytes(B.tensair_norm_workspace_bytes(n, D)))
+    y, e = (v - mean.double()[:, None]) * rstd.double()[:, None], d.double() * w.double()
+    s1, s2, a2 = e.mean(1, keepdim=True), (e * y).mean(1, keepdim=True), (e * y).abs().mean(1, keepdim=True)
+    want = rstd.double()[:, None] * (e - s1 - y * s2)
+    _near(dx, want, rstd.double()[:, None] * U32 * (4 * e.abs() + 8 * e.abs().mean(1, keepdim=True) + 14 * y.abs() * a2) + 3 * U32 * want.abs() + 1e-30, "d_x")
+    # at most 256 additions in a lane, 31 over a workgroup, the rest in 64 bits
+    _near(dw, (d.double() * y).sum(0), 292 * U32 * (d.double() * y).abs().sum(0), "d_weight")
+    _near(db, d.double().sum(0), 289 * U32 * d.double().abs().sum(0), "d_bias")
+
+
 def test_norm_rows_far_apart():
     """Rows whose last offset passes 2^32 bytes, as views of a buffer of 4.3 GB."""
     n, D, stride = 5, 64, 1 << 28
@@ -622,6 +644,20 @@ def test_sample(V, n, dtype, pad):
     _check_draw(z, V, pick(0.0, 0.5, 1.0, 1.7), pick(0, 1, 5, 50, 3_000, V), pick(1.0, 0.9, 0.5, 0.05), pick(0.0, 0.0, 0.1, 0.9), r.rand(n))
 
 
+@pytest.mark.parametrize("V", [8_191, 8_192, 8_193, 12_288, 12_289, 16_385, 65_537])
+def test_sample_where_rows_are_cut(V):
+    """Sizes at which a row is taken whole, and at which its parts end; the first and the last word; more rows than one fills the card with."""
+    n = 40
+    z = torch.randn((n, V), generator=_gen(V), device="cuda").bfloat16()
+    z[1], z[2] = -float("inf"), -float("inf")
+    z[1, 0] = z[2, V - 1] = 1.0
+    z[3, V - 1] = 20.0
+    z[4, 0] = 20.0
+    r = np.random.RandomState(V)
+    pick = lambda *v: np.array([v[j] for j in r.randint(0, len(v), n)])      # noqa: E731
+    _check_draw(z, V, pick(0.0, 0.5, 1.0), pick(0, 2, 700), pick(1.0, 0.8), pick(0.0, 0.05), pick(0.0, 0.3, 0.9, 1.0))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("V", [9, 5_000, 70_000])
 def test_sample_equal_logits(V, dtype):
@@ -675,6 +711,18 @@ def test_sample_long_heads(V, n, k, p, spread):
     z = torch.randn((n, V), generator=_gen(V + k), device="cuda") * spread
     r = np.random.RandomState(5)
     _check_draw(z, V, np.full(n, 1.0), np.full(n, k), np.full(n, p), np.full(n, 0.0), r.rand(n))
+
+
+@pytest.mark.parametrize("k,p", [(5_000, 0.9), (5_000, 1.0), (0, 0.5), (16_000, 0.95), (0, 0.999)])
+def test_sample_sorted_logits(k, p):
+    """The likely words side by side, as in a vocabulary by frequency, first, last and in the middle: one part has them all."""
+    V = 120_000
+    z = torch.arange(V, device="cuda").float().expand(4, V).contiguous() * -2e-4
+    z[1] = z[1].flip(0)
+    z[2] = z[2].roll(50_000)
+    z[3] = z[3].bfloat16().float()
+    r = np.random.RandomState(6)
+    _check_draw(z, V, np.full(4, 1.0), np.full(4, k), np.full(4, p), np.array([0.0, 0.0, 0.01, 0.0]), r.rand(4))
 
 
 def test_sample_frequencies():
