@@ -4,6 +4,7 @@
 //   k_draw_top      the largest logit of every part of a row
 //   k_draw_bins     words and weights by their distance from the row's largest logit, in bins
 //   k_draw_border   the bin that the border falls into
+//   (both again, for vocabularies of more than a million words: where that bin has more words than a list, its 4 096th parts)
 //   k_draw_gather   the words that may be in (those of the border's bin and, where they are few, all of the bins above) as a list, else the parts' weights above it
 //   k_draw          the border among the list, the part that the draw falls into, the word in it
 // A row without top-k and top-p needs no bins, a row of few words only the last of these, which then takes the row itself for the list; so it does where a list is too short
@@ -26,6 +27,7 @@ namespace {
 #define DRAW_PARTS 512           // most parts of a row
 #define DRAW_WORKGROUPS 4096     // parts of all rows that are aimed at
 #define DRAW_BINS 4096           // 256 to a doubling of (distance + 1)
+#define DRAW_COARSE 1048576      // most words for which a bin is taken as it is: the launches that cut it again are 5 us; without them 16.8 million words with top-p 0.9 take 44.8 ms, with them 202 us
 #define DRAW_DIGITS 2048         // of places
 #define DRAW_LIST 16384          // most words of a row's list
 #define DRAW_STAGED 2048         // of a part's words that go to it, most that are put together in LDS before
@@ -43,6 +45,7 @@ struct DrawArgs {
     int *words, *status;
     float *prob;
     int part, parts;             // words of a part, parts of a row; 0 parts: k_draw alone
+    bool fine;                   // bins are cut again where they have more words than a list
     int unit;                    // a part's weights are whole numbers of 2^-unit in the bins
     // in the workspace
     u32 *tops;                   // [n][parts]
@@ -109,11 +112,14 @@ __device__ __forceinline__ Row row_of(const DrawArgs &a, int i)
     return r;
 }
 // The bin of a word: its distance below the largest logit, plus 1, with 8 bits behind the leading one.  Falls with the logit.
-__device__ __forceinline__ int bin_of(u32 key, u32 top)
+#define BIN_SHIFT 15
+#define FINE_SHIFT 3             // a bin's 4 096th parts
+__device__ __forceinline__ int bin_of(u32 key, u32 top, int shift = BIN_SHIFT)
 {
     if (key == top) return 0;
     const float d = of_key(top) - of_key(key);
-    return (int)min((u32)(DRAW_BINS - 1), (__float_as_uint(d + 1.0f) - 0x3F800000u) >> 15);
+    const u32 b = (__float_as_uint(d + 1.0f) - 0x3F800000u) >> shift;
+    return (int)(shift == BIN_SHIFT ? min((u32)(DRAW_BINS - 1), b) : b);
 }
 __device__ __forceinline__ u64 place_of(u32 key, u32 word) { return ((u64)~key << 32) | word; }
 // a weight as a whole number, at least 1 where there is one
@@ -258,6 +264,17 @@ __device__ __forceinline__ double wave_sum64(double x)
 __device__ __forceinline__ double rd_lane(double x, int l) { return __longlong_as_double((long long)rd_lane64((u64)__double_as_longlong(x), l)); }
 __device__ __forceinline__ unsigned long long *atom(u64 *p) { return (unsigned long long *)p; }
 
+// Where a row's border lies, as far as the bins tell.
+struct Border {
+    int bin;                     // the bin that it falls into; all bins above it are in
+    int shift;                   // what bins these are
+    u32 above, in;               // words of the bins above, of this bin
+    int how;
+    double above_mass, whole;    // weight of the bins above and of the row, where that is needed
+};
+enum { BORDER_NONE, BORDER_ALL_LISTED, BORDER_BIN_LISTED, BORDER_ROW };
+// whether a row's bin is to be cut once more: top-p beside top-k looks at what top-k left, and the last bin has no end
+__device__ __forceinline__ bool cut_again(const Row &r, const Border &o) { return o.how == BORDER_ROW && !(r.k && r.p < 1.0) && o.bin < DRAW_BINS - 1; }
 template <int THREADS>
 __device__ __forceinline__ u32 row_top(const DrawArgs &a, int i, u32 *lds)
 {
@@ -285,7 +302,7 @@ __global__ void __launch_bounds__(PART_THREADS) k_draw_top(DrawArgs a)
 
 // A weight in 64 bits for every word of a row with top-p alone, and two additions in LDS: 256 rows, a quarter of them such, 31 us; one of a million 16 (the workgroups add to the same few hundred
 // bins in memory).  Rows with top-k only count.
-template <typename T>
+template <typename T, bool FINE>
 __global__ void __launch_bounds__(PART_THREADS) k_draw_bins(DrawArgs a)
 {
     __shared__ u32 counts[DRAW_BINS], tops[PART_THREADS / WAVE];
@@ -294,6 +311,12 @@ __global__ void __launch_bounds__(PART_THREADS) k_draw_bins(DrawArgs a)
     const Row r = row_of(a, i);
     if (r.first || (r.k == 0 && r.p >= 1.0)) return;
     const bool weigh = r.k == 0;                 // else top-p looks at what top-k left, which is listed
+    int bin = 0;
+    if (FINE) {
+        const Border o = a.borders[i];
+        if (!cut_again(r, o)) return;
+        bin = o.bin;
+    }
     const double unit = (double)(1ull << a.unit);
     for (int b = t; b < DRAW_BINS; b += PART_THREADS) {
         counts[b] = 0;
@@ -302,7 +325,11 @@ __global__ void __launch_bounds__(PART_THREADS) k_draw_bins(DrawArgs a)
     const u32 top = row_top<PART_THREADS>(a, i, tops);           // waits for all threads
     each_word<PART_THREADS>((const T *)a.z + (i64)i * a.stride, c * a.part, min(a.V, (c + 1) * a.part), [&](int, float z) {
         const u32 key = key_of(z);
-        const int b = bin_of(key, top);
+        int b = bin_of(key, top);
+        if (FINE) {
+            if (b != bin) return;
+            b = bin_of(key, top, FINE_SHIFT) & (DRAW_BINS - 1);
+        }
         atomicAdd(&counts[b], 1u);
         if (weigh) atomicAdd(atom(&mass[b]), (u64)(weight_of(key, top, r.slope) * unit));
     });
@@ -317,15 +344,8 @@ __global__ void __launch_bounds__(PART_THREADS) k_draw_bins(DrawArgs a)
     }
 }
 
-// Where a row's border lies, as far as the bins tell.
-struct Border {
-    int bin;                     // the bin that it falls into; all bins above it are in
-    u32 above, in;               // words of the bins above, of this bin
-    int how;
-    double above_mass, whole;    // weight of the bins above and of the row, where that is needed
-};
-enum { BORDER_NONE, BORDER_ALL_LISTED, BORDER_BIN_LISTED, BORDER_ROW };
 // One workgroup to a row, a launch of its own (8 to 10 us, loads and a running sum that wait for each other): made by every workgroup of the next kernel instead it cost more there.
+template <bool FINE>
 __global__ void __launch_bounds__(BORDER_THREADS) k_draw_border(DrawArgs a)
 {
     constexpr int PER = DRAW_BINS / BORDER_THREADS;
@@ -339,20 +359,25 @@ __global__ void __launch_bounds__(BORDER_THREADS) k_draw_border(DrawArgs a)
     const ulong2 h0 = *reinterpret_cast<const ulong2 *>(a.hi + at), h1 = *reinterpret_cast<const ulong2 *>(a.hi + at + 2);
     const ulong2 l0 = *reinterpret_cast<const ulong2 *>(a.lo + at), l1 = *reinterpret_cast<const ulong2 *>(a.lo + at + 2);
     if (r.first || (r.k == 0 && r.p >= 1.0)) return;
+    Border up = {0, BIN_SHIFT, 0, 0, BORDER_ROW, 0.0, 0.0};     // what lies above the bins looked at
+    if (FINE) {
+        up = a.borders[i];
+        if (!cut_again(r, up)) return;
+    }
     // sums up to each of the four bins; weights are 0 where top-k decides
     const Three s0 = {n.x, h0.x, l0.x}, s1 = {s0.n + n.y, s0.hi + h0.y, s0.lo + l0.y}, s2 = {s1.n + n.z, s1.hi + h1.x, s1.lo + l1.x}, s3 = {s2.n + n.w, s2.hi + h1.y, s2.lo + l1.y};
     if (t == 0) pick = DRAW_BINS;
     Three all;
     const Three run = block_before<BORDER_THREADS>(s3, lds, all);
-    const double whole = mass_of(all.hi, all.lo), want = r.p * whole;
-    Border o = {DRAW_BINS, 0, 0, BORDER_ROW, 0.0, whole};
+    const double whole = FINE ? up.whole : mass_of(all.hi, all.lo), want = r.p * whole;
+    Border o = {DRAW_BINS, FINE ? FINE_SHIFT : BIN_SHIFT, 0, 0, BORDER_ROW, 0.0, whole};
     auto look = [&](int j, const Three &before, const Three &to) {
         if (o.bin < DRAW_BINS || to.n == before.n) return;
-        if (r.k ? run.n + to.n >= (u64)r.k : mass_of(run.hi + to.hi, run.lo + to.lo) >= want) {
+        if (r.k ? up.above + run.n + to.n >= (u64)r.k : up.above_mass + mass_of(run.hi + to.hi, run.lo + to.lo) >= want) {
             o.bin = t * PER + j;
-            o.above = (u32)(run.n + before.n);
+            o.above = up.above + (u32)(run.n + before.n);
             o.in = (u32)(to.n - before.n);
-            o.above_mass = mass_of(run.hi + before.hi, run.lo + before.lo);
+            o.above_mass = up.above_mass + mass_of(run.hi + before.hi, run.lo + before.lo);
         }
     };
     look(0, Three{0, 0, 0}, s0);
@@ -361,7 +386,13 @@ __global__ void __launch_bounds__(BORDER_THREADS) k_draw_border(DrawArgs a)
     look(3, s2, s3);
     if (o.bin < DRAW_BINS) atomicMin(&pick, o.bin);
     __syncthreads();
-    if (o.bin == DRAW_BINS || o.bin != pick) return;             // all words' number and weight are enough: there is one
+    if (!FINE && a.fine) {                       // for the same kernels again
+        *reinterpret_cast<uint4 *>(a.counts + at) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<ulong2 *>(a.hi + at) = *reinterpret_cast<ulong2 *>(a.hi + at + 2) = make_ulong2(0, 0);
+        *reinterpret_cast<ulong2 *>(a.lo + at) = *reinterpret_cast<ulong2 *>(a.lo + at + 2) = make_ulong2(0, 0);
+    }
+    if (o.bin == DRAW_BINS || o.bin != pick) return;             // all words' number and weight are enough: there is one (or, FINE, the row itself is looked at)
+    if (FINE) o.bin |= up.bin * DRAW_BINS;
     // top-p looks at what top-k left; else the words above the border's bin need not be listed, and are not where they are many
     const bool both = r.k && r.p < 1.0;
     if (o.above + o.in <= (both ? DRAW_LIST : DRAW_SHORT)) o.how = BORDER_ALL_LISTED;
@@ -370,7 +401,7 @@ __global__ void __launch_bounds__(BORDER_THREADS) k_draw_border(DrawArgs a)
 }
 __device__ __forceinline__ Border border_of(const DrawArgs &a, const Row &r, int i)
 {
-    if (r.k == 0 && r.p >= 1.0) return Border{DRAW_BINS, 0, 0, BORDER_NONE, 0.0, 0.0};
+    if (r.k == 0 && r.p >= 1.0) return Border{DRAW_BINS, BIN_SHIFT, 0, 0, BORDER_NONE, 0.0, 0.0};
     return a.borders[i];
 }
 
@@ -395,7 +426,7 @@ __global__ void __launch_bounds__(PART_THREADS) k_draw_gather(DrawArgs a)
     double m = 0.0;
     each_word<PART_THREADS>((const T *)a.z + (i64)i * a.stride, c * a.part, min(a.V, (c + 1) * a.part), [&](int v, float z) {
         const u32 key = key_of(z);
-        const int b = o.how == BORDER_NONE ? 0 : bin_of(key, top);
+        const int b = o.how == BORDER_NONE ? 0 : bin_of(key, top, o.shift);
         if (b > o.bin) return;
         if (o.how != BORDER_NONE && (b == o.bin || !weigh)) {
             const u32 at = atomicAdd(&some, 1u);
@@ -710,7 +741,7 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
         c = solo ? 0 : lds.pick;
         limit = place_of(top, 0xFFFFFFFFu);      // the first word of that logit: nothing is drawn
     } else {
-        Border o = {DRAW_BINS, 0, 0, r.k == 0 && r.p >= 1.0 ? BORDER_NONE : BORDER_ROW, 0.0, 0.0};
+        Border o = {DRAW_BINS, BIN_SHIFT, 0, 0, r.k == 0 && r.p >= 1.0 ? BORDER_NONE : BORDER_ROW, 0.0, 0.0};
         if (!solo) o = border_of(a, r, i);
         const bool listed = o.how == BORDER_ALL_LISTED || o.how == BORDER_BIN_LISTED;
         const int items = listed ? (int)min(a.listed[i], (u32)DRAW_LIST) : 0;
@@ -739,7 +770,7 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
         };
         // the border is among the words of its bin; where top-p looks at what top-k left, among those
         bool binned = listed;
-        auto among = [&](u64 x) { return x <= limit && (!binned || bin_of(~(u32)(x >> 32), top) == o.bin); };
+        auto among = [&](u64 x) { return x <= limit && (!binned || bin_of(~(u32)(x >> 32), top, o.shift) == o.bin); };
         auto mass_within = [&] {
             u64 h = 0, l = 0;
             each([&](u64 x, auto weight) {
@@ -907,6 +938,7 @@ size_t draw_carve(i64 n, i64 V, char *ws, DrawArgs *a)
     if (a) {
         a->part = part;
         a->parts = parts;
+        a->fine = V > DRAW_COARSE;
         a->unit = 62;
         while (parts && (1ll << (62 - a->unit)) < part) --a->unit;
     }
@@ -939,8 +971,15 @@ void launch_draw(const DrawArgs &a, hipStream_t st)
     if (a.parts) {
         const dim3 grid((unsigned)(a.n * a.parts)), blk(PART_THREADS);
         hipLaunchKernelGGL(k_draw_top<T>, grid, blk, 0, st, a);
-        if (a.top_k || a.top_p) hipLaunchKernelGGL(k_draw_bins<T>, grid, blk, 0, st, a);
-        if (a.top_k || a.top_p) hipLaunchKernelGGL(k_draw_border, dim3((unsigned)a.n), dim3(BORDER_THREADS), 0, st, a);
+        const dim3 rows((unsigned)a.n);
+        if (a.top_k || a.top_p) {
+            hipLaunchKernelGGL((k_draw_bins<T, false>), grid, blk, 0, st, a);
+            hipLaunchKernelGGL(k_draw_border<false>, rows, dim3(BORDER_THREADS), 0, st, a);
+            if (a.fine) {
+                hipLaunchKernelGGL((k_draw_bins<T, true>), grid, blk, 0, st, a);
+                hipLaunchKernelGGL(k_draw_border<true>, rows, dim3(BORDER_THREADS), 0, st, a);
+            }
+        }
         hipLaunchKernelGGL(k_draw_gather<T>, grid, blk, 0, st, a);
     }
     hipLaunchKernelGGL(k_draw<T>, dim3((unsigned)a.n), dim3(DRAW_THREADS), 0, st, a);

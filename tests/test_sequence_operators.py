@@ -704,7 +704,7 @@ def test_sample_masked_rows_and_ends():
     _draw(z[:0], V, u=np.zeros(0))
 
 
-@pytest.mark.parametrize("V,n,k,p,spread", [(9_000, 300, 0, 0.9, 2.0), (70_000, 3, 20_000, 0.9, 2.0), (70_000, 3, 20_000, 1.0, 2.0), (300_000, 2, 0, 0.97, 0.5), (16_777_216, 1, 0, 0.6, 2.0),
+@pytest.mark.parametrize("V,n,k,p,spread", [(9_000, 300, 0, 0.9, 2.0), (70_000, 3, 20_000, 0.9, 2.0), (70_000, 3, 20_000, 1.0, 2.0), (300_000, 2, 0, 0.97, 0.5), (16_777_216, 1, 0, 0.6, 2.0), (4_000_037, 1, 0, 0.95, 2.0), (1_500_001, 1, 0, 0.5, 1e-4), (1_500_001, 1, 400_000, 1.0, 2.0), (2_000_000, 1, 500_000, 0.9, 2.0), (2_000_000, 1, 0, 0.9, 0.0),
                                             (200_000, 2, 150_000, 0.5, 1e-4), (60_000, 4, 600, 0.99, 1.0)])
 def test_sample_long_heads(V, n, k, p, spread):
     """More rows than are taken at a time; borders behind tens of thousands of words, with and without both filters; the largest vocabulary."""
