@@ -622,13 +622,13 @@ __device__ __forceinline__ u64 place_among_few(Each each, Among among, u64 numbe
 }
 
 // A list of at most DRAW_FEW words: each compared with each, a word to a thread.  Sums are of whole numbers, so the list's order does not matter.
-__device__ __forceinline__ void draw_few(const DrawArgs &a, const Row &r, int i, const Border &o, int items, DrawLds &lds)
+__device__ __forceinline__ void draw_few(const DrawArgs &a, const Row &r, int i, double whole, int items, bool here, DrawLds &lds)
 {
     const int t = (int)threadIdx.x;
     ulong2 *list = (ulong2 *)lds.hi;             // DRAW_FEW of them
     ulong2 x = make_ulong2(~0ull, 0);
     if (t < items) {
-        x = a.list[(i64)i * DRAW_LIST + t];
+        x = here ? list[t] : a.list[(i64)i * DRAW_LIST + t];     // here: in LDS already
         list[t] = x;
     }
     __syncthreads();
@@ -644,7 +644,6 @@ __device__ __forceinline__ void draw_few(const DrawArgs &a, const Row &r, int i,
             }
         }
     bool in = t < items && (r.k == 0 || rank < r.k);
-    double whole = o.whole;
     if (r.p < 1.0) {
         if (r.k) {
             const u64 h = block_sum<DRAW_THREADS, u64>(in ? x.y >> 32 : 0, lds.sums), l = block_sum<DRAW_THREADS, u64>(in ? x.y & 0xFFFFFFFFull : 0, lds.sums);
@@ -741,12 +740,48 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
         c = solo ? 0 : lds.pick;
         limit = place_of(top, 0xFFFFFFFFu);      // the first word of that logit: nothing is drawn
     } else {
+        if (solo && r.k && r.k <= DRAW_FEW) {
+            // few words are left of few: the bins (two and two) and the list here, so that the words are compared each with each (256 rows of 8 000, top-k 50, top-p 0.9: 48 -> 19 us)
+            constexpr int PER = DRAW_DIGITS / DRAW_THREADS;
+            __syncthreads();
+            for (int b = t; b < DRAW_DIGITS; b += DRAW_THREADS) lds.counts[b] = 0;
+            if (t == 0) lds.pick = DRAW_DIGITS;
+            __syncthreads();
+            each_word<DRAW_THREADS>(z, 0, V, [&](int, float x) { atomicAdd(&lds.counts[bin_of(key_of(x), top) >> 1], 1u); });
+            __syncthreads();
+            u64 mine = 0, all;
+            for (int j = 0; j < PER; ++j) mine += lds.counts[t * PER + j];
+            u64 run = block_before<DRAW_THREADS>(mine, lds.sums, all);
+            for (int j = 0; j < PER; ++j) {
+                const u64 next = run + lds.counts[t * PER + j];
+                if (run < (u64)r.k && next >= (u64)r.k) {
+                    lds.pick = t * PER + j;
+                    lds.found[0] = next;
+                }
+                run = next;
+            }
+            __syncthreads();
+            const int bin = lds.pick, items = (int)lds.found[0];
+            if (items <= DRAW_FEW) {
+                __syncthreads();
+                if (t == 0) lds.pick = 0;
+                __syncthreads();
+                ulong2 *list = (ulong2 *)lds.hi;
+                each_word<DRAW_THREADS>(z, 0, V, [&](int v, float x) {
+                    const u32 key = key_of(x);
+                    if (bin_of(key, top) >> 1 <= bin) list[atomicAdd(&lds.pick, 1)] = make_ulong2(place_of(key, (u32)v), fixed_of(weight_of(key, top, r.slope)));
+                });
+                __syncthreads();
+                draw_few(a, r, i, 0.0, items, true, lds);
+                return;
+            }
+        }
         Border o = {DRAW_BINS, BIN_SHIFT, 0, 0, r.k == 0 && r.p >= 1.0 ? BORDER_NONE : BORDER_ROW, 0.0, 0.0};
         if (!solo) o = border_of(a, r, i);
         const bool listed = o.how == BORDER_ALL_LISTED || o.how == BORDER_BIN_LISTED;
         const int items = listed ? (int)min(a.listed[i], (u32)DRAW_LIST) : 0;
         if (o.how == BORDER_ALL_LISTED && items <= DRAW_FEW) {
-            draw_few(a, r, i, o, items, lds);
+            draw_few(a, r, i, o.whole, items, false, lds);
             return;
         }
         auto each = [&](auto f) {
@@ -791,7 +826,7 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
         if (r.p < 1.0) {
             binned = listed && !r.k;
             const double want = binned ? r.p * o.whole - o.above_mass : r.p * mass_within();
-            const u64 found = listed ? place_among_few<true>(each, among, 0, want, lds) : ~0ull;
+            const u64 found = listed || (r.k && r.k <= DRAW_PAIRS) ? place_among_few<true>(each, among, 0, want, lds) : ~0ull;
             limit = found == ~0ull ? place_at<true>(each, among, 0, want, lds) : found;
         }
         // weights of the parts
