@@ -18,6 +18,11 @@
  *   scaled lookup and its gradient by sorted tokens  -> tensair_embed, tensair_embed_grad, tensair_embed_grad_dense
  *   softmax loss over the whole vocabulary, gradient -> tensair_softmax_loss, tensair_softmax_grad
  *   AdamW over many tensors at once                  -> tensair_adamw_init, tensair_adamw_step, tensair_adamw_step_at
+ * and for models of word sequences between and behind its two ends:
+ *   layer norm and its gradient                      -> tensair_norm, tensair_norm_grad
+ *   dropout by the counter-based generator           -> tensair_dropout
+ *   a gated linear recurrence, its gradient, its form for single tokens -> tensair_recur, tensair_recur_grad, tensair_recur_step
+ *   words drawn from logits                          -> tensair_sample
  *
  * Conventions for every call
  *   - Plain C ABI.  Pointers marked DEVICE point to GPU memory owned by the caller;
@@ -485,7 +490,7 @@ int tensair_norm(const void *x, int32_t dtype, int64_t x_stride, int64_t n, int3
  *   d_x = d_add + rstd * (g - mean of g - y * (mean of g * y)),   and over the rows   d_weight = sum of d_out * y,   d_bias = sum of d_out.
  * mean, rstd: what tensair_norm gave.  d_add: of x's type or NULL, the gradient that x has from elsewhere (a residual path); d_x may be d_add,
  * with the same stride.  d_weight, d_bias: fp32 [dim], overwritten (n = 0: zeros); either may be NULL, with both NULL no workspace is needed.
- * workspace: DEVICE, 256-byte aligned; holds nothing between calls.  The bytes asked for n rows serve fewer rows, too. */
+ * workspace: DEVICE, 256-byte aligned; holds nothing between calls and may be shared by calls on one stream.  The bytes asked for n rows serve fewer rows, too. */
 size_t tensair_norm_workspace_bytes(int64_t n, int32_t dim);
 int tensair_norm_grad(const void *d_out, int32_t d_dtype, int64_t d_stride, const void *x, int32_t dtype,
                       int64_t x_stride, int64_t n, int32_t dim, const float *weight, const float *mean,
@@ -509,7 +514,8 @@ int tensair_dropout(const void *x, int32_t dtype, int64_t x_stride, int64_t n, i
  * ascending (equal ones: an empty sequence), 0 <= offsets[0], offsets[n_seq] <= n; rows outside [offsets[0], offsets[n_seq]) are neither read for
  * a result nor written.  Offsets out of this order never fault: bit 2 is OR-ed into *status, and no output of the call is to be used.
  * states: fp32 [tensair_recur_state_rows(n)][dim], what the gradient needs of the states; NULL: no gradient is wanted.
- * workspace: DEVICE, 256-byte aligned, of tensair_recur_workspace_bytes; holds nothing between calls; serves both calls and fewer rows, too. */
+ * workspace: DEVICE, 256-byte aligned, of tensair_recur_workspace_bytes; holds nothing between calls; serves both calls and fewer rows, too.  It may be shared by calls on one stream;
+ * calls that use it at the same time race (they end, with wrong results or NaN). */
 #define TENSAIR_MAX_RECUR_STRIDE 1048576 /* 2^20, of the matrices of tensair_recur and tensair_recur_grad */
 int64_t tensair_recur_state_rows(int64_t n);
 size_t tensair_recur_workspace_bytes(int64_t n, int32_t dim);
@@ -542,7 +548,7 @@ int tensair_recur_step(const void *x, int64_t x_stride, const void *gate, int64_
  * temperature (not above 0, or NaN: the largest logit is taken, prob 1; NULL: 1), top_p (not above 0, or NaN: the first word; NULL: 1), min_p (above 1: 1; NaN, NULL: 0), u (below 0,
  * or NaN: 0; 1 or above: the last word that is left): DEVICE fp32 [n]; top_k: DEVICE int32 [n], NULL: 0.  A NaN among the logits counts as minus infinity, and a word of minus infinity has no weight; where
  * the largest is plus infinity, words of plus infinity share all weight.  A row without a word above minus infinity gives -1 and probability 0 and sets bit 1 of *status.
- * workspace: DEVICE, 256-byte aligned; holds nothing between calls; serves fewer rows and words, too. */
+ * workspace: DEVICE, 256-byte aligned; holds nothing between calls; serves fewer rows and words, too, and may be shared by calls on one stream. */
 #define TENSAIR_MAX_SAMPLE_ROWS 65536
 #define TENSAIR_MAX_SAMPLE_VOCAB 16777216 /* 2^24 */
 size_t tensair_sample_workspace_bytes(int64_t n, int64_t vocab);

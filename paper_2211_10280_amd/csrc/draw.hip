@@ -555,6 +555,7 @@ __device__ __forceinline__ u64 place_at(Each each, Among among, u64 number, doub
             if (filled >= 0) atomicMax(&lds.pick, filled);
             __syncthreads();
             b = lds.pick;
+            if (b < 0) return first;             // no word at all: only where another call has changed the list meanwhile
         }
         if (b == filled) {
             lds.found[0] = at.n;
@@ -856,7 +857,7 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
             each([&](u64 x, auto weight) {
                 const u64 f = weight();
                 if (x > limit || f == 0 || (double)f * 0x1p-62 < r.least) return;
-                const int q = (int)((u32)x / (u32)part) << copies | (t & ((1 << copies) - 1));
+                const int q = min((int)((u32)x / (u32)part), parts - 1) << copies | (t & ((1 << copies) - 1));
                 atomicAdd(atom(&lds.hi[q]), f >> 32);
                 atomicAdd(atom(&lds.lo[q]), f & 0xFFFFFFFFull);
             });

@@ -133,16 +133,26 @@ __device__ __forceinline__ Map strands_before(Map m, TileLds<G> &lds, Map &all)
 // counter, so those that a tile waits for run already, and wait for none behind them.
 struct Chain {
     u32 *ticket;
+    u32 *lost;                   // set where a wait was given up
     u64 *maps, *states;          // [tiles][4 * C4], [groups][4 * C4]; zero at the start
     int tiles;
     int group;                   // tiles whose maps are put together by every tile of them; the last of a group hands the state on
 };
 #define MAP_RESET 0xC0000000u
 __device__ __forceinline__ void put_word(u64 *at, u32 hi, float v) { __hip_atomic_store(at, ((u64)hi << 32) | __float_as_uint(v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ u64 wait_word(const u64 *at)
+// Every wait ends: the word comes, or, where another call uses the same workspace at the same time and has cleared it, the wait is given up after some seconds, and all others with
+// it; what is made of it is NaN.
+#define CHAIN_PATIENCE (1u << 22)
+__device__ __forceinline__ u64 wait_word(const u64 *at, u32 *lost)
 {
     u64 w;
-    while ((w = __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) == 0) __builtin_amdgcn_s_sleep(1);
+    for (u32 n = 1; (w = __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) == 0; ++n) {
+        __builtin_amdgcn_s_sleep(1);
+        if (n % 4096 == 0 && (n >= CHAIN_PATIENCE || __hip_atomic_load(lost, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))) {
+            __hip_atomic_store(lost, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            return 0xC00000007FC00000ull;        // a reset to NaN
+        }
+    }
     return w;
 }
 // p is a product of numbers in [0, 1], so its sign is free to say that the word is there
@@ -186,7 +196,7 @@ __device__ __forceinline__ float4 chain_state(const Chain &ch, int v, bool wante
     const int per = (ch.group + RECUR_STRANDS - 1) / RECUR_STRANDS;      // tiles that follow one another to a strand
     for (int tile = first + strand * per; tile < min(v, first + (strand + 1) * per) && col < C4; ++tile) {
         const u64 *at = ch.maps + (size_t)tile * D + 4 * col;
-        const u64 a = wait_word(at), b = wait_word(at + 1), c = wait_word(at + 2), d = wait_word(at + 3);
+        const u64 a = wait_word(at, ch.lost), b = wait_word(at + 1, ch.lost), c = wait_word(at + 2, ch.lost), d = wait_word(at + 3, ch.lost);
         const Map x = {make_float4(__uint_as_float((u32)(a >> 32) & 0x7FFFFFFFu), __uint_as_float((u32)(b >> 32) & 0x7FFFFFFFu), __uint_as_float((u32)(c >> 32) & 0x7FFFFFFFu),
                                    __uint_as_float((u32)(d >> 32) & 0x7FFFFFFFu)),
                        make_float4(low_float(a), low_float(b), low_float(c), low_float(d)), (u32)(a >> 32) == MAP_RESET};
@@ -197,7 +207,7 @@ __device__ __forceinline__ float4 chain_state(const Chain &ch, int v, bool wante
         float4 h = make_float4(0.f, 0.f, 0.f, 0.f);
         if (first > 0 && !all.reset) {
             const u64 *at = ch.states + (size_t)(first / ch.group - 1) * D + 4 * col;
-            h = make_float4(low_float(wait_word(at)), low_float(wait_word(at + 1)), low_float(wait_word(at + 2)), low_float(wait_word(at + 3)));
+            h = make_float4(low_float(wait_word(at, ch.lost)), low_float(wait_word(at + 1, ch.lost)), low_float(wait_word(at + 2, ch.lost)), low_float(wait_word(at + 3, ch.lost)));
         }
         h = apply(all, h);
         if (v % ch.group == ch.group - 1 && !lds.said[l]) put_state(ch.states + (size_t)(v / ch.group) * D + 4 * col, fma4(lds.own_p[l], h, lds.own_q[l]));
@@ -366,6 +376,7 @@ __global__ void __launch_bounds__(RECUR_STRANDS *G, 4) k_recur(RecurArgs a, Chai
         if (threadIdx.x == 0) lds.tile = (int)atomicAdd(ch.ticket, 1u);
         __syncthreads();
         k = uniform(lds.tile);
+        if ((u32)k >= (u32)(ch.tiles * ((a.C4 + G - 1) / G))) return;      // only where another call takes tickets from the same workspace
     }
     k_recur_tile<T, G, CHAINED>(a, ch, k, (a.C4 + G - 1) / G, begin, end, lds);
 }
@@ -474,6 +485,7 @@ __global__ void __launch_bounds__(RECUR_STRANDS *G, sizeof(T) == 2 ? 4 : 3) k_re
         if (threadIdx.x == 0) lds.tile = (int)atomicAdd(ch.ticket, 1u);
         __syncthreads();
         k = uniform(lds.tile);
+        if ((u32)k >= (u32)(ch.tiles * ((a.C4 + G - 1) / G))) return;      // only where another call takes tickets from the same workspace
     }
     k_recur_grad_tile<T, G, CHAINED>(a, ch, k, (a.C4 + G - 1) / G, begin, end, lds, kept_d);
 }
@@ -554,6 +566,7 @@ size_t recur_carve(i64 n, int dim, char *ws, Chain *ch)
     const i64 tiles = std::max<i64>(1, (n + RECUR_TILE - 1) / RECUR_TILE), groups = (tiles + RECUR_LEAST_GROUP - 1) / RECUR_LEAST_GROUP;
     if (ch) {
         ch->ticket = (u32 *)ws;
+        ch->lost = ch->ticket + 1;
         ch->maps = (u64 *)(ws + 256);
         ch->states = ch->maps + (size_t)tiles * dim;
         ch->tiles = (int)tiles;
