@@ -53,7 +53,7 @@ struct DrawArgs {
     u64 *hi, *lo;                // [n][DRAW_BINS] weights in 2^-30, what is below in 2^-62
     struct Border *borders;      // [n]
     u32 *listed;                 // [n]
-    ulong2 *list;                // [n][DRAW_LIST] places in the order (~key, word) and weights in 2^-62
+    ulong2 *list;                // [n][DRAW_LIST] places in the order (~key, word) and weights, as the bits of a double: min_p and the probability look at the weight itself
     double *mass;                // [n][parts]
 };
 
@@ -122,6 +122,8 @@ __device__ __forceinline__ int bin_of(u32 key, u32 top, int shift = BIN_SHIFT)
     return (int)(shift == BIN_SHIFT ? min((u32)(DRAW_BINS - 1), b) : b);
 }
 __device__ __forceinline__ u64 place_of(u32 key, u32 word) { return ((u64)~key << 32) | word; }
+__device__ __forceinline__ ulong2 item_of(u64 place, double w) { return make_ulong2(place, (u64)__double_as_longlong(w)); }
+__device__ __forceinline__ double weight_in_item(ulong2 x) { return __longlong_as_double((long long)x.y); }
 // a weight as a whole number, at least 1 where there is one
 __device__ __forceinline__ u64 fixed_of(double w) { return w > 0.0 ? (u64)fmax(w * 0x1p62, 1.0) : 0; }
 __device__ __forceinline__ double mass_of(u64 hi, u64 lo) { return (double)hi * 0x1p-30 + (double)lo * 0x1p-62; }
@@ -434,7 +436,7 @@ __global__ void __launch_bounds__(PART_THREADS) k_draw_gather(DrawArgs a)
                 staged[at] = place_of(key, (u32)v);
             } else {                             // more than are put together: one by one
                 const u32 to = atomicAdd(&a.listed[i], 1u);
-                if (to < DRAW_LIST) list[to] = make_ulong2(place_of(key, (u32)v), fixed_of(weight_of(key, top, r.slope)));
+                if (to < DRAW_LIST) list[to] = item_of(place_of(key, (u32)v), weight_of(key, top, r.slope));
             }
         } else {
             const double w = weight_of(key, top, r.slope);
@@ -448,7 +450,7 @@ __global__ void __launch_bounds__(PART_THREADS) k_draw_gather(DrawArgs a)
         __syncthreads();
         for (u32 q = t; q < n; q += PART_THREADS) {
             const u64 x = staged[q];
-            if (base + q < DRAW_LIST) list[base + q] = make_ulong2(x, fixed_of(weight_of(~(u32)(x >> 32), top, r.slope)));
+            if (base + q < DRAW_LIST) list[base + q] = item_of(x, weight_of(~(u32)(x >> 32), top, r.slope));
         }
     }
     if (!weigh) return;
@@ -512,7 +514,7 @@ __device__ __forceinline__ u64 place_at(Each each, Among among, u64 number, doub
             const int b = (int)((x - first) >> shift);
             atomicAdd(&lds.counts[b], 1u);
             if (BY_MASS) {
-                const u64 w = weight();
+                const u64 w = fixed_of(weight());
                 atomicAdd(atom(&lds.hi[b]), w >> 32);
                 atomicAdd(atom(&lds.lo[b]), w & 0xFFFFFFFFull);
             }
@@ -599,7 +601,7 @@ __device__ __forceinline__ u64 place_among_few(Each each, Among among, u64 numbe
     each([&](u64 x, auto weight) {
         if (!among(x)) return;
         const int at = atomicAdd(&lds.pick, 1);
-        if (at < DRAW_PAIRS) items[at] = make_ulong2(x, BY_MASS ? weight() : 0);
+        if (at < DRAW_PAIRS) items[at] = make_ulong2(x, BY_MASS ? fixed_of(weight()) : 0);
     });
     __syncthreads();
     const int n = lds.pick;
@@ -622,62 +624,58 @@ __device__ __forceinline__ u64 place_among_few(Each each, Among among, u64 numbe
     return lds.found[0];
 }
 
-// A list of at most DRAW_FEW words: each compared with each, a word to a thread.  Sums are of whole numbers, so the list's order does not matter.
+// A list of at most DRAW_FEW words: each compared with each, a word to a thread, which puts them in order.  Their weights are added up in that order, so the list's own does not matter.
 __device__ __forceinline__ void draw_few(const DrawArgs &a, const Row &r, int i, double whole, int items, bool here, DrawLds &lds)
 {
     const int t = (int)threadIdx.x;
     ulong2 *list = (ulong2 *)lds.hi;             // DRAW_FEW of them
+    double *sorted = (double *)lds.lo;           // their weights in the order of the logits, then, of those that are in, in the order of the words
     ulong2 x = make_ulong2(~0ull, 0);
     if (t < items) {
         x = here ? list[t] : a.list[(i64)i * DRAW_LIST + t];     // here: in LDS already
         list[t] = x;
     }
+    const double w = weight_in_item(x);
     __syncthreads();
     int rank = 0;
-    u64 hi = 0, lo = 0;
-    if (t < items)
-        for (int q = 0; q < items; ++q) {
-            const ulong2 y = list[q];
-            if (y.x < x.x) {
-                ++rank;
-                hi += y.y >> 32;
-                lo += y.y & 0xFFFFFFFFull;
-            }
-        }
-    bool in = t < items && (r.k == 0 || rank < r.k);
-    if (r.p < 1.0) {
-        if (r.k) {
-            const u64 h = block_sum<DRAW_THREADS, u64>(in ? x.y >> 32 : 0, lds.sums), l = block_sum<DRAW_THREADS, u64>(in ? x.y & 0xFFFFFFFFull : 0, lds.sums);
-            whole = mass_of(h, l);
-        }
-        in = in && (rank == 0 || mass_of(hi, lo) < r.p * whole);
-    }
-    in = in && (double)x.y * 0x1p-62 >= r.least;
-    __syncthreads();
     if (t < items) {
-        list[t].x = (u32)x.x;                    // by words now
-        list[t].y = in ? x.y : 0;
+        for (int q = 0; q < items; ++q) rank += list[q].x < x.x;
+        sorted[rank] = w;
     }
+    __syncthreads();
+    bool in = t < items && (r.k == 0 || rank < r.k);
+    if (in && r.p < 1.0) {
+        if (r.k) {
+            whole = 0.0;
+            for (int q = 0; q < min(r.k, items); ++q) whole += sorted[q];
+        }
+        double before = 0.0;
+        for (int q = 0; q < rank; ++q) before += sorted[q];
+        in = rank == 0 || before < r.p * whole;
+    }
+    in = in && w > 0.0 && w >= r.least;
+    __syncthreads();
+    if (t < items) list[t].x = in ? (u32)x.x : ~0ull;            // by words now
     if (t == 0) lds.found[0] = ~0ull;
     __syncthreads();
-    hi = lo = 0;
-    u64 all_hi = 0, all_lo = 0;
+    rank = 0;
+    int left = 0;                                // words that are
     if (t < items)
         for (int q = 0; q < items; ++q) {
-            const ulong2 y = list[q];
-            all_hi += y.y >> 32;
-            all_lo += y.y & 0xFFFFFFFFull;
-            if (y.x <= (u32)x.x) {
-                hi += y.y >> 32;
-                lo += y.y & 0xFFFFFFFFull;
-            }
+            rank += list[q].x < (u32)x.x;
+            left += list[q].x != ~0ull;
         }
-    const double total = mass_of(all_hi, all_lo);
+    if (in) sorted[rank] = w;
+    __syncthreads();
+    double to = 0.0, total = 0.0;
+    if (in)
+        for (int q = 0; q < left; ++q) {
+            total += sorted[q];
+            if (q == rank) to = total;
+        }
     double u = a.u[i];
     u = u > 0.0 ? fmin(u, 1.0) : 0.0;
-    in = in && x.y > 0;
-    const bool above = in && mass_of(hi, lo) > u * total;
-    if (above) atomicMin(atom(&lds.found[0]), (u64)(u32)x.x);
+    if (in && to > u * total) atomicMin(atom(&lds.found[0]), (u64)(u32)x.x);
     __syncthreads();
     if (lds.found[0] == ~0ull) {                 // u is 1: the last word
         __syncthreads();
@@ -688,7 +686,7 @@ __device__ __forceinline__ void draw_few(const DrawArgs &a, const Row &r, int i,
     }
     if (in && (u32)x.x == (u32)lds.found[0]) {
         a.words[i] = (int)(u32)x.x;
-        if (a.prob) a.prob[i] = (float)((double)x.y * 0x1p-62 / total);
+        if (a.prob) a.prob[i] = (float)(w / total);
     }
 }
 
@@ -770,7 +768,7 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
                 ulong2 *list = (ulong2 *)lds.hi;
                 each_word<DRAW_THREADS>(z, 0, V, [&](int v, float x) {
                     const u32 key = key_of(x);
-                    if (bin_of(key, top) >> 1 <= bin) list[atomicAdd(&lds.pick, 1)] = make_ulong2(place_of(key, (u32)v), fixed_of(weight_of(key, top, r.slope)));
+                    if (bin_of(key, top) >> 1 <= bin) list[atomicAdd(&lds.pick, 1)] = item_of(place_of(key, (u32)v), weight_of(key, top, r.slope));
                 });
                 __syncthreads();
                 draw_few(a, r, i, 0.0, items, true, lds);
@@ -795,12 +793,12 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
                         if (q + k * DRAW_THREADS < items) x[k] = list[q + k * DRAW_THREADS];
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        if (q + k * DRAW_THREADS < items) f((u64)x[k].x, [&] { return (u64)x[k].y; });
+                        if (q + k * DRAW_THREADS < items) f((u64)x[k].x, [&] { return weight_in_item(x[k]); });
                 }
             } else {
                 each_word<DRAW_THREADS>(z, 0, V, [&](int v, float x) {
                     const u32 key = key_of(x);
-                    f(place_of(key, (u32)v), [&] { return fixed_of(weight_of(key, top, r.slope)); });
+                    f(place_of(key, (u32)v), [&] { return weight_of(key, top, r.slope); });
                 });
             }
         };
@@ -811,7 +809,7 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
             u64 h = 0, l = 0;
             each([&](u64 x, auto weight) {
                 if (x > limit) return;
-                const u64 w = weight();
+                const u64 w = fixed_of(weight());
                 h += w >> 32;
                 l += w & 0xFFFFFFFFull;
             });
@@ -855,8 +853,9 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
             }
         } else if (listed) {
             each([&](u64 x, auto weight) {
-                const u64 f = weight();
-                if (x > limit || f == 0 || (double)f * 0x1p-62 < r.least) return;
+                const double w = weight();
+                if (x > limit || !(w > 0.0) || w < r.least) return;
+                const u64 f = fixed_of(w);
                 const int q = min((int)((u32)x / (u32)part), parts - 1) << copies | (t & ((1 << copies) - 1));
                 atomicAdd(atom(&lds.hi[q]), f >> 32);
                 atomicAdd(atom(&lds.lo[q]), f & 0xFFFFFFFFull);
@@ -952,6 +951,10 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
             if (a.prob) a.prob[i] = r.first ? 1.f : (float)(w / total);
         }
         return;
+    }
+    if (lane == 0) {                             // no word at all: only where another call has changed the workspace meanwhile
+        a.words[i] = -1;
+        if (a.prob) a.prob[i] = 0.f;
     }
 }
 
