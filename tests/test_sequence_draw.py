@@ -46,3 +46,14 @@ def test_a_word_is_drawn_where_min_p_leaves_none_of_a_part():
             _check(z, V, [u], [0.05], [k], [1.0], [least])
     words, prob, _ = _draw(z, V, temperature=[0.05], top_k=[k], min_p=[1e-21], u=[1.0])
     assert int(words) == 11 and float(prob) > 0
+
+
+@pytest.mark.parametrize("V", [6_000, 8_193, 20_000, 100_003, 1_100_000])
+@pytest.mark.parametrize("k,p", [(0, 1.0), (300, 1.0), (50, 1.0), (0, 0.9999)])
+def test_u_of_one_is_the_last_word(V, k, p):
+    """Whatever its weight is beside the sum, which no running sum of 64 bits may show."""
+    n = 12
+    z = torch.randn((n, V), generator=_gen(V + k + 1), device="cuda") * 4
+    z[4:8, :V // 3] -= 10                                      # the likely words last, or first
+    z[8:, V // 3:] -= 10
+    _check(z, V, np.array([1.0, 1.5, float("inf")] * 4), np.array([0.05, 0.1, 0.05, 1.0] * 3), np.full(n, k), np.full(n, p), np.array([0.0, 1e-28, 1e-20] * 4))
