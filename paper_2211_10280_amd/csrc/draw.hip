@@ -892,6 +892,17 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
         __syncthreads();
         before = lds.mass[0];
         __syncthreads();
+        // Below 2^-24, between 0 and the least number of a generator of 24 bits, what is before the word may be far below the whole numbers' unit: the parts' weights in 64 bits, one part
+        // after the other.
+        if (u > 0.0 && u < 0x1p-24 && parts > 1) {
+            for (c = 0, before = 0.0; c < parts - 1; ++c) {
+                double m = 0.0;
+                each_word<DRAW_THREADS>(z, c * part, min(V, (c + 1) * part), [&](int v, float x) { m += weight_in(place_of(key_of(x), (u32)v)); });
+                m = block_sum<DRAW_THREADS>(m, lds.mass);
+                if (before + m > want) break;
+                before += m;
+            }
+        }
     }
     // the word in part c: an eighth of it to a wave, then an eighth of the one that has it, then 64 words at a time
     constexpr int WAVES = DRAW_THREADS / WAVE;

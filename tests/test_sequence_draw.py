@@ -57,3 +57,13 @@ def test_u_of_one_is_the_last_word(V, k, p):
     z[4:8, :V // 3] -= 10                                      # the likely words last, or first
     z[8:, V // 3:] -= 10
     _check(z, V, np.array([1.0, 1.5, float("inf")] * 4), np.array([0.05, 0.1, 0.05, 1.0] * 3), np.full(n, k), np.full(n, p), np.array([0.0, 1e-28, 1e-20] * 4))
+
+
+@pytest.mark.parametrize("V", [6_000, 8_193, 20_000, 100_003])
+@pytest.mark.parametrize("k,p", [(0, 1.0), (300, 1.0), (50, 1.0), (600, 0.999999)])
+def test_tiny_u(V, k, p):
+    """A u far below the last place of 32 bits falls among words of tiny weights that come before the likely ones."""
+    n = 12
+    z = torch.randn((n, V), generator=_gen(V + k + 2), device="cuda") * 4
+    z[:, 3 * V // 4:] += 8                                     # the likely words last
+    _check(z, V, 10.0 ** -np.arange(8, 44, 3), np.array([0.05, 0.1, 0.2] * 4), np.full(n, k), np.full(n, p), np.array([0.0, 1e-30] * 6))
