@@ -721,7 +721,7 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
     u64 limit = ~0ull;                           // the last place that is in
     double total = 0.0, before = 0.0, want = 0.0;
     int c = 0;                                   // the part that the word is in
-    bool end = u >= 1.0;                         // the last word of it that is in; not left to sums, whose last places differ with what is added up first
+    bool end = !r.first && u >= 1.0;             // the last word of it that is in; not left to sums, whose last places differ with what is added up first
     auto weigh = [&](u64 x) { return weight_of(~(u32)(x >> 32), top, r.slope); };
     auto weight_in = [&](u64 x) {
         if (x > limit) return 0.0;

@@ -67,3 +67,13 @@ def test_tiny_u(V, k, p):
     z = torch.randn((n, V), generator=_gen(V + k + 2), device="cuda") * 4
     z[:, 3 * V // 4:] += 8                                     # the likely words last
     _check(z, V, 10.0 ** -np.arange(8, 44, 3), np.array([0.05, 0.1, 0.2] * 4), np.full(n, k), np.full(n, p), np.array([0.0, 1e-30] * 6))
+
+
+@pytest.mark.parametrize("V", [6_000, 20_000])
+def test_u_does_not_matter_where_the_first_word_is_taken(V):
+    """Two words of the largest logit: the first of them, by temperature, top-k or top-p, whatever u is."""
+    z = torch.randn((6, V), generator=_gen(V), device="cuda")
+    z[:, 17] = z[:, V - 9] = 8.0
+    for u in (0.0, 0.7, 1.0, 2.0):
+        words, prob, _ = _draw(z, V, temperature=[0.0, 0.0, 1.0, 1.0, 1.0, 1.0], top_k=[0, 9, 1, 1, 0, 5], top_p=[1.0, 0.5, 1.0, 0.5, 0.0, 0.0], u=np.full(6, u))
+        assert words.tolist() == [17] * 6 and prob.tolist() == [1.0] * 6
