@@ -1,6 +1,7 @@
 // One word for every row of logits: temperature, top-k, top-p, min-p and the draw by a given random number.  With w[v] = exp((z[v] - max z) / T) in 64 bits, what the
 // filters leave is a head of the words in the order of falling logits (equal ones by their numbers), so a row comes down to one border in that order.  The border's place and the
-// draw are decided by sums of weights: they are taken in 64 bits, or as whole numbers of 2^-62, so that they hang on no order (in 32 bits they would move the border by whole words).
+// draw are decided by sums of weights: they are taken in 64 bits, or, so that they hang on no order, as whole numbers of 2^-78 (in 32 bits they would move the border by whole words; so would 2^-50, since
+// a tail of 2^24 words can decide it with weights of 2^-48).
 //   k_draw_top      the largest logit of every part of a row
 //   k_draw_bins     words and weights by their distance from the row's largest logit, in bins
 //   k_draw_border   the bin that the border falls into
@@ -45,12 +46,12 @@ struct DrawArgs {
     int *words, *status;
     float *prob;
     int part, parts;             // words of a part, parts of a row; 0 parts: k_draw alone
+    int counted;                 // parts that k_draw_bins takes at a time where words are only counted
     bool fine;                   // bins are cut again where they have more words than a list
-    int unit;                    // a part's weights are whole numbers of 2^-unit in the bins
     // in the workspace
     u32 *tops;                   // [n][parts]
     u32 *counts;                 // [n][DRAW_BINS]
-    u64 *hi, *lo;                // [n][DRAW_BINS] weights in 2^-30, what is below in 2^-62
+    u64 *hi, *lo;                // [n][DRAW_BINS] weights as whole numbers (Fixed)
     struct Border *borders;      // [n]
     u32 *listed;                 // [n]
     ulong2 *list;                // [n][DRAW_LIST] places in the order (~key, word) and weights, as the bits of a double: min_p and the probability look at the weight itself
@@ -124,9 +125,21 @@ __device__ __forceinline__ int bin_of(u32 key, u32 top, int shift = BIN_SHIFT)
 __device__ __forceinline__ u64 place_of(u32 key, u32 word) { return ((u64)~key << 32) | word; }
 __device__ __forceinline__ ulong2 item_of(u64 place, double w) { return make_ulong2(place, (u64)__double_as_longlong(w)); }
 __device__ __forceinline__ double weight_in_item(ulong2 x) { return __longlong_as_double((long long)x.y); }
-// a weight as a whole number, at least 1 where there is one
-__device__ __forceinline__ u64 fixed_of(double w) { return w > 0.0 ? (u64)fmax(w * 0x1p62, 1.0) : 0; }
-__device__ __forceinline__ double mass_of(u64 hi, u64 lo) { return (double)hi * 0x1p-30 + (double)lo * 0x1p-62; }
+// A weight, at most 1, as a whole number of 2^-78 in two words, at least 1 where there is one: hi in 2^-39, to nearest, and what is left, signed, in 2^-78.  A row's 2^24 words fit into each, and
+// what they are off by together is at most 2^-55 of the largest weight, less than a sum in 64 bits.
+struct Fixed {
+    u64 hi, lo;
+};
+__device__ __forceinline__ Fixed fixed_of(double w)
+{
+    // a sum with 1.5 * 2^52 has the whole part of the number in its last bits
+    const double x = w * 0x1p39, big = x + 0x1.8p52, rest = (x - (big - 0x1.8p52)) * 0x1p39 + 0x1.8p52;
+    const u64 zero = (u64)__double_as_longlong(0x1.8p52);
+    Fixed f = {(u64)__double_as_longlong(big) - zero, (u64)__double_as_longlong(rest) - zero};
+    if (w > 0.0 && (f.hi | f.lo) == 0) f.lo = 1;
+    return f;
+}
+__device__ __forceinline__ double mass_of(u64 hi, u64 lo) { return (double)hi * 0x1p-39 + (double)(i64)lo * 0x1p-78; }
 
 // f(word, logit) for the words lo..hi of a row, 16 bytes at a time where they are aligned
 template <int THREADS, typename F>
@@ -302,30 +315,35 @@ __global__ void __launch_bounds__(PART_THREADS) k_draw_top(DrawArgs a)
     if (t == 0) a.tops[(i64)i * a.parts + c] = top;
 }
 
-// A weight in 64 bits for every word of a row with top-p alone, and two additions in LDS: 256 rows, a quarter of them such, 31 us; one of a million 16 (the workgroups add to the same few hundred
+// A weight in 64 bits for every word of a row with top-p alone, and three additions in LDS: 256 rows, a quarter of them such, 32 us (sums of 2^-50 and less in one word, which three workgroups to a compute unit have room for, 31); one of a million 16 (the workgroups add to the same few hundred
 // bins in memory).  Rows with top-k only count.
 template <typename T, bool FINE>
 __global__ void __launch_bounds__(PART_THREADS) k_draw_bins(DrawArgs a)
 {
-    __shared__ u32 counts[DRAW_BINS], tops[PART_THREADS / WAVE];
-    __shared__ u64 mass[DRAW_BINS];              // in 2^-unit, so that a part's words fit
-    const int i = (int)blockIdx.x / a.parts, c = (int)blockIdx.x - i * a.parts, t = (int)threadIdx.x;
+    // two workgroups of 80 KB to a compute unit: the largest logits of waves lie where counts do afterwards
+    __shared__ u32 counts[DRAW_BINS];
+    __shared__ u64 hi[DRAW_BINS], lo[DRAW_BINS];
+    // the same part of all rows, then the next one, a row further on: a row's workgroups come neither at the same time, to add to the same bins, nor to the same die
+    const int c = (int)blockIdx.x / a.n, i = ((int)blockIdx.x - c * a.n + c) % a.n, t = (int)threadIdx.x;
     const Row r = row_of(a, i);
     if (r.first || (r.k == 0 && r.p >= 1.0)) return;
     const bool weigh = r.k == 0;                 // else top-p looks at what top-k left, which is listed
+    const int many = weigh ? 1 : a.counted;      // parts to a workgroup
+    if (c % many) return;
     int bin = 0;
     if (FINE) {
         const Border o = a.borders[i];
         if (!cut_again(r, o)) return;
         bin = o.bin;
     }
-    const double unit = (double)(1ull << a.unit);
+    const u32 top = row_top<PART_THREADS>(a, i, counts);
+    __syncthreads();
     for (int b = t; b < DRAW_BINS; b += PART_THREADS) {
         counts[b] = 0;
-        if (weigh) mass[b] = 0;
+        if (weigh) hi[b] = lo[b] = 0;
     }
-    const u32 top = row_top<PART_THREADS>(a, i, tops);           // waits for all threads
-    each_word<PART_THREADS>((const T *)a.z + (i64)i * a.stride, c * a.part, min(a.V, (c + 1) * a.part), [&](int, float z) {
+    __syncthreads();
+    each_word<PART_THREADS>((const T *)a.z + (i64)i * a.stride, c * a.part, min(a.V, (c + many) * a.part), [&](int, float z) {
         const u32 key = key_of(z);
         int b = bin_of(key, top);
         if (FINE) {
@@ -333,7 +351,10 @@ __global__ void __launch_bounds__(PART_THREADS) k_draw_bins(DrawArgs a)
             b = bin_of(key, top, FINE_SHIFT) & (DRAW_BINS - 1);
         }
         atomicAdd(&counts[b], 1u);
-        if (weigh) atomicAdd(atom(&mass[b]), (u64)(weight_of(key, top, r.slope) * unit));
+        if (!weigh) return;
+        const Fixed w = fixed_of(weight_of(key, top, r.slope));
+        atomicAdd(atom(&hi[b]), w.hi);
+        atomicAdd(atom(&lo[b]), w.lo);
     });
     __syncthreads();
     for (int b = t; b < DRAW_BINS; b += PART_THREADS) {
@@ -341,8 +362,8 @@ __global__ void __launch_bounds__(PART_THREADS) k_draw_bins(DrawArgs a)
         const i64 at = (i64)i * DRAW_BINS + b;
         atomicAdd(&a.counts[at], counts[b]);
         if (!weigh) continue;
-        atomicAdd(atom(&a.hi[at]), mass[b] >> (a.unit - 30));
-        atomicAdd(atom(&a.lo[at]), (mass[b] & ((1ull << (a.unit - 30)) - 1)) << (62 - a.unit));
+        atomicAdd(atom(&a.hi[at]), hi[b]);
+        atomicAdd(atom(&a.lo[at]), lo[b]);
     }
 }
 
@@ -514,9 +535,9 @@ __device__ __forceinline__ u64 place_at(Each each, Among among, u64 number, doub
             const int b = (int)((x - first) >> shift);
             atomicAdd(&lds.counts[b], 1u);
             if (BY_MASS) {
-                const u64 w = fixed_of(weight());
-                atomicAdd(atom(&lds.hi[b]), w >> 32);
-                atomicAdd(atom(&lds.lo[b]), w & 0xFFFFFFFFull);
+                const Fixed w = fixed_of(weight());
+                atomicAdd(atom(&lds.hi[b]), w.hi);
+                atomicAdd(atom(&lds.lo[b]), w.lo);
             }
         });
         __syncthreads();
@@ -601,7 +622,10 @@ __device__ __forceinline__ u64 place_among_few(Each each, Among among, u64 numbe
     each([&](u64 x, auto weight) {
         if (!among(x)) return;
         const int at = atomicAdd(&lds.pick, 1);
-        if (at < DRAW_PAIRS) items[at] = make_ulong2(x, BY_MASS ? fixed_of(weight()) : 0);
+        if (at >= DRAW_PAIRS) return;
+        const Fixed w = fixed_of(BY_MASS ? weight() : 0.0);
+        items[at] = make_ulong2(x, w.hi);
+        lds.lo[at] = w.lo;
     });
     __syncthreads();
     const int n = lds.pick;
@@ -614,8 +638,8 @@ __device__ __forceinline__ u64 place_among_few(Each each, Among among, u64 numbe
             const ulong2 y = items[q];
             if (y.x < x) {
                 ++rank;
-                hi += y.y >> 32;
-                lo += y.y & 0xFFFFFFFFull;
+                hi += y.y;
+                lo += lds.lo[q];
             }
         }
         if (rank == 0 || (BY_MASS ? mass_of(hi, lo) < mass : rank < number)) atomicMax(atom(&lds.found[0]), x);
@@ -809,9 +833,9 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
             u64 h = 0, l = 0;
             each([&](u64 x, auto weight) {
                 if (x > limit) return;
-                const u64 w = fixed_of(weight());
-                h += w >> 32;
-                l += w & 0xFFFFFFFFull;
+                const Fixed w = fixed_of(weight());
+                h += w.hi;
+                l += w.lo;
             });
             h = block_sum<DRAW_THREADS>(h, lds.sums);
             l = block_sum<DRAW_THREADS>(l, lds.sums);
@@ -840,9 +864,9 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
             for (int q = 0; q < parts; ++q) {
                 u64 h = 0, l = 0;
                 each_word<DRAW_THREADS>(z, q * part, min(V, (q + 1) * part), [&](int v, float x) {
-                    const u64 w = fixed_of(weight_in(place_of(key_of(x), (u32)v)));
-                    h += w >> 32;
-                    l += w & 0xFFFFFFFFull;
+                    const Fixed w = fixed_of(weight_in(place_of(key_of(x), (u32)v)));
+                    h += w.hi;
+                    l += w.lo;
                 });
                 h = block_sum<DRAW_THREADS>(h, lds.sums);
                 l = block_sum<DRAW_THREADS>(l, lds.sums);
@@ -855,10 +879,10 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
             each([&](u64 x, auto weight) {
                 const double w = weight();
                 if (x > limit || !(w > 0.0) || w < r.least) return;
-                const u64 f = fixed_of(w);
+                const Fixed f = fixed_of(w);
                 const int q = min((int)((u32)x / (u32)part), parts - 1) << copies | (t & ((1 << copies) - 1));
-                atomicAdd(atom(&lds.hi[q]), f >> 32);
-                atomicAdd(atom(&lds.lo[q]), f & 0xFFFFFFFFull);
+                atomicAdd(atom(&lds.hi[q]), f.hi);
+                atomicAdd(atom(&lds.lo[q]), f.lo);
             });
         }
         __syncthreads();
@@ -989,8 +1013,7 @@ size_t draw_carve(i64 n, i64 V, char *ws, DrawArgs *a)
         a->part = part;
         a->parts = parts;
         a->fine = V > DRAW_COARSE;
-        a->unit = 62;
-        while (parts && (1ll << (62 - a->unit)) < part) --a->unit;
+        a->counted = part <= 2 * DRAW_PART && n * parts >= 2048 ? 4 : 1;      // 256 rows of 100 003 with top-k alone: 1 / 4 102 / 94 us
     }
     if (!parts) return 256;
     size_t at = 0;

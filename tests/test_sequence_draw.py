@@ -77,3 +77,57 @@ def test_u_does_not_matter_where_the_first_word_is_taken(V):
     for u in (0.0, 0.7, 1.0, 2.0):
         words, prob, _ = _draw(z, V, temperature=[0.0, 0.0, 1.0, 1.0, 1.0, 1.0], top_k=[0, 9, 1, 1, 0, 5], top_p=[1.0, 0.5, 1.0, 0.5, 0.0, 0.0], u=np.full(6, u))
         assert words.tolist() == [17] * 6 and prob.tolist() == [1.0] * 6
+
+
+def _last_left(row, p):
+    """The first and the last place that the last word left by top-p may have, of a row in falling order: sums in extended precision, moved by what the operator may round.  A weight is off
+    by at most (0.7 |log2 w| + 4) units of 2^-53, which the tails here, below 1e-3 of the sum, make small; sums and products of 64 bits are off by 8 of them with room."""
+    z = row.double().cpu().numpy()
+    # the tail by itself: 2^23 equal words of 2^-43 added to 1 in 64 bits of mantissa may be off by 2^-64 each, which is 4 of them; added to each other by 2^-84, 2^-61 in all
+    run = 1 + np.concatenate([[np.longdouble(0)], np.cumsum(np.exp((z[1:] - z[0]).astype(np.longdouble)))])
+    off = (8 + 1e-3 * (0.7 * 50 + 4)) * 2.0 ** -53 * run[-1]
+    want = np.longdouble(np.float32(p)) * run[-1]
+    lo, hi = (int(np.searchsorted(run, x, side="left")) for x in (want - off, want + off))
+    assert 0 < lo <= hi <= lo + 1 and hi < len(z) - 1          # the places tell
+    return lo, hi
+
+
+@pytest.mark.parametrize("V,p,first,fall,rows", [(128_000, 0.99999, 20.0, 4.0, (1, 64)), (1_000_000, 0.9999, 20.0, 4.0, (1, 25, 256)), (1_048_577, 0.9999, 20.0, 4.0, (1, 130)),
+                                                 (4_000_000, 0.999998, 25.0, 5.0, (1, 64)), (16_777_216, 0.999999, 29.0, 2.0, (1, 16))])
+def test_border_in_a_long_tail(V, p, first, fall, rows):
+    """One likely word and a tail in falling order, in which top-p ends: with u of 1 the word that is drawn is the last one that is left.  A row gives the same word alone and among others."""
+    row = -first - fall * torch.arange(V, device="cuda", dtype=torch.float64) / V
+    row[0] = 0.0
+    row = row.float()
+    lo, hi = _last_left(row, p)
+    got = set()
+    for n in rows:
+        words, _, st = _draw(row.expand(n, V).contiguous(), V, top_p=np.full(n, p), u=np.ones(n))
+        got |= set(words.tolist())
+        assert int(st) == 0
+    assert len(got) == 1 and lo <= min(got) <= hi, (got, lo, hi)
+
+
+@pytest.mark.parametrize("V,p,n", [(300_000, 0.999997, 1), (300_000, 0.999997, 30), (16_777_216, 0.999999, 16)])
+def test_border_among_a_tail_of_equal_words(V, p, n):
+    """The same where all words but one have one logit, so that roundings of their weights are the same ones."""
+    row = torch.full((V,), -25.25 if V < 1 << 20 else -29.75, device="cuda").bfloat16()
+    row[0] = 0.0
+    lo, hi = _last_left(row, p)
+    words, _, st = _draw(row.expand(n, V).contiguous(), V, top_p=np.full(n, p), u=np.ones(n))
+    assert set(words.tolist()) <= {lo, hi} and len(set(words.tolist())) == 1 and int(st) == 0, (words.tolist(), lo, hi)
+
+
+@pytest.mark.parametrize("V,n", [(20_000, 8), (100_003, 6)])
+def test_border_behind_top_k(V, n):
+    """top-p beside top-k, both in a tail of words of 1e-9 and less."""
+    row = -20 - 4 * torch.arange(V, device="cuda", dtype=torch.float64) / V
+    row[0] = 0.0
+    row = row.float()
+    for k in (200, 3_000, 17_000):
+        run = np.cumsum(np.exp(row[:k].double().cpu().numpy().astype(np.longdouble)))
+        p = float(np.float32((run[k // 2] / run[-1])))
+        assert float(run[0] / run[-1]) < p < 1
+        lo, hi = _last_left(row[:k], p)
+        words, _, _ = _draw(row.expand(n, V).contiguous(), V, top_k=np.full(n, k), top_p=np.full(n, p), u=np.ones(n))
+        assert set(words.tolist()) <= {lo, hi}, (k, words.tolist(), lo, hi)
