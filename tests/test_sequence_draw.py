@@ -131,3 +131,20 @@ def test_border_behind_top_k(V, n):
         lo, hi = _last_left(row[:k], p)
         words, _, _ = _draw(row.expand(n, V).contiguous(), V, top_k=np.full(n, k), top_p=np.full(n, p), u=np.ones(n))
         assert set(words.tolist()) <= {lo, hi}, (k, words.tolist(), lo, hi)
+
+
+@pytest.mark.parametrize("V,dtype", [(1, "f32"), (6_000, "f32"), (8_193, "bf16"), (20_000, "f32"), (100_003, "bf16"), (1_100_000, "f32")])
+@pytest.mark.parametrize("given", ["", "T", "m", "k", "p", "Tm", "kp", "Tkpm"])
+def test_filters_that_are_not_given(V, dtype, given):
+    """Every filter's address may be NULL: no vector but u, each by itself, and some together; rows with masked words and with infinite ones."""
+    n, r = 9 if V < 50_000 else 5, np.random.RandomState(V)
+    z = torch.randn((n, V), generator=_gen(V + 7), device="cuda") * 3
+    if V > 1:
+        z[1, ::2] = -float("inf")
+        z[2, V // 2:] = torch.finfo(torch.float32).min
+        z[3, 5] = z[3, V - 3] = float("inf")
+        z[4, ::3] = float("nan")
+    z = z.to(torch.float32 if dtype == "f32" else torch.bfloat16)
+    some = {"T": r.choice([0.0, 0.3, 1.0, 2.0], n), "m": r.choice([0.0, 0.01, 0.5], n), "k": r.choice([0, 1, 40, 900], n), "p": r.choice([0.3, 0.9, 1.0], n)}
+    for u in (np.ones(n), np.zeros(n), r.rand(n), r.rand(n) * 0.01)[:4 if V < 50_000 else 3]:
+        _check(z, V, u, **{x: some[x] for x in given})
