@@ -75,7 +75,7 @@ struct NormGradArgs {
     int per;                     // rows of a group of lanes
     int blocks;
 };
-#define NORM_MOST_ROWS 256       // that one lane adds up in fp32; their sums are added in 64 bits
+#define NORM_MOST_ROWS 256       // that one lane adds up in fp32; so are the sums of a workgroup's 4 to 32 groups of lanes, and the workgroups' shares in 64 bits
 // Workgroups that few rows are spread over: twice what the card holds at the registers of rows of 300 (262 143 of them, fp32, with a residual's gradient: 1 536 workgroups 244 us,
 // 1 024 295, 2 048 257; 16 384 rows of 512 in bfloat16 14 each, but more shares to put together).
 #define NORM_BLOCKS 1536
