@@ -783,8 +783,8 @@ def _recur_inputs(x, gate, dim, offsets, states):
         raise TensairError(EINVAL, "x and gate must have one type")
     if n_seq < 0:
         raise TensairError(EINVAL, "offsets: expected one more than there are sequences")
-    rows = max(1, -(-n // 256))
-    return n, n_seq, xd, (xp, xs, gp, gs, xd, n, dim, _ids(offsets, "offsets"), n_seq), _floats(states, (rows, dim), "states")
+    sp = None if states is None else _floats(states, (tensair_recur_state_rows(n), dim), "states")
+    return n, n_seq, xd, (xp, xs, gp, gs, xd, n, dim, _ids(offsets, "offsets"), n_seq), sp
 
 
 def tensair_recur(x, gate, dim: int, offsets, out, workspace, h0=None, h_last=None, states=None, status=None, stream=None):

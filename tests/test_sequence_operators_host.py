@@ -160,3 +160,14 @@ def test_each_argument_is_looked_at():
                 with pytest.raises(B.TensairError):
                     call(*args[:k], bad, *args[k + 1:])
     torch.cuda.synchronize()
+
+
+def test_rows_of_states_are_the_librarys(monkeypatch):
+    """The binding checks the states' rows against what the library says, not against a tile size of its own."""
+    x, offsets = torch.zeros((300, 8)), torch.zeros(2, dtype=torch.int32)
+    assert B.tensair_recur_state_rows(300) == 2
+    assert B._recur_inputs(x, x, 8, offsets, torch.zeros((2, 8)))[-1] and B._recur_inputs(x, x, 8, offsets, None)[-1] is None
+    monkeypatch.setattr(B, "tensair_recur_state_rows", lambda n: 5)
+    assert B._recur_inputs(x, x, 8, offsets, torch.zeros((5, 8)))[-1]
+    with pytest.raises(B.TensairError):
+        B._recur_inputs(x, x, 8, offsets, torch.zeros((2, 8)))
