@@ -175,7 +175,7 @@ def next_word_batch(tokens, begin, n, sequences):
     """(words, offsets, labels, 1 / labels for every word) of a run of positions of a device int32 stream cut into sequences of nearly equal length; a word's label is the next
     one, the last word of a sequence has the next one too, unless it is the stream's last."""
     words = tokens[begin:begin + n]
-    offsets = torch.linspace(0, n, sequences + 1, device=tokens.device).round().to(torch.int32)
+    offsets = torch.linspace(0, n, sequences + 1, dtype=torch.float64, device=tokens.device).round().to(torch.int32)
     labels = torch.full_like(words, IGNORE)
     more = min(n, tokens.numel() - begin - 1)
     labels[:more] = tokens[begin + 1:begin + 1 + more]

@@ -15,6 +15,13 @@ def test_next_word_batch():
     assert words.dtype == offsets.dtype == labels.dtype == torch.int32
 
 
+def test_next_word_batch_of_more_words_than_32_bits_of_float_count():
+    """Offsets of a long mini-batch: the last one is the number of its words."""
+    n = (1 << 24) + 3
+    _, offsets, labels, _ = next_word_batch(torch.zeros(n, dtype=torch.int32), 0, n, 2)
+    assert offsets.tolist()[::2] == [0, n] and offsets.dtype == torch.int32 and abs(int(offsets[1]) - n / 2) <= 0.5 and int(labels[-1]) == IGNORE
+
+
 def _keep(worker, n, layer):
     """The dropout mask times 1 / (1 - p), by the operator's own definition (its words are checked elsewhere)."""
     from paper_2211_10280_amd import binding as B
