@@ -3,8 +3,9 @@
 Where :mod:`softmax_trainer` scores a word beside one other word, this puts layers between a table's two ends: looked-up
 vectors (``tensair_embed``) with dropout (``tensair_dropout``), then blocks of layer norm (``tensair_norm``), a product that gives inputs and
 gates, a gated linear recurrence over the mini-batch's ragged sequences (``tensair_recur``), dropout and the residual path; a last norm, and the exact
-softmax over all words (``tensair_softmax_loss``).  Gradients go the same way back, and one ``tensair_adamw_step`` updates everything.  The states of the sequences
-are carried from step to step, cut off for the gradient.  ``generate`` is the server's side: a word at a time (``tensair_recur_step``), drawn from the
+softmax over all words (``tensair_softmax_loss``).  Gradients go the same way back, and one ``tensair_adamw_step`` updates everything.  A step may be given the
+sequences' states before it, cut off for the gradient, and leaves those behind it, so that a caller whose sequences go on from step to step can carry them; the command below
+begins every sequence with zeros, since its mini-batches are runs of one stream.  ``generate`` is the server's side: a word at a time (``tensair_recur_step``), drawn from the
 logits (``tensair_sample``).
 
     python -m paper_2211_10280_amd.sequence_trainer --steps 50 --layers 2
@@ -20,7 +21,7 @@ import torch
 
 from . import binding as B
 
-IGNORE = -1      # the label of a sequence's last word
+IGNORE = -1      # the label of a word that has none, as the stream's last one
 
 
 class SequenceWorker:
