@@ -510,7 +510,7 @@ int tensair_dropout(const void *x, int32_t dtype, int64_t x_stride, int64_t n, i
 /* A gated linear recurrence over the sequences of a packed mini-batch: for the tokens t of sequence s, offsets[s] <= t < offsets[s + 1], and every channel
  *   h[t] = a[t] h[t - 1] + (1 - a[t]) x[t],   a[t] = 1 / (1 + exp(-gate[t])),
  * with h0[s] before a sequence's first token (h0: fp32 [n_seq][dim], NULL: 0), in fp32; out[t] is h[t] rounded to x's type, h_last[s] (fp32 [n_seq][dim], NULL: not
- * wanted) the last h of the sequence, h0[s] if it has no token.  x, gate and out have one type; n: rows that they have.  offsets: DEVICE int32 [n_seq + 1],
+ * wanted) the last h of the sequence, h0[s] if it has no token.  Behind an infinite x or h0 a channel's h are infinite or NaN until its sequence ends.  x, gate and out have one type; n: rows that they have.  offsets: DEVICE int32 [n_seq + 1],
  * ascending (equal ones: an empty sequence), 0 <= offsets[0], offsets[n_seq] <= n; rows outside [offsets[0], offsets[n_seq]) are neither read for
  * a result nor written.  Offsets out of this order never fault: bit 2 is OR-ed into *status, and no output of the call is to be used.
  * states: fp32 [tensair_recur_state_rows(n)][dim], what the gradient needs of the states; NULL: no gradient is wanted.
@@ -548,7 +548,8 @@ int tensair_recur_step(const void *x, int64_t x_stride, const void *gate, int64_
  * temperature (not above 0, or NaN: the largest logit is taken, prob 1; NULL: 1), top_p (not above 0, or NaN: the first word; NULL: 1), min_p (above 1: 1; NaN, NULL: 0), u (below 0,
  * or NaN: 0; 1 or above: the last word that is left): DEVICE fp32 [n]; top_k: DEVICE int32 [n], NULL: 0.  A NaN among the logits counts as minus infinity, and a word of minus infinity has no weight; where
  * the largest is plus infinity, words of plus infinity share all weight.  A row without a word above minus infinity gives -1 and probability 0 and sets bit 1 of *status.
- * workspace: DEVICE, 256-byte aligned; holds nothing between calls; serves fewer rows and words, too, and may be shared by calls on one stream. */
+ * workspace: DEVICE, 256-byte aligned; holds nothing between calls; serves fewer rows and words, too, and may be shared by calls on one stream;
+ * calls that use it at the same time race (they end, with other words or -1). */
 #define TENSAIR_MAX_SAMPLE_ROWS 65536
 #define TENSAIR_MAX_SAMPLE_VOCAB 16777216 /* 2^24 */
 size_t tensair_sample_workspace_bytes(int64_t n, int64_t vocab);

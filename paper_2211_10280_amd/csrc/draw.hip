@@ -9,7 +9,7 @@
 //   k_draw_gather   the words that may be in (those of the border's bin and, where they are few, all of the bins above) as a list, else the parts' weights above it
 //   k_draw          the border among the list, the part that the draw falls into, the word in it
 // A row without top-k and top-p needs no bins, a row of few words only the last of these, which then takes the row itself for the list; so it does where a list is too short
-// (thousands of words within a 256th of each other's logits at the border).
+// (thousands of words within a 256th of each other's logits at the border, or of one logit, or more than a list of masked words, which all lie in the last bin, where fewer are left than top-k keeps).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -28,7 +28,7 @@ namespace {
 #define DRAW_PARTS 512           // most parts of a row
 #define DRAW_WORKGROUPS 4096     // parts of all rows that are aimed at
 #define DRAW_BINS 4096           // 256 to a doubling of (distance + 1)
-#define DRAW_COARSE 1048576      // most words for which a bin is taken as it is: the launches that cut it again are 5 us; without them 16.8 million words with top-p 0.9 take 44.8 ms, with them 202 us
+#define DRAW_COARSE 1048576      // most words for which a bin is taken as it is: the launches that cut it again are 5 us; without them 16.8 million words of spread logits with top-p 0.9 take 44.8 ms, with them 206 us
 #define DRAW_DIGITS 2048         // of places
 #define DRAW_LIST 16384          // most words of a row's list
 #define DRAW_STAGED 2048         // of a part's words that go to it, most that are put together in LDS before
@@ -315,7 +315,7 @@ __global__ void __launch_bounds__(PART_THREADS) k_draw_top(DrawArgs a)
     if (t == 0) a.tops[(i64)i * a.parts + c] = top;
 }
 
-// A weight in 64 bits for every word of a row with top-p alone, and three additions in LDS: 256 rows, a quarter of them such, 32 us (sums of 2^-50 and less in one word, which three workgroups to a compute unit have room for, 31); one of a million 16 (the workgroups add to the same few hundred
+// A weight in 64 bits for every word of a row with top-p alone, and three additions in LDS: 256 rows, a quarter of them such, 32 us (sums of 2^-50 and less in one word, which three workgroups to a compute unit have room for, 31); one of a million 17 (the workgroups add to the same few hundred
 // bins in memory).  Rows with top-k only count.
 template <typename T, bool FINE>
 __global__ void __launch_bounds__(PART_THREADS) k_draw_bins(DrawArgs a)
@@ -714,7 +714,7 @@ __device__ __forceinline__ void draw_few(const DrawArgs &a, const Row &r, int i,
     }
 }
 
-// One workgroup to a row: 12 us where a list is short (64 rows, top-k 50), 20 for one of a million with top-p (3 400 words listed), 32 for 256 rows of all kinds: a chain of loads, sums and barriers,
+// One workgroup to a row: 10 us where a list is short (64 rows, top-k 50), 22 for one of a million with top-p (3 400 words listed), 33 for 256 rows of all kinds: a chain of loads, sums and barriers,
 // vector units busy 6 %.
 template <typename T>
 __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
@@ -764,7 +764,7 @@ __global__ void __launch_bounds__(DRAW_THREADS) k_draw(DrawArgs a)
         limit = place_of(top, 0xFFFFFFFFu);      // the first word of that logit: nothing is drawn
     } else {
         if (solo && r.k && r.k <= DRAW_FEW) {
-            // few words are left of few: the bins (two and two) and the list here, so that the words are compared each with each (256 rows of 8 000, top-k 50, top-p 0.9: 48 -> 19 us)
+            // few words are left of few: the bins (two and two) and the list here, so that the words are compared each with each (256 rows of 8 000, top-k 50, top-p 0.9: 15 us, as all rows 48)
             constexpr int PER = DRAW_DIGITS / DRAW_THREADS;
             __syncthreads();
             for (int b = t; b < DRAW_DIGITS; b += DRAW_THREADS) lds.counts[b] = 0;

@@ -381,8 +381,9 @@ __global__ void __launch_bounds__(RECUR_STRANDS *G, 4) k_recur(RecurArgs a, Chai
     k_recur_tile<T, G, CHAINED>(a, ch, k, (a.C4 + G - 1) / G, begin, end, lds);
 }
 
-// Gradient: the states of the tile again, then from behind.  262 144 tokens of 512, bfloat16: 400 us (1.34 GB, 3.4 TB/s), 131 072 of 128 in one sequence 70, 4 096 of 128 in fp32 14.5.  The vector units are busy 61 %
-// of the time.  A gate's two sides held as one number, the gradients of the outputs in LDS, and what is made of them made again rather than held: 128 registers a thread, nothing in memory (595 us
+// Gradient: the states of the tile again, then from behind.  262 144 tokens of 512, bfloat16: 400 us, 131 072 of 128 in one sequence 72, 4 096 of 128 in fp32 14.5.  1.34 GB have to be moved (3.4 TB/s);
+// 1.95 GB are, at the rate of a copy, since a workgroup takes half a line of a token and its other half is fetched again: memory bounds it.  In fp32, by whole lines, 511 us for 2.68 GB.  The vector units
+// are busy 61 % of the time.  A gate's two sides held as one number, the gradients of the outputs in LDS, and what is made of them made again rather than held: 128 registers a thread, nothing in memory (595 us
 // before, with 224; 525 with 128 and spills).
 template <typename T, int G, bool CHAINED>
 __device__ __forceinline__ void k_recur_grad_tile(const RecurArgs &a, const Chain &ch, int k, int sides, i64 begin, i64 end, TileLds<G> &lds, typename Raw4<T>::type (&kept_d)[RECUR_RUN][RECUR_STRANDS * G])
