@@ -126,7 +126,7 @@ __device__ __forceinline__ u64 place_of(u32 key, u32 word) { return ((u64)~key <
 __device__ __forceinline__ ulong2 item_of(u64 place, double w) { return make_ulong2(place, (u64)__double_as_longlong(w)); }
 __device__ __forceinline__ double weight_in_item(ulong2 x) { return __longlong_as_double((long long)x.y); }
 // A weight, at most 1, as a whole number of 2^-78 in two words, at least 1 where there is one: hi in 2^-39, to nearest, and what is left, signed, in 2^-78.  A row's 2^24 words fit into each, and
-// what they are off by together is at most 2^-55 of the largest weight, less than a sum in 64 bits.
+// what they are off by together is at most 2^-54 of the largest weight, less than a sum in 64 bits.
 struct Fixed {
     u64 hi, lo;
 };
